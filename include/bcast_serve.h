@@ -96,7 +96,8 @@ int64_t bcast_serve_linear_workspace(const bcast_serve_linear_args *args);
  * Arguments
  *   dtype        BCAST_SERVE_BF16 or BCAST_SERVE_FP16
  *   batch >= 0, new_tokens >= 0, kv_heads >= 1, q_heads a multiple of kv_heads, prefix_len >= 0,
- *   own_cap >= 0;  dim a multiple of 8, 8..128
+ *   own_cap >= 0;  dim a multiple of 8, 8..128;  new_tokens * q_heads <= 2^19, and at most 2^24 rows
+ *   (batch * new_tokens * q_heads) in all
  *   q, out       [batch][new_tokens][q_heads][dim], strides of the first three
  *   prefix_k/_v  [prefix_len][kv_heads][dim], strides of the first two (not looked at if prefix_len = 0)
  *   own_k/_v     rows:  [batch][own_cap][kv_heads][dim]      (page_table NULL)
@@ -105,7 +106,9 @@ int64_t bcast_serve_linear_workspace(const bcast_serve_linear_args *args);
  *   own_len      [batch] int32
  *   page_table   NULL or [batch][ceil(own_cap / page_size)] int32, rows at page_table_stride
  *   lse          NULL or [batch][new_tokens][q_heads] float: log of the sum of exp(scale * q . k_j)
- * q, out and the caches start on 16-byte boundaries and their strides are multiples of 8.
+ * q, out and the caches start on 16-byte boundaries and their strides are multiples of 8.  A stride of out
+ * and of the prefix is at least dim; those of q and of the own caches may also be 0 (rows that several
+ * requests share).
  */
 typedef struct bcast_serve_attn_args {
     int32_t dtype, batch, new_tokens, q_heads, kv_heads, dim, page_size;

@@ -1,86 +1,684 @@
 // bcast_serve_attn: attention of every request's newest tokens over a prefix that all requests share and
 // the request's own tokens behind it.
 //
-// One block per row (request, new token, query head), one pass over the row's tokens in tiles with the
-// running maximum m and sum l of the softmax: a tile's scores s_j change m to m', and what was summed so far
-// is scaled by exp(m - m').
+// Softmax over a set of tokens that is cut into parts: with m_p >= the largest score of part p (in powers of two),
+// l_p = sum 2^(s - m_p) and o_p = sum 2^(s - m_p) v, the whole is  M = max m_p,
+//   out = sum_p 2^(m_p - M) o_p / sum_p 2^(m_p - M) l_p.
+// Three kernels, the second starting while the first runs out (programmatic launch):
+//   own kernel      a block per (request, key/value head, part of its own tokens): few rows against tokens that
+//                   nobody else reads, so bound by reading them; warps take 16 tokens at a time through mma.sync
+//   prefix kernel   a block per (key/value head, tile of rows, part of the prefix).  The rows are those of ALL
+//                   requests -- request, new token and query head of the group --, so a prefix token is read once
+//                   for 128 or 256 rows and the two products run on tcgen05
+//   join kernel     the formula above, a warp per row
 #include "serve_device.cuh"
 #include "serve_internal.h"
+#include "serve_tma.h"
 
 namespace bcast_serve {
 namespace {
 
-constexpr int kRowThreads = 128;
-
 struct AttnDev {
-    const void *q, *pk, *pv, *ok, *ov;
+    const void *q, *ok, *ov;
     const int32_t *own_len, *page_table;
     void *out;
     float *lse;
-    int64_t qs[3], os[3], pks[2], pvs[2], oks[3], ovs[3];
-    int64_t prefix_len, own_cap, num_pages, pts;
-    int32_t batch, fresh, q_heads, group, dim, page;
+    float2 *part_ml;      // [parts][rows]: (m, l), m = -infinity where a part holds nothing
+    float *part_o;        // [parts][rows][dim]
+    int *status;
+    int64_t qs[3], os[3], oks[3], ovs[3];
+    int64_t own_cap, num_pages, pts, rows;       // rows: batch * fresh * q_heads
+    int32_t batch, fresh, q_heads, kv_heads, group, dim, page, prefix_len;
+    int32_t prefix_splits, prefix_parts, row_tiles, own_splits, own_chunk, parts;
     float scale_log2;     // scale * log2(e): the softmax is taken in powers of two
 };
 
-// Row `at` of a request's own keys (or values), nullptr if its page is not there.
-template <typename T>
-__device__ __forceinline__ const T *own_row(const AttnDev &d, const void *base, const int64_t *s, int b, int64_t at, int kv)
+// fp16 holds weights from 2^-24 to 2^16: shifting them by 2^7 keeps the small ones exact for longer (the factor
+// is in l as well and cancels).  bf16 has the exponents of 32-bit floats.
+template <typename T> constexpr float kShift = std::is_same_v<T, __half> ? 7.0f : 0.0f;
+
+template <typename T> __device__ __forceinline__ uint32_t pack2(float lo, float hi);
+template <> __device__ __forceinline__ uint32_t pack2<__nv_bfloat16>(float lo, float hi)
 {
-    if (!d.page_table) return (const T *)base + b * s[0] + at * s[1] + kv * s[2];
-    const int32_t p = d.page_table[(int64_t)b * d.pts + at / d.page];
-    if (p < 0 || p >= d.num_pages) return nullptr;
-    return (const T *)base + p * s[0] + at % d.page * s[1] + kv * s[2];
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+template <> __device__ __forceinline__ uint32_t pack2<__half>(float lo, float hi)
+{
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kRowThreads)
-serve_attn_row_kernel(const __grid_constant__ AttnDev d)
+// ------------------------------------------------------------------------------------------- own tokens
+constexpr int kOwnWarps = 4, kOwnKeys = 16, kOwnStages = 3;
+
+template <int DB> constexpr size_t own_smem() { return (size_t)kOwnWarps * kOwnStages * 2 * kOwnKeys * DB * 128; }
+
+__device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool there)
 {
-    const int h = blockIdx.x, i = blockIdx.y, b = blockIdx.z, kv = h / d.group, tid = threadIdx.x;
-    __shared__ float q[128], p[kRowThreads], red[kRowThreads / 32];
-    if (tid < d.dim) q[tid] = to_f32(((const T *)d.q)[b * d.qs[0] + i * d.qs[1] + h * d.qs[2] + tid]) * d.scale_log2;
-    const int64_t len = min(max((int64_t)d.own_len[b], (int64_t)0), d.own_cap);
-    const int64_t own = max(len - d.fresh + i + 1, (int64_t)0), total = d.prefix_len + own;
-    float m = -INFINITY, l = 0.0f, o = 0.0f;
-    __syncthreads();
-    for (int64_t j0 = 0; j0 < total; j0 += kRowThreads) {
-        const int64_t j = j0 + tid;
-        const T *k = nullptr;
-        if (j < d.prefix_len) k = (const T *)d.pk + j * d.pks[0] + kv * d.pks[1];
-        else if (j < total) k = own_row<T>(d, d.ok, d.oks, b, j - d.prefix_len, kv);
-        float s = -INFINITY;
-        if (k) {
-            s = 0.0f;
-            for (int c = 0; c < d.dim; c++) s += q[c] * to_f32(k[c]);
-        }
-        float top = s;
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void ldmatrix(uint32_t *r, uint32_t at)
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
+}
+__device__ __forceinline__ void ldmatrix_t(uint32_t *r, uint32_t at)
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
+}
+template <typename T>
+__device__ __forceinline__ void mma_sync(float *c, const uint32_t *a, uint32_t b0, uint32_t b1)
+{
+    if constexpr (std::is_same_v<T, __nv_bfloat16>)
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+    else
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+// Where a request's own token `at` lies: page (or request) and place in it; page -1 if it is not there.
+struct Place {
+    int32_t page, slot;
+};
+__device__ __forceinline__ Place place_of(const AttnDev &d, int b, int at, int end)
+{
+    if (at >= end) return Place{-1, 0};
+    if (!d.page_table) return Place{b, at};
+    const int32_t p = d.page_table[(int64_t)b * d.pts + at / d.page];
+    return Place{p >= 0 && p < d.num_pages ? p : -1, at % d.page};
+}
+
+// A warp holds MT tiles of 16 rows and walks over its share of the block's tokens, 16 at a time: scores by
+// mma.m16n8k16 (rows x tokens), weights, then rows x dim.  Its K and V tiles go through a ring of three stages
+// of its own (cp.async, no barrier between warps); the four warps' results are joined at the end.
+template <typename T, int DB, int MT>
+__global__ void __launch_bounds__(kOwnWarps * 32)
+serve_attn_own_kernel(const __grid_constant__ AttnDev d)
+{
+    constexpr int D = DB * 64, row_bytes = DB * 128, chunks = DB * 8, tile = kOwnKeys * row_bytes;
+    extern __shared__ __align__(128) uint8_t smem[];
+    __shared__ float warp_m[kOwnWarps][MT * 16], warp_l[kOwnWarps][MT * 16];
+    const int b = blockIdx.z, kv = blockIdx.y % d.kv_heads, r0 = blockIdx.y / d.kv_heads * MT * 16, split = blockIdx.x;
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, rows = d.fresh * d.group;
+    launch_next();
+    const int len = (int)min(max((int64_t)d.own_len[b], (int64_t)0), d.own_cap);
+    const int k0 = split * d.own_chunk, k1 = min(len, k0 + d.own_chunk);
+    const int part = d.prefix_parts + split;
+    if (k0 >= k1) {
+        for (int r = r0 + threadIdx.x; r < min(rows, r0 + MT * 16); r += kOwnWarps * 32)
+            d.part_ml[part * d.rows + ((int64_t)b * d.fresh + r / d.group) * d.q_heads + kv * d.group + r % d.group] =
+                make_float2(-INFINITY, 0.0f);
+        return;
+    }
+
+    // queries, as the first operand's fragments; rows and columns that do not exist are zero
+    uint32_t q[MT][DB * 4][4];
+    int limit[MT][2];                         // own tokens that a row sees
 #pragma unroll
-        for (int x = 16; x; x >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, x));
-        if (tid % 32 == 0) red[tid / 32] = top;
-        __syncthreads();
-        for (int w = 0; w < kRowThreads / 32; w++) top = fmaxf(top, red[w]);
-        // nothing seen so far: 0 in the place of -infinity, so that exp(-infinity) is 0 and NaN stays NaN
-        const float next = fmaxf(m, top), base = next == -INFINITY ? 0.0f : next, fix = exp2f(m - base);
-        p[tid] = exp2f(s - base);
-        __syncthreads();
-        l *= fix;
-        o *= fix;
-        m = next;
-        for (int x = 0; x < kRowThreads && j0 + x < total; x++) {
-            l += p[x];
-            if (tid < d.dim && p[x] != 0.0f) {
-                const int64_t at = j0 + x;
-                const T *v = at < d.prefix_len ? (const T *)d.pv + at * d.pvs[0] + kv * d.pvs[1]
-                                               : own_row<T>(d, d.ov, d.ovs, b, at - d.prefix_len, kv);
-                o += p[x] * to_f32(v[tid]);
+    for (int t = 0; t < MT; t++)
+#pragma unroll
+        for (int half = 0; half < 2; half++) {
+            const int r = r0 + t * 16 + half * 8 + lane / 4;
+            limit[t][half] = r < rows ? len - d.fresh + r / d.group + 1 : 0;
+            const T *row = (const T *)d.q + b * d.qs[0] + r / d.group * d.qs[1] + (kv * d.group + r % d.group) * d.qs[2];
+#pragma unroll
+            for (int i = 0; i < DB * 8; i++) {
+                const int c = i * 8 + lane % 4 * 2;
+                q[t][i / 2][half + i % 2 * 2] = r < rows && c < d.dim ? *(const uint32_t *)(row + c) : 0u;
             }
         }
-        __syncthreads();
+
+    const uint32_t base = smem_u32(smem) + warp * kOwnStages * 2 * tile;
+    const int blocks = (k1 - k0 + kOwnKeys - 1) / kOwnKeys, mine = (blocks - warp + kOwnWarps - 1) / kOwnWarps;
+    uint32_t there[kOwnStages];
+    const T *kbase = (const T *)d.ok + kv * d.oks[2], *vbase = (const T *)d.ov + kv * d.ovs[2];
+    // the page of the next block is looked up one block ahead, so that its latency is not in the way of the copies
+    Place ahead = place_of(d, b, k0 + warp * kOwnKeys + lane % 16, k1);
+    auto load = [&](int i, int stage) {
+        const Place p = ahead;
+        ahead = place_of(d, b, k0 + ((i + 1) * kOwnWarps + warp) * kOwnKeys + lane % 16, k1);
+        const uint32_t bits = __ballot_sync(~0u, p.page >= 0) & 0xffffu;
+        const uint32_t ks = base + stage * 2 * tile, vs = ks + tile;
+#pragma unroll
+        for (int j = 0; j < kOwnKeys * chunks / 32; j++) {
+            const int r = (j * 32 + lane) / chunks, c = lane % chunks;
+            const int32_t page = __shfl_sync(~0u, p.page, r), slot = __shfl_sync(~0u, p.slot, r);
+            const bool ok = page >= 0 && c * 8 < d.dim;
+            const uint32_t to = r * row_bytes + ((c ^ (r & 7)) << 4);
+            copy16(ks + to, ok ? kbase + page * d.oks[0] + slot * d.oks[1] + c * 8 : kbase, ok);
+            copy16(vs + to, ok ? vbase + page * d.ovs[0] + slot * d.ovs[1] + c * 8 : vbase, ok);
+        }
+        return bits;
+    };
+#pragma unroll
+    for (int i = 0; i < kOwnStages; i++) {
+        there[i] = 0;
+        if (i < kOwnStages - 1) {
+            if (i < mine) there[i] = load(i, i);
+            asm volatile("cp.async.commit_group;" ::: "memory");
+        }
     }
-    if (tid < d.dim) ((T *)d.out)[b * d.os[0] + i * d.os[1] + h * d.os[2] + tid] = from_f32<T>(l == 0.0f ? 0.0f : o / l);
-    if (d.lse && tid == 0)
-        d.lse[((int64_t)b * d.fresh + i) * d.q_heads + h] = l == 0.0f ? -INFINITY : (m + log2f(l)) * kLn2;
+
+    float o[MT][DB * 8][4], m[MT][2], l[MT][2];
+#pragma unroll
+    for (int t = 0; t < MT; t++) {
+#pragma unroll
+        for (int n = 0; n < DB * 8; n++) o[t][n][0] = o[t][n][1] = o[t][n][2] = o[t][n][3] = 0.0f;
+        m[t][0] = m[t][1] = -INFINITY;
+        l[t][0] = l[t][1] = 0.0f;
+    }
+    for (int i0 = 0; i0 < mine; i0 += kOwnStages) {
+#pragma unroll
+        for (int s = 0; s < kOwnStages; s++) {
+            const int i = i0 + s;
+            if (i >= mine) break;
+            asm volatile("cp.async.wait_group %0;" ::"n"(kOwnStages - 2) : "memory");
+            __syncwarp();
+            {
+                const int next = (s + kOwnStages - 1) % kOwnStages;       // the stage that was used up last
+                if (i + kOwnStages - 1 < mine) there[next] = load(i + kOwnStages - 1, next);
+                asm volatile("cp.async.commit_group;" ::: "memory");
+            }
+            const uint32_t ks = base + s * 2 * tile, vs = ks + tile;
+            const int at = k0 + (i * kOwnWarps + warp) * kOwnKeys;
+            float sc[MT][2][4];
+#pragma unroll
+            for (int t = 0; t < MT; t++)
+#pragma unroll
+                for (int n = 0; n < 2; n++) sc[t][n][0] = sc[t][n][1] = sc[t][n][2] = sc[t][n][3] = 0.0f;
+#pragma unroll
+            for (int k = 0; k < DB * 4; k++) {
+                uint32_t f[4];
+                const int r = lane / 16 * 8 + lane % 8, c = k * 2 + lane / 8 % 2;
+                ldmatrix(f, ks + r * row_bytes + ((c ^ (r & 7)) << 4));
+#pragma unroll
+                for (int t = 0; t < MT; t++) {
+                    mma_sync<T>(sc[t][0], q[t][k], f[0], f[1]);
+                    mma_sync<T>(sc[t][1], q[t][k], f[2], f[3]);
+                }
+            }
+            uint32_t p[MT][4];
+#pragma unroll
+            for (int t = 0; t < MT; t++)
+#pragma unroll
+                for (int half = 0; half < 2; half++) {
+                    float top = -INFINITY;
+                    bool seen[4];
+#pragma unroll
+                    for (int x = 0; x < 4; x++) {
+                        const int key = x / 2 * 8 + lane % 4 * 2 + x % 2;
+                        float &v = sc[t][x / 2][half * 2 + x % 2];
+                        seen[x] = (there[s] >> key & 1u) && at + key < limit[t][half];
+                        v *= d.scale_log2;
+                        if (seen[x]) top = fmaxf(top, v);
+                    }
+                    top = fmaxf(top, __shfl_xor_sync(~0u, top, 1));
+                    top = fmaxf(top, __shfl_xor_sync(~0u, top, 2));
+                    // nothing seen so far: 0 in the place of -infinity, so that 2^-infinity is 0 and NaN stays NaN
+                    const float next = fmaxf(m[t][half], top), from = next == -INFINITY ? 0.0f : next;
+                    const float fix = exp2_approx(m[t][half] - from);
+                    m[t][half] = next;
+                    float w[4];
+#pragma unroll
+                    for (int x = 0; x < 4; x++)
+                        w[x] = seen[x] ? exp2_approx(sc[t][x / 2][half * 2 + x % 2] - (from - kShift<T>)) : 0.0f;
+                    l[t][half] = l[t][half] * fix + ((w[0] + w[1]) + (w[2] + w[3]));
+                    p[t][half] = pack2<T>(w[0], w[1]);
+                    p[t][half + 2] = pack2<T>(w[2], w[3]);
+                    if (__any_sync(~0u, fix != 1.0f)) {
+#pragma unroll
+                        for (int n = 0; n < DB * 8; n++) {
+                            o[t][n][half * 2] *= fix;
+                            o[t][n][half * 2 + 1] *= fix;
+                        }
+                    }
+                }
+#pragma unroll
+            for (int n = 0; n < DB * 4; n++) {
+                uint32_t f[4];
+                const int r = lane / 8 % 2 * 8 + lane % 8, c = n * 2 + lane / 16;
+                ldmatrix_t(f, vs + r * row_bytes + ((c ^ (r & 7)) << 4));
+#pragma unroll
+                for (int t = 0; t < MT; t++) {
+                    mma_sync<T>(o[t][n * 2], p[t], f[0], f[1]);
+                    mma_sync<T>(o[t][n * 2 + 1], p[t], f[2], f[3]);
+                }
+            }
+            __syncwarp();
+        }
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    __syncthreads();                          // the stages' memory is free
+
+    float *all = (float *)smem;               // [warp][row][D]
+#pragma unroll
+    for (int t = 0; t < MT; t++)
+#pragma unroll
+        for (int half = 0; half < 2; half++) {
+            float sum = l[t][half];
+            sum += __shfl_xor_sync(~0u, sum, 1);
+            sum += __shfl_xor_sync(~0u, sum, 2);
+            const int r = t * 16 + half * 8 + lane / 4;
+            if (lane % 4 == 0) {
+                warp_m[warp][r] = m[t][half];
+                warp_l[warp][r] = sum;
+            }
+#pragma unroll
+            for (int n = 0; n < DB * 8; n++)
+                *(float2 *)(all + (warp * MT * 16 + r) * D + n * 8 + lane % 4 * 2) = make_float2(o[t][n][half * 2], o[t][n][half * 2 + 1]);
+        }
+    __syncthreads();
+    for (int i = threadIdx.x; i < MT * 16 * (D / 4); i += kOwnWarps * 32) {
+        const int r = i / (D / 4), c = i % (D / 4) * 4;
+        if (r0 + r >= rows || c >= d.dim) continue;
+        float top = warp_m[0][r];
+        for (int w = 1; w < kOwnWarps; w++) top = fmaxf(top, warp_m[w][r]);
+        const float from = top == -INFINITY ? 0.0f : top;
+        float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        float total = 0.0f;
+        for (int w = 0; w < kOwnWarps; w++) {
+            const float x = exp2_approx(warp_m[w][r] - from);
+            const float4 v = *(const float4 *)(all + (w * MT * 16 + r) * D + c);
+            sum.x += x * v.x;
+            sum.y += x * v.y;
+            sum.z += x * v.z;
+            sum.w += x * v.w;
+            total += x * warp_l[w][r];
+        }
+        const int64_t row = ((int64_t)b * d.fresh + (r0 + r) / d.group) * d.q_heads + kv * d.group + (r0 + r) % d.group;
+        // a row without weights may still hold NaN: l tells
+        if (c == 0) d.part_ml[part * d.rows + row] = make_float2(total == 0.0f ? -INFINITY : from - kShift<T>, total);
+        *(float4 *)(d.part_o + (part * d.rows + row) * d.dim + c) = sum;
+    }
+}
+
+// ------------------------------------------------------------------------------------------- shared prefix
+constexpr int kTileKeys = 128, kKvStages = 4, kPrefixThreads = 320;
+constexpr float kSlack = 8.0f;                // powers of two that a row's maximum may lag behind
+
+template <int DB, bool TWO> constexpr size_t prefix_smem() { return (size_t)(TWO ? 2 : 1) * DB * 16384 + (size_t)kKvStages * DB * 16384 + 1024; }
+
+__device__ __forceinline__ uint64_t pair(float a, float b)
+{
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void unpair(uint64_t v, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c)
+{
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b)
+{
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+
+// The state of one row's softmax.
+struct Row {
+    float m = -INFINITY;  // what the weights are taken against (a power of two); may lag the maximum by kSlack
+    float l = 0.0f;
+};
+
+// One tile of a row's scores (tensor memory at `s`, this thread's lane) to weights, written over them as 16-bit
+// pairs.  Where the row's maximum has grown by more than kSlack, what is summed so far (accumulator at `o`) is
+// scaled down first; below that the weights just grow past 1, by at most 2^kSlack.
+template <typename T, bool MASK>
+__device__ __forceinline__ void softmax_tile(Row &row, uint32_t s, uint32_t o, bool first, int valid, int columns, float c)
+{
+    uint32_t x[128];
+#pragma unroll
+    for (int i = 0; i < 4; i++) tmem_load32(s + i * 32, x + i * 32);
+#pragma unroll
+    for (int i = 0; i < 4; i++) tmem_wait_load32(x + i * 32);
+    if (MASK) {
+#pragma unroll
+        for (int i = 1; i < 128; i++)
+            if (i >= valid) x[i] = x[0];              // the tile's first token is always there
+    }
+    float t0 = __uint_as_float(x[0]), t1 = __uint_as_float(x[1]), t2 = __uint_as_float(x[2]), t3 = __uint_as_float(x[3]);
+    if (c >= 0.0f) {
+#pragma unroll
+        for (int i = 4; i < 128; i += 4) {
+            t0 = fmaxf(t0, __uint_as_float(x[i]));
+            t1 = fmaxf(t1, __uint_as_float(x[i + 1]));
+            t2 = fmaxf(t2, __uint_as_float(x[i + 2]));
+            t3 = fmaxf(t3, __uint_as_float(x[i + 3]));
+        }
+        t0 = fmaxf(fmaxf(t0, t1), fmaxf(t2, t3));
+    } else {
+#pragma unroll
+        for (int i = 4; i < 128; i += 4) {
+            t0 = fminf(t0, __uint_as_float(x[i]));
+            t1 = fminf(t1, __uint_as_float(x[i + 1]));
+            t2 = fminf(t2, __uint_as_float(x[i + 2]));
+            t3 = fminf(t3, __uint_as_float(x[i + 3]));
+        }
+        t0 = fminf(fminf(t0, t1), fminf(t2, t3));
+    }
+    // NaN scores leave the maximum alone (NaN * c is dropped by fmaxf) and become NaN weights
+    const float top = fmaxf(row.m, t0 * c);
+    const bool grow = top > row.m + (first ? 0.0f : kSlack);
+    const float next = grow ? top : row.m, from = next == -INFINITY ? 0.0f : next;
+    if (!first && __any_sync(~0u, grow)) {
+        const float fix = grow ? exp2_approx(row.m - from) : 1.0f;
+        row.l *= fix;
+        for (int i = 0; i < columns; i += 16) {
+            uint32_t v[16];
+            tmem_load16(o + i, v);
+            tmem_wait_load16(v);
+#pragma unroll
+            for (int k = 0; k < 16; k++) v[k] = __float_as_uint(__uint_as_float(v[k]) * fix);
+            tmem_store16(o + i, v);
+        }
+    }
+    row.m = next;
+    const uint64_t cc = pair(c, c), ff = pair(kShift<T> - from, kShift<T> - from);
+    uint64_t sum0 = 0, sum1 = 0;                      // pairs of 0.0f
+    uint32_t w[64];
+#pragma unroll
+    for (int i = 0; i < 64; i++) {
+        float a, b;
+        unpair(fma2(pair(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1])), cc, ff), a, b);
+        a = exp2_approx(a);
+        b = exp2_approx(b);
+        if (MASK) {
+            if (2 * i >= valid) a = 0.0f;
+            if (2 * i + 1 >= valid) b = 0.0f;
+        }
+        if (i & 1) sum1 = add2(sum1, pair(a, b));
+        else sum0 = add2(sum0, pair(a, b));
+        w[i] = pack2<T>(a, b);
+        if (i == 31) tmem_store32(s, w);
+    }
+    tmem_store32(s + 32, w + 32);
+    float a, b;
+    unpair(add2(sum0, sum1), a, b);
+    row.l += a + b;
+    tmem_wait_store();
+}
+
+// TWO: two tiles of 128 rows, each with its own softmax warps and accumulator, take the same tokens, so that
+// one tile's matrix products run under the other's exponentials.  Otherwise (128 rows or fewer) the two halves share
+// the rows and take every other tile of tokens, and their results are two parts.
+template <typename T, int DB, bool TWO>
+__global__ void __launch_bounds__(kPrefixThreads, 1)
+serve_attn_prefix_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+                         const __grid_constant__ AttnDev d)
+{
+    constexpr int block = kTileKeys * 128, stage = DB * block;        // 64 columns of a tile; a tile
+    extern __shared__ uint8_t raw_smem[];
+    __shared__ __align__(8) uint64_t bars[2 * kKvStages + 8];
+    __shared__ uint32_t tmem_at;
+    __shared__ int gave_up;
+    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
+    const int rows = d.batch * d.fresh * d.group;                     // of one key/value head
+    const int rt = blockIdx.x % d.row_tiles, kv = blockIdx.x / d.row_tiles % d.kv_heads, split = blockIdx.x / d.row_tiles / d.kv_heads;
+    const int r0 = rt * (TWO ? 256 : 128);
+    const int tiles = (d.prefix_len + kTileKeys - 1) / kTileKeys;
+    const int j0 = (int)((int64_t)tiles * split / d.prefix_splits), nt = (int)((int64_t)tiles * (split + 1) / d.prefix_splits) - j0;
+    launch_next();
+
+    uint8_t *smem = (uint8_t *)(((uintptr_t)raw_smem + 1023) & ~(uintptr_t)1023);
+    uint8_t *qs = smem;
+    const uint32_t q_at = smem_u32(qs), kv_at = q_at + (TWO ? 2 : 1) * stage;
+    const uint32_t full = smem_u32(bars), empty = full + 8 * kKvStages, q_full = empty + 8 * kKvStages, s_full = q_full + 8,
+                   p_full = s_full + 16, o_full = p_full + 16, drained = o_full + 16;
+    if (tid == 0) {
+        gave_up = 0;
+        for (int i = 0; i < kKvStages; i++) {
+            mbar_init(full + 8 * i, 1);
+            mbar_init(empty + 8 * i, 1);
+        }
+        mbar_init(q_full, 256);
+        for (int i = 0; i < 2; i++) {
+            mbar_init(s_full + 8 * i, 1);
+            mbar_init(p_full + 8 * i, 128);
+            mbar_init(o_full + 8 * i, 1);
+        }
+        mbar_init(drained, 1);
+        mbar_init_fence();
+        tma_prefetch(&map_k);
+        tma_prefetch(&map_v);
+    }
+    if (warp == 9) tmem_alloc(smem_u32(&tmem_at), 512);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = tmem_at;                                    // scores 0, 128; accumulators 256, 384
+
+    if (warp == 8) {
+        if (lane == 0) {
+            // ---- loads, in the order the matrix products take them
+            Ring<kKvStages> ring;
+            int issued = 0;
+            auto load = [&](const CUtensorMap *map, int j) {
+                if (!mbar_wait(empty + 8 * ring.slot, ring.parity ^ 1u, &gave_up)) return false;
+                mbar_expect(full + 8 * ring.slot, stage);
+                for (int i = 0; i < DB; i++)
+                    tma_load(kv_at + ring.slot * stage + i * block, map, i * 64, (j0 + j) * kTileKeys, kv, full + 8 * ring.slot);
+                issued++;
+                ring.step();
+                return true;
+            };
+            bool ok = load(&map_k, 0);
+            for (int j = 0; j < nt && ok; j++) {
+                if (TWO) {
+                    ok = load(&map_v, j) && (j + 1 == nt || load(&map_k, j + 1));
+                } else {
+                    ok = (j + 1 == nt || load(&map_k, j + 1)) && load(&map_v, j);
+                }
+            }
+            if (gave_up) {
+                Ring<kKvStages> r;
+                for (int i = 0; i < issued; i++) {
+                    if (i + kKvStages >= issued) mbar_drain(full + 8 * r.slot, r.parity);
+                    r.step();
+                }
+            }
+        }
+        __syncwarp();
+    } else if (warp == 9) {
+        if (lane == 0) {
+            // ---- matrix products
+            const int n = (d.dim + 15) / 16 * 16;
+            const uint32_t s_desc = mma_desc<T>(128, kTileKeys), o_desc = mma_desc<T>(128, n, true);
+            Ring<kKvStages> ring;
+            auto scores = [&](int w, uint32_t k_at) {                 // S_w = Q_w K^T
+                for (int i = 0; i < n / 16; i++)
+                    mma_ss(tmem + w * 128, smem_desc(q_at + (TWO ? w : 0) * stage + i / 4 * block) + 2 * (i % 4),
+                           smem_desc(k_at + i / 4 * block) + 2 * (i % 4), s_desc, i > 0);
+                mma_commit(s_full + 8 * w);
+            };
+            auto values = [&](int w, uint32_t v_at, bool add) {       // O_w += P_w V
+                for (int i = 0; i < kTileKeys / 16; i++)
+                    mma_ts(tmem + 256 + w * 128, tmem + w * 128 + i * 8, smem_desc(v_at + i * 2048, block), o_desc, add || i > 0);
+            };
+            auto wait_full = [&](uint32_t &at) {
+                if (!mbar_wait(full + 8 * ring.slot, ring.parity, &gave_up)) return -1;
+                tc_fence_after();
+                at = kv_at + ring.slot * stage;
+                const int slot = ring.slot;
+                ring.step();
+                return slot;
+            };
+            auto wait_weights = [&](int w, int it) {
+                if (!mbar_wait(p_full + 8 * w, it & 1, &gave_up)) return false;
+                tc_fence_after();
+                return true;
+            };
+            auto run = [&]() {
+                uint32_t k_at, v_at;
+                int ks, vs;
+                if (!mbar_wait(q_full, 0, &gave_up) || (ks = wait_full(k_at)) < 0) return;
+                scores(0, k_at);
+                if (TWO) {
+                    scores(1, k_at);
+                    mma_commit(empty + 8 * ks);
+                    for (int j = 0; j < nt; j++) {
+                        if ((vs = wait_full(v_at)) < 0 || !wait_weights(0, j)) return;
+                        values(0, v_at, j > 0);
+                        if (j + 1 < nt) {
+                            if ((ks = wait_full(k_at)) < 0) return;
+                            scores(0, k_at);
+                        } else {
+                            mma_commit(o_full);
+                        }
+                        if (!wait_weights(1, j)) return;
+                        values(1, v_at, j > 0);
+                        mma_commit(empty + 8 * vs);
+                        if (j + 1 < nt) {
+                            scores(1, k_at);
+                            mma_commit(empty + 8 * ks);
+                        } else {
+                            mma_commit(o_full + 8);
+                        }
+                    }
+                } else {
+                    mma_commit(empty + 8 * ks);
+                    if (nt > 1) {
+                        if ((ks = wait_full(k_at)) < 0) return;
+                        scores(1, k_at);
+                        mma_commit(empty + 8 * ks);
+                    }
+                    for (int j = 0; j < nt; j++) {
+                        const int w = j & 1;
+                        if ((vs = wait_full(v_at)) < 0 || !wait_weights(w, j / 2)) return;
+                        values(w, v_at, j > 1);
+                        mma_commit(empty + 8 * vs);
+                        if (j + 2 < nt) {
+                            if ((ks = wait_full(k_at)) < 0) return;
+                            scores(w, k_at);
+                            mma_commit(empty + 8 * ks);
+                        } else {
+                            mma_commit(o_full + 8 * w);
+                        }
+                    }
+                }
+            };
+            run();
+            if (gave_up) {
+                mma_commit(drained);
+                mbar_drain(drained, 0);
+            }
+        }
+        __syncwarp();
+    } else {
+        // ---- queries into the swizzled layout; rows and columns that do not exist are zero
+        const int w = warp / 4, live = min(rows - r0, TWO ? 256 : 128);
+        for (int i = tid; i < (TWO ? 256 : 128) * DB * 8; i += 256) {
+            const int r = i / (DB * 8), c = i % (DB * 8), g = r0 + r;
+            uint4 v = make_uint4(0, 0, 0, 0);
+            if (r < live && c * 8 < d.dim) {
+                const int b = g / (d.fresh * d.group), t = g / d.group % d.fresh, h = kv * d.group + g % d.group;
+                v = *(const uint4 *)((const T *)d.q + b * d.qs[0] + t * d.qs[1] + h * d.qs[2] + c * 8);
+            }
+            *(uint4 *)(qs + r / 128 * stage + c / 8 * block + r % 128 * 128 + (((c % 8) ^ (r & 7)) << 4)) = v;
+        }
+        fence_async_proxy();
+        mbar_arrive(q_full);
+
+        // ---- softmax: one thread per row
+        const int quarter = warp % 4, r = (TWO ? w * 128 : 0) + quarter * 32 + lane;
+        const uint32_t lanes = (uint32_t)(quarter * 32) << 16, s_at = tmem + lanes + w * 128, o_at = tmem + lanes + 256 + w * 128;
+        const bool busy = (TWO ? w * 128 : 0) + quarter * 32 < live;  // some row of this warp exists
+        const int mine = TWO ? nt : (nt - w + 1) / 2, columns = (d.dim + 15) / 16 * 16;
+        Row row;
+        bool ok = true;
+        for (int it = 0; it < mine; it++) {
+            ok = mbar_wait(s_full + 8 * w, it & 1, &gave_up);
+            if (!__all_sync(~0u, ok)) {
+                ok = false;
+                break;
+            }
+            tc_fence_after();
+            const int valid = d.prefix_len - (j0 + (TWO ? it : 2 * it + w)) * kTileKeys;
+            if (busy) {
+                if (valid >= kTileKeys) softmax_tile<T, false>(row, s_at, o_at, it == 0, kTileKeys, columns, d.scale_log2);
+                else softmax_tile<T, true>(row, s_at, o_at, it == 0, valid, columns, d.scale_log2);
+            }
+            tc_fence_before();
+            mbar_arrive(p_full + 8 * w);
+        }
+        if (mine > 0 && ok) {
+            ok = mbar_wait(o_full + 8 * w, 0, &gave_up);
+            ok = __all_sync(~0u, ok);
+            tc_fence_after();
+        }
+        if (busy && ok) {
+            const int g = r0 + r, part = TWO ? split : 2 * split + w;
+            const bool exists = r < live;
+            const int64_t at = part * d.rows + ((int64_t)(g / (d.fresh * d.group)) * d.fresh + g / d.group % d.fresh) * d.q_heads +
+                               kv * d.group + g % d.group;
+            if (exists) d.part_ml[at] = make_float2(row.l == 0.0f ? -INFINITY : (row.m == -INFINITY ? 0.0f : row.m) - kShift<T>, row.l);
+            if (mine > 0) {
+                for (int c = 0; c < columns; c += 16) {
+                    uint32_t v[16];
+                    tmem_load16(o_at + c, v);
+                    tmem_wait_load16(v);
+#pragma unroll
+                    for (int k = 0; k < 16; k += 4)
+                        if (exists && c + k < d.dim) *(uint4 *)(d.part_o + at * d.dim + c + k) = *(const uint4 *)(v + k);
+                }
+            }
+        }
+        tc_fence_before();
+    }
+    __syncthreads();
+    tc_fence_after();
+    if (warp == 9) tmem_free(tmem, 512);
+    if (tid == 0 && gave_up) atomicExch(d.status, 1);
+    wait_previous();                                                  // the own kernel's parts are the join's input too
+}
+
+// ------------------------------------------------------------------------------------------- join
+constexpr int kJoinThreads = 128;
+
+template <typename T>
+__global__ void __launch_bounds__(kJoinThreads)
+serve_attn_join_kernel(const __grid_constant__ AttnDev d)
+{
+    const int64_t row = (int64_t)blockIdx.x * (kJoinThreads / 32) + threadIdx.x / 32;
+    const int lane = threadIdx.x % 32;
+    wait_previous();
+    if (row >= d.rows) return;
+    float top = -INFINITY;
+    for (int p = lane; p < d.parts; p += 32) top = fmaxf(top, d.part_ml[p * d.rows + row].x);
+#pragma unroll
+    for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
+    const float from = top == -INFINITY ? 0.0f : top;
+    float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    float total = 0.0f;
+    const bool live = lane * 4 < d.dim;
+#pragma unroll 4
+    for (int p = 0; p < d.parts; p++) {
+        const float2 ml = d.part_ml[p * d.rows + row];
+        if (ml.x == -INFINITY) continue;              // holds nothing, and what its sums hold is not defined
+        const float w = exp2_approx(ml.x - from);
+        total += w * ml.y;
+        if (live) {
+            const float4 v = *(const float4 *)(d.part_o + (p * d.rows + row) * d.dim + lane * 4);
+            sum.x += w * v.x;
+            sum.y += w * v.y;
+            sum.z += w * v.z;
+            sum.w += w * v.w;
+        }
+    }
+    const float inv = total == 0.0f ? 0.0f : 1.0f / total;
+    const int h = (int)(row % d.q_heads), i = (int)(row / d.q_heads % d.fresh), b = (int)(row / d.q_heads / d.fresh);
+    if (live)
+        *(uint2 *)((T *)d.out + b * d.os[0] + i * d.os[1] + h * d.os[2] + lane * 4) =
+            make_uint2(pack2<T>(sum.x * inv, sum.y * inv), pack2<T>(sum.z * inv, sum.w * inv));
+    if (d.lse && lane == 0) d.lse[row] = total == 0.0f ? -INFINITY : (from + log2f(total)) * kLn2;
 }
 
 int check_shape(const bcast_serve_attn_args &a)
@@ -91,8 +689,89 @@ int check_shape(const bcast_serve_attn_args &a)
         return BCAST_ERR_INVAL;
     if (a.dim < 8 || a.dim > 128 || a.dim % 8) return BCAST_ERR_INVAL;
     if (a.prefix_len < 0 || a.prefix_len > kMaxDim - 65536 || a.own_cap < 0 || a.own_cap > kMaxDim - 65536) return BCAST_ERR_INVAL;
-    if ((int64_t)a.batch * a.new_tokens * a.q_heads > kMaxDim) return BCAST_ERR_INVAL;
+    if ((int64_t)a.new_tokens * a.q_heads > (1 << 19) || (int64_t)a.batch * a.new_tokens * a.q_heads > (1 << 24)) return BCAST_ERR_INVAL;
     return BCAST_OK;
+}
+
+// How a call is cut: rows of a key/value head into tiles, the prefix and the own tokens into parts.
+struct Cut {
+    bool two;                                 // 256 rows to a block of the prefix kernel
+    int64_t rows, row_tiles, prefix_splits, prefix_parts, own_tiles, own_chunk, own_splits, parts;
+};
+
+Cut cut_of(const bcast_serve_attn_args &a)
+{
+    Cut c = {};
+    const int64_t group = a.q_heads / a.kv_heads, head_rows = (int64_t)a.batch * a.new_tokens * group;
+    c.rows = head_rows * a.kv_heads;
+    c.two = head_rows > 128;
+    if (a.prefix_len > 0 && c.rows > 0) {
+        c.row_tiles = ceil_div(head_rows, c.two ? 256 : 128);
+        const int64_t items = c.row_tiles * a.kv_heads, tiles = ceil_div(a.prefix_len, 128);
+        // the number of parts that ends first, one block to an SM: a block costs its tiles and about four more to
+        // begin and to end
+        int64_t best = INT64_MAX;
+        for (int64_t s = 1; s <= tiles && s <= 64; s++) {
+            const int64_t cost = ceil_div(items * s, kSms) * (ceil_div(tiles, s) + 4);
+            if (cost < best) {
+                best = cost;
+                c.prefix_splits = s;
+            }
+        }
+        c.prefix_parts = c.prefix_splits * (c.two ? 1 : 2);
+    }
+    if (a.own_cap > 0 && c.rows > 0) {
+        const int64_t own_rows = a.new_tokens * group;
+        c.own_tiles = ceil_div(own_rows, own_rows > 16 ? 32 : 16);
+        // parts of at least 128 tokens, until there are about four blocks for every SM
+        const int64_t blocks = (int64_t)a.batch * a.kv_heads * c.own_tiles;
+        int64_t s = ceil_div(4 * kSms, blocks);
+        s = s < ceil_div(a.own_cap, 128) ? s : ceil_div(a.own_cap, 128);
+        c.own_chunk = round_up(ceil_div(a.own_cap, s), 64);
+        c.own_splits = ceil_div(a.own_cap, c.own_chunk);
+    }
+    c.parts = c.prefix_parts + c.own_splits;
+    return c;
+}
+
+int64_t workspace_of(const bcast_serve_attn_args &a, const Cut &c)
+{
+    return BCAST_SERVE_STATUS_BYTES + round_up(c.parts * c.rows * 8, 256) + c.parts * c.rows * a.dim * 4;
+}
+
+template <typename T, int DB, int MT>
+int run_own(const bcast_serve_attn_args &a, const AttnDev &d, const Cut &c, cudaStream_t st)
+{
+    int rc;
+    if ((rc = allow_smem<serve_attn_own_kernel<T, DB, MT>>(own_smem<DB>()))) return rc;
+    return launch(serve_attn_own_kernel<T, DB, MT>, dim3((unsigned)c.own_splits, (unsigned)(a.kv_heads * c.own_tiles), a.batch),
+                  dim3(kOwnWarps * 32), own_smem<DB>(), st, false, 1, d);
+}
+
+template <typename T, int DB, bool TWO>
+int run_prefix(const bcast_serve_attn_args &a, const AttnDev &d, const Cut &c, cudaStream_t st)
+{
+    const auto type = std::is_same_v<T, __nv_bfloat16> ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+    CUtensorMap mk, mv;
+    int rc;
+    if ((rc = tensor_map(&mk, type, a.prefix_k, {a.dim, a.prefix_len, a.kv_heads}, {a.prefix_k_stride[0], a.prefix_k_stride[1]}, {64, kTileKeys, 1})))
+        return rc;
+    if ((rc = tensor_map(&mv, type, a.prefix_v, {a.dim, a.prefix_len, a.kv_heads}, {a.prefix_v_stride[0], a.prefix_v_stride[1]}, {64, kTileKeys, 1})))
+        return rc;
+    const size_t smem = prefix_smem<DB, TWO>();
+    if ((rc = allow_smem<serve_attn_prefix_kernel<T, DB, TWO>>(smem))) return rc;
+    return launch(serve_attn_prefix_kernel<T, DB, TWO>, dim3((unsigned)(c.row_tiles * a.kv_heads * c.prefix_splits)), dim3(kPrefixThreads), smem, st,
+                  c.own_splits > 0, 1, mk, mv, d);
+}
+
+template <typename T, int DB>
+int run(const bcast_serve_attn_args &a, const AttnDev &d, const Cut &c, cudaStream_t st)
+{
+    int rc = BCAST_OK;
+    if (c.own_splits) rc = a.new_tokens * d.group > 16 ? run_own<T, DB, 2>(a, d, c, st) : run_own<T, DB, 1>(a, d, c, st);
+    if (!rc && c.prefix_splits) rc = c.two ? run_prefix<T, DB, true>(a, d, c, st) : run_prefix<T, DB, false>(a, d, c, st);
+    if (rc) return rc;
+    return launch(serve_attn_join_kernel<T>, dim3((unsigned)ceil_div(c.rows, kJoinThreads / 32)), dim3(kJoinThreads), 0, st, c.parts > 0, 1, d);
 }
 
 }  // namespace
@@ -105,7 +784,7 @@ extern "C" {
 int64_t bcast_serve_attn_workspace(const bcast_serve_attn_args *a)
 {
     if (!a || check_shape(*a)) return BCAST_ERR_INVAL;
-    return BCAST_SERVE_STATUS_BYTES;
+    return workspace_of(*a, cut_of(*a));
 }
 
 int bcast_serve_attn(const bcast_serve_attn_args *a, void *cuda_stream)
@@ -117,12 +796,11 @@ int bcast_serve_attn(const bcast_serve_attn_args *a, void *cuda_stream)
     if (!(a->scale == a->scale) || a->scale > 1e30f || a->scale < -1e30f) return BCAST_ERR_INVAL;
     const bool paged = a->own_cap && a->page_table;
     for (int i = 0; i < 3; i++) {
-        const int64_t least = i == 2 ? a->dim : 0;
-        if (!stride_ok(a->q_stride[i], 0, 8) || !stride_ok(a->out_stride[i], least, 8)) return BCAST_ERR_INVAL;
+        if (!stride_ok(a->q_stride[i], 0, 8) || !stride_ok(a->out_stride[i], a->dim, 8)) return BCAST_ERR_INVAL;
         if (a->own_cap && (!stride_ok(a->own_k_stride[i], 0, 8) || !stride_ok(a->own_v_stride[i], 0, 8))) return BCAST_ERR_INVAL;
     }
     for (int i = 0; i < 2 && a->prefix_len; i++)
-        if (!stride_ok(a->prefix_k_stride[i], 0, 8) || !stride_ok(a->prefix_v_stride[i], 0, 8)) return BCAST_ERR_INVAL;
+        if (!stride_ok(a->prefix_k_stride[i], a->dim, 8) || !stride_ok(a->prefix_v_stride[i], a->dim, 8)) return BCAST_ERR_INVAL;
     if (paged && (a->page_size < 1 || a->num_pages < 0 || a->num_pages > kMaxDim ||
                   !stride_ok(a->page_table_stride, ceil_div(a->own_cap, a->page_size), 1)))
         return BCAST_ERR_INVAL;
@@ -136,41 +814,46 @@ int bcast_serve_attn(const bcast_serve_attn_args *a, void *cuda_stream)
     if (a->lse && (rc = check_array(a->lse, 4, dev.id))) return rc;
     if ((rc = check_workspace(a->workspace, a->workspace_bytes, bcast_serve_attn_workspace(a), dev.id))) return rc;
 
-    AttnDev d;
+    const Cut c = cut_of(*a);
+    AttnDev d = {};
     d.q = a->q;
-    d.pk = a->prefix_k;
-    d.pv = a->prefix_v;
     d.ok = a->own_k;
     d.ov = a->own_v;
     d.own_len = a->own_len;
     d.page_table = paged ? a->page_table : nullptr;
     d.out = a->out;
     d.lse = a->lse;
+    d.status = (int *)a->workspace;
+    d.part_ml = (float2 *)((char *)a->workspace + BCAST_SERVE_STATUS_BYTES);
+    d.part_o = (float *)((char *)d.part_ml + round_up(c.parts * c.rows * 8, 256));
     for (int i = 0; i < 3; i++) {
         d.qs[i] = a->q_stride[i];
         d.os[i] = a->out_stride[i];
         d.oks[i] = a->own_k_stride[i];
         d.ovs[i] = a->own_v_stride[i];
     }
-    for (int i = 0; i < 2; i++) {
-        d.pks[i] = a->prefix_k_stride[i];
-        d.pvs[i] = a->prefix_v_stride[i];
-    }
-    d.prefix_len = a->prefix_len;
     d.own_cap = a->own_cap;
     d.num_pages = a->num_pages;
     d.pts = a->page_table_stride;
+    d.rows = c.rows;
     d.batch = a->batch;
     d.fresh = a->new_tokens;
     d.q_heads = a->q_heads;
+    d.kv_heads = a->kv_heads;
     d.group = a->q_heads / a->kv_heads;
     d.dim = a->dim;
     d.page = paged ? a->page_size : 1;
+    d.prefix_len = (int32_t)a->prefix_len;
+    d.prefix_splits = (int32_t)c.prefix_splits;
+    d.prefix_parts = (int32_t)c.prefix_parts;
+    d.row_tiles = (int32_t)c.row_tiles;
+    d.own_splits = (int32_t)c.own_splits;
+    d.own_chunk = (int32_t)c.own_chunk;
+    d.parts = (int32_t)c.parts;
     d.scale_log2 = a->scale * kLog2e;
     const cudaStream_t st = (cudaStream_t)cuda_stream;
-    const dim3 grid(a->q_heads, a->new_tokens, a->batch);
-    if (a->dtype == BCAST_SERVE_BF16) return launch(serve_attn_row_kernel<__nv_bfloat16>, grid, dim3(kRowThreads), 0, st, false, 1, d);
-    return launch(serve_attn_row_kernel<__half>, grid, dim3(kRowThreads), 0, st, false, 1, d);
+    if (a->dtype == BCAST_SERVE_BF16) return a->dim > 64 ? run<__nv_bfloat16, 2>(*a, d, c, st) : run<__nv_bfloat16, 1>(*a, d, c, st);
+    return a->dim > 64 ? run<__half, 2>(*a, d, c, st) : run<__half, 1>(*a, d, c, st);
 }
 
 }  // extern "C"
