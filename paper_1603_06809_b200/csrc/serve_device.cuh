@@ -112,13 +112,21 @@ __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap *m, int
 __device__ __forceinline__ void fence_async_proxy() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
 // ------------------------------------------------------------------------------------------- tcgen05
-// Shared-memory matrix descriptor for tiles whose rows are 128 bytes in the 128-byte swizzle (what TMA writes;
-// tiles start on 1024 bytes).  K-major operands: eight rows are 1024 bytes (the stride field), a step of 16
-// values along k is 32 bytes further.  MN-major operands (the contiguous dimension is not k): eight k are
-// 1024 bytes, and the next 64 values of the other dimension are `lead` bytes further.
-__device__ __forceinline__ uint64_t smem_desc(uint32_t addr, uint32_t lead = 16)
+// Shared-memory matrix descriptor for tiles whose rows are `row` = 32, 64 or 128 bytes, in the swizzle of that
+// width (what TMA writes; tiles start on eight rows).  K-major operands: the stride field is eight rows, a step of
+// 16 values along k is 32 bytes further.  MN-major operands (the contiguous dimension is not k; row = 128): eight
+// k are 1024 bytes, and the next 64 values of the other dimension are `lead` bytes further.
+__device__ __forceinline__ uint64_t smem_desc(uint32_t addr, uint32_t lead = 16, uint32_t row = 128)
 {
-    return (uint64_t)((addr >> 4) & 0x3fffu) | (uint64_t)((lead >> 4) & 0x3fffu) << 16 | (uint64_t)(1024 >> 4) << 32 | 1ull << 46 | 2ull << 61;
+    const uint64_t swizzle = row == 128 ? 2 : row == 64 ? 4 : 6;
+    return (uint64_t)((addr >> 4) & 0x3fffu) | (uint64_t)((lead >> 4) & 0x3fffu) << 16 | (uint64_t)(row * 8 >> 4) << 32 | 1ull << 46 |
+           swizzle << 61;
+}
+// Where that swizzle puts 16-byte chunk `c` of row `r`: bytes from the tile's start.  Chunk numbers are XORed
+// with the bits of the row that make up address bits 7 and up.
+__device__ __forceinline__ uint32_t swizzled(uint32_t r, uint32_t c, uint32_t row)
+{
+    return r * row + ((c ^ (row == 128 ? r & 7u : row == 64 ? r >> 1 & 3u : r >> 2 & 1u)) << 4);
 }
 // Instruction descriptor, kind::f16: 32-bit accumulators, both operands of type T.
 template <typename T>

@@ -1,4 +1,4 @@
-// Tensor maps for TMA loads of 16-bit tiles whose rows are 64 values (128 bytes, 128-byte swizzle).
+// Tensor maps for TMA loads of 16-bit tiles whose rows are 16, 32 or 64 values, in the swizzle of their width.
 #pragma once
 #include <cuda.h>
 #include <cudaTypedefs.h>
@@ -39,8 +39,10 @@ inline int tensor_map(CUtensorMap *map, CUtensorMapDataType type, const void *ba
     for (int64_t v : stride) st[n++] = (cuuint64_t)v * 2;
     n = 0;
     for (int64_t v : box) b[n++] = (cuuint32_t)v;
+    const int64_t row = *box.begin() * 2;
+    const auto swizzle = row == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : row == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_32B;
     const CUresult r = encode(map, type, n, const_cast<void *>(base), s, st, b, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+                              swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS ? BCAST_OK : bcast_internal_cuda_failed((int)cudaErrorInvalidValue);
 }
 
