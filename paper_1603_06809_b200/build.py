@@ -1,13 +1,16 @@
-"""Build the C-ABI library (libbcast_b200.so) in-tree with nvcc for sm_100a.
+"""Build the C-ABI library (libbcast_b200.so) in-tree with nvcc for sm_100a, and the extension module
+that hands torch tensors to its serving operators (_serve_native.so) with the host compiler.
 
-Run as ``python -m paper_1603_06809_b200.build`` or call :func:`build`.  The shared object is
-placed next to this file so that it travels with the source tree.
+Run as ``python -m paper_1603_06809_b200.build`` or call :func:`build`.  The shared objects are
+placed next to this file so that they travel with the source tree.
 """
 from __future__ import annotations
 
 import os
+import shutil
 import subprocess
 import sys
+import sysconfig
 
 PKG_DIR = os.path.dirname(os.path.abspath(__file__))
 REPO_DIR = os.path.dirname(PKG_DIR)
@@ -20,36 +23,60 @@ HEADERS = [os.path.join(REPO_DIR, "include", f) for f in ("bcast.h", "bcast_serv
 
 NVCC_FLAGS = [
     "-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
-    "-Xcompiler", "-fPIC", "-shared", "-I", os.path.join(REPO_DIR, "include"),
+    "-Xcompiler", "-fPIC", "-shared", "-Xlinker", "-soname=libbcast_b200.so", "-I", os.path.join(REPO_DIR, "include"),
 ]
 
 
+BIND_PATH = os.path.join(PKG_DIR, "_serve_native.so")
+BIND_SOURCES = [os.path.join(PKG_DIR, "csrc", "serve_bind.cpp")]
+BIND_HEADERS = [os.path.join(REPO_DIR, "include", f) for f in ("bcast.h", "bcast_serve.h")]
+
+
+def _older(path: str, sources) -> bool:
+    return not os.path.exists(path) or any(os.path.getmtime(f) > os.path.getmtime(path) for f in sources)
+
+
 def needs_build() -> bool:
-    if not os.path.exists(LIB_PATH):
-        return True
-    t = os.path.getmtime(LIB_PATH)
-    return any(os.path.getmtime(f) > t for f in SOURCES + HEADERS)
+    return _older(LIB_PATH, SOURCES + HEADERS) or _older(BIND_PATH, BIND_SOURCES + BIND_HEADERS)
+
+
+def _run(cmd, path: str) -> None:
+    """Run a compiler command that ends in the name of its output, and put that in place of ``path``."""
+    tmp = path + f".{os.getpid()}.tmp"
+    subprocess.check_call([*cmd, "-o", tmp])
+    os.replace(tmp, path)
+
+
+def _build_bind(nvcc: str) -> None:
+    import torch
+    troot = os.path.dirname(torch.__file__)
+    cuda = os.path.dirname(os.path.dirname(os.path.realpath(shutil.which(nvcc) or nvcc)))
+    include = [os.path.join(REPO_DIR, "include"), os.path.join(troot, "include"), os.path.join(troot, "include", "torch", "csrc", "api", "include"),
+               os.path.join(cuda, "include"), sysconfig.get_paths()["include"]]
+    _run([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-DTORCH_API_INCLUDE_EXTENSION_H",
+          f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", *[a for d in include for a in ("-isystem", d)], *BIND_SOURCES,
+          LIB_PATH, f"-L{troot}/lib", "-lc10", "-lc10_cuda", "-ltorch", "-ltorch_cpu", "-ltorch_python",
+          "-Wl,-rpath,$ORIGIN", f"-Wl,-rpath,{troot}/lib"], BIND_PATH)
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
     """Compile the library if it is missing or older than its sources; return its path."""
-    if force or needs_build():
-        nvcc = os.environ.get("NVCC", "nvcc")
-        tmp = LIB_PATH + f".{os.getpid()}.tmp"
-        cmd = [nvcc, *NVCC_FLAGS, *(["-Xptxas", "-v"] if verbose else []), "-o", tmp, *SOURCES]
-        subprocess.check_call(cmd)
-        os.replace(tmp, LIB_PATH)
+    nvcc = os.environ.get("NVCC", "nvcc")
+    if force or _older(LIB_PATH, SOURCES + HEADERS):
+        _run([nvcc, *NVCC_FLAGS, *(["-Xptxas", "-v"] if verbose else []), *SOURCES], LIB_PATH)
+    if force or _older(BIND_PATH, BIND_SOURCES + BIND_HEADERS):
+        _build_bind(nvcc)
     return LIB_PATH
 
 
 def ensure_built() -> str:
-    """Build the library if it is missing; if it is merely older than its sources, try to rebuild
+    """Build what is missing; if it is merely older than its sources, try to rebuild
     and keep the existing one when no compiler is at hand.  Returns the path of the library."""
-    if not os.path.exists(LIB_PATH):
-        return build(force=True)
+    if not os.path.exists(LIB_PATH) or not os.path.exists(BIND_PATH):
+        return build()
     if needs_build():
         try:
-            return build(force=True)
+            return build()
         except (OSError, subprocess.CalledProcessError):
             pass
     return LIB_PATH

@@ -93,6 +93,27 @@ def test_tensors_on_the_host_are_refused():
         S.bcast_serve_verify(torch.zeros(1, 1, 4), torch.zeros(1, 0, 4), torch.zeros(1, 0, dtype=torch.int32), torch.zeros(1, 0), torch.ones(1, 4), torch.ones(1))
 
 
+def test_tensors_that_do_not_fit_together_are_refused_by_name():
+    bf = dict(dtype=torch.bfloat16)
+    x, w = torch.zeros(2, 64, **bf), torch.zeros(8, 64, **bf)
+    a, b, ad, sc = torch.zeros(3, 8, 64, **bf), torch.zeros(3, 8, 8, **bf), torch.zeros(2, dtype=torch.int32), torch.ones(3)
+    good = dict(lora_a=a, lora_b=b, adapter=ad, scale=sc)
+    for change, word in ((dict(bias=torch.zeros(9, **bf)), "bias"), (dict(lora_b=None), "go together"), (dict(adapter=ad.long()), "adapter"),
+                         (dict(scale=sc.double()), "scale"), (dict(lora_a=a[0]), "three dimensions"), (dict(lora_b=b[:, :7]), "lora_b")):
+        with pytest.raises(BcastError) as e:
+            S.bcast_serve_linear(x, w, **{**good, **change})
+        assert e.value.code == BCAST_ERR_INVAL and word in str(e.value)
+    with pytest.raises(BcastError) as e:
+        S.bcast_serve_linear(x.t().contiguous().t(), w)
+    assert "x: (2, 64) BFloat16 on cpu with strides (1, 2)" in str(e.value)
+    q, p, o, n = torch.zeros(2, 1, 4, 64, **bf), torch.zeros(5, 2, 64, **bf), torch.zeros(2, 7, 2, 64, **bf), torch.zeros(2, dtype=torch.int32)
+    for args, word in (((q, p, p[:4], o, o, n), "prefix_v"), ((q, p, p, o, o[:, :6], n), "own_v"), ((q, p, p, o, o, n.long()), "own_len"),
+                       ((q[0], p, p, o, o, n), "dimensions"), ((q, p.half(), p, o, o, n), "prefix_k")):
+        with pytest.raises(BcastError) as e:
+            S.bcast_serve_attn(*args)
+        assert word in str(e.value)
+
+
 def test_strides_of_dimensions_with_one_entry():
     t = torch.zeros(1, 1, 4, 64).as_strided((1, 1, 4, 64), (3, 5, 64, 1))
     assert S._strides(t, 3) == (256, 256, 64)
