@@ -19,6 +19,7 @@ namespace {
 
 constexpr int kMaxDrafts = 63;
 constexpr int kStatThreads = 256, kPickThreads = 512;
+constexpr unsigned kPickBlocks = 8;           // of a request's cluster
 
 // Statistics of one part of a row; of a row once joined.  z = l * log2(e) / T.
 struct RowStat {
@@ -32,7 +33,7 @@ struct VerifyDev {
     const int32_t *draft_tokens;
     int32_t *accepted, *tokens;
     int64_t ls0, ls1, qs0, qs1, ns;
-    int32_t vocab, drafts, parts, part_len;
+    int32_t vocab, drafts, parts;
     RowStat *stats;       // [batch][drafts + 1][parts]
 };
 
@@ -43,7 +44,7 @@ __device__ __forceinline__ float clean(float l) { return l != l ? -INFINITY : l;
 __device__ __forceinline__ float weight(float l, float top, float c)
 {
     if (top == INFINITY) return l == INFINITY ? 1.0f : 0.0f;
-    return exp2f((l - top) * c);
+    return exp2_approx((l - top) * c);
 }
 
 __device__ __forceinline__ RowStat join(const RowStat &a, const RowStat &b, float c)
@@ -74,24 +75,84 @@ __device__ __forceinline__ float exponent_scale(float temperature)
     return temperature > 0.0f ? fminf(kLog2e / temperature, 1e30f) : 0.0f;
 }
 
+// Sixteen bytes of logits as floats, NaN as -infinity.
+template <typename T> constexpr int kVector = 16 / (int)sizeof(T);
+template <typename T>
+__device__ __forceinline__ void widen(const uint4 &raw, float *l)
+{
+    const T *v = (const T *)&raw;
+#pragma unroll
+    for (int k = 0; k < kVector<T>; k++) l[k] = fmaxf(to_f32(v[k]), -INFINITY);
+}
+
+// `n` logits, token numbers at + 0..n-1, into a thread's statistics: their largest first, so that what is summed so
+// far is scaled at most once and the exponentials are independent of one another.
+template <int N>
+__device__ __forceinline__ void take(RowStat &s, const float *l, int at, float c)
+{
+    float top = l[0];
+#pragma unroll
+    for (int k = 1; k < N; k++) top = fmaxf(top, l[k]);
+    if (top > s.top) {
+        s.sum = s.best < 0 ? 0.0f : s.sum * weight(s.top, top, c);
+        s.top = top;
+#pragma unroll
+        for (int k = N - 1; k >= 0; k--)
+            if (l[k] == top) s.best = at + k;
+    }
+    if (s.best < 0) return;
+    float sum = 0.0f;
+    if (s.top == INFINITY) {
+#pragma unroll
+        for (int k = 0; k < N; k++) sum += weight(l[k], s.top, c);
+    } else {
+#pragma unroll
+        for (int k = 0; k < N; k++) sum += exp2_approx((l[k] - s.top) * c);
+    }
+    s.sum += sum;
+}
+
+// A block takes one part of a row, in 16-byte vectors from the row's first aligned logit on, four under way per
+// thread; the first part also takes the logits before that, the last one those after the last vector.
 template <typename T>
 __global__ void __launch_bounds__(kStatThreads)
 serve_verify_stats_kernel(const __grid_constant__ VerifyDev d)
 {
+    constexpr int E = kVector<T>, U = 4;
     launch_next();
     const int b = blockIdx.z, i = blockIdx.y, part = blockIdx.x;
-    const int lo = part * d.part_len, hi = min(d.vocab, lo + d.part_len);
     const T *row = (const T *)d.logits + (int64_t)b * d.ls0 + (int64_t)i * d.ls1;
     const float c = exponent_scale(d.temperature[b]);
+    const int head = min(d.vocab, (int)((16 - ((uintptr_t)row & 15)) % 16 / sizeof(T))), vectors = (d.vocab - head) / E;
+    const int v0 = (int)((int64_t)vectors * part / d.parts), v1 = (int)((int64_t)vectors * (part + 1) / d.parts);
+    const uint4 *vec = (const uint4 *)(row + head);
     RowStat s{-INFINITY, 0.0f, -1, 0};
-    for (int v = lo + threadIdx.x; v < hi; v += kStatThreads) {
-        const float l = clean(to_f32(row[v]));
-        if (l > s.top) {
-            s.sum = s.best < 0 ? 0.0f : s.sum * weight(s.top, l, c);
-            s.top = l;
-            s.best = v;
+    int v = v0 + threadIdx.x;
+    for (; v + (U - 1) * kStatThreads < v1; v += U * kStatThreads) {
+        uint4 raw[U];
+#pragma unroll
+        for (int u = 0; u < U; u++) raw[u] = __ldg(vec + v + u * kStatThreads);
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            float l[E];
+            widen<T>(raw[u], l);
+            take<E>(s, l, head + (v + u * kStatThreads) * E, c);
         }
-        if (s.best >= 0) s.sum += weight(l, s.top, c);
+    }
+    for (; v < v1; v += kStatThreads) {
+        float l[E];
+        widen<T>(__ldg(vec + v), l);
+        take<E>(s, l, head + v * E, c);
+    }
+    // a thread's tokens come in ascending order but for the head, which thread order would put last
+    if (part == 0 && (int)threadIdx.x < head) {
+        const float l = clean(to_f32(row[threadIdx.x]));
+        s = join(s, RowStat{l, 1.0f, l > -INFINITY ? (int)threadIdx.x : -1, 0}, c);
+    }
+    const int tail = head + vectors * E + threadIdx.x;
+    if (part == d.parts - 1 && tail < d.vocab) {
+        const float l = clean(to_f32(row[tail]));
+        s = join(s, RowStat{l, 1.0f, l > -INFINITY ? tail : -1, 0}, c);
     }
 #pragma unroll
     for (int o = 16; o; o >>= 1) s = join(s, shuffle_xor(s, o), c);
@@ -101,7 +162,7 @@ serve_verify_stats_kernel(const __grid_constant__ VerifyDev d)
     if (threadIdx.x < 32) {
         s = threadIdx.x < kStatThreads / 32 ? warp_stat[threadIdx.x] : RowStat{-INFINITY, 0.0f, -1, 0};
 #pragma unroll
-        for (int o = 16; o; o >>= 1) s = join(s, shuffle_xor(s, o), c);
+        for (int o = kStatThreads / 64; o; o >>= 1) s = join(s, shuffle_xor(s, o), c);
         if (threadIdx.x == 0) d.stats[((int64_t)b * (d.drafts + 1) + i) * d.parts + part] = s;
     }
 }
@@ -121,7 +182,61 @@ __device__ __forceinline__ Runner shuffle_xor(const Runner &a, int d)
     return Runner{__shfl_xor_sync(~0u, a.ratio, d), __shfl_xor_sync(~0u, a.token, d)};
 }
 
-template <typename T>
+__device__ __forceinline__ float reciprocal(float x)
+{
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// One thread's share of a race over a row, `N` neighbouring tokens at a time (their addresses are multiples of N then).
+// `q` may be nullptr: the race by p.
+template <typename T, int N>
+__device__ __forceinline__ Runner run_race(const T *row, const float *q, const float *noise, int vocab, int first, int step, const RowStat &s,
+                                           float c)
+{
+    constexpr int U = N == 1 ? 4 : 2;
+    const float inv = 1.0f / s.sum;
+    Runner best{0.0f, -1};
+    for (int v0 = first * N; v0 < vocab; v0 += U * step * N) {
+        alignas(16) T l[U][N];
+        alignas(16) float e[U][N], qq[U][N];
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            const int v = v0 + u * step * N;
+            if (v < vocab) {
+                if constexpr (N == 1) {
+                    l[u][0] = row[v];
+                    e[u][0] = noise[v];
+                    qq[u][0] = q ? q[v] : 0.0f;
+                } else {
+                    if constexpr (sizeof(T) == 4) *(uint4 *)l[u] = *(const uint4 *)(row + v);
+                    else *(uint2 *)l[u] = *(const uint2 *)(row + v);
+                    *(float4 *)e[u] = *(const float4 *)(noise + v);
+                    *(float4 *)qq[u] = q ? *(const float4 *)(q + v) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                }
+            } else {
+#pragma unroll
+                for (int k = 0; k < N; k++) {
+                    l[u][k] = from_f32<T>(0.0f);
+                    e[u][k] = -1.0f;
+                    qq[u][k] = 0.0f;
+                }
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; u++)
+#pragma unroll
+            for (int k = 0; k < N; k++) {
+                const float p = weight(clean(to_f32(l[u][k])), s.top, c) * inv;
+                const float ratio = (p - qq[u][k]) * reciprocal(e[u][k]);
+                if (e[u][k] > 0.0f && ratio > best.ratio) best = Runner{ratio, v0 + u * step * N + k};
+            }
+    }
+    return best;
+}
+
+template <typename T, int N>
 __global__ void __launch_bounds__(kPickThreads)
 serve_verify_pick_kernel(const __grid_constant__ VerifyDev d)
 {
@@ -130,34 +245,35 @@ serve_verify_pick_kernel(const __grid_constant__ VerifyDev d)
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, warps = kPickThreads / 32;
     __shared__ RowStat row_stat[kMaxDrafts + 1];
     __shared__ uint32_t failed[2];            // bit i: draft i fails
-    __shared__ Runner warp_run[2][kPickThreads / 32];
-    __shared__ Runner block_run[2];
+    __shared__ Runner warp_run[kPickThreads / 32], block_run[2];
 
     if (threadIdx.x < 2) failed[threadIdx.x] = 0;
     const float t = d.temperature[b], c = exponent_scale(t);
-    wait_previous();
     __syncthreads();
     for (int i = warp; i <= d.drafts; i += warps) {
+        // what needs no statistics, while the kernel before this one still runs
+        int32_t x = -1;
+        float l = -INFINITY, uq = 0.0f;
+        if (i < d.drafts) {
+            x = d.draft_tokens[(int64_t)b * d.drafts + i];
+            if (x >= d.vocab) x = -1;
+            if (x >= 0) {
+                l = clean(to_f32(((const T *)d.logits)[(int64_t)b * d.ls0 + (int64_t)i * d.ls1 + x]));
+                uq = d.uniforms[(int64_t)b * d.drafts + i] * d.draft_probs[(int64_t)b * d.qs0 + (int64_t)i * d.qs1 + x];
+            }
+        }
+        wait_previous();
         RowStat s{-INFINITY, 0.0f, -1, 0};
         for (int p = lane; p < d.parts; p += 32) s = join(s, d.stats[((int64_t)b * (d.drafts + 1) + i) * d.parts + p], c);
 #pragma unroll
         for (int o = 16; o; o >>= 1) s = join(s, shuffle_xor(s, o), c);
         if (lane == 0) {
             row_stat[i] = s;
-            if (i < d.drafts) {
-                const int32_t x = d.draft_tokens[(int64_t)b * d.drafts + i];
-                bool good = x >= 0 && x < d.vocab && s.best >= 0;
-                if (good && t > 0.0f) {
-                    const float l = clean(to_f32(((const T *)d.logits)[(int64_t)b * d.ls0 + (int64_t)i * d.ls1 + x]));
-                    const float q = d.draft_probs[(int64_t)b * d.qs0 + (int64_t)i * d.qs1 + x];
-                    good = d.uniforms[(int64_t)b * d.drafts + i] * q < weight(l, s.top, c) / s.sum;
-                } else if (good) {
-                    good = x == s.best;
-                }
-                if (!good) atomicOr(&failed[i / 32], 1u << (i % 32));
-            }
+            const bool good = x >= 0 && s.best >= 0 && (t > 0.0f ? uq < weight(l, s.top, c) / s.sum : x == s.best);
+            if (i < d.drafts && !good) atomicOr(&failed[i / 32], 1u << (i % 32));
         }
     }
+    wait_previous();
     __syncthreads();
     const int accepted = failed[0] ? __ffs(failed[0]) - 1 : failed[1] ? 31 + __ffs(failed[1]) : d.drafts;
     const RowStat s = row_stat[accepted];
@@ -166,47 +282,27 @@ serve_verify_pick_kernel(const __grid_constant__ VerifyDev d)
         const T *row = (const T *)d.logits + (int64_t)b * d.ls0 + (int64_t)accepted * d.ls1;
         const float *noise = d.noise + (int64_t)b * d.ns;
         const float *q = accepted < d.drafts ? d.draft_probs + (int64_t)b * d.qs0 + (int64_t)accepted * d.qs1 : nullptr;
-        const float inv = 1.0f / s.sum;
-        Runner rest{0.0f, -1}, all{0.0f, -1};      // the race by max(p - q, 0), and by p
-        for (int v = rank * kPickThreads + threadIdx.x; v < d.vocab; v += blocks * kPickThreads) {
-            const float e = noise[v];
-            if (!(e > 0.0f)) continue;
-            const float p = weight(clean(to_f32(row[v])), s.top, c) * inv;
-            const float w = q ? p - q[v] : p;
-            if (w / e > rest.ratio) rest = Runner{w / e, v};
-            if (p / e > all.ratio) all = Runner{p / e, v};
-        }
+        // by max(p - q, 0), or by p; where nothing is left of p - q, once more by p
+        for (int round = 0; round < 2; round++) {
+            Runner best = run_race<T, N>(row, round ? nullptr : q, noise, d.vocab, rank * kPickThreads + threadIdx.x, blocks * kPickThreads, s, c);
 #pragma unroll
-        for (int o = 16; o; o >>= 1) {
-            rest = faster(rest, shuffle_xor(rest, o));
-            all = faster(all, shuffle_xor(all, o));
-        }
-        if (lane == 0) {
-            warp_run[0][warp] = rest;
-            warp_run[1][warp] = all;
-        }
-        __syncthreads();
-        if (threadIdx.x < 2) {
-            Runner r = warp_run[threadIdx.x][0];
-            for (int w = 1; w < warps; w++) r = faster(r, warp_run[threadIdx.x][w]);
-            block_run[threadIdx.x] = r;
-        }
-        cluster.sync();
-        if (rank == 0 && threadIdx.x < 32) {
-            rest = all = Runner{0.0f, -1};
-            if (lane < blocks) {
-                const Runner *o = cluster.map_shared_rank(block_run, lane);
-                rest = o[0];
-                all = o[1];
-            }
+            for (int o = 16; o; o >>= 1) best = faster(best, shuffle_xor(best, o));
+            if (lane == 0) warp_run[warp] = best;
+            __syncthreads();
+            if (warp == 0) {
+                best = lane < warps ? warp_run[lane] : Runner{0.0f, -1};
 #pragma unroll
-            for (int o = 16; o; o >>= 1) {
-                rest = faster(rest, shuffle_xor(rest, o));
-                all = faster(all, shuffle_xor(all, o));
+                for (int o = 16; o; o >>= 1) best = faster(best, shuffle_xor(best, o));
+                if (lane == 0) block_run[round] = best;
             }
-            chosen = rest.token >= 0 ? rest.token : all.token;
+            cluster.sync();
+            best = lane < blocks ? *cluster.map_shared_rank(&block_run[round], lane) : Runner{0.0f, -1};
+#pragma unroll
+            for (int o = 16; o; o >>= 1) best = faster(best, shuffle_xor(best, o));
+            chosen = best.token;
+            if (chosen >= 0 || !q) break;          // every thread of the cluster has the same
         }
-        cluster.sync();                            // a block's shared memory stays until rank 0 has read it
+        cluster.sync();                            // a block's shared memory stays until the others have read it
     }
     if (rank == 0 && threadIdx.x < 32) {
         if (lane == 0) d.accepted[b] = accepted;
@@ -238,8 +334,12 @@ int run(const VerifyDev &d, int batch, cudaStream_t st)
 {
     int rc = launch(serve_verify_stats_kernel<T>, dim3(d.parts, d.drafts + 1, batch), dim3(kStatThreads), 0, st, false, 1, d);
     if (rc) return rc;
-    const unsigned blocks = 8;
-    return launch(serve_verify_pick_kernel<T>, dim3(blocks, batch), dim3(kPickThreads), 0, st, true, blocks, d);
+    // four tokens to a load where every row starts on 16 bytes (8 for 16-bit logits)
+    const uintptr_t bits = (uintptr_t)d.logits / (sizeof(T) / 2) | (uintptr_t)d.ls0 * 2 | (uintptr_t)d.ls1 * 2 | (uintptr_t)d.vocab * 2;
+    const uintptr_t floats = (uintptr_t)d.noise | (uintptr_t)d.ns * 4 | (d.drafts ? (uintptr_t)d.draft_probs | (uintptr_t)d.qs0 * 4 | (uintptr_t)d.qs1 * 4 : 0);
+    const bool whole = bits % 8 == 0 && floats % 16 == 0;
+    return launch(whole ? serve_verify_pick_kernel<T, 4> : serve_verify_pick_kernel<T, 1>, dim3(kPickBlocks, batch), dim3(kPickThreads), 0, st, true,
+                  kPickBlocks, d);
 }
 
 }  // namespace
@@ -294,7 +394,6 @@ int bcast_serve_verify(const bcast_serve_verify_args *a, void *cuda_stream)
     d.vocab = (int32_t)V;
     d.drafts = a->drafts;
     d.parts = stat_parts(*a);
-    d.part_len = (int32_t)ceil_div(V, d.parts);
     d.stats = (RowStat *)((char *)a->workspace + BCAST_SERVE_STATUS_BYTES);
     const cudaStream_t st = (cudaStream_t)cuda_stream;
     switch (a->dtype) {
