@@ -299,29 +299,10 @@ serve_attn_own_kernel(const __grid_constant__ AttnDev d)
 
 // ------------------------------------------------------------------------------------------- shared prefix
 constexpr int kTileKeys = 128, kKvStages = 4, kPrefixThreads = 320;
+constexpr int kPolyEvery = 4;                 // every fourth pair of exponentials goes to the multiply-add units
 constexpr float kSlack = 8.0f;                // powers of two that a row's maximum may lag behind
 
 template <int DB, bool TWO> constexpr size_t prefix_smem() { return (size_t)(TWO ? 2 : 1) * DB * 16384 + (size_t)kKvStages * DB * 16384 + 1024; }
-
-__device__ __forceinline__ uint64_t pair(float a, float b)
-{
-    uint64_t r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
-    return r;
-}
-__device__ __forceinline__ void unpair(uint64_t v, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c)
-{
-    uint64_t r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-    return r;
-}
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b)
-{
-    uint64_t r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
 
 // The state of one row's softmax.
 struct Row {
@@ -329,44 +310,69 @@ struct Row {
     float l = 0.0f;
 };
 
+// 2^x for two numbers at once on the multiply-add units, which have time left where the unit for exponentials
+// has none: x = r + f with r the nearest integer (added to 1.5 * 2^23 it stands in the sum's low bits), 2^f on
+// [-1/2, 1/2] by a polynomial (least largest relative error, fitted: 7.5e-5 in degree 3, 2.6e-6 in degree 4, against
+// 2^-9 and 2^-12 of rounding the weight to the type), and r added to the exponent.  Below 2^-126 gives 2^-126.
+template <typename T>
+__device__ __forceinline__ void exp2_pair(uint64_t x, float &a, float &b)
+{
+    unpair(x, a, b);
+    asm("max.NaN.f32 %0, %0, 0fC2FC0000;" : "+f"(a));         // -126; NaN stays NaN
+    asm("max.NaN.f32 %0, %0, 0fC2FC0000;" : "+f"(b));
+    x = pair(a, b);
+    const float magic = 12582912.0f;
+    const uint64_t t = add2(x, pair(magic, magic));
+    const uint64_t f = add2(x, mul2(add2(t, pair(-magic, -magic)), pair(-1.0f, -1.0f)));
+    uint64_t y;
+    if constexpr (std::is_same_v<T, __half>) {
+        y = pair(0.009570102207362652f, 0.009570102207362652f);
+        y = fma2(y, f, pair(0.05591785907745361f, 0.05591785907745361f));
+        y = fma2(y, f, pair(0.240247443318367f, 0.240247443318367f));
+        y = fma2(y, f, pair(0.6931217908859253f, 0.6931217908859253f));
+        y = fma2(y, f, pair(0.9999992847442627f, 0.9999992847442627f));
+    } else {
+        y = pair(0.0551716685295105f, 0.0551716685295105f);
+        y = fma2(y, f, pair(0.2426111251115799f, 0.2426111251115799f));
+        y = fma2(y, f, pair(0.6932609677314758f, 0.6932609677314758f));
+        y = fma2(y, f, pair(0.9999280571937561f, 0.9999280571937561f));
+    }
+    float ta, tb;
+    unpair(t, ta, tb);
+    unpair(y, a, b);
+    a = __uint_as_float(__float_as_uint(a) + (__float_as_uint(ta) << 23));
+    b = __uint_as_float(__float_as_uint(b) + (__float_as_uint(tb) << 23));
+}
+
 // One tile of a row's scores (tensor memory at `s`, this thread's lane) to weights, written over them as 16-bit
 // pairs.  Where the row's maximum has grown by more than kSlack, what is summed so far (accumulator at `o`) is
-// scaled down first; below that the weights just grow past 1, by at most 2^kSlack.
+// scaled down first; below that the weights just grow past 1, by at most 2^kSlack.  `most` is signalled when the
+// weights of the first 96 tokens are there, so that their product with V runs under the last exponentials.
 template <typename T, bool MASK>
-__device__ __forceinline__ void softmax_tile(Row &row, uint32_t s, uint32_t o, bool first, int valid, int columns, float c)
+__device__ __forceinline__ void softmax_tile(Row &row, uint32_t s, uint32_t o, bool first, int valid, int columns, float c, uint32_t most)
 {
-    uint32_t x[128];
+    // The scores are read twice, once for their maximum and once for the weights: reading tensor memory costs
+    // less than keeping 128 of them in registers.  Weights never overwrite scores that are still to be read.
+    float t[4];
+    const bool up = c >= 0.0f;
+    {
+        uint32_t x[2][32];
+        tmem_load32(s, x[0]);
 #pragma unroll
-    for (int i = 0; i < 4; i++) tmem_load32(s + i * 32, x + i * 32);
+        for (int g = 0; g < 4; g++) {
+            tmem_wait_load32(x[g & 1]);
+            if (g < 3) tmem_load32(s + (g + 1) * 32, x[(g + 1) & 1]);
 #pragma unroll
-    for (int i = 0; i < 4; i++) tmem_wait_load32(x + i * 32);
-    if (MASK) {
-#pragma unroll
-        for (int i = 1; i < 128; i++)
-            if (i >= valid) x[i] = x[0];              // the tile's first token is always there
-    }
-    float t0 = __uint_as_float(x[0]), t1 = __uint_as_float(x[1]), t2 = __uint_as_float(x[2]), t3 = __uint_as_float(x[3]);
-    if (c >= 0.0f) {
-#pragma unroll
-        for (int i = 4; i < 128; i += 4) {
-            t0 = fmaxf(t0, __uint_as_float(x[i]));
-            t1 = fmaxf(t1, __uint_as_float(x[i + 1]));
-            t2 = fmaxf(t2, __uint_as_float(x[i + 2]));
-            t3 = fmaxf(t3, __uint_as_float(x[i + 3]));
+            for (int i = 0; i < 32; i++) {
+                const float v = __uint_as_float(x[g & 1][i]);
+                if (g == 0 && i < 4) t[i] = MASK && i >= valid ? t[0] : v;        // the tile's first token is always there
+                else if (!MASK || g * 32 + i < valid) t[i & 3] = up ? fmaxf(t[i & 3], v) : fminf(t[i & 3], v);
+            }
         }
-        t0 = fmaxf(fmaxf(t0, t1), fmaxf(t2, t3));
-    } else {
-#pragma unroll
-        for (int i = 4; i < 128; i += 4) {
-            t0 = fminf(t0, __uint_as_float(x[i]));
-            t1 = fminf(t1, __uint_as_float(x[i + 1]));
-            t2 = fminf(t2, __uint_as_float(x[i + 2]));
-            t3 = fminf(t3, __uint_as_float(x[i + 3]));
-        }
-        t0 = fminf(fminf(t0, t1), fminf(t2, t3));
+        t[0] = up ? fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])) : fminf(fminf(t[0], t[1]), fminf(t[2], t[3]));
     }
     // NaN scores leave the maximum alone (NaN * c is dropped by fmaxf) and become NaN weights
-    const float top = fmaxf(row.m, t0 * c);
+    const float top = fmaxf(row.m, t[0] * c);
     const bool grow = top > row.m + (first ? 0.0f : kSlack);
     const float next = grow ? top : row.m, from = next == -INFINITY ? 0.0f : next;
     if (!first && __any_sync(~0u, grow)) {
@@ -384,23 +390,40 @@ __device__ __forceinline__ void softmax_tile(Row &row, uint32_t s, uint32_t o, b
     row.m = next;
     const uint64_t cc = pair(c, c), ff = pair(kShift<T> - from, kShift<T> - from);
     uint64_t sum0 = 0, sum1 = 0;                      // pairs of 0.0f
-    uint32_t w[64];
+    uint32_t x[2][32];
+    tmem_load32(s, x[0]);
 #pragma unroll
-    for (int i = 0; i < 64; i++) {
-        float a, b;
-        unpair(fma2(pair(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1])), cc, ff), a, b);
-        a = exp2_approx(a);
-        b = exp2_approx(b);
-        if (MASK) {
-            if (2 * i >= valid) a = 0.0f;
-            if (2 * i + 1 >= valid) b = 0.0f;
+    for (int g = 0; g < 4; g++) {
+        uint32_t w[16];
+        tmem_wait_load32(x[g & 1]);
+        if (g < 3) tmem_load32(s + (g + 1) * 32, x[(g + 1) & 1]);
+#pragma unroll
+        for (int i = 0; i < 16; i++) {
+            const int at = g * 32 + 2 * i;
+            const uint64_t z = fma2(pair(__uint_as_float(x[g & 1][2 * i]), __uint_as_float(x[g & 1][2 * i + 1])), cc, ff);
+            float a, b;
+            if (i % kPolyEvery == kPolyEvery - 1) {
+                exp2_pair<T>(z, a, b);
+            } else {
+                unpair(z, a, b);
+                a = exp2_approx(a);
+                b = exp2_approx(b);
+            }
+            if (MASK) {
+                if (at >= valid) a = 0.0f;
+                if (at + 1 >= valid) b = 0.0f;
+            }
+            if (i & 1) sum1 = add2(sum1, pair(a, b));
+            else sum0 = add2(sum0, pair(a, b));
+            w[i] = pack2<T>(a, b);
         }
-        if (i & 1) sum1 = add2(sum1, pair(a, b));
-        else sum0 = add2(sum0, pair(a, b));
-        w[i] = pack2<T>(a, b);
-        if (i == 31) tmem_store32(s, w);
+        tmem_store16(s + g * 16, w);
+        if (g == 2) {
+            tmem_wait_store();
+            tc_fence_before();
+            mbar_arrive(most);
+        }
     }
-    tmem_store32(s + 32, w + 32);
     float a, b;
     unpair(add2(sum0, sum1), a, b);
     row.l += a + b;
@@ -409,7 +432,7 @@ __device__ __forceinline__ void softmax_tile(Row &row, uint32_t s, uint32_t o, b
 
 // TWO: two tiles of 128 rows, each with its own softmax warps and accumulator, take the same tokens, so that
 // one tile's matrix products run under the other's exponentials.  Otherwise (128 rows or fewer) the two halves share
-// the rows and take every other tile of tokens, and their results are two parts.
+// the rows and take every other tile of tokens, and their results are joined at the end.
 template <typename T, int DB, bool TWO>
 __global__ void __launch_bounds__(kPrefixThreads, 1)
 serve_attn_prefix_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
@@ -417,7 +440,8 @@ serve_attn_prefix_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
 {
     constexpr int block = kTileKeys * 128, stage = DB * block;        // 64 columns of a tile; a tile
     extern __shared__ uint8_t raw_smem[];
-    __shared__ __align__(8) uint64_t bars[2 * kKvStages + 8];
+    __shared__ __align__(8) uint64_t bars[2 * kKvStages + 10];
+    __shared__ float half_m[128], half_l[128];
     __shared__ uint32_t tmem_at;
     __shared__ int gave_up;
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
@@ -432,7 +456,7 @@ serve_attn_prefix_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
     uint8_t *qs = smem;
     const uint32_t q_at = smem_u32(qs), kv_at = q_at + (TWO ? 2 : 1) * stage;
     const uint32_t full = smem_u32(bars), empty = full + 8 * kKvStages, q_full = empty + 8 * kKvStages, s_full = q_full + 8,
-                   p_full = s_full + 16, o_full = p_full + 16, drained = o_full + 16;
+                   p_most = s_full + 16, p_full = p_most + 16, o_full = p_full + 16, drained = o_full + 16;
     if (tid == 0) {
         gave_up = 0;
         for (int i = 0; i < kKvStages; i++) {
@@ -442,6 +466,7 @@ serve_attn_prefix_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
         mbar_init(q_full, 256);
         for (int i = 0; i < 2; i++) {
             mbar_init(s_full + 8 * i, 1);
+            mbar_init(p_most + 8 * i, 128);
             mbar_init(p_full + 8 * i, 128);
             mbar_init(o_full + 8 * i, 1);
         }
@@ -488,88 +513,92 @@ serve_attn_prefix_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
         }
         __syncwarp();
     } else if (warp == 9) {
-        if (lane == 0) {
-            // ---- matrix products
-            const int n = (d.dim + 15) / 16 * 16;
-            const uint32_t s_desc = mma_desc<T>(128, kTileKeys), o_desc = mma_desc<T>(128, n, true);
-            Ring<kKvStages> ring;
-            auto scores = [&](int w, uint32_t k_at) {                 // S_w = Q_w K^T
-                for (int i = 0; i < n / 16; i++)
-                    mma_ss(tmem + w * 128, smem_desc(q_at + (TWO ? w : 0) * stage + i / 4 * block) + 2 * (i % 4),
-                           smem_desc(k_at + i / 4 * block) + 2 * (i % 4), s_desc, i > 0);
-                mma_commit(s_full + 8 * w);
-            };
-            auto values = [&](int w, uint32_t v_at, bool add) {       // O_w += P_w V
-                for (int i = 0; i < kTileKeys / 16; i++)
-                    mma_ts(tmem + 256 + w * 128, tmem + w * 128 + i * 8, smem_desc(v_at + i * 2048, block), o_desc, add || i > 0);
-            };
-            auto wait_full = [&](uint32_t &at) {
-                if (!mbar_wait(full + 8 * ring.slot, ring.parity, &gave_up)) return -1;
-                tc_fence_after();
-                at = kv_at + ring.slot * stage;
-                const int slot = ring.slot;
-                ring.step();
-                return slot;
-            };
-            auto wait_weights = [&](int w, int it) {
-                if (!mbar_wait(p_full + 8 * w, it & 1, &gave_up)) return false;
-                tc_fence_after();
-                return true;
-            };
-            auto run = [&]() {
-                uint32_t k_at, v_at;
-                int ks, vs;
-                if (!mbar_wait(q_full, 0, &gave_up) || (ks = wait_full(k_at)) < 0) return;
-                scores(0, k_at);
-                if (TWO) {
-                    scores(1, k_at);
-                    mma_commit(empty + 8 * ks);
-                    for (int j = 0; j < nt; j++) {
-                        if ((vs = wait_full(v_at)) < 0 || !wait_weights(0, j)) return;
-                        values(0, v_at, j > 0);
-                        if (j + 1 < nt) {
-                            if ((ks = wait_full(k_at)) < 0) return;
-                            scores(0, k_at);
-                        } else {
-                            mma_commit(o_full);
-                        }
-                        if (!wait_weights(1, j)) return;
-                        values(1, v_at, j > 0);
-                        mma_commit(empty + 8 * vs);
-                        if (j + 1 < nt) {
-                            scores(1, k_at);
-                            mma_commit(empty + 8 * ks);
-                        } else {
-                            mma_commit(o_full + 8);
-                        }
-                    }
+        // ---- matrix products.  An instruction every 64 cycles is what keeps the tensor cores busy, so issuing them has
+        // to be cheap: the whole warp goes through the loop together, descriptors differ by constants, and a wait that
+        // gives up does not leave the loop -- the ones after it give up at once, and what is still issued only touches this
+        // block's own memory.  (With one thread in a loop of its own that made descriptors as it went, a product
+        // of 128 x 128 x 128 took 900 to 1800 cycles to issue and not 512.)
+        const uint32_t lead = elect_one();
+        const uint32_t s_desc = mma_desc<T>(128, kTileKeys), o_desc = mma_desc<T>(128, (d.dim + 15) / 16 * 16, true);
+        const uint64_t q_desc = smem_desc(q_at), k_desc = smem_desc(kv_at), v_desc = smem_desc(kv_at, block);
+        Ring<kKvStages> ring;
+        auto take = [&]() {                                           // the next tile of K or V, once it is there
+            mbar_wait(full + 8 * ring.slot, ring.parity, &gave_up);
+            tc_fence_after();
+            const int slot = ring.slot;
+            ring.step();
+            return slot;
+        };
+        auto scores = [&](int w, int slot) {                          // S_w = Q_w K^T; columns past the head size are zero
+            const uint64_t a = q_desc + (TWO ? w : 0) * (stage >> 4), b = k_desc + slot * (stage >> 4);
+#pragma unroll 1
+            for (int k = 0; k < DB; k++)
+#pragma unroll
+                for (int i = 0; i < 4; i++)
+                    mma_ss_warp(lead, tmem + w * 128, a + k * (block >> 4) + 2 * i, b + k * (block >> 4) + 2 * i, s_desc, k > 0 || i > 0);
+            mma_commit_warp(lead, s_full + 8 * w);
+        };
+        auto values = [&](int w, int slot, int it) {                  // O_w += P_w V, as the weights come
+            const uint64_t b = v_desc + slot * (stage >> 4);
+            const uint32_t o = tmem + 256 + w * 128, a = tmem + w * 128;
+            mbar_wait(p_most + 8 * w, it & 1, &gave_up);
+            tc_fence_after();
+            mma_ts_warp(lead, o, a, b, o_desc, it > 0);
+#pragma unroll
+            for (int i = 1; i < 6; i++) mma_ts_warp(lead, o, a + i * 8, b + i * (2048 >> 4), o_desc, true);
+            mbar_wait(p_full + 8 * w, it & 1, &gave_up);
+            tc_fence_after();
+#pragma unroll
+            for (int i = 6; i < 8; i++) mma_ts_warp(lead, o, a + i * 8, b + i * (2048 >> 4), o_desc, true);
+        };
+        mbar_wait(q_full, 0, &gave_up);
+        int ks = take();
+        scores(0, ks);
+        if (TWO) {
+            scores(1, ks);
+            mma_commit_warp(lead, empty + 8 * ks);
+            for (int j = 0; j < nt; j++) {
+                const int vs = take();
+                const bool more = j + 1 < nt;
+                values(0, vs, j);
+                if (more) {
+                    ks = take();
+                    scores(0, ks);
                 } else {
-                    mma_commit(empty + 8 * ks);
-                    if (nt > 1) {
-                        if ((ks = wait_full(k_at)) < 0) return;
-                        scores(1, k_at);
-                        mma_commit(empty + 8 * ks);
-                    }
-                    for (int j = 0; j < nt; j++) {
-                        const int w = j & 1;
-                        if ((vs = wait_full(v_at)) < 0 || !wait_weights(w, j / 2)) return;
-                        values(w, v_at, j > 1);
-                        mma_commit(empty + 8 * vs);
-                        if (j + 2 < nt) {
-                            if ((ks = wait_full(k_at)) < 0) return;
-                            scores(w, k_at);
-                            mma_commit(empty + 8 * ks);
-                        } else {
-                            mma_commit(o_full + 8 * w);
-                        }
-                    }
+                    mma_commit_warp(lead, o_full);
                 }
-            };
-            run();
-            if (gave_up) {
-                mma_commit(drained);
-                mbar_drain(drained, 0);
+                values(1, vs, j);
+                mma_commit_warp(lead, empty + 8 * vs);
+                if (more) {
+                    scores(1, ks);
+                    mma_commit_warp(lead, empty + 8 * ks);
+                } else {
+                    mma_commit_warp(lead, o_full + 8);
+                }
             }
+        } else {
+            mma_commit_warp(lead, empty + 8 * ks);
+            if (nt > 1) {
+                ks = take();
+                scores(1, ks);
+                mma_commit_warp(lead, empty + 8 * ks);
+            }
+            for (int j = 0; j < nt; j++) {
+                const int w = j & 1, vs = take();
+                values(w, vs, j / 2);
+                mma_commit_warp(lead, empty + 8 * vs);
+                if (j + 2 < nt) {
+                    ks = take();
+                    scores(w, ks);
+                    mma_commit_warp(lead, empty + 8 * ks);
+                } else {
+                    mma_commit_warp(lead, o_full + 8 * w);
+                }
+            }
+        }
+        if (gave_up) {
+            mma_commit_warp(lead, drained);
+            mbar_drain(drained, 0);
         }
         __syncwarp();
     } else {
@@ -602,33 +631,60 @@ serve_attn_prefix_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
             }
             tc_fence_after();
             const int valid = d.prefix_len - (j0 + (TWO ? it : 2 * it + w)) * kTileKeys;
-            if (busy) {
-                if (valid >= kTileKeys) softmax_tile<T, false>(row, s_at, o_at, it == 0, kTileKeys, columns, d.scale_log2);
-                else softmax_tile<T, true>(row, s_at, o_at, it == 0, valid, columns, d.scale_log2);
-            }
+            if (!busy) mbar_arrive(p_most + 8 * w);
+            else if (valid >= kTileKeys) softmax_tile<T, false>(row, s_at, o_at, it == 0, kTileKeys, columns, d.scale_log2, p_most + 8 * w);
+            else softmax_tile<T, true>(row, s_at, o_at, it == 0, valid, columns, d.scale_log2, p_most + 8 * w);
             tc_fence_before();
             mbar_arrive(p_full + 8 * w);
         }
-        if (mine > 0 && ok) {
-            ok = mbar_wait(o_full + 8 * w, 0, &gave_up);
-            ok = __all_sync(~0u, ok);
-            tc_fence_after();
-        }
-        if (busy && ok) {
-            const int g = r0 + r, part = TWO ? split : 2 * split + w;
-            const bool exists = r < live;
-            const int64_t at = part * d.rows + ((int64_t)(g / (d.fresh * d.group)) * d.fresh + g / d.group % d.fresh) * d.q_heads +
-                               kv * d.group + g % d.group;
-            if (exists) d.part_ml[at] = make_float2(row.l == 0.0f ? -INFINITY : (row.m == -INFINITY ? 0.0f : row.m) - kShift<T>, row.l);
-            if (mine > 0) {
-                for (int c = 0; c < columns; c += 16) {
-                    uint32_t v[16];
-                    tmem_load16(o_at + c, v);
-                    tmem_wait_load16(v);
+        // ---- the way out: a row's sums as they are, with what they were taken against
+        if (mine > 0 && ok) ok = mbar_wait(o_full + 8 * w, 0, &gave_up);
+        if (!TWO && w == 1 && mine > 0 && ok) ok = mbar_wait(o_full, 0, &gave_up);
+        ok = __all_sync(~0u, ok);
+        tc_fence_after();
+        float m = row.l == 0.0f ? -INFINITY : (row.m == -INFINITY ? 0.0f : row.m) - kShift<T>, other = 0.0f, keep = 1.0f;
+        float *half = (float *)(smem + stage);        // [column][row], where K and V were: all products are done
+        if (!TWO) {
+            // the two halves of the tokens become one part: the second hands over its sums
+            if (w == 1) {
+                half_m[quarter * 32 + lane] = m;
+                half_l[quarter * 32 + lane] = row.l;
+                if (busy && ok && mine > 0)
+                    for (int c = 0; c < columns; c += 16) {
+                        uint32_t v[16];
+                        tmem_load16(o_at + c, v);
+                        tmem_wait_load16(v);
 #pragma unroll
-                    for (int k = 0; k < 16; k += 4)
-                        if (exists && c + k < d.dim) *(uint4 *)(d.part_o + at * d.dim + c + k) = *(const uint4 *)(v + k);
+                        for (int k = 0; k < 16; k++) ((uint32_t *)half)[(c + k) * 128 + quarter * 32 + lane] = v[k];
+                    }
+            }
+            asm volatile("bar.sync 1, 256;" ::: "memory");
+            const float m1 = half_m[quarter * 32 + lane], l1 = half_l[quarter * 32 + lane];
+            if (w == 0 && m1 != -INFINITY) {
+                const float top = fmaxf(m, m1);
+                keep = exp2_approx(m - top);
+                other = exp2_approx(m1 - top);
+                row.l = keep * row.l + other * l1;
+                m = top;
+            }
+        }
+        if (busy && ok && (TWO || w == 0)) {
+            const int g = r0 + r;
+            const bool exists = r < live;
+            const int64_t at = split * d.rows + ((int64_t)(g / (d.fresh * d.group)) * d.fresh + g / d.group % d.fresh) * d.q_heads +
+                               kv * d.group + g % d.group;
+            if (exists) d.part_ml[at] = make_float2(m, row.l);
+            for (int c = 0; c < columns; c += 16) {
+                float v[16];
+                tmem_load16(o_at + c, (uint32_t *)v);
+                tmem_wait_load16((uint32_t *)v);
+                if (!TWO && other != 0.0f) {
+#pragma unroll
+                    for (int k = 0; k < 16; k++) v[k] = keep * v[k] + other * half[(c + k) * 128 + quarter * 32 + lane];
                 }
+#pragma unroll
+                for (int k = 0; k < 16; k += 4)
+                    if (exists && c + k < d.dim) *(float4 *)(d.part_o + at * d.dim + c + k) = *(const float4 *)(v + k);
             }
         }
         tc_fence_before();
@@ -641,44 +697,80 @@ serve_attn_prefix_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
 }
 
 // ------------------------------------------------------------------------------------------- join
-constexpr int kJoinThreads = 128;
+constexpr int kJoinThreads = 128, kJoinParts = 256;       // most parts of a row: 64 of the prefix, and what own_cap allows
 
+// A block to a row: the parts' factors first, then dim / 4 threads to a part and as many parts at a time as there
+// are threads for, four columns to a thread.  (With a warp to a row, parts one after the other, a decode step of 32
+// requests took 25 us here.)
 template <typename T>
 __global__ void __launch_bounds__(kJoinThreads)
 serve_attn_join_kernel(const __grid_constant__ AttnDev d)
 {
-    const int64_t row = (int64_t)blockIdx.x * (kJoinThreads / 32) + threadIdx.x / 32;
-    const int lane = threadIdx.x % 32;
+    __shared__ float factor[kJoinParts], warp_top[kJoinThreads / 32], warp_sum[kJoinThreads / 32];
+    __shared__ float4 sums[kJoinThreads];
+    const int64_t row = blockIdx.x;
+    const int tid = threadIdx.x, lane = tid % 32, warp = tid / 32;
     wait_previous();
-    if (row >= d.rows) return;
+    float2 ml[kJoinParts / kJoinThreads];
     float top = -INFINITY;
-    for (int p = lane; p < d.parts; p += 32) top = fmaxf(top, d.part_ml[p * d.rows + row].x);
+#pragma unroll
+    for (int k = 0; k < kJoinParts / kJoinThreads; k++) {
+        const int p = tid + k * kJoinThreads;
+        ml[k] = p < d.parts ? d.part_ml[p * d.rows + row] : make_float2(-INFINITY, 0.0f);
+        top = fmaxf(top, ml[k].x);
+    }
 #pragma unroll
     for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
+    if (lane == 0) warp_top[warp] = top;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kJoinThreads / 32; w++) top = fmaxf(top, warp_top[w]);
     const float from = top == -INFINITY ? 0.0f : top;
-    float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     float total = 0.0f;
-    const bool live = lane * 4 < d.dim;
+#pragma unroll
+    for (int k = 0; k < kJoinParts / kJoinThreads; k++) {
+        // a part that holds nothing has sums that were never written
+        const float x = ml[k].x == -INFINITY ? -1.0f : exp2_approx(ml[k].x - from);
+        if (tid + k * kJoinThreads < d.parts) factor[tid + k * kJoinThreads] = x;
+        if (x >= 0.0f) total += x * ml[k].y;
+    }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) total += __shfl_xor_sync(~0u, total, o);
+    if (lane == 0) warp_sum[warp] = total;
+    __syncthreads();
+    total = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kJoinThreads / 32; w++) total += warp_sum[w];
+
+    const int width = d.dim / 4, at_once = kJoinThreads / width, mine = tid / width, c = tid % width * 4;
+    float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    if (mine < at_once) {
 #pragma unroll 4
-    for (int p = 0; p < d.parts; p++) {
-        const float2 ml = d.part_ml[p * d.rows + row];
-        if (ml.x == -INFINITY) continue;              // holds nothing, and what its sums hold is not defined
-        const float w = exp2_approx(ml.x - from);
-        total += w * ml.y;
-        if (live) {
-            const float4 v = *(const float4 *)(d.part_o + (p * d.rows + row) * d.dim + lane * 4);
-            sum.x += w * v.x;
-            sum.y += w * v.y;
-            sum.z += w * v.z;
-            sum.w += w * v.w;
+        for (int p = mine; p < d.parts; p += at_once) {
+            const float x = factor[p];
+            const float4 v = x >= 0.0f ? *(const float4 *)(d.part_o + (p * d.rows + row) * d.dim + c) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            sum.x += x * v.x;
+            sum.y += x * v.y;
+            sum.z += x * v.z;
+            sum.w += x * v.w;
         }
     }
-    const float inv = total == 0.0f ? 0.0f : 1.0f / total;
-    const int h = (int)(row % d.q_heads), i = (int)(row / d.q_heads % d.fresh), b = (int)(row / d.q_heads / d.fresh);
-    if (live)
-        *(uint2 *)((T *)d.out + b * d.os[0] + i * d.os[1] + h * d.os[2] + lane * 4) =
+    sums[tid] = sum;
+    __syncthreads();
+    if (tid < width) {
+        for (int k = 1; k < at_once; k++) {
+            const float4 v = sums[k * width + tid];
+            sum.x += v.x;
+            sum.y += v.y;
+            sum.z += v.z;
+            sum.w += v.w;
+        }
+        const float inv = total == 0.0f ? 0.0f : 1.0f / total;
+        const int h = (int)(row % d.q_heads), i = (int)(row / d.q_heads % d.fresh), b = (int)(row / d.q_heads / d.fresh);
+        *(uint2 *)((T *)d.out + b * d.os[0] + i * d.os[1] + h * d.os[2] + c) =
             make_uint2(pack2<T>(sum.x * inv, sum.y * inv), pack2<T>(sum.z * inv, sum.w * inv));
-    if (d.lse && lane == 0) d.lse[row] = total == 0.0f ? -INFINITY : (from + log2f(total)) * kLn2;
+        if (d.lse && tid == 0) d.lse[row] = total == 0.0f ? -INFINITY : (from + log2f(total)) * kLn2;
+    }
 }
 
 int check_shape(const bcast_serve_attn_args &a)
@@ -718,15 +810,16 @@ Cut cut_of(const bcast_serve_attn_args &a)
                 c.prefix_splits = s;
             }
         }
-        c.prefix_parts = c.prefix_splits * (c.two ? 1 : 2);
+        c.prefix_parts = c.prefix_splits;
     }
     if (a.own_cap > 0 && c.rows > 0) {
         const int64_t own_rows = a.new_tokens * group;
         c.own_tiles = ceil_div(own_rows, own_rows > 16 ? 32 : 16);
-        // parts of at least 128 tokens, until there are about four blocks for every SM
+        // parts of at least 128 tokens, until there are about two blocks for every SM
         const int64_t blocks = (int64_t)a.batch * a.kv_heads * c.own_tiles;
-        int64_t s = ceil_div(4 * kSms, blocks);
+        int64_t s = ceil_div(2 * kSms, blocks);
         s = s < ceil_div(a.own_cap, 128) ? s : ceil_div(a.own_cap, 128);
+        s = s < kJoinParts - 64 ? s : kJoinParts - 64;
         c.own_chunk = round_up(ceil_div(a.own_cap, s), 64);
         c.own_splits = ceil_div(a.own_cap, c.own_chunk);
     }
@@ -771,7 +864,7 @@ int run(const bcast_serve_attn_args &a, const AttnDev &d, const Cut &c, cudaStre
     if (c.own_splits) rc = a.new_tokens * d.group > 16 ? run_own<T, DB, 2>(a, d, c, st) : run_own<T, DB, 1>(a, d, c, st);
     if (!rc && c.prefix_splits) rc = c.two ? run_prefix<T, DB, true>(a, d, c, st) : run_prefix<T, DB, false>(a, d, c, st);
     if (rc) return rc;
-    return launch(serve_attn_join_kernel<T>, dim3((unsigned)ceil_div(c.rows, kJoinThreads / 32)), dim3(kJoinThreads), 0, st, c.parts > 0, 1, d);
+    return launch(serve_attn_join_kernel<T>, dim3((unsigned)c.rows), dim3(kJoinThreads), 0, st, c.parts > 0, 1, d);
 }
 
 }  // namespace

@@ -19,12 +19,11 @@ namespace {
 
 constexpr int kMaxDrafts = 63;
 constexpr int kStatThreads = 256, kPickThreads = 512;
-constexpr unsigned kPickBlocks = 8;           // of a request's cluster
 
 // Statistics of one part of a row; of a row once joined.  z = l * log2(e) / T.
 struct RowStat {
     float top, sum;       // largest logit; sum of 2^((l - top) * c)
-    int32_t best, pad;    // lowest token with that logit, -1 if no logit is above -infinity
+    int32_t best, pad;    // -1 if no logit is above -infinity; without temperature the lowest token with the largest
 };
 
 struct VerifyDev {
@@ -75,41 +74,89 @@ __device__ __forceinline__ float exponent_scale(float temperature)
     return temperature > 0.0f ? fminf(kLog2e / temperature, 1e30f) : 0.0f;
 }
 
-// Sixteen bytes of logits as floats, NaN as -infinity.
+// Sixteen bytes of logits as floats.
 template <typename T> constexpr int kVector = 16 / (int)sizeof(T);
 template <typename T>
 __device__ __forceinline__ void widen(const uint4 &raw, float *l)
 {
     const T *v = (const T *)&raw;
 #pragma unroll
-    for (int k = 0; k < kVector<T>; k++) l[k] = fmaxf(to_f32(v[k]), -INFINITY);
+    for (int k = 0; k < kVector<T>; k++) l[k] = to_f32(v[k]);
 }
 
-// `n` logits, token numbers at + 0..n-1, into a thread's statistics: their largest first, so that what is summed so
-// far is scaled at most once and the exponentials are independent of one another.
-template <int N>
+// N logits, token numbers at + 0..N-1, into a thread's statistics.  Without a temperature that is the largest logit
+// and where it is.  With one it is their largest (fmaxf passes over NaN) and the sum of the weights against it: what is
+// summed so far is scaled at most once, and the exponentials are independent of one another.  A sum that comes out
+// NaN had NaN or an infinity in it and is taken again, entry by entry.  (Looking for the place of the largest logit
+// there too made the kernel issue-bound: 14 instructions to a logit, 128 x 8 rows of 131072 in 65 us.)
+template <int N, bool SAMPLE>
 __device__ __forceinline__ void take(RowStat &s, const float *l, int at, float c)
 {
-    float top = l[0];
+    float top = -INFINITY;
 #pragma unroll
-    for (int k = 1; k < N; k++) top = fmaxf(top, l[k]);
+    for (int k = 0; k < N; k++) top = fmaxf(top, l[k]);
+    if (!SAMPLE) {
+        if (top > s.top) {
+            s.top = top;
+#pragma unroll
+            for (int k = N - 1; k >= 0; k--)
+                if (l[k] == top) s.best = at + k;
+        }
+        return;
+    }
     if (top > s.top) {
         s.sum = s.best < 0 ? 0.0f : s.sum * weight(s.top, top, c);
         s.top = top;
-#pragma unroll
-        for (int k = N - 1; k >= 0; k--)
-            if (l[k] == top) s.best = at + k;
+        s.best = 0;
     }
     if (s.best < 0) return;
-    float sum = 0.0f;
-    if (s.top == INFINITY) {
+    const uint64_t from = pair(-s.top, -s.top), cc = pair(c, c);
+    uint64_t sums = 0;                        // a pair of 0.0f
 #pragma unroll
-        for (int k = 0; k < N; k++) sum += weight(l[k], s.top, c);
-    } else {
-#pragma unroll
-        for (int k = 0; k < N; k++) sum += exp2_approx((l[k] - s.top) * c);
+    for (int k = 0; k < N; k += 2) {
+        float a, b;
+        unpair(mul2(add2(pair(l[k], l[k + 1]), from), cc), a, b);
+        sums = add2(sums, pair(exp2_approx(a), exp2_approx(b)));
     }
-    s.sum += sum;
+    float a, b;
+    unpair(sums, a, b);
+    a += b;
+    if (a != a) {
+        a = 0.0f;
+#pragma unroll
+        for (int k = 0; k < N; k++) a += weight(clean(l[k]), s.top, c);
+    }
+    s.sum += a;
+}
+
+constexpr int kFetch = 4;                     // vectors that a thread has under way
+
+template <typename T>
+__device__ __forceinline__ void fetch(uint4 *to, const uint4 *vec, int v, int end)
+{
+#pragma unroll
+    for (int u = 0; u < kFetch; u++) to[u] = v + u * kStatThreads < end ? __ldg(vec + v + u * kStatThreads) : make_uint4(0, 0, 0, 0);
+}
+
+// A thread's share of the vectors v..end-1 of a row, vector 0 being token `at`; `next` holds the first of them, and
+// the next ones are fetched before the last ones are worked on.
+template <typename T, bool SAMPLE>
+__device__ __forceinline__ void take_vectors(RowStat &s, uint4 *next, const uint4 *vec, int v, int end, int at, float c)
+{
+    constexpr int E = kVector<T>;
+    for (; v < end; v += kFetch * kStatThreads) {
+        uint4 raw[kFetch];
+#pragma unroll
+        for (int u = 0; u < kFetch; u++) raw[u] = next[u];
+        fetch<T>(next, vec, v + kFetch * kStatThreads, end);
+#pragma unroll
+        for (int u = 0; u < kFetch; u++) {
+            if (v + u * kStatThreads >= end) break;
+            float l[E];
+            widen<T>(raw[u], l);
+            take<E, SAMPLE>(s, l, at + (v + u * kStatThreads) * E, c);
+        }
+    }
 }
 
 // A block takes one part of a row, in 16-byte vectors from the row's first aligned logit on, four under way per
@@ -118,32 +165,19 @@ template <typename T>
 __global__ void __launch_bounds__(kStatThreads)
 serve_verify_stats_kernel(const __grid_constant__ VerifyDev d)
 {
-    constexpr int E = kVector<T>, U = 4;
+    constexpr int E = kVector<T>;
     launch_next();
     const int b = blockIdx.z, i = blockIdx.y, part = blockIdx.x;
     const T *row = (const T *)d.logits + (int64_t)b * d.ls0 + (int64_t)i * d.ls1;
-    const float c = exponent_scale(d.temperature[b]);
     const int head = min(d.vocab, (int)((16 - ((uintptr_t)row & 15)) % 16 / sizeof(T))), vectors = (d.vocab - head) / E;
     const int v0 = (int)((int64_t)vectors * part / d.parts), v1 = (int)((int64_t)vectors * (part + 1) / d.parts);
     const uint4 *vec = (const uint4 *)(row + head);
     RowStat s{-INFINITY, 0.0f, -1, 0};
-    int v = v0 + threadIdx.x;
-    for (; v + (U - 1) * kStatThreads < v1; v += U * kStatThreads) {
-        uint4 raw[U];
-#pragma unroll
-        for (int u = 0; u < U; u++) raw[u] = __ldg(vec + v + u * kStatThreads);
-#pragma unroll
-        for (int u = 0; u < U; u++) {
-            float l[E];
-            widen<T>(raw[u], l);
-            take<E>(s, l, head + (v + u * kStatThreads) * E, c);
-        }
-    }
-    for (; v < v1; v += kStatThreads) {
-        float l[E];
-        widen<T>(__ldg(vec + v), l);
-        take<E>(s, l, head + v * E, c);
-    }
+    uint4 next[kFetch];
+    fetch<T>(next, vec, v0 + threadIdx.x, v1);
+    const float c = exponent_scale(d.temperature[b]);
+    if (c > 0.0f) take_vectors<T, true>(s, next, vec, v0 + threadIdx.x, v1, head, c);
+    else take_vectors<T, false>(s, next, vec, v0 + threadIdx.x, v1, head, c);
     // a thread's tokens come in ascending order but for the head, which thread order would put last
     if (part == 0 && (int)threadIdx.x < head) {
         const float l = clean(to_f32(row[threadIdx.x]));
@@ -195,7 +229,7 @@ template <typename T, int N>
 __device__ __forceinline__ Runner run_race(const T *row, const float *q, const float *noise, int vocab, int first, int step, const RowStat &s,
                                            float c)
 {
-    constexpr int U = N == 1 ? 4 : 2;
+    constexpr int U = N == 1 ? 8 : 4;
     const float inv = 1.0f / s.sum;
     Runner best{0.0f, -1};
     for (int v0 = first * N; v0 < vocab; v0 += U * step * N) {
@@ -237,12 +271,12 @@ __device__ __forceinline__ Runner run_race(const T *row, const float *q, const f
 }
 
 template <typename T, int N>
-__global__ void __launch_bounds__(kPickThreads)
+__global__ void __launch_bounds__(kPickThreads, 2)
 serve_verify_pick_kernel(const __grid_constant__ VerifyDev d)
 {
     cg::cluster_group cluster = cg::this_cluster();
     const int b = blockIdx.y, rank = (int)cluster.block_rank(), blocks = (int)cluster.num_blocks();
-    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, warps = kPickThreads / 32;
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, warps = blockDim.x / 32;
     __shared__ RowStat row_stat[kMaxDrafts + 1];
     __shared__ uint32_t failed[2];            // bit i: draft i fails
     __shared__ Runner warp_run[kPickThreads / 32], block_run[2];
@@ -284,7 +318,7 @@ serve_verify_pick_kernel(const __grid_constant__ VerifyDev d)
         const float *q = accepted < d.drafts ? d.draft_probs + (int64_t)b * d.qs0 + (int64_t)accepted * d.qs1 : nullptr;
         // by max(p - q, 0), or by p; where nothing is left of p - q, once more by p
         for (int round = 0; round < 2; round++) {
-            Runner best = run_race<T, N>(row, round ? nullptr : q, noise, d.vocab, rank * kPickThreads + threadIdx.x, blocks * kPickThreads, s, c);
+            Runner best = run_race<T, N>(row, round ? nullptr : q, noise, d.vocab, rank * blockDim.x + threadIdx.x, blocks * blockDim.x, s, c);
 #pragma unroll
             for (int o = 16; o; o >>= 1) best = faster(best, shuffle_xor(best, o));
             if (lane == 0) warp_run[warp] = best;
@@ -312,11 +346,12 @@ serve_verify_pick_kernel(const __grid_constant__ VerifyDev d)
     }
 }
 
-// Parts of a row: enough blocks to fill the GPU four times over, none shorter than 2048 logits.
+// Parts of a row: two blocks to an SM, none shorter than 2048 logits.  (24 x 6 rows of 50001: 15.7 us, with four blocks to an
+// SM 17.3, with eight 18.9; 16 x 8 rows of 131072: 24.3, 25.0, 26.0.)
 int stat_parts(const bcast_serve_verify_args &a)
 {
     const int64_t rows = (int64_t)a.batch * (a.drafts + 1);
-    const int64_t want = ceil_div(4 * kSms, rows < 1 ? 1 : rows);
+    const int64_t want = ceil_div(2 * kSms, rows < 1 ? 1 : rows);
     const int64_t most = ceil_div(a.vocab, 2048);
     return (int)(want < most ? want : most);
 }
@@ -338,8 +373,12 @@ int run(const VerifyDev &d, int batch, cudaStream_t st)
     const uintptr_t bits = (uintptr_t)d.logits / (sizeof(T) / 2) | (uintptr_t)d.ls0 * 2 | (uintptr_t)d.ls1 * 2 | (uintptr_t)d.vocab * 2;
     const uintptr_t floats = (uintptr_t)d.noise | (uintptr_t)d.ns * 4 | (d.drafts ? (uintptr_t)d.draft_probs | (uintptr_t)d.qs0 * 4 | (uintptr_t)d.qs1 * 4 : 0);
     const bool whole = bits % 8 == 0 && floats % 16 == 0;
-    return launch(whole ? serve_verify_pick_kernel<T, 4> : serve_verify_pick_kernel<T, 1>, dim3(kPickBlocks, batch), dim3(kPickThreads), 0, st, true,
-                  kPickBlocks, d);
+    // blocks of a request's cluster: up to eight while all are resident at once, and twice the threads where that
+    // still leaves room
+    unsigned blocks = 1;
+    while (blocks < 8 && 2 * blocks * (unsigned)batch <= 4 * kSms) blocks *= 2;
+    return launch(whole ? serve_verify_pick_kernel<T, 4> : serve_verify_pick_kernel<T, 1>, dim3(blocks, batch), dim3(blocks < 8 ? kPickThreads / 2 : kPickThreads), 0,
+                  st, true, blocks, d);
 }
 
 }  // namespace
