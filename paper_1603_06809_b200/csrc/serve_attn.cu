@@ -300,13 +300,15 @@ serve_attn_own_kernel(const __grid_constant__ AttnDev d)
 // ------------------------------------------------------------------------------------------- shared prefix
 constexpr int kTileKeys = 128, kKvStages = 4, kPrefixThreads = 320;
 constexpr int kPolyEvery = 4;                 // every fourth pair of exponentials goes to the multiply-add units
-constexpr float kSlack = 8.0f;                // powers of two that a row's maximum may lag behind
+// Powers of two that a row's maximum may lag behind: weights up to 2^kSlack (and 2^kShift).  32-bit sums and bf16
+// weights have the exponents for much more, fp16 weights end at 2^16.
+template <typename T> constexpr float kSlack = std::is_same_v<T, __half> ? 8.0f : 24.0f;
 
 template <int DB, bool TWO> constexpr size_t prefix_smem() { return (size_t)(TWO ? 2 : 1) * DB * 16384 + (size_t)kKvStages * DB * 16384 + 1024; }
 
 // The state of one row's softmax.
 struct Row {
-    float m = -INFINITY;  // what the weights are taken against (a power of two); may lag the maximum by kSlack
+    float m = -INFINITY;  // what the weights are taken against (a power of two); may lag the maximum
     float l = 0.0f;
 };
 
@@ -323,7 +325,7 @@ __device__ __forceinline__ void exp2_pair(uint64_t x, float &a, float &b)
     x = pair(a, b);
     const float magic = 12582912.0f;
     const uint64_t t = add2(x, pair(magic, magic));
-    const uint64_t f = add2(x, mul2(add2(t, pair(-magic, -magic)), pair(-1.0f, -1.0f)));
+    const uint64_t f = fma2(add2(t, pair(-magic, -magic)), pair(-1.0f, -1.0f), x);
     uint64_t y;
     if constexpr (std::is_same_v<T, __half>) {
         y = pair(0.009570102207362652f, 0.009570102207362652f);
@@ -344,63 +346,113 @@ __device__ __forceinline__ void exp2_pair(uint64_t x, float &a, float &b)
     b = __uint_as_float(__float_as_uint(b) + (__float_as_uint(tb) << 23));
 }
 
-// One tile of a row's scores (tensor memory at `s`, this thread's lane) to weights, written over them as 16-bit
-// pairs.  Where the row's maximum has grown by more than kSlack, what is summed so far (accumulator at `o`) is
-// scaled down first; below that the weights just grow past 1, by at most 2^kSlack.  `most` is signalled when the
-// weights of the first 96 tokens are there, so that their product with V runs under the last exponentials.
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+__device__ __forceinline__ float min3(float a, float b, float c)
+{
+    float r;
+    asm("min.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+
+// The first of 16-bit weight `w` times `x`, and the second.
+template <typename T>
+__device__ __forceinline__ uint32_t scale2(uint32_t w, float x)
+{
+    const T *v = (const T *)&w;
+    return pack2<T>(to_f32(v[0]) * x, to_f32(v[1]) * x);
+}
+
+// One tile of a row's scores (tensor memory at `s`, this thread's lane) to weights, 32 tokens at a time, written
+// over scores that have been read already as 16-bit pairs.  The weights are taken against a maximum that may lag: it
+// moves to the largest of 32 scores only where that is more than kSlack above it, and from there on.  What was taken
+// against an earlier one (the sums, the accumulator at `o` among them, and this tile's first weights) is scaled to
+// the last one in a place of its own before anyone may read it, which few tiles get to.  So the scores are read
+// once, no weight waits for the maximum of the tile, and there is one branch in it: a warp has only one other on its
+// scheduler to hide its latencies, so instructions of its own that do not wait for one another have to.  `most` is
+// signalled when the weights of the first 96 tokens are there to stay: their product with V runs under the
+// last exponentials.
 template <typename T, bool MASK>
 __device__ __forceinline__ void softmax_tile(Row &row, uint32_t s, uint32_t o, bool first, int valid, int columns, float c, uint32_t most)
 {
-    // The scores are read twice, once for their maximum and once for the weights: reading tensor memory costs
-    // less than keeping 128 of them in registers.  Weights never overwrite scores that are still to be read.
-    float t[4];
     const bool up = c >= 0.0f;
-    {
-        uint32_t x[2][32];
-        tmem_load32(s, x[0]);
-#pragma unroll
-        for (int g = 0; g < 4; g++) {
-            tmem_wait_load32(x[g & 1]);
-            if (g < 3) tmem_load32(s + (g + 1) * 32, x[(g + 1) & 1]);
-#pragma unroll
-            for (int i = 0; i < 32; i++) {
-                const float v = __uint_as_float(x[g & 1][i]);
-                if (g == 0 && i < 4) t[i] = MASK && i >= valid ? t[0] : v;        // the tile's first token is always there
-                else if (!MASK || g * 32 + i < valid) t[i & 3] = up ? fmaxf(t[i & 3], v) : fminf(t[i & 3], v);
-            }
-        }
-        t[0] = up ? fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])) : fminf(fminf(t[0], t[1]), fminf(t[2], t[3]));
-    }
-    // NaN scores leave the maximum alone (NaN * c is dropped by fmaxf) and become NaN weights
-    const float top = fmaxf(row.m, t[0] * c);
-    const bool grow = top > row.m + (first ? 0.0f : kSlack);
-    const float next = grow ? top : row.m, from = next == -INFINITY ? 0.0f : next;
-    if (!first && __any_sync(~0u, grow)) {
-        const float fix = grow ? exp2_approx(row.m - from) : 1.0f;
-        row.l *= fix;
-        for (int i = 0; i < columns; i += 16) {
-            uint32_t v[16];
-            tmem_load16(o + i, v);
-            tmem_wait_load16(v);
-#pragma unroll
-            for (int k = 0; k < 16; k++) v[k] = __float_as_uint(__uint_as_float(v[k]) * fix);
-            tmem_store16(o + i, v);
-        }
-    }
-    row.m = next;
-    const uint64_t cc = pair(c, c), ff = pair(kShift<T> - from, kShift<T> - from);
-    uint64_t sum0 = 0, sum1 = 0;                      // pairs of 0.0f
+    const uint64_t cc = pair(c, c);
+    const float start = row.m;
+    float m[4];                                       // what the group's weights are taken against
+    uint64_t sum[4];
     uint32_t x[2][32];
     tmem_load32(s, x[0]);
 #pragma unroll
     for (int g = 0; g < 4; g++) {
-        uint32_t w[16];
         tmem_wait_load32(x[g & 1]);
+        const float *v = (const float *)x[g & 1];
         if (g < 3) tmem_load32(s + (g + 1) * 32, x[(g + 1) & 1]);
+        // the largest of scale * score; NaN leaves it alone and becomes a NaN weight
+        float t0 = up ? -INFINITY : INFINITY, t1 = t0;
+        if (MASK) {
+#pragma unroll
+            for (int i = 0; i < 32; i++)
+                if (g * 32 + i < valid) t0 = up ? fmaxf(t0, v[i]) : fminf(t0, v[i]);
+        } else if (up) {
+#pragma unroll
+            for (int i = 0; i < 32; i += 4) {
+                t0 = max3(t0, v[i], v[i + 1]);
+                t1 = max3(t1, v[i + 2], v[i + 3]);
+            }
+            t0 = fmaxf(t0, t1);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 32; i += 4) {
+                t0 = min3(t0, v[i], v[i + 1]);
+                t1 = min3(t1, v[i + 2], v[i + 3]);
+            }
+            t0 = fminf(t0, t1);
+        }
+        const float top = MASK && g * 32 >= valid ? -INFINITY : t0 * c;
+        row.m = top > row.m + (row.m == -INFINITY ? 0.0f : kSlack<T>) ? top : row.m;
+        m[g] = row.m;
+        if (g == 3) {
+            if (__any_sync(~0u, m[3] != m[0] || (!first && m[0] != start))) {
+                const float fix = exp2_approx(start - m[3]);
+                if (m[3] != start) {
+                    row.l *= fix;
+                }
+                for (int i = 0; i < (first ? 0 : columns); i += 16) {
+                    uint32_t y[16];
+                    tmem_load16(o + i, y);
+                    tmem_wait_load16(y);
+#pragma unroll
+                    for (int k = 0; k < 16; k++) y[k] = m[3] == start ? y[k] : __float_as_uint(__uint_as_float(y[k]) * fix);
+                    tmem_store16(o + i, y);
+                }
+                tmem_wait_store();
+#pragma unroll
+                for (int i = 0; i < 3; i++) {
+                    const float part = m[i] == m[3] ? 1.0f : exp2_approx(m[i] - m[3]);
+                    sum[i] = mul2(sum[i], pair(part, part));
+                    uint32_t y[16];
+                    tmem_load16(s + i * 16, y);
+                    tmem_wait_load16(y);
+#pragma unroll
+                    for (int k = 0; k < 16; k++) y[k] = scale2<T>(y[k], part);
+                    tmem_store16(s + i * 16, y);
+                }
+            }
+            tmem_wait_store();
+            tc_fence_before();
+            mbar_arrive(most);
+        }
+        const float less = kShift<T> - (row.m == -INFINITY ? 0.0f : row.m);
+        const uint64_t ll = pair(less, less);
+        uint32_t w[16];
+        sum[g] = 0;                                   // a pair of 0.0f
 #pragma unroll
         for (int i = 0; i < 16; i++) {
-            const int at = g * 32 + 2 * i;
-            const uint64_t z = fma2(pair(__uint_as_float(x[g & 1][2 * i]), __uint_as_float(x[g & 1][2 * i + 1])), cc, ff);
+            const uint64_t z = fma2(pair(v[2 * i], v[2 * i + 1]), cc, ll);
             float a, b;
             if (i % kPolyEvery == kPolyEvery - 1) {
                 exp2_pair<T>(z, a, b);
@@ -410,22 +462,16 @@ __device__ __forceinline__ void softmax_tile(Row &row, uint32_t s, uint32_t o, b
                 b = exp2_approx(b);
             }
             if (MASK) {
-                if (at >= valid) a = 0.0f;
-                if (at + 1 >= valid) b = 0.0f;
+                if (g * 32 + 2 * i >= valid) a = 0.0f;
+                if (g * 32 + 2 * i + 1 >= valid) b = 0.0f;
             }
-            if (i & 1) sum1 = add2(sum1, pair(a, b));
-            else sum0 = add2(sum0, pair(a, b));
+            sum[g] = add2(sum[g], pair(a, b));
             w[i] = pack2<T>(a, b);
         }
         tmem_store16(s + g * 16, w);
-        if (g == 2) {
-            tmem_wait_store();
-            tc_fence_before();
-            mbar_arrive(most);
-        }
     }
     float a, b;
-    unpair(add2(sum0, sum1), a, b);
+    unpair(add2(add2(sum[0], sum[1]), add2(sum[2], sum[3])), a, b);
     row.l += a + b;
     tmem_wait_store();
 }
