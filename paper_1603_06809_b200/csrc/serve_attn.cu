@@ -4,12 +4,13 @@
 // Softmax over a set of tokens that is cut into parts: with m_p >= the largest score of part p (in powers of two),
 // l_p = sum 2^(s - m_p) and o_p = sum 2^(s - m_p) v, the whole is  M = max m_p,
 //   out = sum_p 2^(m_p - M) o_p / sum_p 2^(m_p - M) l_p.
-// Three kernels, the second starting while the first runs out (programmatic launch):
-//   own kernel      a block per (request, key/value head, part of its own tokens): few rows against tokens that
-//                   nobody else reads, so bound by reading them; warps take 16 tokens at a time through mma.sync
+// Three kernels, the second starting once the first is on its way (programmatic launch):
 //   prefix kernel   a block per (key/value head, tile of rows, part of the prefix).  The rows are those of ALL
 //                   requests -- request, new token and query head of the group --, so a prefix token is read once
 //                   for 128 or 256 rows and the two products run on tcgen05
+//   own kernel      a block per (request, key/value head, part of its own tokens): few rows against tokens that
+//                   nobody else reads, so bound by reading them; warps take 16 tokens at a time through mma.sync.
+//                   A block of it fits beside one of the prefix kernel on an SM.
 //   join kernel     the formula above, a warp per row
 #include "serve_device.cuh"
 #include "serve_internal.h"
@@ -28,7 +29,7 @@ struct AttnDev {
     int *status;
     int64_t qs[3], os[3], oks[3], ovs[3];
     int64_t own_cap, num_pages, pts, rows;       // rows: batch * fresh * q_heads
-    int32_t batch, fresh, q_heads, kv_heads, group, dim, page, prefix_len;
+    int32_t batch, fresh, q_heads, kv_heads, group, dim, page, page_shift, prefix_len;
     int32_t prefix_splits, prefix_parts, row_tiles, own_splits, own_chunk, parts;
     float scale_log2;     // scale * log2(e): the softmax is taken in powers of two
 };
@@ -52,7 +53,7 @@ template <> __device__ __forceinline__ uint32_t pack2<__half>(float lo, float hi
 }
 
 // ------------------------------------------------------------------------------------------- own tokens
-constexpr int kOwnWarps = 4, kOwnKeys = 16, kOwnStages = 3;
+constexpr int kOwnWarps = 3, kOwnKeys = 16, kOwnRows = 16, kOwnStages = 2;
 
 template <int DB> constexpr size_t own_smem() { return (size_t)kOwnWarps * kOwnStages * 2 * kOwnKeys * DB * 128; }
 
@@ -81,201 +82,193 @@ __device__ __forceinline__ void mma_sync(float *c, const uint32_t *a, uint32_t b
                      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// Where a request's own token `at` lies: page (or request) and place in it; page -1 if it is not there.
+// Where a request's own token `at` lies: page (or request) and place in it; page -1 if it is not there.  Looked up
+// whether or not the token is in the cache yet (the table has a place for it), so as not to wait for the length.
 struct Place {
     int32_t page, slot;
 };
-__device__ __forceinline__ Place place_of(const AttnDev &d, int b, int at, int end)
+__device__ __forceinline__ Place place_of(const AttnDev &d, int b, int at)
 {
-    if (at >= end) return Place{-1, 0};
+    if (at >= d.own_cap) return Place{-1, 0};
     if (!d.page_table) return Place{b, at};
-    const int32_t p = d.page_table[(int64_t)b * d.pts + at / d.page];
-    return Place{p >= 0 && p < d.num_pages ? p : -1, at % d.page};
+    const int n = d.page_shift >= 0 ? at >> d.page_shift : at / d.page;
+    const int32_t p = d.page_table[(int64_t)b * d.pts + n];
+    return Place{p >= 0 && p < d.num_pages ? p : -1, at - n * d.page};
 }
+// Where chunk `c` of row `r` of a tile lies, rows of 128 or 256 bytes: the eight rows that a matrix load reads at a
+// time are in different banks.
+template <int ROW>
+__device__ __forceinline__ uint32_t own_at(int r, int c) { return r * ROW + ((c ^ (r & 7)) << 4); }
 
-// A warp holds MT tiles of 16 rows and walks over its share of the block's tokens, 16 at a time: scores by
-// mma.m16n8k16 (rows x tokens), weights, then rows x dim.  Its K and V tiles go through a ring of three stages
-// of its own (cp.async, no barrier between warps); the four warps' results are joined at the end.
-template <typename T, int DB, int MT>
-__global__ void __launch_bounds__(kOwnWarps * 32)
+// A warp holds 16 rows and walks over its share of the block's tokens, 16 at a time: scores by mma.m16n8k16 (rows x
+// tokens), weights, then rows x dim.  Its K and V tiles go through two stages of its own (cp.async, no barrier
+// between warps); the warps' results are joined at the end.  Registers and shared memory are kept to what the
+// prefix kernel leaves of an SM, so that these blocks read memory while that one computes.
+template <typename T, int DB>
+__global__ void __launch_bounds__(kOwnWarps * 32, 4)
 serve_attn_own_kernel(const __grid_constant__ AttnDev d)
 {
-    constexpr int D = DB * 64, row_bytes = DB * 128, chunks = DB * 8, tile = kOwnKeys * row_bytes;
+    constexpr int D = DB * 64, row_bytes = DB * 128, tile = kOwnKeys * row_bytes;
     extern __shared__ __align__(128) uint8_t smem[];
-    __shared__ float warp_m[kOwnWarps][MT * 16], warp_l[kOwnWarps][MT * 16];
-    const int b = blockIdx.z, kv = blockIdx.y % d.kv_heads, r0 = blockIdx.y / d.kv_heads * MT * 16, split = blockIdx.x;
+    __shared__ float warp_m[kOwnWarps][kOwnRows], warp_l[kOwnWarps][kOwnRows];
+    const int b = blockIdx.z, kv = blockIdx.y % d.kv_heads, r0 = blockIdx.y / d.kv_heads * kOwnRows, split = blockIdx.x;
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, rows = d.fresh * d.group;
     launch_next();
+    const int k0 = split * d.own_chunk;
+    // length, pages and queries: three loads that do not wait for one another
+    Place ahead[2];                           // of the two tokens of a block that this lane copies parts of
+#pragma unroll
+    for (int h = 0; h < 2; h++) ahead[h] = place_of(d, b, k0 + warp * kOwnKeys + h * 8 + lane / 4);
+    // queries, as the first operand's fragments; rows and columns that do not exist are zero
+    uint32_t q[DB * 4][4];
+#pragma unroll
+    for (int half = 0; half < 2; half++) {
+        const int r = r0 + half * 8 + lane / 4;
+        const T *row = (const T *)d.q + b * d.qs[0] + r / d.group * d.qs[1] + (kv * d.group + r % d.group) * d.qs[2];
+#pragma unroll
+        for (int i = 0; i < DB * 8; i++) {
+            const int c = i * 8 + lane % 4 * 2;
+            q[i / 2][half + i % 2 * 2] = r < rows && c < d.dim ? *(const uint32_t *)(row + c) : 0u;
+        }
+    }
     const int len = (int)min(max((int64_t)d.own_len[b], (int64_t)0), d.own_cap);
-    const int k0 = split * d.own_chunk, k1 = min(len, k0 + d.own_chunk);
-    const int part = d.prefix_parts + split;
-    if (k0 >= k1) {
-        for (int r = r0 + threadIdx.x; r < min(rows, r0 + MT * 16); r += kOwnWarps * 32)
-            d.part_ml[part * d.rows + ((int64_t)b * d.fresh + r / d.group) * d.q_heads + kv * d.group + r % d.group] =
-                make_float2(-INFINITY, 0.0f);
-        return;
+    const int k1 = min(len, k0 + d.own_chunk), part = d.prefix_parts + split;
+    int limit[2];                             // own tokens that a row sees
+#pragma unroll
+    for (int half = 0; half < 2; half++) {
+        const int r = r0 + half * 8 + lane / 4;
+        limit[half] = r < rows ? len - d.fresh + r / d.group + 1 : 0;
     }
 
-    // queries, as the first operand's fragments; rows and columns that do not exist are zero
-    uint32_t q[MT][DB * 4][4];
-    int limit[MT][2];                         // own tokens that a row sees
-#pragma unroll
-    for (int t = 0; t < MT; t++)
-#pragma unroll
-        for (int half = 0; half < 2; half++) {
-            const int r = r0 + t * 16 + half * 8 + lane / 4;
-            limit[t][half] = r < rows ? len - d.fresh + r / d.group + 1 : 0;
-            const T *row = (const T *)d.q + b * d.qs[0] + r / d.group * d.qs[1] + (kv * d.group + r % d.group) * d.qs[2];
-#pragma unroll
-            for (int i = 0; i < DB * 8; i++) {
-                const int c = i * 8 + lane % 4 * 2;
-                q[t][i / 2][half + i % 2 * 2] = r < rows && c < d.dim ? *(const uint32_t *)(row + c) : 0u;
-            }
-        }
-
     const uint32_t base = smem_u32(smem) + warp * kOwnStages * 2 * tile;
-    const int blocks = (k1 - k0 + kOwnKeys - 1) / kOwnKeys, mine = (blocks - warp + kOwnWarps - 1) / kOwnWarps;
-    uint32_t there[kOwnStages];
-    const T *kbase = (const T *)d.ok + kv * d.oks[2], *vbase = (const T *)d.ov + kv * d.ovs[2];
-    // the page of the next block is looked up one block ahead, so that its latency is not in the way of the copies
-    Place ahead = place_of(d, b, k0 + warp * kOwnKeys + lane % 16, k1);
+    const int blocks = k1 > k0 ? (k1 - k0 + kOwnKeys - 1) / kOwnKeys : 0, mine = (blocks - warp + kOwnWarps - 1) / kOwnWarps;
+    const T *kbase = (const T *)d.ok + kv * d.oks[2] + lane % 4 * 8, *vbase = (const T *)d.ov + kv * d.ovs[2] + lane % 4 * 8;
+    // Four lanes copy a token, 64 bytes at a time: whole sectors, and one address per lane and token.  Its page is
+    // looked up one block ahead, so that this is not in the way of the copies.  Returns which tokens are there, token k at
+    // bit 4 (k % 8) of word k / 8.
     auto load = [&](int i, int stage) {
-        const Place p = ahead;
-        ahead = place_of(d, b, k0 + ((i + 1) * kOwnWarps + warp) * kOwnKeys + lane % 16, k1);
-        const uint32_t bits = __ballot_sync(~0u, p.page >= 0) & 0xffffu;
-        const uint32_t ks = base + stage * 2 * tile, vs = ks + tile;
+        uint2 bits;
+        const uint32_t ks = base + stage * 2 * tile;
 #pragma unroll
-        for (int j = 0; j < kOwnKeys * chunks / 32; j++) {
-            const int r = (j * 32 + lane) / chunks, c = lane % chunks;
-            const int32_t page = __shfl_sync(~0u, p.page, r), slot = __shfl_sync(~0u, p.slot, r);
-            const bool ok = page >= 0 && c * 8 < d.dim;
-            const uint32_t to = r * row_bytes + ((c ^ (r & 7)) << 4);
-            copy16(ks + to, ok ? kbase + page * d.oks[0] + slot * d.oks[1] + c * 8 : kbase, ok);
-            copy16(vs + to, ok ? vbase + page * d.ovs[0] + slot * d.ovs[1] + c * 8 : vbase, ok);
+        for (int h = 0; h < 2; h++) {
+            const int r = h * 8 + lane / 4, at = k0 + (i * kOwnWarps + warp) * kOwnKeys + r;
+            const Place p = ahead[h];
+            ahead[h] = place_of(d, b, at + kOwnWarps * kOwnKeys);
+            const bool ok = at < k1 && p.page >= 0;
+            (h ? bits.y : bits.x) = __ballot_sync(~0u, ok);
+            const T *kr = ok ? kbase + p.page * d.oks[0] + p.slot * d.oks[1] : (const T *)d.ok;
+            const T *vr = ok ? vbase + p.page * d.ovs[0] + p.slot * d.ovs[1] : (const T *)d.ov;
+#pragma unroll
+            for (int j = 0; j < DB * 2; j++) {
+                const int c = j * 4 + lane % 4;
+                const bool in = ok && c * 8 < d.dim;
+                copy16(ks + own_at<row_bytes>(r, c), in ? kr + j * 32 : (const T *)d.ok, in);
+                copy16(ks + tile + own_at<row_bytes>(r, c), in ? vr + j * 32 : (const T *)d.ov, in);
+            }
         }
         return bits;
     };
-#pragma unroll
-    for (int i = 0; i < kOwnStages; i++) {
-        there[i] = 0;
-        if (i < kOwnStages - 1) {
-            if (i < mine) there[i] = load(i, i);
-            asm volatile("cp.async.commit_group;" ::: "memory");
-        }
-    }
+    uint2 there[2] = {};
+    if (mine > 0) there[0] = load(0, 0);
+    asm volatile("cp.async.commit_group;" ::: "memory");
 
-    float o[MT][DB * 8][4], m[MT][2], l[MT][2];
+    float o[DB * 8][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {};
 #pragma unroll
-    for (int t = 0; t < MT; t++) {
-#pragma unroll
-        for (int n = 0; n < DB * 8; n++) o[t][n][0] = o[t][n][1] = o[t][n][2] = o[t][n][3] = 0.0f;
-        m[t][0] = m[t][1] = -INFINITY;
-        l[t][0] = l[t][1] = 0.0f;
-    }
-    for (int i0 = 0; i0 < mine; i0 += kOwnStages) {
-#pragma unroll
-        for (int s = 0; s < kOwnStages; s++) {
-            const int i = i0 + s;
-            if (i >= mine) break;
-            asm volatile("cp.async.wait_group %0;" ::"n"(kOwnStages - 2) : "memory");
-            __syncwarp();
-            {
-                const int next = (s + kOwnStages - 1) % kOwnStages;       // the stage that was used up last
-                if (i + kOwnStages - 1 < mine) there[next] = load(i + kOwnStages - 1, next);
-                asm volatile("cp.async.commit_group;" ::: "memory");
-            }
-            const uint32_t ks = base + s * 2 * tile, vs = ks + tile;
-            const int at = k0 + (i * kOwnWarps + warp) * kOwnKeys;
-            float sc[MT][2][4];
-#pragma unroll
-            for (int t = 0; t < MT; t++)
-#pragma unroll
-                for (int n = 0; n < 2; n++) sc[t][n][0] = sc[t][n][1] = sc[t][n][2] = sc[t][n][3] = 0.0f;
-#pragma unroll
-            for (int k = 0; k < DB * 4; k++) {
-                uint32_t f[4];
-                const int r = lane / 16 * 8 + lane % 8, c = k * 2 + lane / 8 % 2;
-                ldmatrix(f, ks + r * row_bytes + ((c ^ (r & 7)) << 4));
-#pragma unroll
-                for (int t = 0; t < MT; t++) {
-                    mma_sync<T>(sc[t][0], q[t][k], f[0], f[1]);
-                    mma_sync<T>(sc[t][1], q[t][k], f[2], f[3]);
-                }
-            }
-            uint32_t p[MT][4];
-#pragma unroll
-            for (int t = 0; t < MT; t++)
-#pragma unroll
-                for (int half = 0; half < 2; half++) {
-                    float top = -INFINITY;
-                    bool seen[4];
-#pragma unroll
-                    for (int x = 0; x < 4; x++) {
-                        const int key = x / 2 * 8 + lane % 4 * 2 + x % 2;
-                        float &v = sc[t][x / 2][half * 2 + x % 2];
-                        seen[x] = (there[s] >> key & 1u) && at + key < limit[t][half];
-                        v *= d.scale_log2;
-                        if (seen[x]) top = fmaxf(top, v);
-                    }
-                    top = fmaxf(top, __shfl_xor_sync(~0u, top, 1));
-                    top = fmaxf(top, __shfl_xor_sync(~0u, top, 2));
-                    // nothing seen so far: 0 in the place of -infinity, so that 2^-infinity is 0 and NaN stays NaN
-                    const float next = fmaxf(m[t][half], top), from = next == -INFINITY ? 0.0f : next;
-                    const float fix = exp2_approx(m[t][half] - from);
-                    m[t][half] = next;
-                    float w[4];
-#pragma unroll
-                    for (int x = 0; x < 4; x++)
-                        w[x] = seen[x] ? exp2_approx(sc[t][x / 2][half * 2 + x % 2] - (from - kShift<T>)) : 0.0f;
-                    l[t][half] = l[t][half] * fix + ((w[0] + w[1]) + (w[2] + w[3]));
-                    p[t][half] = pack2<T>(w[0], w[1]);
-                    p[t][half + 2] = pack2<T>(w[2], w[3]);
-                    if (__any_sync(~0u, fix != 1.0f)) {
-#pragma unroll
-                        for (int n = 0; n < DB * 8; n++) {
-                            o[t][n][half * 2] *= fix;
-                            o[t][n][half * 2 + 1] *= fix;
-                        }
-                    }
-                }
-#pragma unroll
-            for (int n = 0; n < DB * 4; n++) {
-                uint32_t f[4];
-                const int r = lane / 8 % 2 * 8 + lane % 8, c = n * 2 + lane / 16;
-                ldmatrix_t(f, vs + r * row_bytes + ((c ^ (r & 7)) << 4));
-#pragma unroll
-                for (int t = 0; t < MT; t++) {
-                    mma_sync<T>(o[t][n * 2], p[t], f[0], f[1]);
-                    mma_sync<T>(o[t][n * 2 + 1], p[t], f[2], f[3]);
-                }
-            }
-            __syncwarp();
+    for (int n = 0; n < DB * 8; n++) o[n][0] = o[n][1] = o[n][2] = o[n][3] = 0.0f;
+    for (int i = 0; i < mine; i++) {
+        const int s = i & 1;
+        if (i + 1 < mine) {
+            const uint2 bits = load(i + 1, s ^ 1);
+            if (s) there[0] = bits;
+            else there[1] = bits;
         }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        asm volatile("cp.async.wait_group 1;" ::: "memory");
+        __syncwarp();
+        const uint32_t ks = base + s * 2 * tile, vs = ks + tile;
+        const uint2 here = s ? there[1] : there[0];
+        const int at = k0 + (i * kOwnWarps + warp) * kOwnKeys;
+        float sc[2][4] = {};
+#pragma unroll
+        for (int k = 0; k < DB * 4; k++) {
+            uint32_t f[4];
+            const int r = lane / 16 * 8 + lane % 8, c = k * 2 + lane / 8 % 2;
+            ldmatrix(f, ks + own_at<row_bytes>(r, c));
+            mma_sync<T>(sc[0], q[k], f[0], f[1]);
+            mma_sync<T>(sc[1], q[k], f[2], f[3]);
+        }
+        uint32_t p[4];
+#pragma unroll
+        for (int half = 0; half < 2; half++) {
+            float top = -INFINITY;
+            bool seen[4];
+#pragma unroll
+            for (int x = 0; x < 4; x++) {
+                const int key = lane % 4 * 2 + x % 2;  // of eight
+                float &v = sc[x / 2][half * 2 + x % 2];
+                seen[x] = ((x < 2 ? here.x : here.y) >> 4 * key & 1u) && at + x / 2 * 8 + key < limit[half];
+                v *= d.scale_log2;
+                if (seen[x]) top = fmaxf(top, v);
+            }
+            top = fmaxf(top, __shfl_xor_sync(~0u, top, 1));
+            top = fmaxf(top, __shfl_xor_sync(~0u, top, 2));
+            // nothing seen so far: 0 in the place of -infinity, so that 2^-infinity is 0 and NaN stays NaN
+            const float next = fmaxf(m[half], top), from = next == -INFINITY ? 0.0f : next;
+            const float fix = exp2_approx(m[half] - from);
+            m[half] = next;
+            float w[4];
+#pragma unroll
+            for (int x = 0; x < 4; x++) w[x] = seen[x] ? exp2_approx(sc[x / 2][half * 2 + x % 2] - (from - kShift<T>)) : 0.0f;
+            l[half] = l[half] * fix + ((w[0] + w[1]) + (w[2] + w[3]));
+            p[half] = pack2<T>(w[0], w[1]);
+            p[half + 2] = pack2<T>(w[2], w[3]);
+            if (__any_sync(~0u, fix != 1.0f)) {
+#pragma unroll
+                for (int n = 0; n < DB * 8; n++) {
+                    o[n][half * 2] *= fix;
+                    o[n][half * 2 + 1] *= fix;
+                }
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < DB * 4; n++) {
+            uint32_t f[4];
+            const int r = lane / 8 % 2 * 8 + lane % 8, c = n * 2 + lane / 16;
+            ldmatrix_t(f, vs + own_at<row_bytes>(r, c));
+            mma_sync<T>(o[n * 2], p, f[0], f[1]);
+            mma_sync<T>(o[n * 2 + 1], p, f[2], f[3]);
+        }
+        __syncwarp();
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
     __syncthreads();                          // the stages' memory is free
 
     float *all = (float *)smem;               // [warp][row][D]
 #pragma unroll
-    for (int t = 0; t < MT; t++)
-#pragma unroll
-        for (int half = 0; half < 2; half++) {
-            float sum = l[t][half];
-            sum += __shfl_xor_sync(~0u, sum, 1);
-            sum += __shfl_xor_sync(~0u, sum, 2);
-            const int r = t * 16 + half * 8 + lane / 4;
-            if (lane % 4 == 0) {
-                warp_m[warp][r] = m[t][half];
-                warp_l[warp][r] = sum;
-            }
+    for (int half = 0; half < 2; half++) {
+        float sum = l[half];
+        sum += __shfl_xor_sync(~0u, sum, 1);
+        sum += __shfl_xor_sync(~0u, sum, 2);
+        const int r = half * 8 + lane / 4;
+        if (lane % 4 == 0) {
+            warp_m[warp][r] = m[half];
+            warp_l[warp][r] = sum;
+        }
+        if (blocks > 0) {
 #pragma unroll
             for (int n = 0; n < DB * 8; n++)
-                *(float2 *)(all + (warp * MT * 16 + r) * D + n * 8 + lane % 4 * 2) = make_float2(o[t][n][half * 2], o[t][n][half * 2 + 1]);
+                *(float2 *)(all + (warp * kOwnRows + r) * D + n * 8 + lane % 4 * 2) = make_float2(o[n][half * 2], o[n][half * 2 + 1]);
         }
+    }
     __syncthreads();
-    for (int i = threadIdx.x; i < MT * 16 * (D / 4); i += kOwnWarps * 32) {
+    for (int i = threadIdx.x; i < kOwnRows * (D / 4); i += kOwnWarps * 32) {
         const int r = i / (D / 4), c = i % (D / 4) * 4;
         if (r0 + r >= rows || c >= d.dim) continue;
+        const int64_t row = ((int64_t)b * d.fresh + (r0 + r) / d.group) * d.q_heads + kv * d.group + (r0 + r) % d.group;
+        if (blocks == 0) {
+            if (c == 0) d.part_ml[part * d.rows + row] = make_float2(-INFINITY, 0.0f);
+            continue;
+        }
         float top = warp_m[0][r];
         for (int w = 1; w < kOwnWarps; w++) top = fmaxf(top, warp_m[w][r]);
         const float from = top == -INFINITY ? 0.0f : top;
@@ -283,28 +276,31 @@ serve_attn_own_kernel(const __grid_constant__ AttnDev d)
         float total = 0.0f;
         for (int w = 0; w < kOwnWarps; w++) {
             const float x = exp2_approx(warp_m[w][r] - from);
-            const float4 v = *(const float4 *)(all + (w * MT * 16 + r) * D + c);
+            const float4 v = *(const float4 *)(all + (w * kOwnRows + r) * D + c);
             sum.x += x * v.x;
             sum.y += x * v.y;
             sum.z += x * v.z;
             sum.w += x * v.w;
             total += x * warp_l[w][r];
         }
-        const int64_t row = ((int64_t)b * d.fresh + (r0 + r) / d.group) * d.q_heads + kv * d.group + (r0 + r) % d.group;
         // a row without weights may still hold NaN: l tells
         if (c == 0) d.part_ml[part * d.rows + row] = make_float2(total == 0.0f ? -INFINITY : from - kShift<T>, total);
         *(float4 *)(d.part_o + (part * d.rows + row) * d.dim + c) = sum;
     }
+    // the join kernel waits for this one; so this one does not end before the prefix kernel has
+    if (blockIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0) wait_previous();
 }
 
 // ------------------------------------------------------------------------------------------- shared prefix
-constexpr int kTileKeys = 128, kKvStages = 4, kPrefixThreads = 320;
+constexpr int kTileKeys = 128, kPrefixThreads = 320;
+template <bool TWO> constexpr int kKvStages = TWO ? 3 : 4;
 constexpr int kPolyEvery = 4;                 // every fourth pair of exponentials goes to the multiply-add units
 // Powers of two that a row's maximum may lag behind: weights up to 2^kSlack (and 2^kShift).  32-bit sums and bf16
 // weights have the exponents for much more, fp16 weights end at 2^16.
 template <typename T> constexpr float kSlack = std::is_same_v<T, __half> ? 8.0f : 24.0f;
 
-template <int DB, bool TWO> constexpr size_t prefix_smem() { return (size_t)(TWO ? 2 : 1) * DB * 16384 + (size_t)kKvStages * DB * 16384 + 1024; }
+// (on the way out the same memory holds, with a pitch of 64 DB + 4, 128 or 256 rows of sums, and 128 more columnwise)
+template <int DB, bool TWO> constexpr size_t prefix_smem() { return (size_t)(TWO ? 2 : 1) * DB * 16384 + (size_t)kKvStages<TWO> * DB * 16384 + 1024; }
 
 // The state of one row's softmax.
 struct Row {
@@ -479,14 +475,16 @@ __device__ __forceinline__ void softmax_tile(Row &row, uint32_t s, uint32_t o, b
 // TWO: two tiles of 128 rows, each with its own softmax warps and accumulator, take the same tokens, so that
 // one tile's matrix products run under the other's exponentials.  Otherwise (128 rows or fewer) the two halves share
 // the rows and take every other tile of tokens, and their results are joined at the end.
+// Launched first; its 160 KB and 128 registers a thread (the bound of 512 threads asks for that) leave room on an SM for
+// a block of the own kernel.
 template <typename T, int DB, bool TWO>
-__global__ void __launch_bounds__(kPrefixThreads, 1)
+__global__ void __launch_bounds__(512, 1)
 serve_attn_prefix_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                          const __grid_constant__ AttnDev d)
 {
-    constexpr int block = kTileKeys * 128, stage = DB * block;        // 64 columns of a tile; a tile
+    constexpr int block = kTileKeys * 128, stage = DB * block, stages = kKvStages<TWO>;       // 64 columns of a tile; a tile
     extern __shared__ uint8_t raw_smem[];
-    __shared__ __align__(8) uint64_t bars[2 * kKvStages + 10];
+    __shared__ __align__(8) uint64_t bars[2 * stages + 10];
     __shared__ float half_m[128], half_l[128];
     __shared__ uint32_t tmem_at;
     __shared__ int gave_up;
@@ -501,11 +499,11 @@ serve_attn_prefix_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
     uint8_t *smem = (uint8_t *)(((uintptr_t)raw_smem + 1023) & ~(uintptr_t)1023);
     uint8_t *qs = smem;
     const uint32_t q_at = smem_u32(qs), kv_at = q_at + (TWO ? 2 : 1) * stage;
-    const uint32_t full = smem_u32(bars), empty = full + 8 * kKvStages, q_full = empty + 8 * kKvStages, s_full = q_full + 8,
+    const uint32_t full = smem_u32(bars), empty = full + 8 * stages, q_full = empty + 8 * stages, s_full = q_full + 8,
                    p_most = s_full + 16, p_full = p_most + 16, o_full = p_full + 16, drained = o_full + 16;
     if (tid == 0) {
         gave_up = 0;
-        for (int i = 0; i < kKvStages; i++) {
+        for (int i = 0; i < stages; i++) {
             mbar_init(full + 8 * i, 1);
             mbar_init(empty + 8 * i, 1);
         }
@@ -530,7 +528,7 @@ serve_attn_prefix_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
     if (warp == 8) {
         if (lane == 0) {
             // ---- loads, in the order the matrix products take them
-            Ring<kKvStages> ring;
+            Ring<stages> ring;
             int issued = 0;
             auto load = [&](const CUtensorMap *map, int j) {
                 if (!mbar_wait(empty + 8 * ring.slot, ring.parity ^ 1u, &gave_up)) return false;
@@ -550,9 +548,9 @@ serve_attn_prefix_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
                 }
             }
             if (gave_up) {
-                Ring<kKvStages> r;
+                Ring<stages> r;
                 for (int i = 0; i < issued; i++) {
-                    if (i + kKvStages >= issued) mbar_drain(full + 8 * r.slot, r.parity);
+                    if (i + stages >= issued) mbar_drain(full + 8 * r.slot, r.parity);
                     r.step();
                 }
             }
@@ -567,7 +565,7 @@ serve_attn_prefix_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
         const uint32_t lead = elect_one();
         const uint32_t s_desc = mma_desc<T>(128, kTileKeys), o_desc = mma_desc<T>(128, (d.dim + 15) / 16 * 16, true);
         const uint64_t q_desc = smem_desc(q_at), k_desc = smem_desc(kv_at), v_desc = smem_desc(kv_at, block);
-        Ring<kKvStages> ring;
+        Ring<stages> ring;
         auto take = [&]() {                                           // the next tile of K or V, once it is there
             mbar_wait(full + 8 * ring.slot, ring.parity, &gave_up);
             tc_fence_after();
@@ -650,14 +648,24 @@ serve_attn_prefix_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
     } else {
         // ---- queries into the swizzled layout; rows and columns that do not exist are zero
         const int w = warp / 4, live = min(rows - r0, TWO ? 256 : 128);
-        for (int i = tid; i < (TWO ? 256 : 128) * DB * 8; i += 256) {
-            const int r = i / (DB * 8), c = i % (DB * 8), g = r0 + r;
-            uint4 v = make_uint4(0, 0, 0, 0);
-            if (r < live && c * 8 < d.dim) {
-                const int b = g / (d.fresh * d.group), t = g / d.group % d.fresh, h = kv * d.group + g % d.group;
-                v = *(const uint4 *)((const T *)d.q + b * d.qs[0] + t * d.qs[1] + h * d.qs[2] + c * 8);
+        constexpr int batch = DB * 4;                                 // chunks of 16 bytes that a thread has under way
+        for (int i0 = tid; i0 < (TWO ? 256 : 128) * DB * 8; i0 += batch * 256) {
+            uint4 v[batch];
+#pragma unroll
+            for (int u = 0; u < batch; u++) {
+                const int i = i0 + u * 256, row = i / (DB * 8), c = i % (DB * 8);
+                v[u] = make_uint4(0, 0, 0, 0);
+                if (row < live && c * 8 < d.dim) {
+                    const uint32_t g = r0 + row, bt = g / (uint32_t)d.group, b = bt / (uint32_t)d.fresh;
+                    v[u] = __ldg((const uint4 *)((const T *)d.q + b * d.qs[0] + (bt - b * d.fresh) * d.qs[1] +
+                                                 (kv * d.group + (g - bt * d.group)) * d.qs[2] + c * 8));
+                }
             }
-            *(uint4 *)(qs + r / 128 * stage + c / 8 * block + r % 128 * 128 + (((c % 8) ^ (r & 7)) << 4)) = v;
+#pragma unroll
+            for (int u = 0; u < batch; u++) {
+                const int i = i0 + u * 256, row = i / (DB * 8), c = i % (DB * 8);
+                *(uint4 *)(qs + row / 128 * stage + c / 8 * block + swizzled(row % 128, c % 8, 128)) = v[u];
+            }
         }
         fence_async_proxy();
         mbar_arrive(q_full);
@@ -667,7 +675,7 @@ serve_attn_prefix_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
         const uint32_t lanes = (uint32_t)(quarter * 32) << 16, s_at = tmem + lanes + w * 128, o_at = tmem + lanes + 256 + w * 128;
         const bool busy = (TWO ? w * 128 : 0) + quarter * 32 < live;  // some row of this warp exists
         const int mine = TWO ? nt : (nt - w + 1) / 2, columns = (d.dim + 15) / 16 * 16;
-        Row row;
+        Row state;
         bool ok = true;
         for (int it = 0; it < mine; it++) {
             ok = mbar_wait(s_full + 8 * w, it & 1, &gave_up);
@@ -678,23 +686,24 @@ serve_attn_prefix_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
             tc_fence_after();
             const int valid = d.prefix_len - (j0 + (TWO ? it : 2 * it + w)) * kTileKeys;
             if (!busy) mbar_arrive(p_most + 8 * w);
-            else if (valid >= kTileKeys) softmax_tile<T, false>(row, s_at, o_at, it == 0, kTileKeys, columns, d.scale_log2, p_most + 8 * w);
-            else softmax_tile<T, true>(row, s_at, o_at, it == 0, valid, columns, d.scale_log2, p_most + 8 * w);
+            else if (valid >= kTileKeys) softmax_tile<T, false>(state, s_at, o_at, it == 0, kTileKeys, columns, d.scale_log2, p_most + 8 * w);
+            else softmax_tile<T, true>(state, s_at, o_at, it == 0, valid, columns, d.scale_log2, p_most + 8 * w);
             tc_fence_before();
             mbar_arrive(p_full + 8 * w);
         }
         // ---- the way out: a row's sums as they are, with what they were taken against
         if (mine > 0 && ok) ok = mbar_wait(o_full + 8 * w, 0, &gave_up);
-        if (!TWO && w == 1 && mine > 0 && ok) ok = mbar_wait(o_full, 0, &gave_up);
+        // (both halves' products are done then, and what they read may be written over)
+        if (ok && (TWO || (w == 1 && mine > 0))) ok = mbar_wait(o_full + 8 * (w ^ 1), 0, &gave_up);
         ok = __all_sync(~0u, ok);
         tc_fence_after();
-        float m = row.l == 0.0f ? -INFINITY : (row.m == -INFINITY ? 0.0f : row.m) - kShift<T>, other = 0.0f, keep = 1.0f;
-        float *half = (float *)(smem + stage);        // [column][row], where K and V were: all products are done
+        float m = state.l == 0.0f ? -INFINITY : (state.m == -INFINITY ? 0.0f : state.m) - kShift<T>, other = 0.0f, keep = 1.0f;
+        float *half = (float *)smem;                  // [column][row], where the tiles were: all products are done
         if (!TWO) {
             // the two halves of the tokens become one part: the second hands over its sums
             if (w == 1) {
                 half_m[quarter * 32 + lane] = m;
-                half_l[quarter * 32 + lane] = row.l;
+                half_l[quarter * 32 + lane] = state.l;
                 if (busy && ok && mine > 0)
                     for (int c = 0; c < columns; c += 16) {
                         uint32_t v[16];
@@ -710,16 +719,18 @@ serve_attn_prefix_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
                 const float top = fmaxf(m, m1);
                 keep = exp2_approx(m - top);
                 other = exp2_approx(m1 - top);
-                row.l = keep * row.l + other * l1;
+                state.l = keep * state.l + other * l1;
                 m = top;
             }
         }
         if (busy && ok && (TWO || w == 0)) {
-            const int g = r0 + r;
-            const bool exists = r < live;
-            const int64_t at = split * d.rows + ((int64_t)(g / (d.fresh * d.group)) * d.fresh + g / d.group % d.fresh) * d.q_heads +
-                               kv * d.group + g % d.group;
-            if (exists) d.part_ml[at] = make_float2(m, row.l);
+            const uint32_t g = r0 + r, bt = g / (uint32_t)d.group;    // request and new token: rows come in that order
+            const int64_t row = split * d.rows + (int64_t)bt * d.q_heads + kv * d.group + (g - bt * d.group);
+            if (r < live) d.part_ml[row] = make_float2(m, state.l);
+            // through shared memory, where each warp has 32 rows of its own, and out row by row
+            constexpr int pitch = DB * 64 + 4;
+            static_assert((TWO ? 0 : 128 * DB * 64 * 4) + (TWO ? 8 : 4) * 32 * pitch * 4 <= (TWO ? 2 : 1) * stage + stages * stage);
+            float *rows32 = (float *)(smem + (TWO ? 0 : 128 * DB * 64 * 4)) + warp * 32 * pitch;
             for (int c = 0; c < columns; c += 16) {
                 float v[16];
                 tmem_load16(o_at + c, (uint32_t *)v);
@@ -729,8 +740,14 @@ serve_attn_prefix_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
                     for (int k = 0; k < 16; k++) v[k] = keep * v[k] + other * half[(c + k) * 128 + quarter * 32 + lane];
                 }
 #pragma unroll
-                for (int k = 0; k < 16; k += 4)
-                    if (exists && c + k < d.dim) *(float4 *)(d.part_o + at * d.dim + c + k) = *(const float4 *)(v + k);
+                for (int k = 0; k < 16; k += 4) *(float4 *)(rows32 + lane * pitch + c + k) = *(const float4 *)(v + k);
+            }
+            __syncwarp();
+            const int count = min(32, live - (r - lane));
+            float *to = d.part_o + row * d.dim;
+            for (int k = 0; k < count; k++) {
+                float *other_row = (float *)__shfl_sync(~0u, (unsigned long long)to, k);
+                if (lane * 4 < d.dim) *(float4 *)(other_row + lane * 4) = *(const float4 *)(rows32 + k * pitch + lane * 4);
             }
         }
         tc_fence_before();
@@ -739,7 +756,6 @@ serve_attn_prefix_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
     tc_fence_after();
     if (warp == 9) tmem_free(tmem, 512);
     if (tid == 0 && gave_up) atomicExch(d.status, 1);
-    wait_previous();                                                  // the own kernel's parts are the join's input too
 }
 
 // ------------------------------------------------------------------------------------------- join
@@ -846,11 +862,12 @@ Cut cut_of(const bcast_serve_attn_args &a)
     if (a.prefix_len > 0 && c.rows > 0) {
         c.row_tiles = ceil_div(head_rows, c.two ? 256 : 128);
         const int64_t items = c.row_tiles * a.kv_heads, tiles = ceil_div(a.prefix_len, 128);
-        // the number of parts that ends first, one block to an SM: a block costs its tiles and about four more to
-        // begin and to end
+        // the number of parts that ends first, one block to an SM: a block costs its tiles and about six more to
+        // begin and to end; a tenth more where there are more blocks than SMs, since the own kernel only starts when
+        // the last of them has
         int64_t best = INT64_MAX;
         for (int64_t s = 1; s <= tiles && s <= 64; s++) {
-            const int64_t cost = ceil_div(items * s, kSms) * (ceil_div(tiles, s) + 4);
+            const int64_t rounds = ceil_div(items * s, kSms), cost = rounds * (ceil_div(tiles, s) + 6) * (rounds > 1 ? 11 : 10);
             if (cost < best) {
                 best = cost;
                 c.prefix_splits = s;
@@ -859,12 +876,13 @@ Cut cut_of(const bcast_serve_attn_args &a)
         c.prefix_parts = c.prefix_splits;
     }
     if (a.own_cap > 0 && c.rows > 0) {
-        const int64_t own_rows = a.new_tokens * group;
-        c.own_tiles = ceil_div(own_rows, own_rows > 16 ? 32 : 16);
-        // parts of at least 128 tokens, until there are about two blocks for every SM
-        const int64_t blocks = (int64_t)a.batch * a.kv_heads * c.own_tiles;
-        int64_t s = ceil_div(2 * kSms, blocks);
-        s = s < ceil_div(a.own_cap, 128) ? s : ceil_div(a.own_cap, 128);
+        c.own_tiles = ceil_div(a.new_tokens * group, kOwnRows);
+        // parts of 256 tokens, 512 once that makes six blocks to an SM (a decode step of 32 requests with up to 700 own
+        // tokens: 36 us, with 512 38, with 128 39; 64 requests with up to 1024: 259, 251, 268), 128 where there are
+        // too few blocks otherwise
+        const int64_t blocks = (int64_t)a.batch * a.kv_heads * c.own_tiles, more = ceil_div(2 * kSms, blocks);
+        int64_t s = ceil_div(a.own_cap, blocks * ceil_div(a.own_cap, 512) >= 6 * kSms ? 512 : 256);
+        if (s < more) s = more < ceil_div(a.own_cap, 128) ? more : ceil_div(a.own_cap, 128);
         s = s < kJoinParts - 64 ? s : kJoinParts - 64;
         c.own_chunk = round_up(ceil_div(a.own_cap, s), 64);
         c.own_splits = ceil_div(a.own_cap, c.own_chunk);
@@ -878,13 +896,13 @@ int64_t workspace_of(const bcast_serve_attn_args &a, const Cut &c)
     return BCAST_SERVE_STATUS_BYTES + round_up(c.parts * c.rows * 8, 256) + c.parts * c.rows * a.dim * 4;
 }
 
-template <typename T, int DB, int MT>
+template <typename T, int DB>
 int run_own(const bcast_serve_attn_args &a, const AttnDev &d, const Cut &c, cudaStream_t st)
 {
     int rc;
-    if ((rc = allow_smem<serve_attn_own_kernel<T, DB, MT>>(own_smem<DB>()))) return rc;
-    return launch(serve_attn_own_kernel<T, DB, MT>, dim3((unsigned)c.own_splits, (unsigned)(a.kv_heads * c.own_tiles), a.batch),
-                  dim3(kOwnWarps * 32), own_smem<DB>(), st, false, 1, d);
+    if ((rc = allow_smem<serve_attn_own_kernel<T, DB>>(own_smem<DB>()))) return rc;
+    return launch(serve_attn_own_kernel<T, DB>, dim3((unsigned)c.own_splits, (unsigned)(a.kv_heads * c.own_tiles), a.batch),
+                  dim3(kOwnWarps * 32), own_smem<DB>(), st, c.prefix_splits > 0, 1, d);
 }
 
 template <typename T, int DB, bool TWO>
@@ -900,15 +918,15 @@ int run_prefix(const bcast_serve_attn_args &a, const AttnDev &d, const Cut &c, c
     const size_t smem = prefix_smem<DB, TWO>();
     if ((rc = allow_smem<serve_attn_prefix_kernel<T, DB, TWO>>(smem))) return rc;
     return launch(serve_attn_prefix_kernel<T, DB, TWO>, dim3((unsigned)(c.row_tiles * a.kv_heads * c.prefix_splits)), dim3(kPrefixThreads), smem, st,
-                  c.own_splits > 0, 1, mk, mv, d);
+                  false, 1, mk, mv, d);
 }
 
 template <typename T, int DB>
 int run(const bcast_serve_attn_args &a, const AttnDev &d, const Cut &c, cudaStream_t st)
 {
     int rc = BCAST_OK;
-    if (c.own_splits) rc = a.new_tokens * d.group > 16 ? run_own<T, DB, 2>(a, d, c, st) : run_own<T, DB, 1>(a, d, c, st);
-    if (!rc && c.prefix_splits) rc = c.two ? run_prefix<T, DB, true>(a, d, c, st) : run_prefix<T, DB, false>(a, d, c, st);
+    if (c.prefix_splits) rc = c.two ? run_prefix<T, DB, true>(a, d, c, st) : run_prefix<T, DB, false>(a, d, c, st);
+    if (!rc && c.own_splits) rc = run_own<T, DB>(a, d, c, st);
     if (rc) return rc;
     return launch(serve_attn_join_kernel<T>, dim3((unsigned)c.rows), dim3(kJoinThreads), 0, st, c.parts > 0, 1, d);
 }
@@ -982,6 +1000,9 @@ int bcast_serve_attn(const bcast_serve_attn_args *a, void *cuda_stream)
     d.group = a->q_heads / a->kv_heads;
     d.dim = a->dim;
     d.page = paged ? a->page_size : 1;
+    d.page_shift = -1;
+    for (int i = 0; i < 31; i++)
+        if (d.page == 1 << i) d.page_shift = i;
     d.prefix_len = (int32_t)a->prefix_len;
     d.prefix_splits = (int32_t)c.prefix_splits;
     d.prefix_parts = (int32_t)c.prefix_parts;
