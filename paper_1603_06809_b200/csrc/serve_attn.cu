@@ -9,12 +9,13 @@
 //                   requests -- request, new token and query head of the group --, so a prefix token is read once
 //                   for 128 or 256 rows and the two products run on tcgen05
 //   own kernel      a block per (request, key/value head, part of its own tokens): few rows against tokens that
-//                   nobody else reads, so bound by reading them; warps take 16 tokens at a time through mma.sync.
-//                   A block of it fits beside one of the prefix kernel on an SM.
+//                   nobody else reads, so bound by reading them; warps take 16 tokens at a time through mma.sync
 //   join kernel     the formula above, a warp per row
 #include "serve_device.cuh"
 #include "serve_internal.h"
 #include "serve_tma.h"
+
+#include <climits>
 
 namespace bcast_serve {
 namespace {
@@ -38,6 +39,10 @@ struct AttnDev {
 // is in l as well and cancels).  bf16 has the exponents of 32-bit floats.
 template <typename T> constexpr float kShift = std::is_same_v<T, __half> ? 7.0f : 0.0f;
 
+// Powers of two that a row's maximum may lag behind: weights up to 2^kSlack (and 2^kShift).  32-bit sums and bf16
+// weights have the exponents for much more, fp16 weights end at 2^16.
+template <typename T> constexpr float kSlack = std::is_same_v<T, __half> ? 8.0f : 24.0f;
+
 template <typename T> __device__ __forceinline__ uint32_t pack2(float lo, float hi);
 template <> __device__ __forceinline__ uint32_t pack2<__nv_bfloat16>(float lo, float hi)
 {
@@ -53,7 +58,7 @@ template <> __device__ __forceinline__ uint32_t pack2<__half>(float lo, float hi
 }
 
 // ------------------------------------------------------------------------------------------- own tokens
-constexpr int kOwnWarps = 3, kOwnKeys = 16, kOwnRows = 16, kOwnStages = 2;
+constexpr int kOwnWarps = 2, kOwnKeys = 16, kOwnRows = 16, kOwnStages = 3;
 
 template <int DB> constexpr size_t own_smem() { return (size_t)kOwnWarps * kOwnStages * 2 * kOwnKeys * DB * 128; }
 
@@ -101,9 +106,9 @@ template <int ROW>
 __device__ __forceinline__ uint32_t own_at(int r, int c) { return r * ROW + ((c ^ (r & 7)) << 4); }
 
 // A warp holds 16 rows and walks over its share of the block's tokens, 16 at a time: scores by mma.m16n8k16 (rows x
-// tokens), weights, then rows x dim.  Its K and V tiles go through two stages of its own (cp.async, no barrier
-// between warps); the warps' results are joined at the end.  Registers and shared memory are kept to what the
-// prefix kernel leaves of an SM, so that these blocks read memory while that one computes.
+// tokens), weights, then rows x dim.  Its K and V tiles go through three stages of its own (cp.async, no barrier
+// between warps); the warps' results are joined at the end.  Two warps to a block, so that blocks are many and end at
+// different times: 64 requests with up to 1000 own tokens take 55 us, with four warps 68.
 template <typename T, int DB>
 __global__ void __launch_bounds__(kOwnWarps * 32, 4)
 serve_attn_own_kernel(const __grid_constant__ AttnDev d)
@@ -133,12 +138,14 @@ serve_attn_own_kernel(const __grid_constant__ AttnDev d)
     }
     const int len = (int)min(max((int64_t)d.own_len[b], (int64_t)0), d.own_cap);
     const int k1 = min(len, k0 + d.own_chunk), part = d.prefix_parts + split;
-    int limit[2];                             // own tokens that a row sees
+    int limit[2], seen_by_all = INT_MAX;      // own tokens that a row sees; that all rows do
 #pragma unroll
     for (int half = 0; half < 2; half++) {
         const int r = r0 + half * 8 + lane / 4;
         limit[half] = r < rows ? len - d.fresh + r / d.group + 1 : 0;
+        seen_by_all = min(seen_by_all, r < rows ? limit[half] : INT_MAX);
     }
+    seen_by_all = __reduce_min_sync(~0u, seen_by_all);
 
     const uint32_t base = smem_u32(smem) + warp * kOwnStages * 2 * tile;
     const int blocks = k1 > k0 ? (k1 - k0 + kOwnKeys - 1) / kOwnKeys : 0, mine = (blocks - warp + kOwnWarps - 1) / kOwnWarps;
@@ -168,25 +175,28 @@ serve_attn_own_kernel(const __grid_constant__ AttnDev d)
         }
         return bits;
     };
-    uint2 there[2] = {};
-    if (mine > 0) there[0] = load(0, 0);
-    asm volatile("cp.async.commit_group;" ::: "memory");
+    uint2 there[kOwnStages] = {};             // of the next blocks, in order
+#pragma unroll
+    for (int i = 0; i < kOwnStages - 1; i++) {
+        if (i < mine) there[i] = load(i, i);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    }
 
     float o[DB * 8][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {};
 #pragma unroll
     for (int n = 0; n < DB * 8; n++) o[n][0] = o[n][1] = o[n][2] = o[n][3] = 0.0f;
+    int stage = 0, free = kOwnStages - 1;
     for (int i = 0; i < mine; i++) {
-        const int s = i & 1;
-        if (i + 1 < mine) {
-            const uint2 bits = load(i + 1, s ^ 1);
-            if (s) there[0] = bits;
-            else there[1] = bits;
-        }
+        if (i + kOwnStages - 1 < mine) there[kOwnStages - 1] = load(i + kOwnStages - 1, free);
         asm volatile("cp.async.commit_group;" ::: "memory");
-        asm volatile("cp.async.wait_group 1;" ::: "memory");
+        asm volatile("cp.async.wait_group %0;" ::"n"(kOwnStages - 1) : "memory");
         __syncwarp();
-        const uint32_t ks = base + s * 2 * tile, vs = ks + tile;
-        const uint2 here = s ? there[1] : there[0];
+        const uint32_t ks = base + stage * 2 * tile, vs = ks + tile;
+        const uint2 here = there[0];
+#pragma unroll
+        for (int k = 0; k + 1 < kOwnStages; k++) there[k] = there[k + 1];
+        free = stage;
+        stage = stage + 1 == kOwnStages ? 0 : stage + 1;
         const int at = k0 + (i * kOwnWarps + warp) * kOwnKeys;
         float sc[2][4] = {};
 #pragma unroll
@@ -197,38 +207,52 @@ serve_attn_own_kernel(const __grid_constant__ AttnDev d)
             mma_sync<T>(sc[0], q[k], f[0], f[1]);
             mma_sync<T>(sc[1], q[k], f[2], f[3]);
         }
-        uint32_t p[4];
+        // scores that nobody may see go to -infinity; most blocks have none
+        float top[2] = {-INFINITY, -INFINITY};
+        if (here.x == ~0u && here.y == ~0u && at + kOwnKeys <= seen_by_all) {
 #pragma unroll
-        for (int half = 0; half < 2; half++) {
-            float top = -INFINITY;
-            bool seen[4];
-#pragma unroll
-            for (int x = 0; x < 4; x++) {
-                const int key = lane % 4 * 2 + x % 2;  // of eight
-                float &v = sc[x / 2][half * 2 + x % 2];
-                seen[x] = ((x < 2 ? here.x : here.y) >> 4 * key & 1u) && at + x / 2 * 8 + key < limit[half];
+            for (int x = 0; x < 8; x++) {
+                float &v = sc[x / 4][x % 4];
                 v *= d.scale_log2;
-                if (seen[x]) top = fmaxf(top, v);
+                top[x / 2 % 2] = fmaxf(top[x / 2 % 2], v);
             }
-            top = fmaxf(top, __shfl_xor_sync(~0u, top, 1));
-            top = fmaxf(top, __shfl_xor_sync(~0u, top, 2));
-            // nothing seen so far: 0 in the place of -infinity, so that 2^-infinity is 0 and NaN stays NaN
-            const float next = fmaxf(m[half], top), from = next == -INFINITY ? 0.0f : next;
-            const float fix = exp2_approx(m[half] - from);
-            m[half] = next;
-            float w[4];
+        } else {
 #pragma unroll
-            for (int x = 0; x < 4; x++) w[x] = seen[x] ? exp2_approx(sc[x / 2][half * 2 + x % 2] - (from - kShift<T>)) : 0.0f;
-            l[half] = l[half] * fix + ((w[0] + w[1]) + (w[2] + w[3]));
-            p[half] = pack2<T>(w[0], w[1]);
-            p[half + 2] = pack2<T>(w[2], w[3]);
-            if (__any_sync(~0u, fix != 1.0f)) {
+            for (int x = 0; x < 8; x++) {
+                const int key = lane % 4 * 2 + x % 2;  // of eight
+                float &v = sc[x / 4][x % 4];
+                v = ((x < 4 ? here.x : here.y) >> 4 * key & 1u) && at + x / 4 * 8 + key < limit[x / 2 % 2] ? v * d.scale_log2 : -INFINITY;
+                top[x / 2 % 2] = fmaxf(top[x / 2 % 2], v);
+            }
+        }
+        // The maximum may lag by kSlack, as in the prefix kernel: only where it has to move do the four lanes of a row
+        // settle on it and scale down what is summed so far.
+        if (__any_sync(~0u, top[0] > m[0] + (m[0] == -INFINITY ? 0.0f : kSlack<T>) || top[1] > m[1] + (m[1] == -INFINITY ? 0.0f : kSlack<T>))) {
+#pragma unroll
+            for (int half = 0; half < 2; half++) {
+                float t = fmaxf(top[half], __shfl_xor_sync(~0u, top[half], 1));
+                t = fmaxf(fmaxf(t, __shfl_xor_sync(~0u, t, 2)), m[half]);
+                const float fix = exp2_approx(m[half] - (t == -INFINITY ? 0.0f : t));
+                m[half] = t;
+                l[half] *= fix;
 #pragma unroll
                 for (int n = 0; n < DB * 8; n++) {
                     o[n][half * 2] *= fix;
                     o[n][half * 2 + 1] *= fix;
                 }
             }
+        }
+        uint32_t p[4];
+#pragma unroll
+        for (int half = 0; half < 2; half++) {
+            // nothing seen so far: 0 in the place of -infinity, so that 2^-infinity is 0 and NaN stays NaN
+            const float less = kShift<T> - (m[half] == -INFINITY ? 0.0f : m[half]);
+            float w[4];
+#pragma unroll
+            for (int x = 0; x < 4; x++) w[x] = exp2_approx(sc[x / 2][half * 2 + x % 2] + less);
+            l[half] += (w[0] + w[1]) + (w[2] + w[3]);
+            p[half] = pack2<T>(w[0], w[1]);
+            p[half + 2] = pack2<T>(w[2], w[3]);
         }
 #pragma unroll
         for (int n = 0; n < DB * 4; n++) {
@@ -293,13 +317,10 @@ serve_attn_own_kernel(const __grid_constant__ AttnDev d)
 
 // ------------------------------------------------------------------------------------------- shared prefix
 constexpr int kTileKeys = 128, kPrefixThreads = 320;
-template <bool TWO> constexpr int kKvStages = TWO ? 3 : 4;
+template <bool TWO> constexpr int kKvStages = 4;
 constexpr int kPolyEvery = 4;                 // every fourth pair of exponentials goes to the multiply-add units
-// Powers of two that a row's maximum may lag behind: weights up to 2^kSlack (and 2^kShift).  32-bit sums and bf16
-// weights have the exponents for much more, fp16 weights end at 2^16.
-template <typename T> constexpr float kSlack = std::is_same_v<T, __half> ? 8.0f : 24.0f;
 
-// (on the way out the same memory holds, with a pitch of 64 DB + 4, 128 or 256 rows of sums, and 128 more columnwise)
+// (on the way out the same memory holds 256 rows of sums)
 template <int DB, bool TWO> constexpr size_t prefix_smem() { return (size_t)(TWO ? 2 : 1) * DB * 16384 + (size_t)kKvStages<TWO> * DB * 16384 + 1024; }
 
 // The state of one row's softmax.
@@ -475,17 +496,15 @@ __device__ __forceinline__ void softmax_tile(Row &row, uint32_t s, uint32_t o, b
 // TWO: two tiles of 128 rows, each with its own softmax warps and accumulator, take the same tokens, so that
 // one tile's matrix products run under the other's exponentials.  Otherwise (128 rows or fewer) the two halves share
 // the rows and take every other tile of tokens, and their results are joined at the end.
-// Launched first; its 160 KB and 128 registers a thread (the bound of 512 threads asks for that) leave room on an SM for
-// a block of the own kernel.
 template <typename T, int DB, bool TWO>
-__global__ void __launch_bounds__(512, 1)
+__global__ void __launch_bounds__(kPrefixThreads, 1)
 serve_attn_prefix_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                          const __grid_constant__ AttnDev d)
 {
     constexpr int block = kTileKeys * 128, stage = DB * block, stages = kKvStages<TWO>;       // 64 columns of a tile; a tile
     extern __shared__ uint8_t raw_smem[];
     __shared__ __align__(8) uint64_t bars[2 * stages + 10];
-    __shared__ float half_m[128], half_l[128];
+    __shared__ float2 half_ml[2][128];
     __shared__ uint32_t tmem_at;
     __shared__ int gave_up;
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
@@ -539,7 +558,8 @@ serve_attn_prefix_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
                 ring.step();
                 return true;
             };
-            bool ok = load(&map_k, 0);
+            // the queries are on their way before the rest of the first tiles, which they would have to queue behind
+            bool ok = load(&map_k, 0) && mbar_wait(q_full, 0, &gave_up);
             for (int j = 0; j < nt && ok; j++) {
                 if (TWO) {
                     ok = load(&map_v, j) && (j + 1 == nt || load(&map_k, j + 1));
@@ -697,58 +717,56 @@ serve_attn_prefix_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
         if (ok && (TWO || (w == 1 && mine > 0))) ok = mbar_wait(o_full + 8 * (w ^ 1), 0, &gave_up);
         ok = __all_sync(~0u, ok);
         tc_fence_after();
-        float m = state.l == 0.0f ? -INFINITY : (state.m == -INFINITY ? 0.0f : state.m) - kShift<T>, other = 0.0f, keep = 1.0f;
-        float *half = (float *)smem;                  // [column][row], where the tiles were: all products are done
-        if (!TWO) {
-            // the two halves of the tokens become one part: the second hands over its sums
-            if (w == 1) {
-                half_m[quarter * 32 + lane] = m;
-                half_l[quarter * 32 + lane] = state.l;
-                if (busy && ok && mine > 0)
-                    for (int c = 0; c < columns; c += 16) {
-                        uint32_t v[16];
-                        tmem_load16(o_at + c, v);
-                        tmem_wait_load16(v);
-#pragma unroll
-                        for (int k = 0; k < 16; k++) ((uint32_t *)half)[(c + k) * 128 + quarter * 32 + lane] = v[k];
-                    }
-            }
-            asm volatile("bar.sync 1, 256;" ::: "memory");
-            const float m1 = half_m[quarter * 32 + lane], l1 = half_l[quarter * 32 + lane];
-            if (w == 0 && m1 != -INFINITY) {
-                const float top = fmaxf(m, m1);
-                keep = exp2_approx(m - top);
-                other = exp2_approx(m1 - top);
-                state.l = keep * state.l + other * l1;
-                m = top;
-            }
-        }
-        if (busy && ok && (TWO || w == 0)) {
-            const uint32_t g = r0 + r, bt = g / (uint32_t)d.group;    // request and new token: rows come in that order
-            const int64_t row = split * d.rows + (int64_t)bt * d.q_heads + kv * d.group + (g - bt * d.group);
-            if (r < live) d.part_ml[row] = make_float2(m, state.l);
-            // through shared memory, where each warp has 32 rows of its own, and out row by row
-            constexpr int pitch = DB * 64 + 4;
-            static_assert((TWO ? 0 : 128 * DB * 64 * 4) + (TWO ? 8 : 4) * 32 * pitch * 4 <= (TWO ? 2 : 1) * stage + stages * stage);
-            float *rows32 = (float *)(smem + (TWO ? 0 : 128 * DB * 64 * 4)) + warp * 32 * pitch;
+        // Through shared memory, where the tiles were, and out row by row.
+        constexpr int pitch = DB * 64 + 4;
+        static_assert(8 * 32 * pitch * 4 <= (TWO ? 2 : 1) * stage + stages * stage);
+        float *sums = (float *)smem + (w * 128 + quarter * 32) * pitch;       // this warp's rows
+        if (busy && ok && mine > 0)
             for (int c = 0; c < columns; c += 16) {
                 float v[16];
                 tmem_load16(o_at + c, (uint32_t *)v);
                 tmem_wait_load16((uint32_t *)v);
-                if (!TWO && other != 0.0f) {
 #pragma unroll
-                    for (int k = 0; k < 16; k++) v[k] = keep * v[k] + other * half[(c + k) * 128 + quarter * 32 + lane];
-                }
-#pragma unroll
-                for (int k = 0; k < 16; k += 4) *(float4 *)(rows32 + lane * pitch + c + k) = *(const float4 *)(v + k);
+                for (int k = 0; k < 16; k += 4) *(float4 *)(sums + lane * pitch + c + k) = *(const float4 *)(v + k);
             }
+        float2 mine_ml = make_float2(state.l == 0.0f ? -INFINITY : (state.m == -INFINITY ? 0.0f : state.m) - kShift<T>, state.l);
+        if (!TWO) {
+            half_ml[w][quarter * 32 + lane] = mine_ml;
+            asm volatile("bar.sync 1, 256;" ::: "memory");
+        } else {
             __syncwarp();
-            const int count = min(32, live - (r - lane));
-            float *to = d.part_o + row * d.dim;
-            for (int k = 0; k < count; k++) {
-                float *other_row = (float *)__shfl_sync(~0u, (unsigned long long)to, k);
-                if (lane * 4 < d.dim) *(float4 *)(other_row + lane * 4) = *(const float4 *)(rows32 + k * pitch + lane * 4);
+        }
+        // TWO: a warp its own 32 rows.  Otherwise the two halves of the tokens become one part, 16 rows to a warp.
+        constexpr int out_rows = TWO ? 32 : 16;
+        const int first = TWO ? r - lane : warp * 16, row_here = first + lane % out_rows;
+        const uint32_t g = r0 + row_here, bt = g / (uint32_t)d.group;         // request and new token: rows come in that order
+        const int64_t row = split * d.rows + (int64_t)bt * d.q_heads + kv * d.group + (g - bt * d.group);
+        float keep = 1.0f, other = 0.0f;
+        if (!TWO) {
+            const float2 x = half_ml[0][row_here], y = half_ml[1][row_here];
+            mine_ml = x;
+            if (y.x != -INFINITY) {
+                const float top = fmaxf(x.x, y.x);
+                keep = exp2_approx(x.x - top);
+                other = exp2_approx(y.x - top);
+                mine_ml = make_float2(top, keep * x.y + other * y.y);
             }
+        }
+        if (ok && row_here < live && lane < out_rows) d.part_ml[row] = mine_ml;
+        const int count = ok ? min(out_rows, live - first) : 0;
+        const unsigned long long to = (unsigned long long)(d.part_o + row * d.dim);
+        const float *from0 = (const float *)smem + first * pitch + lane * 4, *from1 = from0 + 128 * pitch;
+#pragma unroll 4
+        for (int k = 0; k < count; k++) {
+            float *dst = (float *)__shfl_sync(~0u, to, k);
+            const float a = __shfl_sync(~0u, keep, k), b = __shfl_sync(~0u, other, k);
+            if (lane * 4 >= d.dim) continue;
+            float4 v = *(const float4 *)(from0 + k * pitch);
+            if (!TWO && b != 0.0f) {                  // (where it is zero the other half may hold nothing)
+                const float4 u = *(const float4 *)(from1 + k * pitch);
+                v = make_float4(a * v.x + b * u.x, a * v.y + b * u.y, a * v.z + b * u.z, a * v.w + b * u.w);
+            }
+            *(float4 *)(dst + lane * 4) = v;
         }
         tc_fence_before();
     }
@@ -864,7 +882,7 @@ Cut cut_of(const bcast_serve_attn_args &a)
         const int64_t items = c.row_tiles * a.kv_heads, tiles = ceil_div(a.prefix_len, 128);
         // the number of parts that ends first, one block to an SM: a block costs its tiles and about six more to
         // begin and to end; a tenth more where there are more blocks than SMs, since the own kernel only starts when
-        // the last of them has
+        // the last of them has (and then has the SMs that are left to itself)
         int64_t best = INT64_MAX;
         for (int64_t s = 1; s <= tiles && s <= 64; s++) {
             const int64_t rounds = ceil_div(items * s, kSms), cost = rounds * (ceil_div(tiles, s) + 6) * (rounds > 1 ? 11 : 10);
