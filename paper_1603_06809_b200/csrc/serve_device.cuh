@@ -135,6 +135,11 @@ __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap *m, int
     asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
                  ::"r"(dst), "l"((uint64_t)m), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
 }
+// The box that a load will ask for is on its way to L2.
+__device__ __forceinline__ void tma_prefetch_box(const CUtensorMap *m, int x, int y, int z)
+{
+    asm volatile("cp.async.bulk.prefetch.tensor.3d.L2.global.tile [%0, {%1, %2, %3}];" ::"l"((uint64_t)m), "r"(x), "r"(y), "r"(z) : "memory");
+}
 // Writes to shared memory by ordinary stores become visible to TMA and the tensor cores.
 __device__ __forceinline__ void fence_async_proxy() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 

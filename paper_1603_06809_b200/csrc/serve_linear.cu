@@ -64,16 +64,16 @@ __device__ __forceinline__ void tile_adapters(const int32_t *ad, uint32_t *first
 #pragma unroll
     for (int i = 0; i * 128 < NT; i++) {
         const int t = tid + i * 128;
-        first[i] = t < NT && known(ad[t < NT ? t : 0], d);
-        if (first[i]) {
-            const int32_t a = ad[t];
-            const int4 *four = (const int4 *)ad;
-#pragma unroll 4
-            for (int o = 0; o < (t + 3) / 4; o++) {
-                const int4 v = four[o];
-                if ((v.x == a && o * 4 < t) || (v.y == a && o * 4 + 1 < t) || (v.z == a && o * 4 + 2 < t) || (v.w == a && o * 4 + 3 < t))
-                    first[i] = false;
-            }
+        const int32_t a = t < NT ? ad[t] : -1;
+        // the first of its 32 tokens, and in none of the 32s before
+        const uint32_t same = __match_any_sync(~0u, a);       // by every lane, whatever its token
+        first[i] = known(a, d) && (same & ((1u << lane) - 1u)) == 0;
+        const int4 *four = (const int4 *)ad;
+        const int before = t < NT ? t / 32 * 8 : 0;
+#pragma unroll 8
+        for (int o = 0; o < before; o++) {
+            const int4 v = four[o];
+            if (v.x == a || v.y == a || v.z == a || v.w == a) first[i] = false;
         }
         const uint32_t bits = __ballot_sync(~0u, first[i]);
         if (lane == 0) firsts[t / 32] = bits;
@@ -193,6 +193,12 @@ serve_linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
             for (int tile = first_tile; tile < tiles && ok; tile += tile_step) {
                 const int f0 = LOW ? 0 : tile % d.f_tiles * kFeatures, t0 = (LOW ? tile : tile / d.f_tiles) * NT;
                 for (int kb = kb0; kb < kb1; kb++) {
+                    if (!LOW && kb == kb0 + S::stages && tile == first_tile && d.adapters) {
+                        // while the first stages are on their way: the adapters' tiles too, as far as L2
+                        if (!(ok = mbar_wait(meta, 0, &gave_up))) break;
+                        for (int j = part; j < count; j += split)
+                            for (int cb = 0; cb < form.column_blocks; cb++) tma_prefetch_box(&map_b, cb * kDepth, f0, list[j]);
+                    }
                     if (!(ok = mbar_wait(empty + 8 * ring.slot, ring.parity ^ 1u, &gave_up))) break;
                     const uint32_t bar = full + 8 * ring.slot, at = stage0 + ring.slot * S::stage;
                     mbar_expect(bar, (LOW ? mine * d.rank : kFeatures) * 128 + NT * 128);
@@ -318,7 +324,7 @@ serve_linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
                         float u[8] = {};
                         if (t < NT && col < d.rank && known(ad[t], d)) {
                             const float4 *src = (const float4 *)(d.low + (int64_t)(t0 + t) * d.rank + col);
-#pragma unroll 4
+#pragma unroll 8
                             for (int k = 0; k < d.low_splits; k++, src += (int64_t)d.tokens * d.rank / 4) {
                                 const float4 p = __ldcg(src), q = __ldcg(src + 1);
                                 u[0] += p.x;
