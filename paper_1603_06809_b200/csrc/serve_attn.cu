@@ -9,7 +9,8 @@
 //                   requests -- request, new token and query head of the group --, so a prefix token is read once
 //                   for 128 or 256 rows and the two products run on tcgen05
 //   own kernel      a block per (request, key/value head, part of its own tokens): few rows against tokens that
-//                   nobody else reads, so bound by reading them; warps take 16 tokens at a time through mma.sync
+//                   nobody else reads, so bound by reading them; warps take 16 tokens at a time through mma.sync.  A
+//                   short prefix goes with them, and the prefix kernel is left out.
 //   join kernel     the formula above, a warp per row
 #include "serve_device.cuh"
 #include "serve_internal.h"
@@ -21,17 +22,17 @@ namespace bcast_serve {
 namespace {
 
 struct AttnDev {
-    const void *q, *ok, *ov;
+    const void *q, *ok, *ov, *pk, *pv;
     const int32_t *own_len, *page_table;
     void *out;
     float *lse;
     float2 *part_ml;      // [parts][rows]: (m, l), m = -infinity where a part holds nothing
     float *part_o;        // [parts][rows][dim]
     int *status;
-    int64_t qs[3], os[3], oks[3], ovs[3];
+    int64_t qs[3], os[3], oks[3], ovs[3], pks[2], pvs[2];
     int64_t own_cap, num_pages, pts, rows;       // rows: batch * fresh * q_heads
     int32_t batch, fresh, q_heads, kv_heads, group, dim, page, page_shift, prefix_len;
-    int32_t prefix_splits, prefix_parts, row_tiles, own_splits, own_chunk, parts;
+    int32_t prefix_splits, prefix_parts, row_tiles, own_chunk, folded, fold_chunk, parts;
     float scale_log2;     // scale * log2(e): the softmax is taken in powers of two
 };
 
@@ -92,10 +93,10 @@ __device__ __forceinline__ void mma_sync(float *c, const uint32_t *a, uint32_t b
 struct Place {
     int32_t page, slot;
 };
-__device__ __forceinline__ Place place_of(const AttnDev &d, int b, int at)
+__device__ __forceinline__ Place place_of(const AttnDev &d, bool own, int b, int at)
 {
-    if (at >= d.own_cap) return Place{-1, 0};
-    if (!d.page_table) return Place{b, at};
+    if (at >= (own ? d.own_cap : (int64_t)d.prefix_len)) return Place{-1, 0};
+    if (!own || !d.page_table) return Place{b, at};
     const int n = d.page_shift >= 0 ? at >> d.page_shift : at / d.page;
     const int32_t p = d.page_table[(int64_t)b * d.pts + n];
     return Place{p >= 0 && p < d.num_pages ? p : -1, at - n * d.page};
@@ -119,11 +120,13 @@ serve_attn_own_kernel(const __grid_constant__ AttnDev d)
     const int b = blockIdx.z, kv = blockIdx.y % d.kv_heads, r0 = blockIdx.y / d.kv_heads * kOwnRows, split = blockIdx.x;
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, rows = d.fresh * d.group;
     launch_next();
-    const int k0 = split * d.own_chunk;
+    // the first parts are the shared prefix's where that is too short for a kernel of its own (Cut::fold)
+    const bool own = split >= d.folded;
+    const int chunk = own ? d.own_chunk : d.fold_chunk, k0 = (own ? split - d.folded : split) * chunk;
     // length, pages and queries: three loads that do not wait for one another
     Place ahead[2];                           // of the two tokens of a block that this lane copies parts of
 #pragma unroll
-    for (int h = 0; h < 2; h++) ahead[h] = place_of(d, b, k0 + warp * kOwnKeys + h * 8 + lane / 4);
+    for (int h = 0; h < 2; h++) ahead[h] = place_of(d, own, b, k0 + warp * kOwnKeys + h * 8 + lane / 4);
     // queries, as the first operand's fragments; rows and columns that do not exist are zero
     uint32_t q[DB * 4][4];
 #pragma unroll
@@ -136,20 +139,22 @@ serve_attn_own_kernel(const __grid_constant__ AttnDev d)
             q[i / 2][half + i % 2 * 2] = r < rows && c < d.dim ? *(const uint32_t *)(row + c) : 0u;
         }
     }
-    const int len = (int)min(max((int64_t)d.own_len[b], (int64_t)0), d.own_cap);
-    const int k1 = min(len, k0 + d.own_chunk), part = d.prefix_parts + split;
+    const int len = own ? (int)min(max((int64_t)d.own_len[b], (int64_t)0), d.own_cap) : d.prefix_len;
+    const int k1 = min(len, k0 + chunk), part = d.prefix_parts + split;
     int limit[2], seen_by_all = INT_MAX;      // own tokens that a row sees; that all rows do
 #pragma unroll
     for (int half = 0; half < 2; half++) {
         const int r = r0 + half * 8 + lane / 4;
-        limit[half] = r < rows ? len - d.fresh + r / d.group + 1 : 0;
+        limit[half] = r >= rows ? 0 : own ? len - d.fresh + r / d.group + 1 : INT_MAX;
         seen_by_all = min(seen_by_all, r < rows ? limit[half] : INT_MAX);
     }
     seen_by_all = __reduce_min_sync(~0u, seen_by_all);
 
     const uint32_t base = smem_u32(smem) + warp * kOwnStages * 2 * tile;
     const int blocks = k1 > k0 ? (k1 - k0 + kOwnKeys - 1) / kOwnKeys : 0, mine = (blocks - warp + kOwnWarps - 1) / kOwnWarps;
-    const T *kbase = (const T *)d.ok + kv * d.oks[2] + lane % 4 * 8, *vbase = (const T *)d.ov + kv * d.ovs[2] + lane % 4 * 8;
+    const T *const karray = (const T *)(own ? d.ok : d.pk), *const varray = (const T *)(own ? d.ov : d.pv);
+    const T *kbase = karray + kv * (own ? d.oks[2] : d.pks[1]) + lane % 4 * 8, *vbase = varray + kv * (own ? d.ovs[2] : d.pvs[1]) + lane % 4 * 8;
+    const int64_t kpage = own ? d.oks[0] : 0, vpage = own ? d.ovs[0] : 0, kslot = own ? d.oks[1] : d.pks[0], vslot = own ? d.ovs[1] : d.pvs[0];
     // Four lanes copy a token, 64 bytes at a time: whole sectors, and one address per lane and token.  Its page is
     // looked up one block ahead, so that this is not in the way of the copies.  Returns which tokens are there, token k at
     // bit 4 (k % 8) of word k / 8.
@@ -160,17 +165,17 @@ serve_attn_own_kernel(const __grid_constant__ AttnDev d)
         for (int h = 0; h < 2; h++) {
             const int r = h * 8 + lane / 4, at = k0 + (i * kOwnWarps + warp) * kOwnKeys + r;
             const Place p = ahead[h];
-            ahead[h] = place_of(d, b, at + kOwnWarps * kOwnKeys);
+            ahead[h] = place_of(d, own, b, at + kOwnWarps * kOwnKeys);
             const bool ok = at < k1 && p.page >= 0;
             (h ? bits.y : bits.x) = __ballot_sync(~0u, ok);
-            const T *kr = ok ? kbase + p.page * d.oks[0] + p.slot * d.oks[1] : (const T *)d.ok;
-            const T *vr = ok ? vbase + p.page * d.ovs[0] + p.slot * d.ovs[1] : (const T *)d.ov;
+            const T *kr = ok ? kbase + p.page * kpage + p.slot * kslot : karray;
+            const T *vr = ok ? vbase + p.page * vpage + p.slot * vslot : varray;
 #pragma unroll
             for (int j = 0; j < DB * 2; j++) {
                 const int c = j * 4 + lane % 4;
                 const bool in = ok && c * 8 < d.dim;
-                copy16(ks + own_at<row_bytes>(r, c), in ? kr + j * 32 : (const T *)d.ok, in);
-                copy16(ks + tile + own_at<row_bytes>(r, c), in ? vr + j * 32 : (const T *)d.ov, in);
+                copy16(ks + own_at<row_bytes>(r, c), in ? kr + j * 32 : karray, in);
+                copy16(ks + tile + own_at<row_bytes>(r, c), in ? vr + j * 32 : varray, in);
             }
         }
         return bits;
@@ -869,6 +874,7 @@ int check_shape(const bcast_serve_attn_args &a)
 struct Cut {
     bool two;                                 // 256 rows to a block of the prefix kernel
     int64_t rows, row_tiles, prefix_splits, prefix_parts, own_tiles, own_chunk, own_splits, parts;
+    int64_t folded, fold_chunk;               // parts of the prefix that the own kernel takes, among own_splits
 };
 
 Cut cut_of(const bcast_serve_attn_args &a)
@@ -877,7 +883,21 @@ Cut cut_of(const bcast_serve_attn_args &a)
     const int64_t group = a.q_heads / a.kv_heads, head_rows = (int64_t)a.batch * a.new_tokens * group;
     c.rows = head_rows * a.kv_heads;
     c.two = head_rows > 128;
-    if (a.prefix_len > 0 && c.rows > 0) {
+    c.own_tiles = ceil_div(a.new_tokens * group, kOwnRows);
+    const int64_t own_blocks = (int64_t)a.batch * a.kv_heads * c.own_tiles;
+    // A prefix that is little to read, even once per request and 16 rows, goes with the own tokens: one launch less, and
+    // no blocks of 128 rows for a few.  Measured (us, with the own kernel / with its own), by what the own kernel then
+    // reads: 2000 tokens 6.9 / 9.5; 8000 7.4 / 10.0; 32000 10.3 / 12.4, 13.2 / 17.8 and 12.8 / 13.9; 65000 16.4 / 16.1
+    // and 21.9 / 18.3; 128000 17.2 / 15.7.
+    const bool fold = a.prefix_len > 0 && c.rows > 0 && own_blocks * a.prefix_len <= 1 << 15;
+    if (fold) {
+        int64_t s = ceil_div(2 * kSms, own_blocks);
+        s = s < ceil_div(a.prefix_len, 128) ? s : ceil_div(a.prefix_len, 128);
+        s = s < 64 ? s : 64;
+        c.fold_chunk = round_up(ceil_div(a.prefix_len, s), 32);
+        c.folded = ceil_div(a.prefix_len, c.fold_chunk);
+    }
+    if (a.prefix_len > 0 && c.rows > 0 && !fold) {
         c.row_tiles = ceil_div(head_rows, c.two ? 256 : 128);
         const int64_t items = c.row_tiles * a.kv_heads, tiles = ceil_div(a.prefix_len, 128);
         // the number of parts that ends first, one block to an SM: a block costs its tiles and about six more to
@@ -894,17 +914,17 @@ Cut cut_of(const bcast_serve_attn_args &a)
         c.prefix_parts = c.prefix_splits;
     }
     if (a.own_cap > 0 && c.rows > 0) {
-        c.own_tiles = ceil_div(a.new_tokens * group, kOwnRows);
         // parts of 256 tokens, 512 once that makes six blocks to an SM (a decode step of 32 requests with up to 700 own
         // tokens: 36 us, with 512 38, with 128 39; 64 requests with up to 1024: 259, 251, 268), 128 where there are
         // too few blocks otherwise
-        const int64_t blocks = (int64_t)a.batch * a.kv_heads * c.own_tiles, more = ceil_div(2 * kSms, blocks);
-        int64_t s = ceil_div(a.own_cap, blocks * ceil_div(a.own_cap, 512) >= 6 * kSms ? 512 : 256);
+        const int64_t more = ceil_div(2 * kSms, own_blocks);
+        int64_t s = ceil_div(a.own_cap, own_blocks * ceil_div(a.own_cap, 512) >= 6 * kSms ? 512 : 256);
         if (s < more) s = more < ceil_div(a.own_cap, 128) ? more : ceil_div(a.own_cap, 128);
         s = s < kJoinParts - 64 ? s : kJoinParts - 64;
         c.own_chunk = round_up(ceil_div(a.own_cap, s), 64);
         c.own_splits = ceil_div(a.own_cap, c.own_chunk);
     }
+    c.own_splits += c.folded;
     c.parts = c.prefix_parts + c.own_splits;
     return c;
 }
@@ -962,11 +982,14 @@ int64_t bcast_serve_attn_workspace(const bcast_serve_attn_args *a)
     return workspace_of(*a, cut_of(*a));
 }
 
-int bcast_serve_attn(const bcast_serve_attn_args *a, void *cuda_stream)
+int bcast_serve_attn(const bcast_serve_attn_args *args, void *cuda_stream)
 {
-    if (!a) return BCAST_ERR_INVAL;
-    int rc = check_shape(*a);
+    if (!args) return BCAST_ERR_INVAL;
+    int rc = check_shape(*args);
     if (rc) return rc;
+    bcast_serve_attn_args given = *args;
+    const bcast_serve_attn_args *const a = &given;
+    if (given.page_table && given.num_pages == 0) given.own_cap = 0;      // a cache without pages holds no token
     if (a->batch == 0 || a->new_tokens == 0) return BCAST_OK;
     if (!(a->scale == a->scale) || a->scale > 1e30f || a->scale < -1e30f) return BCAST_ERR_INVAL;
     const bool paged = a->own_cap && a->page_table;
@@ -994,6 +1017,12 @@ int bcast_serve_attn(const bcast_serve_attn_args *a, void *cuda_stream)
     d.q = a->q;
     d.ok = a->own_k;
     d.ov = a->own_v;
+    d.pk = a->prefix_k;
+    d.pv = a->prefix_v;
+    for (int i = 0; i < 2; i++) {
+        d.pks[i] = a->prefix_k_stride[i];
+        d.pvs[i] = a->prefix_v_stride[i];
+    }
     d.own_len = a->own_len;
     d.page_table = paged ? a->page_table : nullptr;
     d.out = a->out;
@@ -1025,7 +1054,8 @@ int bcast_serve_attn(const bcast_serve_attn_args *a, void *cuda_stream)
     d.prefix_splits = (int32_t)c.prefix_splits;
     d.prefix_parts = (int32_t)c.prefix_parts;
     d.row_tiles = (int32_t)c.row_tiles;
-    d.own_splits = (int32_t)c.own_splits;
+    d.folded = (int32_t)c.folded;
+    d.fold_chunk = (int32_t)c.fold_chunk;
     d.own_chunk = (int32_t)c.own_chunk;
     d.parts = (int32_t)c.parts;
     d.scale_log2 = a->scale * kLog2e;

@@ -95,6 +95,15 @@ def test_linear_assignments(how, T, L):
     check_linear(linear_case(T + L, T, 128, 136, L, 16, "bf16", bias=False, how=how))
 
 
+@pytest.mark.parametrize("T,K,N,L,rank,how", [(300, 72, 28500, 3, 16, "mixed"), (700, 136, 19100, 40, 64, "runs"), (513, 72, 19007, 5, 128, "mixed"),
+                                              (1025, 200, 12000, 2, 24, "one"), (290, 64, 57000, 0, 0, "none")])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_linear_several_rounds_of_tiles(T, K, N, L, rank, how, dtype):
+    # three rounds of tiles of 256 tokens and more: blocks that take one after the other
+    assert -(-T // 256) * -(-N // 128) >= 3 * 148
+    check_linear(linear_case(T + N, T, K, N, L, rank, dtype, how=how))
+
+
 @pytest.mark.parametrize("T", [1, 30, 200])
 def test_linear_without_adapters(T):
     check_linear(linear_case(T, T, 320, 136, 0, 0, "fp16"))
@@ -355,6 +364,94 @@ def test_attn_repeats_bit_for_bit():
     for _ in range(20):
         assert torch.equal(first, go())
     S.bcast_serve_status(ws)
+
+
+# ---- prefixes long enough for a kernel of their own: batch * kv_heads * ceil(n * G / 16) * P above 2^15
+@pytest.mark.parametrize("P", [1025, 1151, 1152, 1153, 1279, 1281, 2100, 5000])
+@pytest.mark.parametrize("B,H,G", [(17, 2, 4), (40, 1, 4)])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_attn_long_prefix_lengths(P, B, H, G, dtype):
+    check_attn(attn_case(P + B, B, 1, H, G, 64, P, 30, 16, dtype))
+
+
+@pytest.mark.parametrize("D", [8, 16, 24, 40, 64, 72, 80, 96, 104, 128])
+@pytest.mark.parametrize("B,H", [(17, 2), (34, 1)])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_attn_long_prefix_head_sizes(D, B, H, dtype):
+    check_attn(attn_case(D + B, B, 1, H, 4, D, 1100, 20, 0, dtype))
+
+
+@pytest.mark.parametrize("B,n,H,G", [(1, 1, 1, 1), (1, 3, 2, 5), (5, 4, 1, 7), (33, 2, 1, 2), (32, 1, 1, 4), (33, 1, 1, 4), (64, 1, 1, 4), (65, 1, 1, 4), (20, 5, 1, 8)])
+def test_attn_long_prefix_rows(B, n, H, G):
+    # rows of a key/value head from one to several tiles of 256, the last one with few
+    P = -(-(1 << 15) // (B * H * -(-n * G // 16))) + 77
+    check_attn(attn_case(B * 10 + n, B, n, H, G, 128, P, 9, 4, "bf16"))
+
+
+@pytest.mark.parametrize("B", [17, 40])
+def test_attn_long_prefix_without_own_tokens(B):
+    c = attn_case(81, B, 3, 2, 2, 64, 1200, 16, 8, "bf16", lengths=[b % 6 for b in range(B)])
+    check_attn(c)
+    c["own_k"], c["own_v"] = torch.zeros(0, 8, 2, 64, dtype=torch.bfloat16), torch.zeros(0, 8, 2, 64, dtype=torch.bfloat16)
+    check_attn(c)
+
+
+@pytest.mark.parametrize("B", [17, 40])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_attn_long_prefix_maximum_that_grows(B, dtype):
+    g = gen(82)
+    c = attn_case(82, B, 1, 2, 4, 64, 1300, 16, 0, dtype)
+    for lo, factor in ((100, 3), (140, 8), (500, 20), (530, 30), (1000, 60), (1290, 90)):
+        c["prefix_k"][lo:] = rand(g, 1300 - lo, 2, 64, std=factor, dtype=TYPES[dtype])      # it grows within tiles and between
+    check_attn(c)
+    c["q"] = torch.zeros_like(c["q"])
+    check_attn(c)
+    for scale in (0.0, 0.7, -0.2):
+        check_attn(attn_case(83, B, 1, 2, 4, 64, 1300, 16, 0, dtype), scale=scale)
+
+
+@pytest.mark.parametrize("B", [17, 40])
+def test_attn_long_prefix_requests_do_not_touch_each_other(B):
+    c = attn_case(84, B, 2, 1, 4, 64, 2000, 12, 16, "bf16")
+    clean = check_attn(c).cpu()
+    c["q"][3] = math.nan
+    c["q"][7, :, 0, 0] = math.inf
+    d = {k: on_gpu(v) for k, v in c.items()}
+    out = S.bcast_serve_attn(d["q"], d["prefix_k"], d["prefix_v"], d["own_k"], d["own_v"], d["own_len"], page_table=d["page_table"]).cpu()
+    keep = [b for b in range(B) if b not in (3, 7)]
+    assert torch.equal(out[keep], clean[keep])
+    assert bool(torch.isnan(out[3]).all()) and not bool(torch.isfinite(out[7, :, 0]).all())
+    assert torch.equal(out[7, :, 1:], clean[7, :, 1:])
+
+
+def test_attn_long_prefix_strides_and_far_heads():
+    # heads 2^32 bytes apart, rows in wider ones
+    B, D, P, far = 40, 72, 1000, 1 << 31
+    bf = torch.bfloat16
+    c = attn_case(85, B, 1, 2, 4, D, P, 20, 0, "bf16")
+    want, bound, _, _ = R.attn(**c)
+    d = {k: on_gpu(v) for k, v in c.items()}
+    flat = torch.full((far + (1 << 20),), math.nan, dtype=bf, device=DEV)
+
+    def place(at, rows):
+        v = torch.as_strided(flat, rows.shape, (88, far, 1), at)
+        v.copy_(rows)
+        return v
+    out = S.bcast_serve_attn(d["q"], place(0, d["prefix_k"]), place(1 << 18, d["prefix_v"]), d["own_k"], d["own_v"], d["own_len"])
+    inside(out, want, bound, "out")
+
+
+def test_attn_long_prefix_repeats_bit_for_bit():
+    for B in (17, 40):
+        c = attn_case(86, B, 3, 2, 4, 128, 3000, 300, 16, "bf16")
+        d = {k: on_gpu(v) for k, v in c.items()}
+        ws = S.Workspace(DEV)
+        go = lambda: S.bcast_serve_attn(d["q"], d["prefix_k"], d["prefix_v"], d["own_k"], d["own_v"], d["own_len"],  # noqa: E731
+                                        page_table=d["page_table"], workspace=ws)
+        first = go()
+        for _ in range(20):
+            assert torch.equal(first, go())
+        S.bcast_serve_status(ws)
 
 
 # ------------------------------------------------------------------------------------------ verify
