@@ -53,7 +53,10 @@ enum { BCAST_SERVE_BF16 = 0, BCAST_SERVE_FP16 = 1, BCAST_SERVE_FP32 = 2 };
  * bcast_serve_linear -- y[t] = W x[t] + bias + scale[a] * B[a] (A[a] x[t]),  a = adapter[t].
  * A token whose adapter is outside 0..num_adapters-1 (-1, say) gets W x[t] + bias alone.  Sums are
  * held in 32 bits; the low-rank product A[a] x[t] is passed on as the sum of two numbers of the data
- * type (16 or more significant bits), y is rounded once.
+ * type (16 or more significant bits; scale[a] * A[a] x[t] has to be in its range), y is rounded once.
+ *   - Adapters that no token of the call names are not read.  Those that are hold finite numbers: a token's own x
+ *     may hold NaN or infinity without touching other tokens, an adapter's values may not (tokens of one tile pass
+ *     through the same products, multiplied by zero for the adapters they do not have).
  *   dtype         BCAST_SERVE_BF16 or BCAST_SERVE_FP16: x, weight, bias, lora_a, lora_b and y
  *   tokens        T >= 0;  k, n >= 1, k a multiple of 8
  *   num_adapters  L >= 0 (0: none; lora_*, adapter and scale are then not looked at)
@@ -93,6 +96,8 @@ int64_t bcast_serve_linear_workspace(const bcast_serve_linear_args *args);
  *   - own_len[b] is taken as 0 where negative and as own_cap where larger.  Nothing is read behind it:
  *     cache rows that hold no token yet may hold anything, NaN included.
  *   - A page number outside 0..num_pages-1 stands for a page of tokens that are not there.
+ *   - The values of the tokens that are there are finite: a new token that may not see a later one still has it
+ *     multiplied by a weight of zero.
  * Arguments
  *   dtype        BCAST_SERVE_BF16 or BCAST_SERVE_FP16
  *   batch >= 0, new_tokens >= 0, kv_heads >= 1, q_heads a multiple of kv_heads, prefix_len >= 0,
