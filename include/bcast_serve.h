@@ -58,8 +58,8 @@ enum { BCAST_SERVE_BF16 = 0, BCAST_SERVE_FP16 = 1, BCAST_SERVE_FP32 = 2 };
  *     may hold NaN or infinity without touching other tokens, an adapter's values may not (tokens of one tile pass
  *     through the same products, multiplied by zero for the adapters they do not have).
  *   dtype         BCAST_SERVE_BF16 or BCAST_SERVE_FP16: x, weight, bias, lora_a, lora_b and y
- *   tokens        T >= 0;  k, n >= 1, k a multiple of 8
- *   num_adapters  L >= 0 (0: none; lora_*, adapter and scale are then not looked at)
+ *   tokens        0 <= T <= 2^21;  1 <= k, n <= 2^24, k a multiple of 8
+ *   num_adapters  0 <= L <= 65536 (0: none; lora_*, adapter and scale are then not looked at)
  *   rank          R, a multiple of 8, 8..128 (an adapter of lower rank is padded with zeros)
  *   x [T][k], weight [n][k], y [T][n]: rows at x_stride, weight_stride, y_stride
  *   bias [n] or NULL
@@ -100,8 +100,8 @@ int64_t bcast_serve_linear_workspace(const bcast_serve_linear_args *args);
  *     multiplied by a weight of zero.
  * Arguments
  *   dtype        BCAST_SERVE_BF16 or BCAST_SERVE_FP16
- *   batch >= 0, new_tokens >= 0, kv_heads >= 1, q_heads a multiple of kv_heads, prefix_len >= 0,
- *   own_cap >= 0;  dim a multiple of 8, 8..128;  new_tokens * q_heads <= 2^19, and at most 2^24 rows
+ *   0 <= batch, new_tokens <= 65535;  1 <= kv_heads <= 1024, q_heads a multiple of kv_heads, at most 65535;
+ *   0 <= prefix_len, own_cap < 2^31 - 65536;  dim a multiple of 8, 8..128;  new_tokens * q_heads <= 2^19, and at most 2^24 rows
  *   (batch * new_tokens * q_heads) in all
  *   q, out       [batch][new_tokens][q_heads][dim], strides of the first three
  *   prefix_k/_v  [prefix_len][kv_heads][dim], strides of the first two (not looked at if prefix_len = 0)
@@ -150,7 +150,7 @@ int64_t bcast_serve_attn_workspace(const bcast_serve_attn_args *args);
  * probabilities: its draft is not accepted, and the token is -1.  A drafted token outside
  * 0..vocab-1 is not accepted.  Entries of noise that are not positive never win.
  *   dtype        of logits: BCAST_SERVE_BF16, BCAST_SERVE_FP16 or BCAST_SERVE_FP32
- *   batch >= 0;  0 <= drafts <= 63;  1 <= vocab < 2^31
+ *   0 <= batch <= 65535;  0 <= drafts <= 63;  1 <= vocab < 2^31 - 65536
  *   logits       [batch][drafts + 1][vocab], strides of the first two
  *   draft_probs  [batch][drafts][vocab] float, strides of the first two
  *   noise        [batch][vocab] float, rows at noise_stride

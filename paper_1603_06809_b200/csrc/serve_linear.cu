@@ -479,7 +479,7 @@ serve_linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
 int check_shape(const bcast_serve_linear_args &a)
 {
     if (a.dtype != BCAST_SERVE_BF16 && a.dtype != BCAST_SERVE_FP16) return BCAST_ERR_INVAL;
-    if (a.tokens < 0 || a.tokens > (1 << 22) || a.k < 8 || a.k > (1 << 24) || a.k % 8 || a.n < 1 || a.n > (1 << 24))
+    if (a.tokens < 0 || a.tokens > (1 << 21) || a.k < 8 || a.k > (1 << 24) || a.k % 8 || a.n < 1 || a.n > (1 << 24))
         return BCAST_ERR_INVAL;
     if (a.num_adapters < 0 || a.num_adapters > 65536 || (a.num_adapters && (a.rank < 8 || a.rank > 128 || a.rank % 8)))
         return BCAST_ERR_INVAL;

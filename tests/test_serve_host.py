@@ -46,7 +46,7 @@ def verify_args(**change):
 
 MAKE = {"linear": linear_args, "attn": attn_args, "verify": verify_args}
 BAD = [("linear", c) for c in (dict(dtype=2), dict(dtype=-1), dict(k=0), dict(k=60), dict(n=0), dict(tokens=-1), dict(rank=12), dict(rank=0), dict(rank=136),
-                               dict(num_adapters=-1), dict(k=1 << 40), dict(tokens=1 << 40))] + \
+                               dict(num_adapters=-1), dict(k=1 << 40), dict(tokens=1 << 40), dict(tokens=(1 << 21) + 1), dict(n=1 << 25), dict(num_adapters=65537))] + \
       [("attn", c) for c in (dict(dtype=2), dict(dim=0), dict(dim=12), dict(dim=136), dict(q_heads=3), dict(q_heads=0), dict(kv_heads=0), dict(batch=-1),
                              dict(new_tokens=-1), dict(prefix_len=-1), dict(own_cap=-1), dict(prefix_len=1 << 40), dict(batch=65535, new_tokens=65535))] + \
       [("verify", c) for c in (dict(dtype=3), dict(drafts=-1), dict(drafts=64), dict(vocab=0), dict(vocab=1 << 31), dict(batch=-1), dict(batch=1 << 20))]
