@@ -890,7 +890,12 @@ Cut cut_of(const bcast_serve_attn_args &a)
     Cut c = {};
     const int64_t group = a.q_heads / a.kv_heads, head_rows = (int64_t)a.batch * a.new_tokens * group;
     c.rows = head_rows * a.kv_heads;
-    c.two = head_rows > 128;
+    // 256 rows to a block read the prefix half as often; 128 rows leave fewer of the last tile's rows empty and end sooner,
+    // their two halves taking every other tile of tokens.  Measured (us, 256 / 128): 1024 rows to a head, prefix 65536
+    // 248 / 255, prefix 16384 114 / 112; 256 rows, 8192 53 / 49; 640 rows, 16384 87 / 77; 520 rows, 20011 42 / 38.  So
+    // 256 only where the rows come in pairs of tiles and every SM has 64 tiles of tokens to go through.
+    const int64_t row_tiles = ceil_div(head_rows, 128);
+    c.two = row_tiles % 2 == 0 && row_tiles / 2 * a.kv_heads * ceil_div(a.prefix_len, 128) >= 64 * kSms;
     c.own_tiles = ceil_div(a.new_tokens * group, kOwnRows);
     const int64_t own_blocks = (int64_t)a.batch * a.kv_heads * c.own_tiles;
     // A prefix that is little to read, even once per request and 16 rows, goes with the own tokens: one launch less, and

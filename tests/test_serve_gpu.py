@@ -388,6 +388,30 @@ def test_attn_long_prefix_rows(B, n, H, G):
     check_attn(attn_case(B * 10 + n, B, n, H, G, 128, P, 9, 4, "bf16"))
 
 
+@pytest.mark.parametrize("P,H,B,D,dtype", [(303105, 1, 1100, 64, "bf16"), (75791, 8, 300, 128, "fp16"), (134801, 3, 610, 96, "bf16")])
+def test_attn_prefix_of_many_rows_and_tiles(P, H, B, D, dtype):
+    # pairs of 128-row tiles and 64 tiles of tokens to an SM; a few rows of the result are compared
+    G = 1
+    tiles = -(-B * G // 128)
+    B = B if tiles % 2 == 0 else B + 128
+    tiles = -(-B * G // 128)
+    assert tiles % 2 == 0 and tiles // 2 * H * -(-P // 128) >= 64 * 148
+    g = gen(P)
+    dt = TYPES[dtype]
+    pool = rand(g, 4096 + 77, H, D, dtype=dt)                       # the prefix repeats a pool of tokens, shifted for its values
+    at = torch.arange(P)
+    pk, pv = pool[at % 4173], pool[(at * 7 + 5) % 4173]
+    q, ok, ov = (rand(g, *shape, dtype=dt) for shape in ((B, 1, H * G, D), (B, 3, H, D), (B, 3, H, D)))
+    ln = torch.randint(0, 4, (B,), generator=g).to(torch.int32)
+    lse = torch.zeros(B, 1, H * G, device=DEV)
+    out = S.bcast_serve_attn(*(t.to(DEV) for t in (q, pk, pv, ok, ov, ln)), lse=lse)
+    torch.cuda.synchronize()
+    rows = [0, 127, 128, B - 129, B - 1]
+    want, bound, wl, wb = R.attn(q[rows], pk, pv, ok[rows], ov[rows], ln[rows])
+    inside(out[rows], want, bound, "out")
+    assert bool(((lse[rows].double().cpu() - wl).abs() <= wb).all())
+
+
 @pytest.mark.parametrize("B", [17, 40])
 def test_attn_long_prefix_without_own_tokens(B):
     c = attn_case(81, B, 3, 2, 2, 64, 1200, 16, 8, "bf16", lengths=[b % 6 for b in range(B)])
