@@ -7,13 +7,13 @@
 // Three kernels, the second starting once the first is on its way (programmatic launch):
 //   prefix kernel   a block per (key/value head, tile of rows, part of the prefix).  The rows are those of ALL
 //                   requests -- request, new token and query head of the group --, so a prefix token is read once
-//                   for 128 or 256 rows and the two products run on tcgen05
+//                   for 128 or 256 rows (cut_of) and the two products run on tcgen05
 //   own kernel      a block per (request, key/value head, part of its own tokens): few rows against tokens that
 //                   nobody else reads, so bound by reading them; warps take 16 tokens at a time through mma.sync.  A
 //                   short prefix goes with them, and the prefix kernel is left out.
 //   join kernel     the formula above, a block per row
 // What bounds them, and what they take on one B200 (bf16, 8 key/value heads of 128, 4 query heads to each):
-//   64 requests x 4 new tokens, prefix 65536, up to 1024 own: 254 us, 1.09 PFLOP/s.  A pair of 128-row tiles against
+//   64 requests x 4 new tokens, prefix 65536, up to 1024 own: 250 us, 1.11 PFLOP/s.  A pair of 128-row tiles against
 //     128 tokens takes about 3050 cycles, where its products need 2048: a tile's softmax (about 2000 cycles, half
 //     of them on the exponentials) is longer than the other tile's products, and nothing is left to run under it
 //   32 requests x 1, prefix 8192, up to 700 own in pages: 34 us for 80 MB.  The prefix kernel takes 14 us of it (4 to
@@ -507,8 +507,8 @@ __device__ __forceinline__ void softmax_tile(Row &row, uint32_t s, uint32_t o, b
 }
 
 // TWO: two tiles of 128 rows, each with its own softmax warps and accumulator, take the same tokens, so that
-// one tile's matrix products run under the other's exponentials.  Otherwise (128 rows or fewer) the two halves share
-// the rows and take every other tile of tokens, and their results are joined at the end.
+// one tile's matrix products run under the other's exponentials.  Otherwise the two halves share 128 rows and take every
+// other tile of tokens, and their results are joined at the end.
 template <typename T, int DB, bool TWO>
 __global__ void __launch_bounds__(kPrefixThreads, 1)
 serve_attn_prefix_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
