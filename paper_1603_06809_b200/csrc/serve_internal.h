@@ -18,7 +18,6 @@ namespace bcast_serve {
 
 constexpr int64_t kMaxDim = (1ll << 31) - 1;       // largest length of one dimension
 constexpr int64_t kMaxStride = 1ll << 38;          // largest stride, in elements (a tensor map's limit is 2^40 bytes)
-constexpr int kStatusWords = BCAST_SERVE_STATUS_BYTES / 4;
 
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline int64_t round_up(int64_t a, int64_t b) { return ceil_div(a, b) * b; }

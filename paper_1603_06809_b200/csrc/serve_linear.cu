@@ -571,8 +571,7 @@ int run_type(const bcast_serve_linear_args &a, const LinearDev &d, const Cut &c,
         switch (c.low_tile) {
         case 16: rc = run_low<T, 16>(a, d, c, st); break;
         case 32: rc = run_low<T, 32>(a, d, c, st); break;
-        case 64: rc = run_low<T, 64>(a, d, c, st); break;
-        default: rc = run_low<T, 128>(a, d, c, st);
+        default: rc = run_low<T, 64>(a, d, c, st);
         }
         if (rc) return rc;
     }
