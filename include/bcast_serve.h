@@ -142,8 +142,9 @@ int64_t bcast_serve_attn_workspace(const bcast_serve_attn_args *args);
  *     and w = p_c if all were accepted.  With noise drawn from the unit exponential distribution this
  *     is a draw from w / sum(w), and the whole output is distributed as if drawn from p.  Where w is
  *     zero everywhere, p_c takes its place.
- *   - At temperature[b] <= 0, x_i is accepted while it is the token of the largest logit, and the token
- *     after the accepted ones is that of the largest logit.
+ *   - Where temperature[b] is not above 0 (NaN among them), x_i is accepted while it is the token of the
+ *     largest logit, and the token after the accepted ones is that of the largest logit.  At an infinite
+ *     temperature every token whose logit is above -infinity is as likely as any other.
  *   - tokens[b] = the accepted drafts, the token after them, then -1.
  * Ties go to the lowest token number.  A logit that is NaN counts as -infinity; where some are
  * +infinity, these share the probability evenly.  A row without any logit above -infinity has no

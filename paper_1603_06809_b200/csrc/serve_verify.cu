@@ -71,10 +71,14 @@ __device__ __forceinline__ RowStat shuffle_xor(const RowStat &a, int d)
     return r;
 }
 
-// 1 / temperature in units of log2, kept finite; a request without temperature only needs its largest logit.
+// Does a request draw at random?  (Not at zero, below it, or at NaN.)
+__device__ __forceinline__ bool samples(float temperature) { return temperature > 0.0f; }
+// 1 / temperature in units of log2, kept finite and, for a request that samples, above zero: at an infinite temperature
+// the smallest number there is makes every exponent round to 0 but that of a logit of -infinity, which 0 would turn into
+// NaN.  A request without temperature only needs its largest logit.
 __device__ __forceinline__ float exponent_scale(float temperature)
 {
-    return temperature > 0.0f ? fminf(kLog2e / temperature, 1e30f) : 0.0f;
+    return samples(temperature) ? fmaxf(fminf(kLog2e / temperature, 1e30f), 1.4e-45f) : 0.0f;
 }
 
 // Sixteen bytes of logits as floats.
@@ -178,8 +182,8 @@ serve_verify_stats_kernel(const __grid_constant__ VerifyDev d)
     RowStat s{-INFINITY, 0.0f, -1, 0};
     uint4 next[kFetch];
     fetch<T>(next, vec, v0 + threadIdx.x, v1);
-    const float c = exponent_scale(d.temperature[b]);
-    if (c > 0.0f) take_vectors<T, true>(s, next, vec, v0 + threadIdx.x, v1, head, c);
+    const float t = d.temperature[b], c = exponent_scale(t);
+    if (samples(t)) take_vectors<T, true>(s, next, vec, v0 + threadIdx.x, v1, head, c);
     else take_vectors<T, false>(s, next, vec, v0 + threadIdx.x, v1, head, c);
     // a thread's tokens come in ascending order but for the head, which thread order would put last
     if (part == 0 && (int)threadIdx.x < head) {
@@ -306,7 +310,7 @@ serve_verify_pick_kernel(const __grid_constant__ VerifyDev d)
         for (int o = 16; o; o >>= 1) s = join(s, shuffle_xor(s, o), c);
         if (lane == 0) {
             row_stat[i] = s;
-            const bool good = x >= 0 && s.best >= 0 && (t > 0.0f ? uq < weight(l, s.top, c) / s.sum : x == s.best);
+            const bool good = x >= 0 && s.best >= 0 && (samples(t) ? uq < weight(l, s.top, c) / s.sum : x == s.best);
             if (i < d.drafts && !good) atomicOr(&failed[i / 32], 1u << (i % 32));
         }
     }
@@ -315,7 +319,7 @@ serve_verify_pick_kernel(const __grid_constant__ VerifyDev d)
     const int accepted = failed[0] ? __ffs(failed[0]) - 1 : failed[1] ? 31 + __ffs(failed[1]) : d.drafts;
     const RowStat s = row_stat[accepted];
     int32_t chosen = s.best;                       // no temperature, or no probabilities: the largest logit, or -1
-    if (t > 0.0f && s.best >= 0) {                 // the same for every block of the cluster
+    if (samples(t) && s.best >= 0) {                 // the same for every block of the cluster
         const T *row = (const T *)d.logits + (int64_t)b * d.ls0 + (int64_t)accepted * d.ls1;
         const float *noise = d.noise + (int64_t)b * d.ns;
         const float *q = accepted < d.drafts ? d.draft_probs + (int64_t)b * d.qs0 + (int64_t)accepted * d.qs1 : nullptr;
