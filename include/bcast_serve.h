@@ -97,7 +97,8 @@ int64_t bcast_serve_linear_workspace(const bcast_serve_linear_args *args);
  *     cache rows that hold no token yet may hold anything, NaN included.
  *   - A page number outside 0..num_pages-1 stands for a page of tokens that are not there.
  *   - The values of the tokens that are there are finite: a new token that may not see a later one still has it
- *     multiplied by a weight of zero.
+ *     multiplied by a weight of zero.  A key may hold NaN: the rows that see it become NaN, in out and in lse, and no
+ *     others.
  * Arguments
  *   dtype        BCAST_SERVE_BF16 or BCAST_SERVE_FP16
  *   0 <= batch, new_tokens <= 65535;  1 <= kv_heads <= 1024, q_heads a multiple of kv_heads, at most 65535;

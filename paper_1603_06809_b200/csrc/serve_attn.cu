@@ -345,7 +345,8 @@ struct Row {
 // 2^x for two numbers at once on the multiply-add units, which have time left where the unit for exponentials
 // has none: x = r + f with r the nearest integer (added to 1.5 * 2^23 it stands in the sum's low bits), 2^f on
 // [-1/2, 1/2] by a polynomial (least largest relative error, fitted: 7.5e-5 in degree 3, 2.6e-6 in degree 4, against
-// 2^-9 and 2^-12 of rounding the weight to the type), and r added to the exponent.  Below 2^-126 gives 2^-126.
+// 2^-9 and 2^-12 of rounding the weight to the type), times 2^r, whose bits are r's in the place of the exponent.  (r
+// added to the exponent of 2^f would spare the product, but turns a NaN into a number.)  Below 2^-126 gives 2^-126.
 template <typename T>
 __device__ __forceinline__ void exp2_pair(uint64_t x, float &a, float &b)
 {
@@ -371,9 +372,7 @@ __device__ __forceinline__ void exp2_pair(uint64_t x, float &a, float &b)
     }
     float ta, tb;
     unpair(t, ta, tb);
-    unpair(y, a, b);
-    a = __uint_as_float(__float_as_uint(a) + (__float_as_uint(ta) << 23));
-    b = __uint_as_float(__float_as_uint(b) + (__float_as_uint(tb) << 23));
+    unpair(mul2(y, pair(__uint_as_float((__float_as_uint(ta) << 23) + 0x3f800000u), __uint_as_float((__float_as_uint(tb) << 23) + 0x3f800000u))), a, b);
 }
 
 __device__ __forceinline__ float max3(float a, float b, float c)

@@ -6,7 +6,7 @@ import torch
 
 import serve_reference as R
 from paper_1603_06809_b200 import serve as S
-from test_serve_gpu import check_verify, on_gpu, verify_case
+from test_serve_gpu import attn_case, check_verify, on_gpu, verify_case
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -61,3 +61,47 @@ def test_verify_temperatures_that_are_none():
     c["temperature"][:] = torch.tensor([-1.0, math.nan, -math.inf, -0.0])
     got = S.bcast_serve_verify(*(on_gpu(v) for v in c.values()))
     assert all(torch.equal(x, y) for x, y in zip(want, got))
+
+
+# ------------------------------------------------------------------------------------------ attn: keys that are NaN
+def attn_on_gpu(c):
+    """(out, lse) on the host."""
+    d = {k: on_gpu(v) for k, v in c.items()}
+    lse = torch.zeros(d["q"].shape[:3], device=DEV)
+    out = S.bcast_serve_attn(d["q"], d["prefix_k"], d["prefix_v"], d["own_k"], d["own_v"], d["own_len"], page_table=d.get("page_table"), lse=lse)
+    return out.cpu(), lse.cpu()
+
+
+# few rows and a short prefix; tiles of 128 rows; pairs of them
+@pytest.mark.parametrize("B,P,first", [(2, 300, 0), (2, 300, 292), (40, 1300, 0), (40, 1300, 32), (40, 1300, 700), (40, 1300, 1288),
+                                       (256, 151700, 0), (256, 151700, 151688)])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_attn_prefix_key_that_is_nan_reaches_its_head_only(B, P, first, dtype):
+    # head h has its NaN in key first + h: all places of eight
+    H, G = 8, 1 if B > 100 else 4
+    c = attn_case(91, B, 1, H, G, 64, P, 6, 0, dtype)
+    clean, clean_lse = attn_on_gpu(c)
+    assert bool(clean.isfinite().all())
+    for h in range(0, H, 2):
+        c["prefix_k"][first + h, h] = math.nan
+    out, lse = attn_on_gpu(c)
+    head = torch.arange(H).repeat_interleave(G)
+    assert bool(out[:, :, head % 2 == 0].isnan().all()) and bool(lse[:, :, head % 2 == 0].isnan().all())
+    assert torch.equal(out[:, :, head % 2 == 1], clean[:, :, head % 2 == 1]) and torch.equal(lse[:, :, head % 2 == 1], clean_lse[:, :, head % 2 == 1])
+    for h in range(H):
+        c["prefix_k"][first + h, h, 3] = math.nan
+    out, lse = attn_on_gpu(c)
+    assert bool(out.isnan().all()) and bool(lse.isnan().all())
+
+
+@pytest.mark.parametrize("P", [0, 40, 3000])
+def test_attn_own_key_that_is_nan_reaches_the_rows_that_see_it(P):
+    c = attn_case(92, 12, 4, 2, 2, 64, P, 40, 16, "bf16", lengths=[4 + 3 * b for b in range(12)])
+    clean, clean_lse = attn_on_gpu(c)
+    for b, length in enumerate(c["own_len"].tolist()):
+        at = length - 2                                       # the last new token but one: rows 2 and 3 see it
+        c["own_k"][c["page_table"][b, at // 16], at % 16, 1] = math.nan
+    out, lse = attn_on_gpu(c)
+    assert bool(out[:, 2:, 2:].isnan().all()) and bool(lse[:, 2:, 2:].isnan().all())
+    assert torch.equal(out[:, :2], clean[:, :2]) and torch.equal(out[:, :, :2], clean[:, :, :2])
+    assert torch.equal(lse[:, :2], clean_lse[:, :2]) and torch.equal(lse[:, :, :2], clean_lse[:, :, :2])
