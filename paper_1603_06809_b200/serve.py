@@ -69,7 +69,7 @@ _lib.bcast_serve_status.restype, _lib.bcast_serve_status.argtypes = ctypes.c_int
 
 class Workspace:
     """Device scratch that grows to what the calls need.  Calls that share one must be ordered on the
-    GPU: use one per stream."""
+    GPU: use one per stream.  What its status word holds stays when it grows."""
 
     def __init__(self, device="cuda", nbytes: int = 0):
         self.device = torch.device(device)
@@ -78,13 +78,20 @@ class Workspace:
             self.reserve(nbytes)
 
     def reserve(self, nbytes: int, stream=None) -> torch.Tensor:
-        """Memory of at least ``nbytes`` whose status word has been zeroed."""
+        """Memory of at least ``nbytes``; its status word is zero at first."""
         if self._t is None or self._t.numel() < nbytes:
             with torch.cuda.stream(_torch_stream(stream, self.device)):
-                # the old memory goes back to torch's allocator, which reuses it in the order of its streams
-                self._t = torch.empty(max(int(nbytes * 1.25), 1 << 16), dtype=torch.uint8, device=self.device)
-                self._t[:BCAST_SERVE_STATUS_BYTES].zero_()
-                self._of = torch.cuda.current_stream(self.device).cuda_stream
+                here, old = torch.cuda.current_stream(self.device), self._t
+                new = torch.empty(max(int(nbytes * 1.25), 1 << 16), dtype=torch.uint8, device=self.device)
+                status = new[:BCAST_SERVE_STATUS_BYTES]
+                if old is None:
+                    status.zero_()
+                else:
+                    # the old memory goes back to torch's allocator, which reuses it in the order of its streams
+                    status.copy_(old[:BCAST_SERVE_STATUS_BYTES])
+                    if self._of != here.cuda_stream:
+                        old.record_stream(here)
+                self._t, self._of = new, here.cuda_stream
         return self._t
 
 

@@ -6,6 +6,7 @@ import torch
 
 import serve_reference as R
 from paper_1603_06809_b200 import serve as S
+from paper_1603_06809_b200.bcast import BCAST_ERR_TIMEOUT, BcastError
 from test_serve_gpu import attn_case, check_verify, on_gpu, verify_case
 
 pytestmark = pytest.mark.gpu
@@ -105,3 +106,30 @@ def test_attn_own_key_that_is_nan_reaches_the_rows_that_see_it(P):
     assert bool(out[:, 2:, 2:].isnan().all()) and bool(lse[:, 2:, 2:].isnan().all())
     assert torch.equal(out[:, :2], clean[:, :2]) and torch.equal(out[:, :, :2], clean[:, :, :2])
     assert torch.equal(lse[:, :2], clean_lse[:, :2]) and torch.equal(lse[:, :, :2], clean_lse[:, :, :2])
+
+
+# ------------------------------------------------------------------------------------------ workspaces
+def timed_out(ws, stream=None):
+    with pytest.raises(BcastError) as e:
+        S.bcast_serve_status(ws, stream)
+    assert e.value.code == BCAST_ERR_TIMEOUT
+
+
+def test_status_stays_when_the_workspace_grows():
+    ws = S.Workspace(DEV)
+    ws.reserve(1000)[0] = 1                                   # as a kernel that gave up leaves it
+    assert ws.reserve(1 << 20).numel() >= 1 << 20
+    timed_out(ws)
+    S.bcast_serve_status(ws)                                  # told once
+    ws.reserve(1 << 20)[0] = 1
+    c = attn_case(95, 40, 4, 2, 4, 128, 3000, 20, 16, "bf16")
+    d = {k: on_gpu(v) for k, v in c.items()}
+    size = ws.reserve(0).numel()
+    S.bcast_serve_attn(d["q"], d["prefix_k"], d["prefix_v"], d["own_k"], d["own_v"], d["own_len"], page_table=d["page_table"], workspace=ws)
+    assert ws.reserve(0).numel() > size                       # a call that needed more
+    timed_out(ws)
+    side = torch.cuda.Stream()
+    ws.reserve(0)[0] = 1
+    side.wait_stream(torch.cuda.current_stream())
+    ws.reserve(ws.reserve(0).numel() + 1, side)
+    timed_out(ws, side)
