@@ -3,10 +3,11 @@
 // A call's tensors are checked against each other here (types, shapes, device, contiguous innermost dimension)
 // and described to the C entry point, which checks the rest; nothing is computed.  Native because a decode step's
 // kernels take about as long as marshalling a dozen tensors in Python does (33 us of 44 us measured).
-// Every function returns (code, outputs or what was wrong).
+// Every function returns (code, outputs or what was wrong, whether the stream is being captured into a graph).
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
 #include <c10/cuda/CUDACachingAllocator.h>
+#include <c10/cuda/CUDAGraphsC10Utils.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/utils/pybind.h>
@@ -115,9 +116,10 @@ py::tuple finish(int (*call)(const Args *, void *), int64_t (*size)(const Args *
 {
     int64_t bytes = size(&a);
     int code = bytes < 0 ? (int)bytes : (uint64_t)bytes > a.workspace_bytes ? BCAST_ERR_CAPACITY : call(&a, place.stream.stream());
-    if (code == BCAST_ERR_CAPACITY) return py::make_tuple(code, bytes);
-    if (code) return py::make_tuple(code, "");
-    return py::make_tuple(code, std::move(outputs));
+    if (code == BCAST_ERR_CAPACITY) return py::make_tuple(code, bytes, false);
+    if (code) return py::make_tuple(code, "", false);
+    // (asked of the stream of `place`, which is the current one here)
+    return py::make_tuple(code, std::move(outputs), c10::cuda::currentStreamCaptureStatusMayInitCtx() != c10::cuda::CaptureStatus::None);
 }
 
 template <typename F>
@@ -126,7 +128,7 @@ py::tuple guarded(F f)
     try {
         return f();
     } catch (const Refused &r) {
-        return py::make_tuple((int)BCAST_ERR_INVAL, r.why);
+        return py::make_tuple((int)BCAST_ERR_INVAL, r.why, false);
     }
 }
 

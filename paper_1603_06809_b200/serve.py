@@ -69,11 +69,16 @@ _lib.bcast_serve_status.restype, _lib.bcast_serve_status.argtypes = ctypes.c_int
 
 class Workspace:
     """Device scratch that grows to what the calls need.  Calls that share one must be ordered on the
-    GPU: use one per stream.  What its status word holds stays when it grows."""
+    GPU: use one per stream.  What its status word holds stays when it grows.
+
+    Calls may be captured into a CUDA graph with a workspace that is large enough by then (:meth:`reserve`, or
+    the same calls once before): it does not grow during a capture (``BCAST_ERR_CAPACITY``).  A larger call
+    afterwards leaves the graph the memory it was captured with; keep the workspace as long as the graph."""
 
     def __init__(self, device="cuda", nbytes: int = 0):
         self.device = torch.device(device)
         self._t, self._of = None, 0
+        self._captured, self._kept = False, []            # is a graph using _t; what graphs use of what it was before
         if nbytes:
             self.reserve(nbytes)
 
@@ -82,6 +87,8 @@ class Workspace:
         if self._t is None or self._t.numel() < nbytes:
             with torch.cuda.stream(_torch_stream(stream, self.device)):
                 here, old = torch.cuda.current_stream(self.device), self._t
+                if torch.cuda.is_current_stream_capturing():
+                    raise BcastError(BCAST_ERR_CAPACITY, f"serve.Workspace.reserve ({nbytes} bytes have to be there before the capture)")
                 new = torch.empty(max(int(nbytes * 1.25), 1 << 16), dtype=torch.uint8, device=self.device)
                 status = new[:BCAST_SERVE_STATUS_BYTES]
                 if old is None:
@@ -91,8 +98,24 @@ class Workspace:
                     status.copy_(old[:BCAST_SERVE_STATUS_BYTES])
                     if self._of != here.cuda_stream:
                         old.record_stream(here)
-                self._t, self._of = new, here.cuda_stream
+                    if self._captured:
+                        self._kept.append(old)
+                self._t, self._of, self._captured = new, here.cuda_stream, False
         return self._t
+
+
+class _Fresh:
+    """The memory of one call.  In a capture it is the graph's: torch keeps what such a call allocates for the graph
+    alone, and zeroing the status word is part of it."""
+
+    def __init__(self, device):
+        self.device, self._t, self._of = device, None, 0
+
+    def reserve(self, nbytes: int, stream=None) -> None:
+        with torch.cuda.stream(_torch_stream(stream, self.device)):
+            self._t = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+            self._t[:BCAST_SERVE_STATUS_BYTES].zero_()
+            self._of = torch.cuda.current_stream(self.device).cuda_stream
 
 
 def _torch_stream(stream, device):
@@ -112,11 +135,13 @@ def _call(where: str, native, device, workspace, stream, *tensors):
     """The native call, once more with a larger workspace where it asks for one."""
     raw = -1 if stream is None else int(getattr(stream, "cuda_stream", stream))
     if workspace is None:
-        workspace = Workspace(device)
-    code, result = native(*tensors, workspace._t, workspace._of, raw)
+        workspace = _Fresh(device)
+    code, result, captured = native(*tensors, workspace._t, workspace._of, raw)
     if code == BCAST_ERR_CAPACITY:
         workspace.reserve(result, stream)
-        code, result = native(*tensors, workspace._t, workspace._of, raw)
+        code, result, captured = native(*tensors, workspace._t, workspace._of, raw)
+    if captured:
+        workspace._captured = True
     if code == BCAST_OK:
         return result
     raise BcastError(code, f"{where} ({result})" if code == BCAST_ERR_INVAL and result else where)
@@ -155,4 +180,5 @@ def bcast_serve_status(workspace: Workspace, stream=None) -> None:
     mem = workspace.reserve(BCAST_SERVE_STATUS_BYTES)
     raw = torch.cuda.current_stream(workspace.device).cuda_stream if stream is None else _B._stream_ptr(stream)
     with torch.cuda.device(mem.device):
-        _check(_lib.bcast_serve_status(mem.data_ptr(), raw), "bcast_serve_status")
+        for code in [_lib.bcast_serve_status(m.data_ptr(), raw) for m in (mem, *workspace._kept)]:
+            _check(code, "bcast_serve_status")

@@ -6,7 +6,7 @@ import torch
 
 import serve_reference as R
 from paper_1603_06809_b200 import serve as S
-from paper_1603_06809_b200.bcast import BCAST_ERR_TIMEOUT, BcastError
+from paper_1603_06809_b200.bcast import BCAST_ERR_CAPACITY, BCAST_ERR_TIMEOUT, BcastError
 from test_serve_gpu import attn_case, check_verify, on_gpu, verify_case
 
 pytestmark = pytest.mark.gpu
@@ -133,3 +133,78 @@ def test_status_stays_when_the_workspace_grows():
     side.wait_stream(torch.cuda.current_stream())
     ws.reserve(ws.reserve(0).numel() + 1, side)
     timed_out(ws, side)
+
+
+def attn_calls():
+    """A call that needs little workspace and one that needs much more; each takes workspace and out."""
+    def call(c):
+        d = {k: on_gpu(v) for k, v in c.items()}
+        return lambda ws, **more: S.bcast_serve_attn(d["q"], d["prefix_k"], d["prefix_v"], d["own_k"], d["own_v"], d["own_len"],
+                                                     page_table=d["page_table"], workspace=ws, **more)
+    return call(attn_case(96, 5, 2, 2, 4, 64, 300, 50, 16, "bf16")), call(attn_case(97, 40, 4, 2, 4, 128, 3000, 20, 16, "bf16"))
+
+
+@pytest.mark.parametrize("named", [False, True])
+def test_graph_keeps_its_memory_when_the_workspace_grows(named):
+    small, large = attn_calls()
+    ws, side = S.Workspace(DEV), torch.cuda.Stream()
+    want, more = small(ws), large(S.Workspace(DEV))
+    out = torch.zeros_like(want)
+    was = ws.reserve(0)
+    at, size = was.data_ptr(), was.numel()
+    del was
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        small(ws, out=out, **(dict(stream=side) if named else {}))
+    assert torch.equal(large(ws), more)
+    assert ws.reserve(0).data_ptr() != at
+    # whoever asks for memory of that size now does not get what the graph writes to
+    others = [torch.full((size,), 7, dtype=torch.uint8, device=DEV) for _ in range(3)]
+    assert all(t.data_ptr() != at for t in others)
+    for _ in range(2):
+        out.zero_()
+        graph.replay()
+        assert torch.equal(out, want) and torch.equal(large(ws), more)
+    assert all(bool((t == 7).all()) for t in others)
+    S.bcast_serve_status(ws)
+    ws._kept[0][0] = 1                                        # a replay that gave up
+    timed_out(ws)
+    S.bcast_serve_status(ws)
+    graph.reset()
+
+
+def test_workspace_does_not_grow_in_a_capture():
+    small, large = attn_calls()
+    want = small(None)
+    out = torch.zeros_like(want)
+    torch.cuda.synchronize()
+    for ws in (S.Workspace(DEV), S.Workspace(DEV, 1000)):
+        held, call = ws._t, small if ws._t is None else large
+        graph = torch.cuda.CUDAGraph()
+        with pytest.raises(BcastError) as e:
+            with torch.cuda.graph(graph):
+                call(ws)
+        assert e.value.code == BCAST_ERR_CAPACITY and "before the capture" in str(e.value)
+        graph.reset()
+        assert ws._t is held                                  # as it was, and of use
+        torch.cuda.synchronize()
+        assert torch.equal(small(ws), want)
+        S.bcast_serve_status(ws)
+    # without a workspace the call's memory is the graph's
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        small(None, out=out)
+    for _ in range(2):
+        out.zero_()
+        graph.replay()
+        assert torch.equal(out, want)
+    graph.reset()
+
+
+def test_calls_outside_a_capture_keep_nothing():
+    small, large = attn_calls()
+    ws = S.Workspace(DEV)
+    small(ws)
+    large(ws)
+    assert ws._kept == [] and not ws._captured
