@@ -177,7 +177,9 @@ def bcast_serve_verify(logits, draft_probs, draft_tokens, uniforms, noise, tempe
 def bcast_serve_status(workspace: Workspace, stream=None) -> None:
     """Waits for ``stream`` and raises ``BcastError`` (``BCAST_ERR_TIMEOUT``) if a kernel that used this
     workspace gave up on one of its bounded waits; returns None otherwise."""
-    mem = workspace.reserve(BCAST_SERVE_STATUS_BYTES)
+    mem = workspace._t
+    if mem is None:                                       # no call used it yet
+        return _torch_stream(stream, workspace.device).synchronize()
     raw = torch.cuda.current_stream(workspace.device).cuda_stream if stream is None else _B._stream_ptr(stream)
     with torch.cuda.device(mem.device):
         for code in [_lib.bcast_serve_status(m.data_ptr(), raw) for m in (mem, *workspace._kept)]:

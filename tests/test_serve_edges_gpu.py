@@ -208,3 +208,14 @@ def test_calls_outside_a_capture_keep_nothing():
     small(ws)
     large(ws)
     assert ws._kept == [] and not ws._captured
+
+
+def test_status_of_a_workspace_that_no_call_used():
+    side = torch.cuda.Stream()
+    for stream in (None, side, side.cuda_stream):
+        ws = S.Workspace(DEV)
+        S.bcast_serve_status(ws, stream)
+        assert ws._t is None                                  # nothing was made on another stream than the one that is read
+        small, _ = attn_calls()
+        small(ws, stream=stream)
+        S.bcast_serve_status(ws, stream)
