@@ -94,14 +94,25 @@ class Replica:
         self.own_v = torch.zeros(pages, dtype=s.dtype, device=buf.device)
         self.table = torch.arange(requests * each, dtype=torch.int32, device=buf.device).reshape(requests, each)
         self.length = torch.zeros(requests, dtype=torch.int32, device=buf.device)
+        self.cap, self.at_most = each * s.page, 0         # tokens of a request's cache; no length is above at_most
         self.workspace = S.Workspace(buf.device)
+
+    def _make_room(self, n: int) -> None:
+        # The lengths are on the GPU, which is waited for only when all drafts so far would have filled the cache.
+        if self.at_most + n > self.cap:
+            self.at_most = int(self.length.max()) if len(self.length) else 0
+        if self.at_most + n > self.cap:
+            raise ValueError(f"{n} new tokens: a request has {self.at_most} of its own already, and its cache holds {self.cap}")
+        self.at_most += n
 
     def step(self, x, adapter, draft_probs, draft_tokens, uniforms, noise, temperature):
         """``x`` [requests, drafts + 1, hidden], the states of the last accepted token and of the drafts after it;
         ``adapter`` [requests] int32.  The tokens that are accepted stay in the cache, the others leave it.
-        Returns (accepted, tokens) as ``bcast_serve_verify`` does."""
+        Returns (accepted, tokens) as ``bcast_serve_verify`` does; ``ValueError``, and nothing changed, where some
+        request's cache has no room for all the new tokens."""
         s, w = self.s, self.shared
         R, n, _ = x.shape
+        self._make_room(n)
         # the projection of all tokens at once, each with its request's adapter
         qkv = S.bcast_serve_linear(x.reshape(R * n, s.hidden), w["w_qkv"], lora_a=w["lora_a"], lora_b=w["lora_b"],
                                    adapter=adapter.repeat_interleave(n), scale=w["lora_scale"], workspace=self.workspace)
@@ -109,6 +120,8 @@ class Replica:
         q, k, v = qkv.split((s.q_heads, s.kv_heads, s.kv_heads), dim=2)
         # the new tokens' keys and values go behind the requests' own ones
         at = self.length.long()[:, None] + torch.arange(n, device=x.device)
+        # (a graph that replays a step is not counted by _make_room: no index leaves the table there either)
+        at.clamp_(max=self.cap - 1)
         page = self.table.gather(1, at // s.page).long()
         self.own_k[page, at % s.page] = k
         self.own_v[page, at % s.page] = v

@@ -5,6 +5,7 @@ import pytest
 import torch
 
 import serve_reference as R
+from paper_1603_06809_b200 import replica as P
 from paper_1603_06809_b200 import serve as S
 from paper_1603_06809_b200.bcast import BCAST_ERR_CAPACITY, BCAST_ERR_TIMEOUT, BcastError
 from test_serve_gpu import attn_case, check_verify, on_gpu, verify_case
@@ -219,3 +220,25 @@ def test_status_of_a_workspace_that_no_call_used():
         small, _ = attn_calls()
         small(ws, stream=stream)
         S.bcast_serve_status(ws, stream)
+
+
+# ------------------------------------------------------------------------------------------ replicas
+def test_replica_steps_until_its_cache_is_full():
+    s = P.Shape(hidden=128, q_heads=4, kv_heads=2, dim=64, vocab=500, adapters=3, rank=8, prompt=150, page=8)
+    layout = P.Layout(s)
+    rep = P.Replica(s, layout, P.random_model(s, layout, 7, DEV), 5, 40)
+    steps = 0
+    with pytest.raises(ValueError):
+        while steps < 100:
+            rep.step(**P.drafted(s, 5, 3, 30 + steps, DEV))
+            steps += 1
+    before = rep.length.clone()
+    assert 40 - 4 < int(before.max()) <= 40 and steps >= 10     # at most four tokens of a request to a step
+    with pytest.raises(ValueError):
+        rep.step(**P.drafted(s, 5, 3, 99, DEV))
+    assert torch.equal(rep.length, before)
+    while int(rep.length.max()) < 40:
+        rep.step(**P.drafted(s, 5, 0, 60, DEV))                 # one token each still fits
+    with pytest.raises(ValueError):
+        rep.step(**P.drafted(s, 5, 0, 60, DEV))
+    S.bcast_serve_status(rep.workspace)
