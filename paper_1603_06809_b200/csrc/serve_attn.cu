@@ -725,8 +725,9 @@ serve_attn_prefix_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
         }
         // ---- the way out: a row's sums as they are, with what they were taken against
         if (mine > 0 && ok) ok = mbar_wait(o_full + 8 * w, 0, &gave_up);
-        // (both halves' products are done then, and what they read may be written over)
-        if (ok && (TWO || (w == 1 && mine > 0))) ok = mbar_wait(o_full + 8 * (w ^ 1), 0, &gave_up);
+        // Both halves' products are done then, and what they read may be written over: a half waits for the other's too,
+        // unless that has none (one tile of tokens, of which half 1 has no part).
+        if (ok && (TWO || nt > 1)) ok = mbar_wait(o_full + 8 * (w ^ 1), 0, &gave_up);
         ok = __all_sync(~0u, ok);
         tc_fence_after();
         // Through shared memory, where the tiles were, and out row by row.

@@ -8,7 +8,7 @@ import serve_reference as R
 from paper_1603_06809_b200 import replica as P
 from paper_1603_06809_b200 import serve as S
 from paper_1603_06809_b200.bcast import BCAST_ERR_CAPACITY, BCAST_ERR_TIMEOUT, BcastError
-from test_serve_gpu import attn_case, check_verify, on_gpu, verify_case
+from test_serve_gpu import attn_case, check_verify, inside, on_gpu, verify_case
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -107,6 +107,21 @@ def test_attn_own_key_that_is_nan_reaches_the_rows_that_see_it(P):
     assert bool(out[:, 2:, 2:].isnan().all()) and bool(lse[:, 2:, 2:].isnan().all())
     assert torch.equal(out[:, :2], clean[:, :2]) and torch.equal(out[:, :, :2], clean[:, :, :2])
     assert torch.equal(lse[:, :2], clean_lse[:, :2]) and torch.equal(lse[:, :, :2], clean_lse[:, :, :2])
+
+
+@pytest.mark.parametrize("tiles", range(1, 10))
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_attn_every_number_of_tiles_to_a_block(tiles, dtype):
+    # 192 blocks of 128 rows with the whole prefix each: the two halves of a block take every other tile of tokens
+    B, H, D = 300, 64, 128
+    c = attn_case(93 + tiles, B, 1, H, 1, D, 128 * tiles - 5, 3, 0, dtype)
+    out, lse = attn_on_gpu(c)
+    rows = [0, 127, 128, B - 1]
+    want, bound, wl, wb = R.attn(**{k: v if k.startswith("prefix") else v[rows] for k, v in c.items()})
+    inside(out[rows], want, bound, "out")
+    assert bool(((lse[rows].double() - wl).abs() <= wb).all())
+    for _ in range(5):
+        assert torch.equal(attn_on_gpu(c)[0], out)
 
 
 # ------------------------------------------------------------------------------------------ workspaces
