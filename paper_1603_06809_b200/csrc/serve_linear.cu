@@ -123,7 +123,7 @@ serve_linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
 {
     using S = Tile<NT>;
     extern __shared__ uint8_t raw_smem[];
-    __shared__ __align__(8) uint64_t bars[4 * S::stages + 2 * S::accs + 2];
+    __shared__ __align__(8) uint64_t bars[4 * S::stages + 2 * S::accs + 3];
     __shared__ __align__(16) int32_t ad[NT];
     __shared__ int32_t list[NT];
     __shared__ uint32_t firsts[(NT + 127) / 128 * 4], tmem_at;
@@ -138,7 +138,7 @@ serve_linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
     const uint32_t stage0 = smem_u32(smem);
     const uint32_t full = smem_u32(bars), empty = full + 8 * S::stages, ready = empty + 8 * S::stages,
                    filled = ready + 8 * S::stages, acc_full = filled + 8 * S::stages, acc_empty = acc_full + 8 * S::accs,
-                   meta = acc_empty + 8 * S::accs, drained = meta + 8;
+                   meta = acc_empty + 8 * S::accs, taken = meta + 8, drained = taken + 8;
 
     // which tiles, and of k which stages
     const int k_blocks = (d.k + kDepth - 1) / kDepth;
@@ -172,6 +172,7 @@ serve_linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
             mbar_init(acc_empty + 8 * i, 128);
         }
         mbar_init(meta, 128);
+        mbar_init(taken, 1);
         mbar_init(drained, 1);
         mbar_init_fence();
         tma_prefetch(&map_x);
@@ -230,6 +231,7 @@ serve_linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
                         issued++;
                         ring.step();
                     }
+                if (ok) mbar_arrive(taken);           // count and list are the next tile's now
             }
             if (gave_up) {                            // loads still under way end before the block does
                 Ring<S::stages> r;
@@ -304,13 +306,18 @@ serve_linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
         const int quarter = warp % 4, f = quarter * 32 + lane, id = tid - 64;
         Ring<S::stages> ring;
         Ring<S::accs> acc;
-        uint32_t uses = 0;
+        uint32_t uses = 0, taken_parity = 0;
         bool waited = false;
         for (int tile = first_tile; tile < tiles; tile += tile_step) {
             const int f0 = LOW ? 0 : tile % d.f_tiles * kFeatures, t0 = (LOW ? tile : tile / d.f_tiles) * NT;
             bool ok = true;
             for (int kb = kb0; kb < kb1; kb++) ring.step();
             if (!LOW && d.adapters) {
+                if (S::accs > 1 && tile != first_tile) {
+                    // a tile without adapters sends nothing that says the loading thread has seen so
+                    mbar_wait(taken, taken_parity, &gave_up);
+                    taken_parity ^= 1u;
+                }
                 for (int t = id; t < NT; t += 128) ad[t] = t0 + t < d.tokens ? d.adapter[t0 + t] : -1;
                 asm volatile("bar.sync 1, 128;" ::: "memory");
                 tile_adapters<NT>(ad, firsts, list, &count, d);

@@ -8,7 +8,7 @@ import serve_reference as R
 from paper_1603_06809_b200 import replica as P
 from paper_1603_06809_b200 import serve as S
 from paper_1603_06809_b200.bcast import BCAST_ERR_CAPACITY, BCAST_ERR_TIMEOUT, BcastError
-from test_serve_gpu import attn_case, check_verify, inside, on_gpu, verify_case
+from test_serve_gpu import attn_case, check_linear, check_verify, inside, linear_case, on_gpu, verify_case
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -122,6 +122,27 @@ def test_attn_every_number_of_tiles_to_a_block(tiles, dtype):
     assert bool(((lse[rows].double() - wl).abs() <= wb).all())
     for _ in range(5):
         assert torch.equal(attn_on_gpu(c)[0], out)
+
+
+# ------------------------------------------------------------------------------------------ linear: tiles without adapters
+@pytest.mark.parametrize("which", ["none", "even", "odd", "one"])
+@pytest.mark.parametrize("rank", [16, 128])
+def test_linear_blocks_that_go_from_tiles_with_adapters_to_tiles_without(which, rank):
+    # blocks that take several tiles of 256 tokens, in some of which no token has an adapter
+    T, K, N, L = 1300, 72, 19000, 6
+    assert -(-T // 256) * -(-N // 128) >= 3 * 148
+    c = linear_case(98, T, K, N, L, rank, "bf16", how="mixed")
+    tile = torch.arange(T) // 256
+    has = {"none": tile < 0, "even": tile % 2 == 0, "odd": tile % 2 == 1, "one": tile == 3}[which]
+    c["adapter"][~has] = -1
+    first = check_linear(c)
+    for _ in range(10):
+        assert torch.equal(check_linear_again(c), first)
+
+
+def check_linear_again(c):
+    d = {k: on_gpu(v) for k, v in c.items()}
+    return S.bcast_serve_linear(d.pop("x"), d.pop("weight"), **d)
 
 
 # ------------------------------------------------------------------------------------------ workspaces
