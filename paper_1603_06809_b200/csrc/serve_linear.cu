@@ -59,6 +59,15 @@ struct LinearDev {
 
 __device__ __forceinline__ bool known(int32_t a, const LinearDev &d) { return (uint32_t)a < (uint32_t)d.adapters; }
 
+// Does `v` hold for all threads of the four warps after the first two?
+__device__ __forceinline__ bool all_of_four(bool v)
+{
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.and.pred q, 1, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                 : "=r"(r) : "r"((uint32_t)v) : "memory");
+    return r;
+}
+
 // The adapters of a tile's tokens, each once, in the order of their first token.  For the four warps after
 // the first two; `list` and `count` are complete for them on return.
 template <int NT>
@@ -307,16 +316,18 @@ serve_linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
         Ring<S::stages> ring;
         Ring<S::accs> acc;
         uint32_t uses = 0, taken_parity = 0;
-        bool waited = false;
+        bool waited = false, alive = true;
         for (int tile = first_tile; tile < tiles; tile += tile_step) {
             const int f0 = LOW ? 0 : tile % d.f_tiles * kFeatures, t0 = (LOW ? tile : tile / d.f_tiles) * NT;
             bool ok = true;
             for (int kb = kb0; kb < kb1; kb++) ring.step();
             if (!LOW && d.adapters) {
                 if (S::accs > 1 && tile != first_tile) {
-                    // a tile without adapters sends nothing that says the loading thread has seen so
-                    mbar_wait(taken, taken_parity, &gave_up);
+                    // A tile without adapters sends nothing that says the loading thread has seen so; and all four warps
+                    // go on to the barriers below, or none.
+                    alive = alive && mbar_wait(taken, taken_parity, &gave_up);
                     taken_parity ^= 1u;
+                    if (!(alive = all_of_four(alive))) break;
                 }
                 for (int t = id; t < NT; t += 128) ad[t] = t0 + t < d.tokens ? d.adapter[t0 + t] : -1;
                 asm volatile("bar.sync 1, 128;" ::: "memory");
@@ -384,7 +395,11 @@ serve_linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
                 }
             }
             ok = ok && mbar_wait(acc_full + 8 * acc.slot, acc.parity, &gave_up);
-            if (!__all_sync(~0u, ok)) break;
+            if (!__all_sync(~0u, ok)) {
+                alive = false;                        // told to the other warps where they wait for this one
+                if (!LOW && d.adapters) continue;
+                break;
+            }
             tc_fence_after();
             const uint32_t src = tmem + ((uint32_t)(quarter * 32) << 16) + acc.slot * NT;
             if (!LOW && split > 1) break;             // goes on below, with the other blocks of the cluster
