@@ -37,6 +37,7 @@ struct AttnDev {
     float2 *part_ml;      // [parts][rows]: (m, l), m = -infinity where a part holds nothing
     float *part_o;        // [parts][rows][dim]
     int *status;
+    uint32_t wait_limit;  // polls of a bounded wait
     int64_t qs[3], os[3], oks[3], ovs[3], pks[2], pvs[2];
     int64_t own_cap, num_pages, pts, rows;       // rows: batch * fresh * q_heads
     int32_t batch, fresh, q_heads, kv_heads, group, dim, page, page_shift, prefix_len;
@@ -519,6 +520,7 @@ serve_attn_prefix_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
     __shared__ float2 half_ml[2][128];
     __shared__ uint32_t tmem_at;
     __shared__ int gave_up;
+    const Waits waits{&gave_up, d.wait_limit};
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
     const int rows = d.batch * d.fresh * d.group;                     // of one key/value head
     const int rt = blockIdx.x % d.row_tiles, kv = blockIdx.x / d.row_tiles % d.kv_heads, split = blockIdx.x / d.row_tiles / d.kv_heads;
@@ -533,7 +535,7 @@ serve_attn_prefix_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
     const uint32_t full = smem_u32(bars), empty = full + 8 * stages, q_full = empty + 8 * stages, s_full = q_full + 8,
                    p_most = s_full + 16, p_full = p_most + 16, o_full = p_full + 16, drained = o_full + 16;
     if (tid == 0) {
-        gave_up = 0;
+        gave_up = d.wait_limit == 0;
         for (int i = 0; i < stages; i++) {
             mbar_init(full + 8 * i, 1);
             mbar_init(empty + 8 * i, 1);
@@ -555,14 +557,15 @@ serve_attn_prefix_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = tmem_at;                                    // scores 0, 128; accumulators 256, 384
+    int issued = 0;                                                   // loads, of the thread that issues them
 
     if (warp == 8) {
         if (lane == 0) {
             // ---- loads, in the order the matrix products take them
             Ring<stages> ring;
-            int issued = 0;
             auto load = [&](const CUtensorMap *map, int j) {
-                if (!mbar_wait(empty + 8 * ring.slot, ring.parity ^ 1u, &gave_up)) return false;
+                // (the warp that issues the products goes on after it gave up: a slot may be free then that is not filled)
+                if (!mbar_wait(empty + 8 * ring.slot, ring.parity ^ 1u, waits) || *waits.gave_up) return false;
                 mbar_expect(full + 8 * ring.slot, stage);
                 for (int i = 0; i < DB; i++)
                     tma_load(kv_at + ring.slot * stage + i * block, map, i * 64, (j0 + j) * kTileKeys, kv, full + 8 * ring.slot);
@@ -571,19 +574,12 @@ serve_attn_prefix_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
                 return true;
             };
             // the queries are on their way before the rest of the first tiles, which they would have to queue behind
-            bool ok = load(&map_k, 0) && mbar_wait(q_full, 0, &gave_up);
+            bool ok = load(&map_k, 0) && mbar_wait(q_full, 0, waits);
             for (int j = 0; j < nt && ok; j++) {
                 if (TWO) {
                     ok = load(&map_v, j) && (j + 1 == nt || load(&map_k, j + 1));
                 } else {
                     ok = (j + 1 == nt || load(&map_k, j + 1)) && load(&map_v, j);
-                }
-            }
-            if (gave_up) {
-                Ring<stages> r;
-                for (int i = 0; i < issued; i++) {
-                    if (i + stages >= issued) mbar_drain(full + 8 * r.slot, r.parity);
-                    r.step();
                 }
             }
         }
@@ -594,12 +590,12 @@ serve_attn_prefix_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
         // gives up does not leave the loop -- the ones after it give up at once, and what is still issued only touches this
         // block's own memory.  (With one thread in a loop of its own that made descriptors as it went, a product
         // of 128 x 128 x 128 took 900 to 1800 cycles to issue and not 512.)
-        const uint32_t lead = elect_one();
+        const uint32_t lead = elect_one();            // (chosen outside this branch, it made a long prefix take 5 % longer)
         const uint32_t s_desc = mma_desc<T>(128, kTileKeys), o_desc = mma_desc<T>(128, (d.dim + 15) / 16 * 16, true);
         const uint64_t q_desc = smem_desc(q_at), k_desc = smem_desc(kv_at), v_desc = smem_desc(kv_at, block);
         Ring<stages> ring;
         auto take = [&]() {                                           // the next tile of K or V, once it is there
-            mbar_wait(full + 8 * ring.slot, ring.parity, &gave_up);
+            mbar_wait(full + 8 * ring.slot, ring.parity, waits);
             tc_fence_after();
             const int slot = ring.slot;
             ring.step();
@@ -617,17 +613,17 @@ serve_attn_prefix_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
         auto values = [&](int w, int slot, int it) {                  // O_w += P_w V, as the weights come
             const uint64_t b = v_desc + slot * (stage >> 4);
             const uint32_t o = tmem + 256 + w * 128, a = tmem + w * 128;
-            mbar_wait(p_most + 8 * w, it & 1, &gave_up);
+            mbar_wait(p_most + 8 * w, it & 1, waits);
             tc_fence_after();
             mma_ts_warp(lead, o, a, b, o_desc, it > 0);
 #pragma unroll
             for (int i = 1; i < 6; i++) mma_ts_warp(lead, o, a + i * 8, b + i * (2048 >> 4), o_desc, true);
-            mbar_wait(p_full + 8 * w, it & 1, &gave_up);
+            mbar_wait(p_full + 8 * w, it & 1, waits);
             tc_fence_after();
 #pragma unroll
             for (int i = 6; i < 8; i++) mma_ts_warp(lead, o, a + i * 8, b + i * (2048 >> 4), o_desc, true);
         };
-        mbar_wait(q_full, 0, &gave_up);
+        mbar_wait(q_full, 0, waits);
         int ks = take();
         scores(0, ks);
         if (TWO) {
@@ -672,10 +668,6 @@ serve_attn_prefix_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
                 }
             }
         }
-        if (gave_up) {
-            mma_commit_warp(lead, drained);
-            mbar_drain(drained, 0);
-        }
         __syncwarp();
     } else {
         // ---- queries into the swizzled layout; rows and columns that do not exist are zero
@@ -710,7 +702,7 @@ serve_attn_prefix_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
         Row state;
         bool ok = true;
         for (int it = 0; it < mine; it++) {
-            ok = mbar_wait(s_full + 8 * w, it & 1, &gave_up);
+            ok = mbar_wait(s_full + 8 * w, it & 1, waits);
             if (!__all_sync(~0u, ok)) {
                 ok = false;
                 break;
@@ -724,10 +716,10 @@ serve_attn_prefix_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
             mbar_arrive(p_full + 8 * w);
         }
         // ---- the way out: a row's sums as they are, with what they were taken against
-        if (mine > 0 && ok) ok = mbar_wait(o_full + 8 * w, 0, &gave_up);
+        if (mine > 0 && ok) ok = mbar_wait(o_full + 8 * w, 0, waits);
         // Both halves' products are done then, and what they read may be written over: a half waits for the other's too,
         // unless that has none (one tile of tokens, of which half 1 has no part).
-        if (ok && (TWO || nt > 1)) ok = mbar_wait(o_full + 8 * (w ^ 1), 0, &gave_up);
+        if (ok && (TWO || nt > 1)) ok = mbar_wait(o_full + 8 * (w ^ 1), 0, waits);
         ok = __all_sync(~0u, ok);
         tc_fence_after();
         // Through shared memory, where the tiles were, and out row by row.
@@ -784,6 +776,14 @@ serve_attn_prefix_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
         tc_fence_before();
     }
     __syncthreads();
+    if (gave_up) {                                                    // (nobody sets it from here on)
+        if (warp == 8 && lane == 0) drain_loads<stages>(full, issued);
+        if (warp == 9) {
+            mma_commit_warp(elect_one(), drained);                    // the thread that issued the products
+            mbar_drain(drained, 0);
+        }
+        __syncthreads();
+    }
     tc_fence_after();
     if (warp == 9) tmem_free(tmem, 512);
     if (tid == 0 && gave_up) atomicExch(d.status, 1);
@@ -1041,6 +1041,7 @@ int bcast_serve_attn(const bcast_serve_attn_args *args, void *cuda_stream)
     d.out = a->out;
     d.lse = a->lse;
     d.status = (int *)a->workspace;
+    d.wait_limit = wait_limit();
     d.part_ml = (float2 *)((char *)a->workspace + BCAST_SERVE_STATUS_BYTES);
     d.part_o = (float *)((char *)d.part_ml + round_up(c.parts * c.rows * 8, 256));
     for (int i = 0; i < 3; i++) {

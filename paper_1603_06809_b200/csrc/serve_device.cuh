@@ -8,6 +8,8 @@
 #include <cstdint>
 #include <type_traits>
 
+#include "serve_internal.h"
+
 namespace bcast_serve {
 
 constexpr float kLog2e = 1.4426950408889634f;
@@ -85,18 +87,23 @@ __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity)
     return done;
 }
 
-// Every wait is bounded.  The limit is seconds of polling, far beyond any wait of a working kernel; when it
-// runs out the waiting thread sets the block's `gave_up` flag, which ends the other waits of the block too, and
-// the kernel drains what it has in flight, frees its tensor memory and reports through the status word.
-constexpr uint32_t kWaitLimit = 1u << 24;
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int *gave_up)
+// Every wait is bounded.  The limit (kWaitLimit where nothing else is asked for) is seconds of polling, far beyond any
+// wait of a working kernel; when it runs out the waiting thread sets the block's `gave_up` flag, which ends the other
+// waits of the block too.  Once all its threads have come to the end and see the flag alike, the block waits (again with
+// a limit) for the copies and matrix instructions that it has in flight, frees its tensor memory and reports through
+// the status word.  With a limit of 0 a block begins as one that has given up.
+struct Waits {
+    volatile int *gave_up;
+    uint32_t limit;
+};
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, const Waits &w)
 {
-    if (mbar_try(bar, parity)) return true;
-    for (uint32_t i = 0; i < kWaitLimit; i++) {
+    if (mbar_try(bar, parity)) return true;                   // (in the loop alone, attention's long prefixes took 6 % longer)
+    for (uint32_t i = 0; i < w.limit; i++) {
         if (mbar_try(bar, parity)) return true;
-        if ((i & 31u) == 31u && *gave_up) return false;
+        if ((i & 31u) == 31u && *w.gave_up) return false;
     }
-    *gave_up = 1;
+    *w.gave_up = 1;
     return false;
 }
 // The drain's wait: bounded by itself, whatever the flag says.
@@ -119,6 +126,17 @@ struct Ring {
         }
     }
 };
+
+// The same for the last `issued` passes of a ring of loads, of which no more than its stages can be under way.
+template <int N>
+__device__ __forceinline__ void drain_loads(uint32_t full, int issued)
+{
+    Ring<N> r;
+    for (int i = 0; i < issued; i++) {
+        if (i + N >= issued) mbar_drain(full + 8 * r.slot, r.parity);
+        r.step();
+    }
+}
 
 // ------------------------------------------------------------------------------------------- TMA
 __device__ __forceinline__ void tma_prefetch(const CUtensorMap *m)

@@ -4,6 +4,7 @@
 
 #include <atomic>
 #include <cstdint>
+#include <cstdlib>
 
 #include "bcast_serve.h"
 #include "exec_internal.h"
@@ -46,6 +47,18 @@ inline int check_workspace(void *ws, uint64_t have, int64_t need, int device)
     if (need < 0) return (int)need;
     if (have < (uint64_t)need) return BCAST_ERR_CAPACITY;
     return check_array(ws, 256, device);
+}
+
+// Polls of a bounded wait.
+constexpr uint32_t kWaitLimit = 1u << 24;
+inline uint32_t wait_limit()
+{
+    static const uint32_t limit = [] {
+        const char *v = std::getenv("BCAST_SERVE_SPIN_LIMIT");
+        const long n = v && *v ? std::strtol(v, nullptr, 10) : (long)kWaitLimit;
+        return (uint32_t)(n < 0 ? 0 : n > (long)kWaitLimit ? (long)kWaitLimit : n);
+    }();
+    return limit;
 }
 
 struct Device {

@@ -1,10 +1,14 @@
 """Arguments and arrays at the edge of what the serving operators take, against the plain 64-bit forms."""
 import math
+import os
+import subprocess
+import sys
 
 import pytest
 import torch
 
 import serve_reference as R
+from helpers import ROOT
 from paper_1603_06809_b200 import replica as P
 from paper_1603_06809_b200 import serve as S
 from paper_1603_06809_b200.bcast import BCAST_ERR_CAPACITY, BCAST_ERR_TIMEOUT, BcastError
@@ -278,3 +282,56 @@ def test_replica_steps_until_its_cache_is_full():
     with pytest.raises(ValueError):
         rep.step(**P.drafted(s, 5, 0, 60, DEV))
     S.bcast_serve_status(rep.workspace)
+
+
+# ------------------------------------------------------------------------------------------ waits that run out
+WAITS_CHILD = r"""
+import sys
+import torch
+sys.path[:0] = [sys.argv[1], sys.argv[1] + "/tests"]
+from paper_1603_06809_b200 import bcast as B, serve as S
+from test_serve_gpu import attn_case, linear_case, on_gpu
+
+
+def told(ws):
+    try:
+        S.bcast_serve_status(ws)
+        return "ok"
+    except B.BcastError as e:
+        return str(e.code)
+
+
+def linear(ws, *size, **more):
+    d = {k: on_gpu(v) for k, v in linear_case(1, *size, **more).items()}
+    return S.bcast_serve_linear(d.pop("x"), d.pop("weight"), workspace=ws, **d)
+
+
+def attn(ws, *size):
+    d = {k: on_gpu(v) for k, v in attn_case(2, *size).items()}
+    return S.bcast_serve_attn(d["q"], d["prefix_k"], d["prefix_v"], d["own_k"], d["own_v"], d["own_len"], workspace=ws)
+
+
+calls = [lambda ws: linear(ws, 24, 1024, 200, 3, 16, "bf16"), lambda ws: linear(ws, 100, 512, 300, 0, 0, "fp16"),
+         lambda ws: linear(ws, 1300, 72, 19000, 6, 128, "bf16"), lambda ws: attn(ws, 40, 1, 2, 4, 64, 1300, 6, 0, "bf16"),
+         lambda ws: attn(ws, 40, 1, 2, 4, 128, 1300, 6, 0, "fp16"), lambda ws: attn(ws, 256, 1, 8, 1, 64, 151700, 6, 0, "bf16")]
+for i, call in enumerate(calls):
+    ws = S.Workspace("cuda:0")
+    call(ws)
+    first = told(ws)
+    print("CALL", i, first, told(ws))                           # the word was cleared by the read
+torch.cuda.synchronize()
+print("END")
+"""
+
+
+@pytest.mark.parametrize("limit,want", [("0", str(BCAST_ERR_TIMEOUT)), ("", "ok")])
+def test_waits_that_run_out_end_the_kernel_and_are_told(limit, want):
+    # With no polls allowed the kernels have given up from the start: what they still issue touches the block's own memory
+    # alone and is waited for, they come to their end and tell of it.
+    env = dict(os.environ)
+    env.pop("BCAST_SERVE_SPIN_LIMIT", None)
+    if limit:
+        env["BCAST_SERVE_SPIN_LIMIT"] = limit
+    out = subprocess.run([sys.executable, "-c", WAITS_CHILD, ROOT], env=env, capture_output=True, text=True, timeout=300)
+    assert out.returncode == 0, out.stderr[-2000:]
+    assert out.stdout.split("\n") == [f"CALL {i} {want} ok" for i in range(6)] + ["END", ""], out.stdout
