@@ -1015,15 +1015,15 @@ int bcast_serve_attn(const bcast_serve_attn_args *args, void *cuda_stream)
     if (paged && (a->page_size < 1 || a->num_pages < 0 || a->num_pages > kMaxDim ||
                   !stride_ok(a->page_table_stride, ceil_div(a->own_cap, a->page_size), 1)))
         return BCAST_ERR_INVAL;
-    Device dev;
-    if ((rc = current_device(&dev))) return rc;
-    if ((rc = check_array(a->q, 16, dev.id)) || (rc = check_array(a->out, 16, dev.id)) || (rc = check_array(a->own_len, 4, dev.id)))
+    int device = 0;
+    SERVE_TRY(cudaGetDevice(&device));
+    if ((rc = check_array(a->q, 16, device)) || (rc = check_array(a->out, 16, device)) || (rc = check_array(a->own_len, 4, device)))
         return rc;
-    if (a->prefix_len && ((rc = check_array(a->prefix_k, 16, dev.id)) || (rc = check_array(a->prefix_v, 16, dev.id)))) return rc;
-    if (a->own_cap && ((rc = check_array(a->own_k, 16, dev.id)) || (rc = check_array(a->own_v, 16, dev.id)))) return rc;
-    if (paged && (rc = check_array(a->page_table, 4, dev.id))) return rc;
-    if (a->lse && (rc = check_array(a->lse, 4, dev.id))) return rc;
-    if ((rc = check_workspace(a->workspace, a->workspace_bytes, bcast_serve_attn_workspace(a), dev.id))) return rc;
+    if (a->prefix_len && ((rc = check_array(a->prefix_k, 16, device)) || (rc = check_array(a->prefix_v, 16, device)))) return rc;
+    if (a->own_cap && ((rc = check_array(a->own_k, 16, device)) || (rc = check_array(a->own_v, 16, device)))) return rc;
+    if (paged && (rc = check_array(a->page_table, 4, device))) return rc;
+    if (a->lse && (rc = check_array(a->lse, 4, device))) return rc;
+    if ((rc = check_workspace(a->workspace, a->workspace_bytes, bcast_serve_attn_workspace(a), device))) return rc;
 
     const Cut c = cut_of(*a);
     AttnDev d = {};

@@ -61,17 +61,6 @@ inline uint32_t wait_limit()
     return limit;
 }
 
-struct Device {
-    int id = -1, sms = 0;
-};
-
-inline int current_device(Device *d)
-{
-    SERVE_TRY(cudaGetDevice(&d->id));
-    SERVE_TRY(cudaDeviceGetAttribute(&d->sms, cudaDevAttrMultiProcessorCount, d->id));
-    return BCAST_OK;
-}
-
 // The SM count that workspace sizes are computed with: they must not depend on whether a device is
 // there, so it is the B200's.
 constexpr int kSms = 148;

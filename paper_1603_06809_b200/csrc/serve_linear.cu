@@ -630,15 +630,15 @@ int bcast_serve_linear(const bcast_serve_linear_args *a, void *cuda_stream)
         (!stride_ok(a->lora_a_stride[1], a->k, 8) || !stride_ok(a->lora_a_stride[0], a->lora_a_stride[1] * (a->rank - 1) + a->k, 8) ||
          !stride_ok(a->lora_b_stride[1], a->rank, 8) || !stride_ok(a->lora_b_stride[0], a->lora_b_stride[1] * (a->n - 1) + a->rank, 8)))
         return BCAST_ERR_INVAL;
-    Device dev;
-    if ((rc = current_device(&dev))) return rc;
-    if ((rc = check_array(a->x, 16, dev.id)) || (rc = check_array(a->weight, 16, dev.id)) || (rc = check_array(a->y, 2, dev.id)))
+    int device = 0;
+    SERVE_TRY(cudaGetDevice(&device));
+    if ((rc = check_array(a->x, 16, device)) || (rc = check_array(a->weight, 16, device)) || (rc = check_array(a->y, 2, device)))
         return rc;
-    if (a->bias && (rc = check_array(a->bias, 2, dev.id))) return rc;
-    if (a->num_adapters && ((rc = check_array(a->lora_a, 16, dev.id)) || (rc = check_array(a->lora_b, 16, dev.id)) ||
-                            (rc = check_array(a->adapter, 4, dev.id)) || (rc = check_array(a->scale, 4, dev.id))))
+    if (a->bias && (rc = check_array(a->bias, 2, device))) return rc;
+    if (a->num_adapters && ((rc = check_array(a->lora_a, 16, device)) || (rc = check_array(a->lora_b, 16, device)) ||
+                            (rc = check_array(a->adapter, 4, device)) || (rc = check_array(a->scale, 4, device))))
         return rc;
-    if ((rc = check_workspace(a->workspace, a->workspace_bytes, bcast_serve_linear_workspace(a), dev.id))) return rc;
+    if ((rc = check_workspace(a->workspace, a->workspace_bytes, bcast_serve_linear_workspace(a), device))) return rc;
 
     LinearDev d = {};
     d.bias = a->bias;

@@ -411,17 +411,17 @@ int bcast_serve_verify(const bcast_serve_verify_args *a, void *cuda_stream)
     if (!stride_ok(a->logits_stride[0], 0, 1) || !stride_ok(a->logits_stride[1], 0, 1) || !stride_ok(a->noise_stride, 0, 1) ||
         (a->drafts && (!stride_ok(a->draft_probs_stride[0], 0, 1) || !stride_ok(a->draft_probs_stride[1], 0, 1))))
         return BCAST_ERR_INVAL;
-    Device dev;
-    if ((rc = current_device(&dev))) return rc;
+    int device = 0;
+    SERVE_TRY(cudaGetDevice(&device));
     const uintptr_t size = a->dtype == BCAST_SERVE_FP32 ? 4 : 2;
-    if ((rc = check_array(a->logits, size, dev.id)) || (rc = check_array(a->noise, 4, dev.id)) ||
-        (rc = check_array(a->temperature, 4, dev.id)) || (rc = check_array(a->accepted, 4, dev.id)) ||
-        (rc = check_array(a->tokens, 4, dev.id)))
+    if ((rc = check_array(a->logits, size, device)) || (rc = check_array(a->noise, 4, device)) ||
+        (rc = check_array(a->temperature, 4, device)) || (rc = check_array(a->accepted, 4, device)) ||
+        (rc = check_array(a->tokens, 4, device)))
         return rc;
-    if (a->drafts && ((rc = check_array(a->draft_probs, 4, dev.id)) || (rc = check_array(a->draft_tokens, 4, dev.id)) ||
-                      (rc = check_array(a->uniforms, 4, dev.id))))
+    if (a->drafts && ((rc = check_array(a->draft_probs, 4, device)) || (rc = check_array(a->draft_tokens, 4, device)) ||
+                      (rc = check_array(a->uniforms, 4, device))))
         return rc;
-    if ((rc = check_workspace(a->workspace, a->workspace_bytes, bcast_serve_verify_workspace(a), dev.id))) return rc;
+    if ((rc = check_workspace(a->workspace, a->workspace_bytes, bcast_serve_verify_workspace(a), device))) return rc;
 
     VerifyDev d;
     d.logits = a->logits;
@@ -451,10 +451,9 @@ int bcast_serve_verify(const bcast_serve_verify_args *a, void *cuda_stream)
 
 int bcast_serve_status(void *workspace, void *cuda_stream)
 {
-    Device dev;
-    int rc = current_device(&dev);
-    if (rc) return rc;
-    if ((rc = check_array(workspace, 256, dev.id))) return rc;
+    int device = 0, rc;
+    SERVE_TRY(cudaGetDevice(&device));
+    if ((rc = check_array(workspace, 256, device))) return rc;
     const cudaStream_t st = (cudaStream_t)cuda_stream;
     int32_t word = 0;
     SERVE_TRY(cudaMemcpyAsync(&word, workspace, sizeof word, cudaMemcpyDeviceToHost, st));
