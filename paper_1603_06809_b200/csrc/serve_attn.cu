@@ -594,9 +594,15 @@ serve_attn_prefix_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
         const uint32_t s_desc = mma_desc<T>(128, kTileKeys), o_desc = mma_desc<T>(128, (d.dim + 15) / 16 * 16, true);
         const uint64_t q_desc = smem_desc(q_at), k_desc = smem_desc(kv_at), v_desc = smem_desc(kv_at, block);
         Ring<stages> ring;
-        auto take = [&]() {                                           // the next tile of K or V, once it is there
-            mbar_wait(full + 8 * ring.slot, ring.parity, waits);
+        // Every lane polls for itself; none may fall so far behind the one that issues that a barrier has gone on to its
+        // next phase but one.
+        auto wait = [&](uint32_t bar, uint32_t parity) {
+            mbar_wait(bar, parity, waits);
+            __syncwarp();
             tc_fence_after();
+        };
+        auto take = [&]() {                                           // the next tile of K or V, once it is there
+            wait(full + 8 * ring.slot, ring.parity);
             const int slot = ring.slot;
             ring.step();
             return slot;
@@ -613,17 +619,15 @@ serve_attn_prefix_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
         auto values = [&](int w, int slot, int it) {                  // O_w += P_w V, as the weights come
             const uint64_t b = v_desc + slot * (stage >> 4);
             const uint32_t o = tmem + 256 + w * 128, a = tmem + w * 128;
-            mbar_wait(p_most + 8 * w, it & 1, waits);
-            tc_fence_after();
+            wait(p_most + 8 * w, it & 1);
             mma_ts_warp(lead, o, a, b, o_desc, it > 0);
 #pragma unroll
             for (int i = 1; i < 6; i++) mma_ts_warp(lead, o, a + i * 8, b + i * (2048 >> 4), o_desc, true);
-            mbar_wait(p_full + 8 * w, it & 1, waits);
-            tc_fence_after();
+            wait(p_full + 8 * w, it & 1);
 #pragma unroll
             for (int i = 6; i < 8; i++) mma_ts_warp(lead, o, a + i * 8, b + i * (2048 >> 4), o_desc, true);
         };
-        mbar_wait(q_full, 0, waits);
+        wait(q_full, 0);
         int ks = take();
         scores(0, ks);
         if (TWO) {
