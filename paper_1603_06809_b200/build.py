@@ -59,25 +59,40 @@ def _build_bind(nvcc: str) -> None:
           "-Wl,-rpath,$ORIGIN", f"-Wl,-rpath,{troot}/lib"], BIND_PATH)
 
 
+def _build_library(nvcc: str, verbose: bool = False) -> None:
+    _run([nvcc, *NVCC_FLAGS, *(["-Xptxas", "-v"] if verbose else []), *SOURCES], LIB_PATH)
+
+
+def _nvcc() -> str:
+    return os.environ.get("NVCC", "nvcc")
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
-    """Compile the library if it is missing or older than its sources; return its path."""
-    nvcc = os.environ.get("NVCC", "nvcc")
+    """Compile the library and the extension module if they are missing or older than their sources; return the
+    library's path."""
     if force or _older(LIB_PATH, SOURCES + HEADERS):
-        _run([nvcc, *NVCC_FLAGS, *(["-Xptxas", "-v"] if verbose else []), *SOURCES], LIB_PATH)
+        _build_library(_nvcc(), verbose)
     if force or _older(BIND_PATH, BIND_SOURCES + BIND_HEADERS):
-        _build_bind(nvcc)
+        _build_bind(_nvcc())
     return LIB_PATH
 
 
 def ensure_built() -> str:
-    """Build what is missing; if it is merely older than its sources, try to rebuild
-    and keep the existing one when no compiler is at hand.  Returns the path of the library."""
-    if not os.path.exists(LIB_PATH) or not os.path.exists(BIND_PATH):
-        return build()
-    if needs_build():
+    """Build what is missing or older than its sources; keep what there is when no compiler is at hand.  The library has
+    to be there in the end.  The extension module need not: only ``serve`` loads it, and says so if it cannot.
+    Returns the path of the library."""
+    failed = (OSError, subprocess.CalledProcessError)
+    if not os.path.exists(LIB_PATH):
+        _build_library(_nvcc())
+    elif _older(LIB_PATH, SOURCES + HEADERS):
         try:
-            return build()
-        except (OSError, subprocess.CalledProcessError):
+            _build_library(_nvcc())
+        except failed:
+            pass
+    if _older(BIND_PATH, BIND_SOURCES + BIND_HEADERS):
+        try:
+            _build_bind(_nvcc())
+        except (*failed, ImportError):                # no compiler, no headers, no torch
             pass
     return LIB_PATH
 

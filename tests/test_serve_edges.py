@@ -1,7 +1,11 @@
 """What the serving side refuses or does without on the host, without a GPU."""
+import os
+import subprocess
+
 import pytest
 import torch
 
+from paper_1603_06809_b200 import build as BU
 from paper_1603_06809_b200 import replica as P
 
 
@@ -35,3 +39,42 @@ def test_replica_reads_the_lengths_when_all_drafts_would_fill_the_cache():
     with pytest.raises(ValueError):
         rep._make_room(3)
     rep._make_room(2)
+
+
+# ---- what has to be built for whom
+def refuse(error):
+    def run(*_, **__):
+        raise error
+    return run
+
+
+@pytest.mark.parametrize("error", [OSError("no compiler"), subprocess.CalledProcessError(1, "c++"), ImportError("no torch")])
+@pytest.mark.parametrize("there", [False, True])
+def test_the_library_alone_does_without_the_extension_module(error, there, tmp_path, monkeypatch):
+    lib, bind = tmp_path / "lib.so", tmp_path / "bind.so"
+    lib.touch()
+    if there:                                                 # but older than its source
+        bind.touch()
+        (tmp_path / "bind.cpp").touch()
+        os.utime(bind, (1, 1))
+        monkeypatch.setattr(BU, "BIND_SOURCES", [str(tmp_path / "bind.cpp")])
+    monkeypatch.setattr(BU, "LIB_PATH", str(lib))
+    monkeypatch.setattr(BU, "BIND_PATH", str(bind))
+    monkeypatch.setattr(BU, "_build_bind", refuse(error))
+    assert BU.ensure_built() == str(lib)
+    with pytest.raises(type(error)):                          # asked for by name, it is an error
+        BU.build()
+
+
+@pytest.mark.parametrize("error", [OSError("no compiler"), subprocess.CalledProcessError(1, "nvcc")])
+def test_without_the_library_there_is_nothing_to_go_on_with(error, tmp_path, monkeypatch):
+    lib, bind = tmp_path / "lib.so", tmp_path / "bind.so"
+    bind.touch()
+    monkeypatch.setattr(BU, "LIB_PATH", str(lib))
+    monkeypatch.setattr(BU, "BIND_PATH", str(bind))
+    monkeypatch.setattr(BU, "_run", refuse(error))
+    with pytest.raises(type(error)):
+        BU.ensure_built()
+    lib.touch()
+    os.utime(lib, (1, 1))                                     # older than its sources: kept
+    assert BU.ensure_built() == str(lib)
