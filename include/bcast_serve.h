@@ -15,6 +15,8 @@
  *   bcast_serve_verify   acceptance of drafted tokens against the target's probabilities from given
  *                        random numbers, and the choice of the token that follows them
  *
+ * They go forward only: what they compute has no backward pass here.
+ *
  * Conventions
  *   - As in bcast.h: every function returns BCAST_OK or a negative BCAST_ERR_* code, nothing throws
  *     across this boundary, and work is enqueued on the caller's stream of the current device and
@@ -54,8 +56,9 @@ enum { BCAST_SERVE_BF16 = 0, BCAST_SERVE_FP16 = 1, BCAST_SERVE_FP32 = 2 };
 /*
  * bcast_serve_linear -- y[t] = W x[t] + bias + scale[a] * B[a] (A[a] x[t]),  a = adapter[t].
  * A token whose adapter is outside 0..num_adapters-1 (-1, say) gets W x[t] + bias alone.  Sums are
- * held in 32 bits; the low-rank product A[a] x[t] is passed on as the sum of two numbers of the data
- * type (16 or more significant bits; scale[a] * A[a] x[t] has to be in its range), y is rounded once.
+ * held in 32 bits; the low-rank product u = scale[a] * A[a] x[t] is passed on as the sum of two numbers of
+ * the data type (bf16: a relative error of 2^-16 at most; fp16: 2^-22, or 2^-25 as such where that is more;
+ * u has to be in the type's range), y is rounded once.
  *   - Adapters that no token of the call names are not read.  Those that are hold finite numbers: a token's own x
  *     may hold NaN or infinity without touching other tokens, an adapter's values may not (tokens of one tile pass
  *     through the same products, multiplied by zero for the adapters they do not have).

@@ -432,7 +432,7 @@ serve_linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
         // The blocks' sums are joined: each puts its own where its stages were, block r of the cluster adds up all
         // of them for its share of the tokens, always in the same order.  (Sending them to where they are added
         // instead of fetching them from there was slower: 4-byte remote stores, 32 us against 25 us for 333
-        // tokens, 2056 -> 5003, two blocks to a tile.)
+        // tokens, 2056 -> 5003, when the rule still gave these two blocks to a tile; it gives one now, 27 us.)
         const int f0 = first_tile % d.f_tiles * kFeatures, t0 = first_tile / d.f_tiles * NT, share = NT / split;
         if (warp >= 2) {
             const int quarter = warp % 4, f = quarter * 32 + lane;
@@ -510,7 +510,8 @@ int check_shape(const bcast_serve_linear_args &a)
 // How a call is cut.  Measured on one B200 (us, inputs not in L2), k = 4096, n = 4096 where nothing else is said:
 //   main kernel, tokens of a tile x parts of k:  64 tokens: 64 x 4 20.1, 64 x 2 23.6, 32 x 2 20.3, 128 x 4 24.3;
 //     128 tokens: 64 x 2 25.4, 64 x 4 25.8, 128 x 4 30.2;  512: 128 x 2 35, 128 x 1 37, 64 x 1 36, 256 x 2 76;
-//     1024: 128 47, 64 58, 256 81;  2048: 128 88, 256 105;  8192: 256 260, 128 289.  So a block to an SM,
+//     1024: 128 47, 64 58, 256 81;  2048: 128 88, 256 105;  8192: 256 260, 128 289.  So no more blocks than SMs
+//     (twice as many: 2 us ahead at 512 tokens, level at 128),
 //     and the widest tile, which reads W least often, once there are three rounds of it.
 //   low kernel, parts of k (more parts end sooner, but the main kernel adds them up):  64 tokens: 16 parts 21.1, 8 21.9,
 //     4 24.6;  512: 4 parts 37, 8 44, 2 40, 1 49;  1024: 2 parts 41, 4 47, 1 49.  So at most one for every

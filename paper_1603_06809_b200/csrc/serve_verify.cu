@@ -223,6 +223,8 @@ __device__ __forceinline__ Runner shuffle_xor(const Runner &a, int d)
     return Runner{__shfl_xor_sync(~0u, a.ratio, d), __shfl_xor_sync(~0u, a.token, d)};
 }
 
+// (1 / x within 2^-23, a few instructions less than the division: two runners whose ratios are nearer to each other than
+// the probabilities' own rounding may come in in either order)
 __device__ __forceinline__ float reciprocal(float x)
 {
     float y;

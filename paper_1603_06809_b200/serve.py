@@ -8,7 +8,10 @@ that hold pointers instead of tensors.
 
 ``stream``: a ``torch.cuda.Stream``, a raw ``cudaStream_t`` value, or None for torch's current stream.
 ``workspace``: a :class:`Workspace`, which a program keeps and hands to one call after the other on one
-stream; without one, a call takes fresh memory from torch.
+stream; without one, a call takes fresh memory from torch, and nobody can ask afterwards (:func:`bcast_serve_status`)
+whether a wait in it ran out and left its output incomplete.
+
+The operators go forward only: inputs may require gradients, results have none.
 """
 from __future__ import annotations
 
