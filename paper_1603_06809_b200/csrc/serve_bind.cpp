@@ -12,6 +12,7 @@
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/utils/pybind.h>
 
+#include <initializer_list>
 #include <optional>
 #include <string>
 #include <vector>
@@ -73,6 +74,7 @@ void strides(const Tensor &t, int n, int64_t *out)
     }
 }
 
+const Tensor *given(const Maybe &t) { return t ? &*t : nullptr; }
 const void *pointer(const Maybe &t) { return t ? t->data_ptr() : nullptr; }
 
 // Where a call runs: the device of its tensors, the stream that was named (-1: torch's current one) and the
@@ -88,6 +90,14 @@ struct Place {
         stream = raw ? c10::cuda::getStreamFromExternal((cudaStream_t)raw, (c10::DeviceIndex)t.get_device())
                      : c10::cuda::getDefaultCUDAStream((c10::DeviceIndex)t.get_device());
         guard.emplace(stream);
+    }
+    // On a stream that was named, torch does not know of the tensors' use: their memory is not to be handed out again
+    // before this stream is done with it, should the caller let go of them.
+    void use(std::initializer_list<const Tensor *> tensors) const
+    {
+        if (!guard) return;
+        for (const Tensor *t : tensors)
+            if (t) c10::cuda::CUDACachingAllocator::recordStream(t->storage().data_ptr(), stream);
     }
     static at::Device check(const Tensor &t)
     {
@@ -163,6 +173,7 @@ py::tuple linear(const Tensor &x, const Tensor &weight, const Maybe &bias, const
             strides(*lora_b, 2, a.lora_b_stride);
         }
         const Place place(x, raw);
+        place.use({&x, &weight, given(bias), given(lora_a), given(lora_b), given(adapter), given(scale), given(out)});
         const Tensor y = output(out, "out", {a.tokens, a.n}, type, dev);
         a.x = x.data_ptr();
         a.weight = weight.data_ptr();
@@ -212,6 +223,7 @@ py::tuple attn(const Tensor &q, const Tensor &prefix_k, const Tensor &prefix_v, 
             need(lse->is_contiguous(), "lse is contiguous");
         }
         const Place place(q, raw);
+        place.use({&q, &prefix_k, &prefix_v, &own_k, &own_v, &own_len, given(page_table), given(out), given(lse)});
         const Tensor o = output(out, "out", {B, n, HQ, D}, type, dev);
         a.batch = (int32_t)B;
         a.new_tokens = (int32_t)n;
@@ -258,6 +270,7 @@ py::tuple verify(const Tensor &logits, const Tensor &draft_probs, const Tensor &
         expect(noise, "noise", at::kFloat, {B, V}, dev);
         expect(temperature, "temperature", at::kFloat, {B}, dev);
         const Place place(logits, raw);
+        place.use({&logits, &draft_probs, &draft_tokens, &uniforms, &noise, &temperature, given(accepted), given(tokens)});
         const Tensor c = output(accepted, "accepted", {B}, at::kInt, dev), t = output(tokens, "tokens", {B, n + 1}, at::kInt, dev);
         need(t.is_contiguous(), "tokens is contiguous");
         a.batch = (int32_t)B;

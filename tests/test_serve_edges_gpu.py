@@ -262,6 +262,37 @@ def test_status_of_a_workspace_that_no_call_used():
         S.bcast_serve_status(ws, stream)
 
 
+@pytest.mark.parametrize("op", ["linear", "attn", "verify"])
+@pytest.mark.parametrize("raw", [False, True])
+def test_inputs_let_go_of_before_a_named_stream_is_done(op, raw):
+    if op == "linear":
+        c = linear_case(99, 300, 256, 200, 3, 16, "bf16")
+        call = lambda d, **k: S.bcast_serve_linear(d["x"], d["weight"], **{n: d[n] for n in ("bias", "lora_a", "lora_b", "adapter", "scale")}, **k)  # noqa: E731
+    elif op == "attn":
+        c = attn_case(99, 40, 2, 2, 4, 64, 1300, 50, 16, "bf16")
+        call = lambda d, **k: S.bcast_serve_attn(d["q"], d["prefix_k"], d["prefix_v"], d["own_k"], d["own_v"], d["own_len"],  # noqa: E731
+                                                 page_table=d["page_table"], **k)
+    else:
+        c = verify_case(99, 6, 3, 2000, "bf16")
+        call = lambda d, **k: S.bcast_serve_verify(*d.values(), **k)  # noqa: E731
+    d = {k: on_gpu(v) for k, v in c.items()}
+    want = call(d)
+    ws, side = S.Workspace(DEV, 1 << 24), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    copies = {k: v.clone() for k, v in d.items()}
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(20_000_000)                         # the stream is busy for some milliseconds
+    got = call(copies, workspace=ws, stream=side.cuda_stream if raw else side)
+    del copies
+    # memory of the copies' sizes, if it were free already
+    others = [torch.zeros_like(v) for v in d.values() for _ in range(2)]
+    torch.cuda.synchronize()
+    for x, y in zip(want if op == "verify" else (want,), got if op == "verify" else (got,)):
+        assert torch.equal(x, y)
+    del others
+
+
 # ------------------------------------------------------------------------------------------ replicas
 def test_replica_steps_until_its_cache_is_full():
     s = P.Shape(hidden=128, q_heads=4, kv_heads=2, dim=64, vocab=500, adapters=3, rank=8, prompt=150, page=8)
