@@ -36,8 +36,8 @@
  *     with different workspaces may overlap.
  *   - The kernels' waits on the copy engine and on the tensor cores are bounded.  One that runs out
  *     sets the status word and ends the kernel early, its output incomplete: see bcast_serve_status().
- *     The environment variable BCAST_SERVE_SPIN_LIMIT (polls of a wait, read at the first call) lowers the
- *     bound for tests; at 0 every wait that is not over at once has run out.
+ *     With the environment variable BCAST_SERVE_GIVE_UP=1 (for tests; read at the first call) the kernels
+ *     begin as if a wait had run out.
  *   - The calls may be captured into a CUDA graph.
  */
 #ifndef BCAST_SERVE_B200_H

@@ -37,7 +37,7 @@ struct AttnDev {
     float2 *part_ml;      // [parts][rows]: (m, l), m = -infinity where a part holds nothing
     float *part_o;        // [parts][rows][dim]
     int *status;
-    uint32_t wait_limit;  // polls of a bounded wait
+    int give_up;          // 1: begin as if a wait had run out
     int64_t qs[3], os[3], oks[3], ovs[3], pks[2], pvs[2];
     int64_t own_cap, num_pages, pts, rows;       // rows: batch * fresh * q_heads
     int32_t batch, fresh, q_heads, kv_heads, group, dim, page, page_shift, prefix_len;
@@ -523,7 +523,6 @@ serve_attn_prefix_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
     __shared__ float2 half_ml[2][128];
     __shared__ uint32_t tmem_at;
     __shared__ int gave_up;
-    const Waits waits{&gave_up, d.wait_limit};
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
     const int rows = d.batch * d.fresh * d.group;                     // of one key/value head
     const int rt = blockIdx.x % d.row_tiles, kv = blockIdx.x / d.row_tiles % d.kv_heads, split = blockIdx.x / d.row_tiles / d.kv_heads;
@@ -538,7 +537,7 @@ serve_attn_prefix_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
     const uint32_t full = smem_u32(bars), empty = full + 8 * stages, q_full = empty + 8 * stages, s_full = q_full + 8,
                    p_most = s_full + 16, p_full = p_most + 16, o_full = p_full + 16, drained = o_full + 16;
     if (tid == 0) {
-        gave_up = d.wait_limit == 0;
+        gave_up = d.give_up;
         for (int i = 0; i < stages; i++) {
             mbar_init(full + 8 * i, 1);
             mbar_init(empty + 8 * i, 1);
@@ -568,7 +567,7 @@ serve_attn_prefix_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
             Ring<stages> ring;
             auto load = [&](const CUtensorMap *map, int j) {
                 // (the warp that issues the products goes on after it gave up: a slot may be free then that is not filled)
-                if (!mbar_wait(empty + 8 * ring.slot, ring.parity ^ 1u, waits) || *waits.gave_up) return false;
+                if (!mbar_wait(empty + 8 * ring.slot, ring.parity ^ 1u, &gave_up) || *(volatile int *)&gave_up) return false;
                 mbar_expect(full + 8 * ring.slot, stage);
                 for (int i = 0; i < DB; i++)
                     tma_load(kv_at + ring.slot * stage + i * block, map, i * 64, (j0 + j) * kTileKeys, kv, full + 8 * ring.slot);
@@ -577,7 +576,7 @@ serve_attn_prefix_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
                 return true;
             };
             // the queries are on their way before the rest of the first tiles, which they would have to queue behind
-            bool ok = load(&map_k, 0) && mbar_wait(q_full, 0, waits);
+            bool ok = load(&map_k, 0) && mbar_wait(q_full, 0, &gave_up);
             for (int j = 0; j < nt && ok; j++) {
                 if (TWO) {
                     ok = load(&map_v, j) && (j + 1 == nt || load(&map_k, j + 1));
@@ -600,7 +599,7 @@ serve_attn_prefix_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
         // Every lane polls for itself; none may fall so far behind the one that issues that a barrier has gone on to its
         // next phase but one.
         auto wait = [&](uint32_t bar, uint32_t parity) {
-            mbar_wait(bar, parity, waits);
+            mbar_wait(bar, parity, &gave_up);
             __syncwarp();
             tc_fence_after();
         };
@@ -712,7 +711,7 @@ serve_attn_prefix_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
         Row state;
         bool ok = true;
         for (int it = 0; it < mine; it++) {
-            ok = mbar_wait(s_full + 8 * w, it & 1, waits);
+            ok = mbar_wait(s_full + 8 * w, it & 1, &gave_up);
             if (!__all_sync(~0u, ok)) {
                 ok = false;
                 break;
@@ -726,10 +725,10 @@ serve_attn_prefix_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
             mbar_arrive(p_full + 8 * w);
         }
         // ---- the way out: a row's sums as they are, with what they were taken against
-        if (mine > 0 && ok) ok = mbar_wait(o_full + 8 * w, 0, waits);
+        if (mine > 0 && ok) ok = mbar_wait(o_full + 8 * w, 0, &gave_up);
         // Both halves' products are done then, and what they read may be written over: a half waits for the other's too,
         // unless that has none (one tile of tokens, of which half 1 has no part).
-        if (ok && (TWO || nt > 1)) ok = mbar_wait(o_full + 8 * (w ^ 1), 0, waits);
+        if (ok && (TWO || nt > 1)) ok = mbar_wait(o_full + 8 * (w ^ 1), 0, &gave_up);
         ok = __all_sync(~0u, ok);
         tc_fence_after();
         // Through shared memory, where the tiles were, and out row by row.
@@ -786,17 +785,20 @@ serve_attn_prefix_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
         tc_fence_before();
     }
     __syncthreads();
-    if (gave_up) {                                                    // (nobody sets it from here on)
-        if (warp == 8 && lane == 0) drain_loads<stages>(full, issued);
-        if (warp == 9) {
-            mma_commit_warp(elect_one(), drained);                    // the thread that issued the products
-            mbar_drain(drained, 0);
-        }
-        __syncthreads();
-    }
     tc_fence_after();
-    if (warp == 9) tmem_free(tmem, 512);
-    if (tid == 0 && gave_up) atomicExch(d.status, 1);
+    // (nobody sets gave_up from here on)
+    if (warp == 9) {
+        if (gave_up) {                                                // what was issued ends before tensor memory is given up
+            mma_commit_warp(elect_one(), drained);
+            mbar_drain(drained, 0);
+            __syncwarp();
+        }
+        tmem_free(tmem, 512);
+    }
+    if (warp == 8 && lane == 0 && gave_up) {                          // and loads, before the block's memory is
+        drain_loads<stages>(full, issued);
+        atomicExch(d.status, 1);
+    }
 }
 
 // ------------------------------------------------------------------------------------------- join
@@ -1051,7 +1053,7 @@ int bcast_serve_attn(const bcast_serve_attn_args *args, void *cuda_stream)
     d.out = a->out;
     d.lse = a->lse;
     d.status = (int *)a->workspace;
-    d.wait_limit = wait_limit();
+    d.give_up = give_up_at_once();
     d.part_ml = (float2 *)((char *)a->workspace + BCAST_SERVE_STATUS_BYTES);
     d.part_o = (float *)((char *)d.part_ml + round_up(c.parts * c.rows * 8, 256));
     for (int i = 0; i < 3; i++) {

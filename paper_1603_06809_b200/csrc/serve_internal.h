@@ -49,16 +49,14 @@ inline int check_workspace(void *ws, uint64_t have, int64_t need, int device)
     return check_array(ws, 256, device);
 }
 
-// Polls of a bounded wait.
-constexpr uint32_t kWaitLimit = 1u << 24;
-inline uint32_t wait_limit()
+// Are the kernels to begin as if one of their bounded waits had run out?  (For tests of what they do then.)
+inline int give_up_at_once()
 {
-    static const uint32_t limit = [] {
-        const char *v = std::getenv("BCAST_SERVE_SPIN_LIMIT");
-        const long n = v && *v ? std::strtol(v, nullptr, 10) : (long)kWaitLimit;
-        return (uint32_t)(n < 0 ? 0 : n > (long)kWaitLimit ? (long)kWaitLimit : n);
+    static const int yes = [] {
+        const char *v = std::getenv("BCAST_SERVE_GIVE_UP");
+        return v && *v && std::atoi(v) ? 1 : 0;
     }();
-    return limit;
+    return yes;
 }
 
 // The SM count that workspace sizes are computed with: they must not depend on whether a device is

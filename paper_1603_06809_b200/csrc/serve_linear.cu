@@ -53,7 +53,7 @@ struct LinearDev {
     void *y;
     float *low;                           // [low_splits][T][R]: parts of A x
     int *status;
-    uint32_t wait_limit;                  // polls of a bounded wait
+    int give_up;                          // 1: begin as if a wait had run out
     int64_t ys;
     int32_t tokens, k, n, adapters, rank, f_tiles, t_tiles, low_splits;
 };
@@ -139,7 +139,6 @@ serve_linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
     __shared__ uint32_t firsts[(NT + 127) / 128 * 4], tmem_at;
     __shared__ int count, gave_up;
 
-    const Waits waits{&gave_up, d.wait_limit};
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
     const cg::cluster_group cluster = cg::this_cluster();
     const int split = LOW ? d.low_splits : (int)cluster.num_blocks(), part = LOW ? blockIdx.x % split : (int)cluster.block_rank();
@@ -171,7 +170,7 @@ serve_linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
     } else if (warp == 1) {
         tmem_alloc(smem_u32(&tmem_at), S::columns);
     } else if (tid == 0) {
-        gave_up = d.wait_limit == 0;
+        gave_up = d.give_up;
         for (int i = 0; i < S::stages; i++) {
             mbar_init(full + 8 * i, 1);
             mbar_init(empty + 8 * i, 1);
@@ -183,7 +182,7 @@ serve_linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
             mbar_init(acc_empty + 8 * i, 128);
         }
         mbar_init(meta, 128);
-        mbar_init(taken, 1);
+        if (S::accs > 1) mbar_init(taken, 1);
         mbar_init(drained, 1);
         mbar_init_fence();
         tma_prefetch(&map_x);
@@ -212,11 +211,11 @@ serve_linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
                 for (int kb = kb0; kb < kb1; kb++) {
                     if (!LOW && kb == kb0 + S::stages && tile == first_tile && d.adapters) {
                         // while the first stages are on their way: the adapters' tiles too, as far as L2
-                        if (!(ok = mbar_wait(meta, 0, waits))) break;
+                        if (!(ok = mbar_wait(meta, 0, &gave_up))) break;
                         for (int j = part; j < count; j += split)
                             for (int cb = 0; cb < form.column_blocks; cb++) tma_prefetch_box(&map_b, cb * kDepth, f0, list[j]);
                     }
-                    if (!(ok = mbar_wait(empty + 8 * ring.slot, ring.parity ^ 1u, waits))) break;
+                    if (!(ok = mbar_wait(empty + 8 * ring.slot, ring.parity ^ 1u, &gave_up))) break;
                     const uint32_t bar = full + 8 * ring.slot, at = stage0 + ring.slot * S::stage;
                     mbar_expect(bar, (LOW ? mine * d.rank : kFeatures) * 128 + NT * 128);
                     if (LOW) {
@@ -229,20 +228,20 @@ serve_linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
                     ring.step();
                 }
                 if (LOW || !d.adapters || !ok) continue;
-                if (!(ok = mbar_wait(meta, meta_parity, waits))) break;
+                if (!(ok = mbar_wait(meta, meta_parity, &gave_up))) break;
                 meta_parity ^= 1u;
                 const int adapters = count;
                 const int stages = (adapters - part + split - 1) / split * form.halves;
                 for (int cb = 0; cb < form.column_blocks && ok; cb++)
                     for (int i = 0; i < stages; i++) {
-                        if (!(ok = mbar_wait(empty + 8 * ring.slot, ring.parity ^ 1u, waits))) break;
+                        if (!(ok = mbar_wait(empty + 8 * ring.slot, ring.parity ^ 1u, &gave_up))) break;
                         mbar_arrive(ready + 8 * ring.slot);
                         mbar_expect(full + 8 * ring.slot, kFeatures * form.row);
                         tma_load(stage0 + ring.slot * S::stage, &map_b, cb * kDepth, f0, list[part + i / form.halves * split], full + 8 * ring.slot);
                         issued++;
                         ring.step();
                     }
-                if (ok) mbar_arrive(taken);           // count and list are the next tile's now
+                if (S::accs > 1 && ok) mbar_arrive(taken);    // count and list are the next tile's now
             }
         }
         __syncwarp();
@@ -255,12 +254,12 @@ serve_linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
             uint32_t meta_parity = 0, uses = 0;       // bit s: parity of the next use of stage s for an adapter
             bool ok = true;
             for (int tile = first_tile; tile < tiles && ok; tile += tile_step) {
-                if (!(ok = mbar_wait(acc_empty + 8 * acc.slot, acc.parity ^ 1u, waits))) break;
+                if (!(ok = mbar_wait(acc_empty + 8 * acc.slot, acc.parity ^ 1u, &gave_up))) break;
                 tc_fence_after();
                 const uint32_t out = tmem + acc.slot * NT;
                 bool add = false;
                 for (int kb = kb0; kb < kb1; kb++) {
-                    if (!(ok = mbar_wait(full + 8 * ring.slot, ring.parity, waits))) break;
+                    if (!(ok = mbar_wait(full + 8 * ring.slot, ring.parity, &gave_up))) break;
                     tc_fence_after();
                     const uint32_t at = stage0 + ring.slot * S::stage;
                     const uint64_t a = smem_desc(at), b = smem_desc(at + kFeatures * 128);
@@ -273,14 +272,14 @@ serve_linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
                     ring.step();
                 }
                 if (!LOW && d.adapters && ok) {
-                    if (!(ok = mbar_wait(meta, meta_parity, waits))) break;
+                    if (!(ok = mbar_wait(meta, meta_parity, &gave_up))) break;
                     meta_parity ^= 1u;
                     const int adapters = count;
                     const int stages = (adapters - part + split - 1) / split * form.halves;
                     for (int cb = 0; cb < form.column_blocks && ok; cb++)
                         for (int i = 0; i < stages; i++) {
-                            if (!(ok = mbar_wait(full + 8 * ring.slot, ring.parity, waits) &&
-                                       mbar_wait(filled + 8 * ring.slot, uses >> ring.slot & 1u, waits)))
+                            if (!(ok = mbar_wait(full + 8 * ring.slot, ring.parity, &gave_up) &&
+                                       mbar_wait(filled + 8 * ring.slot, uses >> ring.slot & 1u, &gave_up)))
                                 break;
                             uses ^= 1u << ring.slot;
                             tc_fence_after();
@@ -316,7 +315,7 @@ serve_linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
                 if (S::accs > 1 && tile != first_tile) {
                     // A tile without adapters sends nothing that says the loading thread has seen so; and all four warps
                     // go on to the barriers below, or none.
-                    alive = alive && mbar_wait(taken, taken_parity, waits);
+                    alive = alive && mbar_wait(taken, taken_parity, &gave_up);
                     taken_parity ^= 1u;
                     if (!(alive = all_of_four(alive))) break;
                 }
@@ -364,7 +363,7 @@ serve_linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
                         lo[i] = *(const uint4 *)l;
                     }
                     for (int j = 0; j < stages; j++) {
-                        if (!(ok = mbar_wait(ready + 8 * ring.slot, uses >> ring.slot & 1u, waits))) break;
+                        if (!(ok = mbar_wait(ready + 8 * ring.slot, uses >> ring.slot & 1u, &gave_up))) break;
                         uses ^= 1u << ring.slot;
                         uint8_t *dst = smem + ring.slot * S::stage + kFeatures * 128;
                         const int32_t a = list[part + j / form.halves * split];
@@ -385,10 +384,10 @@ serve_linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
                     }
                 }
             }
-            ok = ok && mbar_wait(acc_full + 8 * acc.slot, acc.parity, waits);
+            ok = ok && mbar_wait(acc_full + 8 * acc.slot, acc.parity, &gave_up);
             if (!__all_sync(~0u, ok)) {
                 alive = false;                        // told to the other warps where they wait for this one
-                if (!LOW && d.adapters) continue;
+                if (S::accs > 1 && d.adapters) continue;
                 break;
             }
             tc_fence_after();
@@ -484,17 +483,22 @@ serve_linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
         cluster_wait();
     }
     __syncthreads();
-    if (gave_up) {                                    // (nobody sets it from here on)
-        if (tid == 0) drain_loads<S::stages>(full, issued);
-        if (warp == 1 && lane == 0) {
-            mma_commit(drained);
-            mbar_drain(drained, 0);
-        }
-        __syncthreads();
-    }
     tc_fence_after();
-    if (warp == 1) tmem_free(tmem, S::columns);
-    if (tid == 0 && gave_up) atomicExch(d.status, 1);
+    // (nobody sets gave_up from here on)
+    if (warp == 1) {
+        if (gave_up) {                                // what was issued ends before tensor memory is given up
+            if (lane == 0) {
+                mma_commit(drained);
+                mbar_drain(drained, 0);
+            }
+            __syncwarp();
+        }
+        tmem_free(tmem, S::columns);
+    }
+    if (tid == 0 && gave_up) {                        // and loads, before the block's memory is
+        drain_loads<S::stages>(full, issued);
+        atomicExch(d.status, 1);
+    }
 }
 
 int check_shape(const bcast_serve_linear_args &a)
@@ -648,7 +652,7 @@ int bcast_serve_linear(const bcast_serve_linear_args *a, void *cuda_stream)
     d.y = a->y;
     d.low = (float *)((char *)a->workspace + BCAST_SERVE_STATUS_BYTES);
     d.status = (int *)a->workspace;
-    d.wait_limit = wait_limit();
+    d.give_up = give_up_at_once();
     d.ys = a->y_stride;
     d.tokens = (int32_t)a->tokens;
     d.k = (int32_t)a->k;

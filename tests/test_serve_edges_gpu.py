@@ -355,14 +355,14 @@ print("END")
 """
 
 
-@pytest.mark.parametrize("limit,want", [("0", str(BCAST_ERR_TIMEOUT)), ("", "ok")])
-def test_waits_that_run_out_end_the_kernel_and_are_told(limit, want):
-    # With no polls allowed the kernels have given up from the start: what they still issue touches the block's own memory
-    # alone and is waited for, they come to their end and tell of it.
+@pytest.mark.parametrize("given_up,want", [("1", str(BCAST_ERR_TIMEOUT)), ("0", "ok"), ("", "ok")])
+def test_waits_that_run_out_end_the_kernel_and_are_told(given_up, want):
+    # The kernels have given up from the start: what they still issue touches the block's own memory alone and is waited
+    # for, they come to their end and tell of it.
     env = dict(os.environ)
-    env.pop("BCAST_SERVE_SPIN_LIMIT", None)
-    if limit:
-        env["BCAST_SERVE_SPIN_LIMIT"] = limit
+    env.pop("BCAST_SERVE_GIVE_UP", None)
+    if given_up:
+        env["BCAST_SERVE_GIVE_UP"] = given_up
     out = subprocess.run([sys.executable, "-c", WAITS_CHILD, ROOT], env=env, capture_output=True, text=True, timeout=300)
     assert out.returncode == 0, out.stderr[-2000:]
     assert out.stdout.split("\n") == [f"CALL {i} {want} ok" for i in range(6)] + ["END", ""], out.stdout
