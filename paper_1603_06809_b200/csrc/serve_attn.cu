@@ -726,14 +726,18 @@ serve_attn_prefix_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
         }
         // ---- the way out: a row's sums as they are, with what they were taken against
         if (mine > 0 && ok) ok = mbar_wait(o_full + 8 * w, 0, &gave_up);
-        // Both halves' products are done then, and what they read may be written over: a half waits for the other's too,
-        // unless that has none (one tile of tokens, of which half 1 has no part).
-        if (ok && (TWO || nt > 1)) ok = mbar_wait(o_full + 8 * (w ^ 1), 0, &gave_up);
+        // What is written now goes over the tiles that products read.  All of them are done where both halves' sums are.
+        // One tile of rows: products are issued in the order of the tiles of tokens, so after half 1's last only half 0's
+        // last can be under way, and the other way round.  Half 1 waits for that.  Half 0 need not: it is half 1's that is
+        // last where the tiles are even in number, and loads, taken K 0, K 1, V 0, K 2, V 1, ..., V n - 1, bring V n - 1 as
+        // number 2 n - 1 then, into the last of four stages, behind what half 0 writes.
+        if (ok && (TWO || (w == 1 && mine > 0))) ok = mbar_wait(o_full + 8 * (w ^ 1), 0, &gave_up);
         ok = __all_sync(~0u, ok);
         tc_fence_after();
         // Through shared memory, where the tiles were, and out row by row.
         constexpr int pitch = DB * 64 + 4;
         static_assert(8 * 32 * pitch * 4 <= (TWO ? 2 : 1) * stage + stages * stage);
+        static_assert(TWO || (stages == 4 && 128 * pitch * 4 <= stage + 3 * stage));     // half 0's, up to the last stage
         float *sums = (float *)smem + (w * 128 + quarter * 32) * pitch;       // this warp's rows
         if (busy && ok && mine > 0)
             for (int c = 0; c < columns; c += 16) {
