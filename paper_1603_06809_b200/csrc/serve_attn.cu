@@ -12,14 +12,15 @@
 //                   nobody else reads, so bound by reading them; warps take 16 tokens at a time through mma.sync.  A
 //                   short prefix goes with them, and the prefix kernel is left out.
 //   join kernel     the formula above, a block per row
-// What bounds them, and what they take on one B200 (bf16, 8 key/value heads of 128, 4 query heads to each):
-//   64 requests x 4 new tokens, prefix 65536, up to 1024 own: 250 us, 1.11 PFLOP/s.  A pair of 128-row tiles against
+// What bounds them, and what they take on one B200 (bf16, 8 key/value heads of 128, 4 query heads to each; time on the
+// device, in brackets that of a public call among others of its kind):
+//   64 requests x 4 new tokens, prefix 65536, up to 1024 own: 257 us, 1.08 PFLOP/s (300, the power cap).  A pair of 128-row tiles against
 //     128 tokens takes about 3050 cycles, where its products need 2048: a tile's softmax (about 2000 cycles, half
 //     of them on the exponentials) is longer than the other tile's products, and nothing is left to run under it
-//   32 requests x 1, prefix 8192, up to 700 own in pages: 34 us for 80 MB.  The prefix kernel takes 14 us of it (4 to
+//   32 requests x 1, prefix 8192, up to 700 own in pages: 36 us for 80 MB (37).  The prefix kernel takes 14 us of it (4 to
 //     its first scores, 5 for its four tiles, 3.5 for its sums), the own kernel 15 (latency: a block has 8 rounds
 //     of loads), the join 5
-//   one request, 8 heads of 64, 509 + 60 tokens: 7 us, two launches
+//   one request, 8 heads of 64, 509 + 60 tokens: 7 us, two launches (9.5)
 #include "serve_device.cuh"
 #include "serve_internal.h"
 #include "serve_tma.h"

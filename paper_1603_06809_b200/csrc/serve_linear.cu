@@ -13,11 +13,12 @@
 //                cores as the sum of two numbers of the data type, so that 16 or more bits of it count.
 // A block has one warp that loads tiles by TMA, one that issues the matrix instructions and four that fill
 // in u and bring accumulators from tensor memory to y.
-// What bounds it, and what it takes on one B200 (bf16, 4096 -> 4096): 8192 tokens of 16 requests, 8 adapters of rank
-// 64, 246 us, 1.15 PFLOP/s -- the product alone runs at 1.40 (a library's at 1.49), the rest is the low kernel,
-// which is not overlapped, and its 6 more stages of k to a tile; 64 tokens with 32 adapters of rank 16, 19 us for
-// 43 MB -- reading W takes until 10 us, then come u (1), eight stages of adapters (3) and the sum over the cluster
-// (3); one token, 2048 -> 2048, 10 us: two launches' latency.
+// What bounds it, and what it takes on one B200 (bf16, 4096 -> 4096; time on the device, in brackets that of a public
+// call among others of its kind): 8192 tokens of 16 requests, 8 adapters of rank 64, 254 us, 1.12 PFLOP/s (290, the
+// power cap) -- the product alone runs at 1.40 (a library's at 1.47), the rest is the low kernel, which is not
+// overlapped, and its 6 more stages of k to a tile; 64 tokens with 32 adapters of rank 16, 19 us for 43 MB (20.5) --
+// reading W takes until 10 us, then come u (1), eight stages of adapters (3) and the sum over the cluster (3); one
+// token, 2048 -> 2048, 10 us: two launches' latency (11.6).
 #include "serve_device.cuh"
 #include "serve_internal.h"
 #include "serve_tma.h"

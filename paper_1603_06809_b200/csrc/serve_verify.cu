@@ -7,8 +7,8 @@
 // the first draft that fails, and runs the race argmax w_v / e_v over that one row: a cluster of blocks per
 // request, joined through distributed shared memory.  Bound by memory and, close behind, by the unit for
 // exponentials: drafts + 1 rows of logits are read once, one row of logits a second time (from L2 where it is still
-// there), one of q and one of noise.  128 requests x 8 rows of 131072 bf16 logits take 88 us (the bytes at the
-// measured copy rate: 62), one request with 5 rows of 32000 8 us.  (One kernel for both, a cluster per request that
+// there), one of q and one of noise.  128 requests x 8 rows of 131072 bf16 logits take 89 us on the device (the
+// bytes at the measured copy rate: 62), one request with 5 rows of 32000 9 us; public calls among others 94 and 10.5.  (One kernel for both, a cluster per request that
 // takes its rows one after the other, was slower everywhere: 105 and 15 us.)
 #include "serve_device.cuh"
 #include "serve_internal.h"
