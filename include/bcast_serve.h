@@ -6,14 +6,21 @@
  * the cache of a prompt that all requests start with, the next thing a replica does is answer
  * requests, and the rule of the tuned ring -- do not move again what the receiver already holds --
  * carries over: what all requests share is read once for all of them, and only what is a request's
- * own is added per request.  Three operators, one decode step's worth:
+ * own is added per request.  The operators of a decode step, in the order of their use:
  *
  *   bcast_serve_linear   a projection that all tokens share, plus the low-rank adapter of each
  *                        token's request
+ *   bcast_serve_linear4  the same without adapters, the weights in 4 bits: a message a quarter as
+ *                        long.  bcast_serve_pack4 makes such weights before the broadcast,
+ *                        bcast_serve_unpack4 makes numbers of them again
+ *   bcast_serve_append   new tokens' queries and keys normed and rotated, keys and values put into
+ *                        the requests' caches
  *   bcast_serve_attn     attention of the newest tokens of every request over a prefix that all
  *                        requests share, followed by the request's own tokens
  *   bcast_serve_verify   acceptance of drafted tokens against the target's probabilities from given
  *                        random numbers, and the choice of the token that follows them
+ *   bcast_serve_logprobs log probabilities of given tokens, the rows' entropy, and their most
+ *                        probable tokens
  *
  * They go forward only: what they compute has no backward pass here.
  *
@@ -28,8 +35,8 @@
  *     What only the device knows (adapter numbers, lengths, page numbers, token numbers) cannot be
  *     refused; each operator says what it makes of values out of range.  None of them leads to an
  *     access outside the arrays described.
- *   - Inputs may not overlap outputs or the workspace.
- *   - Workspace: scratch of at least bcast_serve_*_workspace() bytes, 256-byte aligned.  Its first
+ *   - Inputs may not overlap outputs or the workspace, unless an operator says so.
+ *   - Workspace (where a call has one): scratch of at least bcast_serve_*_workspace() bytes, 256-byte aligned.  Its first
  *     BCAST_SERVE_STATUS_BYTES hold the status word and must have been zeroed once, before the first
  *     call; nothing else in it has to be initialised, and nothing in it is kept from one call for the
  *     next.  Calls that share a workspace must be ordered on the GPU (one stream, or events); calls
@@ -179,6 +186,136 @@ typedef struct bcast_serve_verify_args {
 
 int bcast_serve_verify(const bcast_serve_verify_args *args /* HOST */, void *cuda_stream);
 int64_t bcast_serve_verify_workspace(const bcast_serve_verify_args *args);
+
+/*
+ * bcast_serve_append -- the newest tokens of every request on their way from a projection to
+ * bcast_serve_attn.  For request b, new token i < new_tokens (own_len as in bcast_serve_attn: the own
+ * tokens in the cache, the new ones among them):
+ *     slot = own_len[b] - new_tokens + i
+ *     out[b][i][h]        = R(norm(q[b][i][h]) * q_norm)         for every query head
+ *     own_k at slot, head = R(norm(k[b][i][h]) * k_norm),   own_v at slot, head = v[b][i][h]
+ * with norm(x) = x / sqrt(mean(x^2) + eps) where norm weights are given, and x itself where not.
+ * R turns the pairs of the first `rot` numbers of a head, pair p = 0..rot/2-1 being (p, p + rot/2), or
+ * (2p, 2p + 1) where `interleaved`: (x, y) -> (x cos t - y sin t, x sin t + y cos t),
+ *     t = position * inv_freq[p],  position = first + slot, or positions[b][i][axis[p]] where given.
+ * The angle is reduced exactly, however far the position.  Arithmetic is in 32 bits, results are rounded
+ * once; what is neither normed nor rotated is copied bit for bit.
+ *   - A token is padding if i < new_tokens - new_len[b] (where new_len is given: a request with fewer new tokens
+ *     has them at the end), or if its slot is negative.  Padding goes nowhere, and its rows of out are zero.
+ *   - Keys and values whose slot is not below own_cap, or whose page is outside 0..num_pages-1, are not
+ *     stored; their queries are still written.  Nothing else of the caches is touched.
+ *   - Where two tokens of a call have the same place (a page that stands in the table twice), either may
+ *     stay.
+ *   - An axis outside 0..axes-1 is taken as 0.  inv_freq is finite.
+ *   dtype        BCAST_SERVE_BF16 or BCAST_SERVE_FP16: q, k, v, q_norm, k_norm, out and the caches
+ *   0 <= batch, new_tokens <= 65535, at most 2^24 tokens and 2^31 - 1 heads of them in all;  0 <= q_heads <= 65535, 1 <= kv_heads
+ *   <= 1024;  dim a multiple of 8, 8..128;  rot a multiple of 16, 0..dim (0: no rotation; inv_freq, axis and positions are then not
+ *   looked at);  0 <= first < 2^31;  0 <= own_cap < 2^31 - 65536;  0 <= axes <= 16 (0: by slot)
+ *   q, out       [batch][new_tokens][q_heads][dim] (not looked at if q_heads = 0); out may be q itself
+ *   k, v         [batch][new_tokens][kv_heads][dim]; strides of the first three
+ *   q_norm, k_norm  NULL or [dim] each;  eps >= 0
+ *   inv_freq     [rot / 2] float
+ *   positions    [batch][new_tokens][axes] int32 if axes > 0, strides of the first two;  axis [rot / 2] int32, or NULL
+ *                for axis 0 throughout
+ *   own_k/_v, page_table, page_size, num_pages   as in bcast_serve_attn
+ *   own_len [batch] int32, new_len NULL or [batch] int32
+ * q, k, v, out, the norms and the caches start on 16-byte boundaries and their strides are multiples of 8; strides of
+ * out and the caches are at least dim, those of q, k and v may be 0.
+ */
+typedef struct bcast_serve_append_args {
+    int32_t dtype, batch, new_tokens, q_heads, kv_heads, dim, page_size, rot, interleaved, axes;
+    float eps;
+    int64_t own_cap, num_pages, first;
+    const void *q, *k, *v, *q_norm, *k_norm;
+    const float *inv_freq;
+    const int32_t *positions, *axis, *own_len, *new_len, *page_table;
+    void *out, *own_k, *own_v;
+    int64_t q_stride[3], k_stride[3], v_stride[3], out_stride[3], own_k_stride[3], own_v_stride[3], positions_stride[2];
+    int64_t page_table_stride;
+} bcast_serve_append_args;
+
+int bcast_serve_append(const bcast_serve_append_args *args /* HOST */, void *cuda_stream);
+
+/*
+ * bcast_serve_logprobs -- for every row of logits l, with p = softmax(l):
+ *     logprobs[r]     = log p(tokens[r])
+ *     entropy[r]      = -sum p log p
+ *     top_tokens[r]   = the `top` tokens with the largest logits, the lower number first among equals
+ *     top_logprobs[r] = their log p
+ * Statistics are held in 32 bits, the logits read once (a few of them twice).
+ *   - A logit that is NaN counts as -infinity; where some are +infinity, these share the probability evenly.
+ *     Tokens that so have no probability, and those outside 0..vocab-1, have -infinity as their log p.  They are no
+ *     alternatives: where there are fewer than `top` others, the row goes on with token -1 and -infinity.  A row
+ *     without any logit above -infinity has the entropy 0.
+ *   dtype     of logits: BCAST_SERVE_BF16, BCAST_SERVE_FP16 or BCAST_SERVE_FP32
+ *   0 <= rows < 2^24;  1 <= vocab < 2^31 - 65536;  0 <= top <= 32
+ *   logits    [rows][vocab], rows at logits_stride (which may be 0)
+ *   tokens    [rows] int32;  logprobs [rows] float
+ *   entropy   NULL or [rows] float
+ *   top_tokens [rows][top] int32, top_logprobs [rows][top] float (not looked at if top = 0)
+ */
+typedef struct bcast_serve_logprobs_args {
+    int32_t dtype, top;
+    int64_t rows, vocab;
+    const void *logits;
+    const int32_t *tokens;
+    float *logprobs, *entropy, *top_logprobs;
+    int32_t *top_tokens;
+    int64_t logits_stride;
+} bcast_serve_logprobs_args;
+
+int bcast_serve_logprobs(const bcast_serve_logprobs_args *args /* HOST */, void *cuda_stream);
+
+/*
+ * Microscaled 4-bit numbers: 32 neighbours of a row share a power of two.
+ *   codes   [rows][k / 2] bytes, rows at codes_stride (bytes): number 2j in the low half of byte j.  A code is a
+ *           sign and one of 0, 1/2, 1, 3/2, 2, 3, 4, 6.
+ *   scales  a byte e per block, which stands for 2^(e - 127); 255: the block's numbers are NaN.  They lie in tiles
+ *           of 128 rows x 4 blocks, [ceil(rows / 128)][ceil(k / 128)][32][4][4] bytes: block c of row r at
+ *           [r / 128][c / 4][r % 32][r % 128 / 32][c % 4].  Places that stand for no block are zero.
+ *
+ * bcast_serve_pack4 -- values to codes and scales.  e is the largest magnitude's exponent less 2 (so that it
+ * becomes 4 to 8), at least 0; a number divided by 2^(e - 127) goes to the nearest code, to the even one of two as near,
+ * and to 6 above that.  A block with NaN or an infinity in it becomes NaN.
+ * bcast_serve_unpack4 -- codes and scales to values, rounded once to the data type.
+ *   dtype   of values: BCAST_SERVE_BF16, BCAST_SERVE_FP16 or BCAST_SERVE_FP32
+ *   0 <= rows < 2^31 - 65536;  k a multiple of 32, 32..2^24
+ *   values  [rows][k], rows at values_stride: at least k, a multiple of 8; starts on a 16-byte boundary
+ *   codes_stride at least k / 2, a multiple of 16; codes and scales start on 16-byte boundaries
+ */
+typedef struct bcast_serve_pack4_args {
+    int32_t dtype;
+    int64_t rows, k;
+    void *values;              /* pack4: read only */
+    uint8_t *codes, *scales;   /* unpack4: read only */
+    int64_t values_stride, codes_stride;
+} bcast_serve_pack4_args;
+
+int bcast_serve_pack4(const bcast_serve_pack4_args *args /* HOST */, void *cuda_stream);
+int bcast_serve_unpack4(const bcast_serve_pack4_args *args /* HOST */, void *cuda_stream);
+
+/*
+ * bcast_serve_linear4 -- y[t] = W x4[t] + bias: W in microscaled 4-bit numbers as bcast_serve_pack4 makes
+ * them, x4[t] what pack4 makes of x[t].  Sums are held in 32 bits, y is rounded once.  A block of x[t] with NaN or an
+ * infinity in it makes y[t] NaN, a block of W that is NaN its feature.
+ *   dtype        BCAST_SERVE_BF16 or BCAST_SERVE_FP16: x, bias and y
+ *   tokens       0 <= T <= 2^21;  k a multiple of 32, 32..2^24;  1 <= n <= 2^24
+ *   x [T][k], y [T][n]: rows at x_stride (a multiple of 8), y_stride;  bias [n] or NULL
+ *   codes, codes_stride, scales: of W [n][k], as above
+ */
+typedef struct bcast_serve_linear4_args {
+    int32_t dtype;
+    int64_t tokens, k, n;
+    const void *x, *bias;
+    const uint8_t *codes, *scales;
+    void *y;
+    int64_t x_stride, codes_stride, y_stride;
+    void *workspace;
+    uint64_t workspace_bytes;
+} bcast_serve_linear4_args;
+
+int bcast_serve_linear4(const bcast_serve_linear4_args *args /* HOST */, void *cuda_stream);
+int64_t bcast_serve_linear4_workspace(const bcast_serve_linear4_args *args);
 
 /*
  * bcast_serve_status -- did a kernel that used this workspace give up on a bounded wait?  Reads the

@@ -120,6 +120,14 @@ Tensor output(const Maybe &out, const char *name, at::IntArrayRef shape, at::Sca
     return *out;
 }
 
+// How a call that was made ended.
+py::tuple ended(int code, py::object outputs)
+{
+    if (code) return py::make_tuple(code, "", false);
+    // (asked of the stream of `place`, which is the current one here)
+    return py::make_tuple(code, std::move(outputs), c10::cuda::currentStreamCaptureStatusMayInitCtx() != c10::cuda::CaptureStatus::None);
+}
+
 // The call itself; BCAST_ERR_CAPACITY comes back with the bytes that are needed.
 template <typename Args>
 py::tuple finish(int (*call)(const Args *, void *), int64_t (*size)(const Args *), const Args &a, const Place &place, py::object outputs)
@@ -127,9 +135,7 @@ py::tuple finish(int (*call)(const Args *, void *), int64_t (*size)(const Args *
     int64_t bytes = size(&a);
     int code = bytes < 0 ? (int)bytes : (uint64_t)bytes > a.workspace_bytes ? BCAST_ERR_CAPACITY : call(&a, place.stream.stream());
     if (code == BCAST_ERR_CAPACITY) return py::make_tuple(code, bytes, false);
-    if (code) return py::make_tuple(code, "", false);
-    // (asked of the stream of `place`, which is the current one here)
-    return py::make_tuple(code, std::move(outputs), c10::cuda::currentStreamCaptureStatusMayInitCtx() != c10::cuda::CaptureStatus::None);
+    return ended(code, std::move(outputs));
 }
 
 template <typename F>
@@ -292,6 +298,220 @@ py::tuple verify(const Tensor &logits, const Tensor &draft_probs, const Tensor &
     });
 }
 
+py::object or_none(const Maybe &t) { return t ? py::cast(*t) : py::none(); }
+
+py::tuple append(const Maybe &q, const Tensor &k, const Tensor &v, const Tensor &own_k, const Tensor &own_v, const Tensor &own_len,
+                 const Maybe &page_table, const Maybe &new_len, int64_t first, const Maybe &positions, const Maybe &inv_freq, const Maybe &axis,
+                 bool interleaved, const Maybe &q_norm, const Maybe &k_norm, double eps, const Maybe &out, int64_t raw)
+{
+    return guarded([&] {
+        need(k.dim() == 4 && own_k.dim() == 4 && (!q || q->dim() == 4), "q, k and own_k have four dimensions");
+        bcast_serve_append_args a = {};
+        a.dtype = dtype_of(k, false);
+        const auto type = k.scalar_type();
+        const at::Device dev = k.device();
+        const int64_t B = k.size(0), n = k.size(1), H = k.size(2), D = k.size(3), HQ = q ? q->size(2) : 0;
+        need(std::max({B, n, HQ, D, H}) < (1 << 30), "k is too large");
+        if (q) expect(*q, "q", type, {B, n, HQ, D}, dev);
+        expect(k, "k", type, k.sizes(), dev);
+        expect(v, "v", type, k.sizes(), dev);
+        const int64_t own = page_table ? own_k.size(0) : B, each = own_k.size(1);
+        expect(own_k, "own_k", type, {own, each, H, D}, dev);
+        expect(own_v, "own_v", type, {own, each, H, D}, dev);
+        expect(own_len, "own_len", at::kInt, {B}, dev);
+        need(own_len.is_contiguous() && (!new_len || new_len->is_contiguous()), "own_len and new_len are contiguous");
+        a.own_cap = each;
+        if (page_table) {
+            need(page_table->dim() == 2 && each >= 1 && each < (1 << 30), "page_table has two dimensions, a page at least one token");
+            expect(*page_table, "page_table", at::kInt, {B, page_table->size(1)}, dev);
+            a.page_size = (int32_t)each;
+            a.num_pages = own;
+            a.own_cap = each * page_table->size(1);
+            strides(*page_table, 1, &a.page_table_stride);
+        }
+        if (new_len) expect(*new_len, "new_len", at::kInt, {B}, dev);
+        if (q_norm) expect(*q_norm, "q_norm", type, {D}, dev);
+        if (k_norm) expect(*k_norm, "k_norm", type, {D}, dev);
+        need(inv_freq.has_value() || !(positions || axis), "positions and axis go with inv_freq");
+        need(positions.has_value() || !axis, "axis goes with positions");
+        if (inv_freq) {
+            need(inv_freq->dim() == 1 && inv_freq->size(0) <= 64, "inv_freq has one dimension and at most 64 entries");
+            expect(*inv_freq, "inv_freq", at::kFloat, inv_freq->sizes(), dev);
+            a.rot = 2 * (int32_t)inv_freq->size(0);
+        }
+        if (positions) {
+            need(positions->dim() == 2 || positions->dim() == 3, "positions has two dimensions or three");
+            const int64_t axes = positions->dim() == 3 ? positions->size(2) : 1;
+            need(axes >= 1 && axes <= 16, "positions has 1 to 16 axes");
+            if (positions->dim() == 3) {
+                expect(*positions, "positions", at::kInt, {B, n, axes}, dev);
+            } else {
+                // its last dimension is that of the tokens, and taken with its stride
+                need(positions->scalar_type() == at::kInt && positions->sizes() == at::IntArrayRef({B, n}) && positions->device() == dev,
+                     "positions is [batch, new tokens] or [batch, new tokens, axes], int32, where the other tensors are");
+            }
+            if (axis) {
+                expect(*axis, "axis", at::kInt, {a.rot / 2}, dev);
+            }
+            a.axes = (int32_t)axes;
+            a.positions_stride[0] = positions->stride(0);
+            a.positions_stride[1] = positions->stride(1);
+            for (int i = 0; i < 2; i++)
+                if (positions->size(i) == 1) a.positions_stride[i] = 0;
+        }
+        const Place place(k, raw);
+        place.use({given(q), &k, &v, &own_k, &own_v, &own_len, given(page_table), given(new_len), given(positions), given(inv_freq), given(axis),
+                   given(q_norm), given(k_norm), given(out)});
+        need(q.has_value() || !out, "out goes with q");
+        Maybe o;
+        if (q) o = output(out, "out", q->sizes(), type, dev);
+        a.batch = (int32_t)B;
+        a.new_tokens = (int32_t)n;
+        a.q_heads = (int32_t)HQ;
+        a.kv_heads = (int32_t)H;
+        a.dim = (int32_t)D;
+        a.interleaved = interleaved;
+        a.eps = (float)eps;
+        a.first = first;
+        a.q = pointer(q);
+        a.k = k.data_ptr();
+        a.v = v.data_ptr();
+        a.q_norm = pointer(q_norm);
+        a.k_norm = pointer(k_norm);
+        a.inv_freq = (const float *)pointer(inv_freq);
+        a.positions = (const int32_t *)pointer(positions);
+        a.axis = (const int32_t *)pointer(axis);
+        a.own_len = (const int32_t *)own_len.data_ptr();
+        a.new_len = (const int32_t *)pointer(new_len);
+        a.page_table = (const int32_t *)pointer(page_table);
+        a.out = o ? o->data_ptr() : nullptr;
+        a.own_k = own_k.data_ptr();
+        a.own_v = own_v.data_ptr();
+        if (q) {
+            strides(*q, 3, a.q_stride);
+            strides(*o, 3, a.out_stride);
+        }
+        strides(k, 3, a.k_stride);
+        strides(v, 3, a.v_stride);
+        strides(own_k, 3, a.own_k_stride);
+        strides(own_v, 3, a.own_v_stride);
+        return ended(bcast_serve_append(&a, place.stream.stream()), or_none(o));
+    });
+}
+
+py::tuple logprobs(const Tensor &logits, const Tensor &tokens, int64_t top, const Maybe &logprobs, const Maybe &entropy, const Maybe &top_tokens,
+                   const Maybe &top_logprobs, int64_t raw)
+{
+    return guarded([&] {
+        need(logits.dim() == 2, "logits has two dimensions");
+        bcast_serve_logprobs_args a = {};
+        a.dtype = dtype_of(logits, true);
+        const at::Device dev = logits.device();
+        const int64_t T = logits.size(0), V = logits.size(1);
+        need(top >= 0 && top <= 32, "top is 0 to 32");
+        expect(logits, "logits", logits.scalar_type(), logits.sizes(), dev);
+        expect(tokens, "tokens", at::kInt, {T}, dev);
+        const Place place(logits, raw);
+        place.use({&logits, &tokens, given(logprobs), given(entropy), given(top_tokens), given(top_logprobs)});
+        const Tensor lp = output(logprobs, "logprobs", {T}, at::kFloat, dev), h = output(entropy, "entropy", {T}, at::kFloat, dev),
+                     x = output(top_tokens, "top_tokens", {T, top}, at::kInt, dev), l = output(top_logprobs, "top_logprobs", {T, top}, at::kFloat, dev);
+        need(tokens.is_contiguous() && lp.is_contiguous() && h.is_contiguous() && x.is_contiguous() && l.is_contiguous(), "tokens and results are contiguous");
+        a.rows = T;
+        a.vocab = V;
+        a.top = (int32_t)top;
+        a.logits = logits.data_ptr();
+        a.tokens = (const int32_t *)tokens.data_ptr();
+        a.logprobs = (float *)lp.data_ptr();
+        a.entropy = (float *)h.data_ptr();
+        a.top_tokens = (int32_t *)x.data_ptr();
+        a.top_logprobs = (float *)l.data_ptr();
+        strides(logits, 1, &a.logits_stride);
+        return ended(bcast_serve_logprobs(&a, place.stream.stream()), py::make_tuple(lp, h, x, l));
+    });
+}
+
+// The shape of the scales of `rows` rows of `k` numbers.
+std::vector<int64_t> scales_shape(int64_t rows, int64_t k) { return {(rows + 127) / 128, (k + 127) / 128, 32, 4, 4}; }
+
+py::tuple pack4(const Tensor &x, const Maybe &codes, const Maybe &scales, int64_t raw)
+{
+    return guarded([&] {
+        need(x.dim() == 2, "x has two dimensions");
+        bcast_serve_pack4_args a = {};
+        a.dtype = dtype_of(x, true);
+        const at::Device dev = x.device();
+        a.rows = x.size(0);
+        a.k = x.size(1);
+        expect(x, "x", x.scalar_type(), x.sizes(), dev);
+        const Place place(x, raw);
+        place.use({&x, given(codes), given(scales)});
+        const Tensor c = output(codes, "codes", {a.rows, a.k / 2}, at::kByte, dev), s = output(scales, "scales", scales_shape(a.rows, a.k), at::kByte, dev);
+        need(s.is_contiguous(), "scales is contiguous");
+        a.values = x.data_ptr();
+        a.codes = (uint8_t *)c.data_ptr();
+        a.scales = (uint8_t *)s.data_ptr();
+        strides(x, 1, &a.values_stride);
+        strides(c, 1, &a.codes_stride);
+        return ended(bcast_serve_pack4(&a, place.stream.stream()), py::make_tuple(c, s));
+    });
+}
+
+py::tuple unpack4(const Tensor &codes, const Tensor &scales, at::ScalarType type, const Maybe &out, int64_t raw)
+{
+    return guarded([&] {
+        need(codes.dim() == 2, "codes has two dimensions");
+        const at::Device dev = codes.device();
+        bcast_serve_pack4_args a = {};
+        a.rows = codes.size(0);
+        a.k = codes.size(1) * 2;
+        expect(codes, "codes", at::kByte, codes.sizes(), dev);
+        expect(scales, "scales", at::kByte, scales_shape(a.rows, a.k), dev);
+        need(scales.is_contiguous(), "scales is contiguous");
+        const Place place(codes, raw);
+        place.use({&codes, &scales, given(out)});
+        const Tensor x = output(out, "out", {a.rows, a.k}, type, dev);
+        a.dtype = dtype_of(x, true);
+        a.values = x.data_ptr();
+        a.codes = (uint8_t *)codes.data_ptr();
+        a.scales = (uint8_t *)scales.data_ptr();
+        strides(x, 1, &a.values_stride);
+        strides(codes, 1, &a.codes_stride);
+        return ended(bcast_serve_unpack4(&a, place.stream.stream()), py::cast(x));
+    });
+}
+
+py::tuple linear4(const Tensor &x, const Tensor &codes, const Tensor &scales, const Maybe &bias, const Maybe &out, const Maybe &ws, int64_t ws_of, int64_t raw)
+{
+    return guarded([&] {
+        need(x.dim() == 2 && codes.dim() == 2, "x and codes have two dimensions");
+        bcast_serve_linear4_args a = {};
+        a.dtype = dtype_of(x, false);
+        const auto type = x.scalar_type();
+        const at::Device dev = x.device();
+        a.tokens = x.size(0);
+        a.k = x.size(1);
+        a.n = codes.size(0);
+        expect(x, "x", type, x.sizes(), dev);
+        expect(codes, "codes", at::kByte, {a.n, a.k / 2}, dev);
+        expect(scales, "scales", at::kByte, scales_shape(a.n, a.k), dev);
+        need(scales.is_contiguous(), "scales is contiguous");
+        if (bias) expect(*bias, "bias", type, {a.n}, dev);
+        const Place place(x, raw);
+        place.use({&x, &codes, &scales, given(bias), given(out)});
+        const Tensor y = output(out, "out", {a.tokens, a.n}, type, dev);
+        a.x = x.data_ptr();
+        a.bias = pointer(bias);
+        a.codes = (const uint8_t *)codes.data_ptr();
+        a.scales = (const uint8_t *)scales.data_ptr();
+        a.y = y.data_ptr();
+        strides(x, 1, &a.x_stride);
+        strides(codes, 1, &a.codes_stride);
+        strides(y, 1, &a.y_stride);
+        place.use(a, ws, ws_of);
+        return finish(bcast_serve_linear4, bcast_serve_linear4_workspace, a, place, py::cast(y));
+    });
+}
+
 }  // namespace
 
 PYBIND11_MODULE(_serve_native, m)
@@ -299,6 +519,11 @@ PYBIND11_MODULE(_serve_native, m)
     m.def("linear", &linear);
     m.def("attn", &attn);
     m.def("verify", &verify);
+    m.def("append", &append);
+    m.def("logprobs", &logprobs);
+    m.def("pack4", &pack4);
+    m.def("unpack4", &unpack4);
+    m.def("linear4", &linear4);
     m.def("strides", [](const Tensor &t, int n) {
         std::vector<int64_t> s((size_t)std::max(n, 0));
         strides(t, n, s.data());

@@ -1,0 +1,636 @@
+// Microscaled 4-bit numbers: bcast_serve_pack4, bcast_serve_unpack4, and bcast_serve_linear4, the projection whose
+// weights are held so.
+//
+//   block of 32 along k:  e = max(exponent of its largest magnitude - 2, -127),  code = e2m1(x / 2^e),  x ~ code * 2^e
+//   y[t][f] = sum over blocks  2^(eW + ex) * (sum of 32 products of codes)  + bias
+// The tensor cores take both operands as they lie (kind::mxf4: 64 values of k to an instruction, a scale to every 32 of
+// a row), so W is read once, in 17/32 of a byte a number, and nothing is unpacked on the way.
+//   pack kernel     x to codes and scales, four lanes to a block: the call's own x first, in the workspace
+//   product kernel  tiles of 128 features x NT tokens as in bcast_serve_linear: features on the 128 lanes of tensor memory,
+//                   tokens the instruction's N.  A stage is 256 values of k: codes by TMA, rows of 128 bytes, and scales,
+//                   which are laid out so that a stage's are one run of memory, by bulk copies; tcgen05.cp brings
+//                   them to tensor memory, where the instruction wants them
+#include "serve_device.cuh"
+#include "serve_internal.h"
+#include "serve_tma.h"
+
+#include <cooperative_groups.h>
+
+namespace cg = cooperative_groups;
+
+namespace bcast_serve {
+namespace {
+
+constexpr int kBlock = 32;                // numbers that share a scale
+constexpr int kAtom = 512;                // bytes of the scales of 128 rows x 4 blocks
+
+// ------------------------------------------------------------------------------------------- to 4 bits and back
+constexpr int kPackThreads = 256, kPackRows = 4;      // rows of a thread, whose loads are under way together
+
+// Rows of codes, and scales in tiles of `tile` rows of `atoms` x 128 places each, of which each four blocks along k lie
+// together: tile r / tile, then block / 4, then the atom.  (Of weights: tile = 128, one atom.)
+struct PackDev {
+    void *values;
+    uint8_t *codes, *scales;
+    int64_t vs, cs, rows, tiles_k;        // tiles_k: of four blocks, to a row
+    int32_t k, tile, atoms, segments;     // segments: blocks of threads to a row
+    int64_t padded;                       // rows that have a place among the scales, up to which zeros are written
+};
+
+__device__ __forceinline__ int64_t scale_at(const PackDev &d, int64_t row, int32_t block)
+{
+    const int64_t tile = row / d.tile;
+    const int r = (int)(row - tile * d.tile);
+    return ((tile * d.tiles_k + block / 4) * d.atoms + r / 128) * kAtom + r % 32 * 16 + r % 128 / 32 * 4 + block % 4;
+}
+
+// The scale's byte from the largest magnitude's bits: its exponent field less 2; 255 for what is not finite.
+__device__ __forceinline__ uint32_t scale_of(uint32_t most) { return most >= 0x7f800000u ? 255u : (uint32_t)max((int)(most >> 23) - 2, 0); }
+// What a block's numbers are multiplied by before they are rounded: 2^(127 - e).
+__device__ __forceinline__ float inverse_of(uint32_t e) { return __uint_as_float(e == 255 ? 0u : (254u - e) << 23); }
+// The number a scale's byte stands for: 2^(e - 127).
+__device__ __forceinline__ float power_of(uint32_t e) { return __uint_as_float(e == 255 ? 0x7fc00000u : e ? e << 23 : 0x00400000u); }
+
+// Eight numbers to codes, the first in the lowest bits: to nearest, to the even code of two as near, 6 at most.
+__device__ __forceinline__ uint32_t codes_of(const float *x)
+{
+    uint32_t r;
+    asm("{\n\t.reg .b8 a, b, c, d;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\t"
+        "mov.b32 %0, {a, b, c, d};\n\t}"
+        : "=r"(r) : "f"(x[0]), "f"(x[1]), "f"(x[2]), "f"(x[3]), "f"(x[4]), "f"(x[5]), "f"(x[6]), "f"(x[7]));
+    return r;
+}
+__device__ __forceinline__ void numbers_of(uint32_t codes, float *x)
+{
+    uint32_t h[4];
+    asm("{\n\t.reg .b8 a, b, c, d;\n\tmov.b32 {a, b, c, d}, %4;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %0, a;\n\tcvt.rn.f16x2.e2m1x2 %1, b;\n\tcvt.rn.f16x2.e2m1x2 %2, c;\n\tcvt.rn.f16x2.e2m1x2 %3, d;\n\t}"
+        : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3]) : "r"(codes));
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        const float2 v = __half22float2(*(const __half2 *)&h[i]);
+        x[2 * i] = v.x;
+        x[2 * i + 1] = v.y;
+    }
+}
+
+template <typename T> struct Eight {
+    uint4 v[sizeof(T) / 2];
+};
+template <typename T>
+__device__ __forceinline__ void widen8(const Eight<T> &raw, float *x)
+{
+    const T *v = (const T *)&raw;
+#pragma unroll
+    for (int i = 0; i < 8; i++) x[i] = to_f32(v[i]);
+}
+
+// A block of the row's eights, to codes; four neighbouring lanes hold a block of 32, sixteen a scale tile's four.
+template <typename T>
+__global__ void __launch_bounds__(kPackThreads)
+serve_pack4_kernel(const __grid_constant__ PackDev d)
+{
+    const int segment = blockIdx.x % d.segments, eight = segment * kPackThreads + threadIdx.x;
+    const int64_t row0 = (int64_t)(blockIdx.x / d.segments) * kPackRows;
+    const int lane = threadIdx.x % 32;
+    const bool in = eight * 8 < d.k;
+    launch_next();
+    Eight<T> raw[kPackRows];
+#pragma unroll
+    for (int r = 0; r < kPackRows; r++) {
+        const uint4 *src = (const uint4 *)((const T *)d.values + (row0 + r) * d.vs + (int64_t)eight * 8);
+#pragma unroll
+        for (int i = 0; i < (int)(sizeof(T) / 2); i++) raw[r].v[i] = in && row0 + r < d.rows ? __ldg(src + i) : make_uint4(0, 0, 0, 0);
+    }
+#pragma unroll
+    for (int r = 0; r < kPackRows; r++) {
+        const int64_t row = row0 + r;
+        float x[8];
+        widen8<T>(raw[r], x);
+        uint32_t most = 0;                    // of the magnitudes' bits: NaN is the largest
+#pragma unroll
+        for (int i = 0; i < 8; i++) most = max(most, __float_as_uint(x[i]) & 0x7fffffffu);
+        most = max(most, __shfl_xor_sync(~0u, most, 1));
+        most = max(most, __shfl_xor_sync(~0u, most, 2));
+        const uint32_t e = scale_of(most);
+        const float by = inverse_of(e);
+#pragma unroll
+        for (int i = 0; i < 8; i++) x[i] *= by;
+        if (in && row < d.rows) *(uint32_t *)(d.codes + row * d.cs + (int64_t)eight * 4) = e == 255 ? 0u : codes_of(x);
+        uint32_t four = e | __shfl_down_sync(~0u, e, 4) << 8;
+        four |= __shfl_down_sync(~0u, four, 8) << 16;
+        // (what is past k read as zeros, whose scale is 0)
+        if (lane % 16 == 0 && in && row < d.padded) *(uint32_t *)(d.scales + scale_at(d, row, eight / 4)) = four;
+    }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kPackThreads)
+serve_unpack4_kernel(const __grid_constant__ PackDev d)
+{
+    const int segment = blockIdx.x % d.segments, eight = segment * kPackThreads + threadIdx.x;
+    const int64_t row0 = (int64_t)(blockIdx.x / d.segments) * kPackRows;
+    if (eight * 8 >= d.k) return;
+    uint32_t codes[kPackRows], e[kPackRows];
+#pragma unroll
+    for (int r = 0; r < kPackRows; r++) {
+        const bool in = row0 + r < d.rows;
+        codes[r] = in ? __ldg((const uint32_t *)(d.codes + (row0 + r) * d.cs + (int64_t)eight * 4)) : 0u;
+        e[r] = in ? __ldg(d.scales + scale_at(d, row0 + r, eight / 4)) : 0u;
+    }
+#pragma unroll
+    for (int r = 0; r < kPackRows; r++) {
+        if (row0 + r >= d.rows) break;
+        float x[8];
+        numbers_of(codes[r], x);
+        const float by = power_of(e[r]);
+        Eight<T> raw;
+#pragma unroll
+        for (int i = 0; i < 8; i++) ((T *)&raw)[i] = from_f32<T>(x[i] * by);
+        uint4 *dst = (uint4 *)((T *)d.values + (row0 + r) * d.vs + (int64_t)eight * 8);
+#pragma unroll
+        for (int i = 0; i < (int)(sizeof(T) / 2); i++) dst[i] = raw.v[i];
+    }
+}
+
+// ------------------------------------------------------------------------------------------- product
+constexpr int kFeatures = 128;            // features per tile: the lanes of tensor memory
+constexpr int kDepth = 256;               // values of k per stage: 128 bytes of codes, one swizzled row
+constexpr int kProductThreads = 192;
+constexpr int kMaxSplit = 8;              // blocks of a cluster that share one tile's k
+
+template <int NT> struct Tile {
+    static constexpr int atoms = (NT + 127) / 128;                 // of the tokens' scales
+    static constexpr int codes_w = kFeatures * 128, codes_x = NT * 128, scales_w = 2 * kAtom, scales_x = 2 * atoms * kAtom;
+    static constexpr int stage = codes_w + codes_x + scales_w + scales_x;
+    static constexpr int stages = NT > 128 ? 4 : NT == 128 ? 3 : 4;
+    static constexpr int accs = NT > 128 ? 2 : 1;                  // accumulators: a second one where blocks are persistent
+    static constexpr int at_w = accs * NT, at_x = at_w + 8;        // tensor memory's columns of scales
+    static constexpr int used = at_x + 8 * atoms;
+    static constexpr int columns = used <= 64 ? 64 : used <= 128 ? 128 : used <= 256 ? 256 : 512;
+    static constexpr size_t smem = (size_t)stage * stages + 1024;  // + alignment
+    static_assert(stage % 1024 == 0 && used <= columns, "");
+    static_assert(accs > 1 || NT * kFeatures * 4 <= stage * stages, "partial sums take the stages' place");
+};
+
+struct ProductDev {
+    const void *bias;
+    const uint8_t *scales_w, *scales_x;
+    void *y;
+    int *status;
+    int give_up;                          // 1: begin as if a wait had run out
+    int64_t ys, tiles_k;
+    int32_t tokens, k, n, f_tiles, t_tiles;
+};
+
+// Sixteen bytes and more, both ends on 16-byte boundaries.
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
+// 32 rows of 16 bytes, one after the other, to 32 lanes of four columns, the same for each of the four warps' lanes.
+__device__ __forceinline__ void scales_to_tmem(uint32_t dst, uint32_t src)
+{
+    const uint64_t desc = (uint64_t)((src >> 4) & 0x3fffu) | (uint64_t)(128 >> 4) << 32 | 1ull << 46;
+    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(dst), "l"(desc) : "memory");
+}
+// Instruction descriptor, kind::mxf4: e2m1 operands, scales that are powers of two; `which` of a column's two pairs of
+// scales the instruction takes.
+__device__ __forceinline__ constexpr uint32_t mx4_desc(int m, int n, int which)
+{
+    return 1u << 7 | 1u << 10 | (uint32_t)(n >> 3) << 17 | 1u << 23 | (uint32_t)(m >> 4) << 24 | (uint32_t)(2 * which) << 4 | (uint32_t)(2 * which) << 29;
+}
+__device__ __forceinline__ void mma_mx4(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t scales_a, uint32_t scales_b, bool add)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %6, 0;\n\t"
+                 "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.block32 [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(scales_a), "r"(scales_b), "r"((uint32_t)add) : "memory");
+}
+
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
+
+// Grid: one tile per cluster where a tile's k is split over a cluster, otherwise blocks that take tiles in turn, features
+// first.  A block has one warp that loads, one that issues the matrix instructions and four that bring accumulators from
+// tensor memory to y.
+template <typename T, int NT>
+__global__ void __launch_bounds__(kProductThreads, NT > 128 ? 1 : 2)
+serve_linear4_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w, const __grid_constant__ ProductDev d)
+{
+    using S = Tile<NT>;
+    extern __shared__ uint8_t raw_smem[];
+    __shared__ __align__(8) uint64_t bars[2 * S::stages + 2 * S::accs + 1];
+    __shared__ uint32_t tmem_at;
+    __shared__ int gave_up;
+
+    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
+    const cg::cluster_group cluster = cg::this_cluster();
+    const int split = (int)cluster.num_blocks(), part = (int)cluster.block_rank();
+
+    uint8_t *smem = (uint8_t *)(((uintptr_t)raw_smem + 1023) & ~(uintptr_t)1023);
+    const uint32_t stage0 = smem_u32(smem);
+    const uint32_t full = smem_u32(bars), empty = full + 8 * S::stages, acc_full = empty + 8 * S::stages, acc_empty = acc_full + 8 * S::accs,
+                   drained = acc_empty + 8 * S::accs;
+
+    // which tiles, and of k which stages
+    const int k_blocks = (d.k + kDepth - 1) / kDepth;
+    const int kb0 = (int)((int64_t)k_blocks * part / split), kb1 = (int)((int64_t)k_blocks * (part + 1) / split);
+    const int first_tile = blockIdx.x / split, tiles = d.f_tiles * d.t_tiles, tile_step = gridDim.x / split;
+
+    if (warp == 1) {
+        tmem_alloc(smem_u32(&tmem_at), S::columns);
+    } else if (tid == 0) {
+        gave_up = d.give_up;
+        for (int i = 0; i < S::stages; i++) {
+            mbar_init(full + 8 * i, 1);
+            mbar_init(empty + 8 * i, 1);
+        }
+        for (int i = 0; i < S::accs; i++) {
+            mbar_init(acc_full + 8 * i, 1);
+            mbar_init(acc_empty + 8 * i, 128);
+        }
+        mbar_init(drained, 1);
+        mbar_init_fence();
+        tma_prefetch(&map_x);
+        tma_prefetch(&map_w);
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = tmem_at;
+
+    int issued = 0;                                   // loads, of the thread that issues them
+    if (warp == 0) {
+        if (lane == 0) {
+            // ---- loads.  W is there already: its first stages are on their way before x is packed.
+            Ring<S::stages> ring;
+            bool ok = true, waited = false;
+            for (int tile = first_tile; tile < tiles && ok; tile += tile_step) {
+                const int f_tile = tile % d.f_tiles, t_tile = tile / d.f_tiles;
+                auto load = [&](int kb, int slot, bool w) {
+                    const uint32_t bar = full + 8 * slot, at = stage0 + slot * S::stage;
+                    const int64_t kt = 2 * (int64_t)kb, have = min((int64_t)2, d.tiles_k - kt);      // tiles of scales
+                    if (w) {
+                        mbar_expect(bar, S::codes_w + S::codes_x + (uint32_t)have * (1 + S::atoms) * kAtom);
+                        tma_load(at, &map_w, kb * 64, f_tile * kFeatures, bar);
+                        bulk_load(at + S::codes_w + S::codes_x, d.scales_w + (f_tile * d.tiles_k + kt) * kAtom, (uint32_t)have * kAtom, bar);
+                        issued++;
+                    } else {
+                        tma_load(at + S::codes_w, &map_x, kb * 64, t_tile * NT, bar);
+                        bulk_load(at + S::codes_w + S::codes_x + S::scales_w, d.scales_x + (t_tile * d.tiles_k + kt) * S::atoms * kAtom,
+                                  (uint32_t)have * S::atoms * kAtom, bar);
+                    }
+                };
+                int ahead = 0;
+                if (!waited) {
+                    ahead = min(S::stages, kb1 - kb0);
+                    for (int i = 0; i < ahead; i++) load(kb0 + i, i, true);
+                    wait_previous();                  // the codes and scales of x
+                    waited = true;
+                }
+                for (int kb = kb0; kb < kb1; kb++) {
+                    if (kb - kb0 >= ahead) {
+                        if (!(ok = mbar_wait(empty + 8 * ring.slot, ring.parity ^ 1u, &gave_up))) break;
+                        load(kb, ring.slot, true);
+                    }
+                    load(kb, ring.slot, false);
+                    ring.step();
+                }
+            }
+        }
+        __syncwarp();
+    } else if (warp == 1) {
+        if (lane == 0) {
+            // ---- matrix instructions
+            Ring<S::stages> ring;
+            Ring<S::accs> acc;
+            bool ok = true;
+            for (int tile = first_tile; tile < tiles && ok; tile += tile_step) {
+                if (!(ok = mbar_wait(acc_empty + 8 * acc.slot, acc.parity ^ 1u, &gave_up))) break;
+                tc_fence_after();
+                const uint32_t out = tmem + acc.slot * NT;
+                for (int kb = kb0; kb < kb1; kb++) {
+                    if (!(ok = mbar_wait(full + 8 * ring.slot, ring.parity, &gave_up))) break;
+                    tc_fence_after();
+                    const uint32_t at = stage0 + ring.slot * S::stage, scales = at + S::codes_w + S::codes_x;
+                    const uint64_t a = smem_desc(at), b = smem_desc(at + S::codes_w);
+                    const int steps = min(kDepth / 64, (d.k - kb * kDepth + 63) / 64);
+#pragma unroll
+                    for (int h = 0; h < 2; h++) {
+                        if (2 * h >= steps) break;
+                        scales_to_tmem(tmem + S::at_w + 4 * h, scales + h * kAtom);
+#pragma unroll
+                        for (int i = 0; i < S::atoms; i++)
+                            scales_to_tmem(tmem + S::at_x + 4 * (h * S::atoms + i), scales + S::scales_w + (h * S::atoms + i) * kAtom);
+                    }
+#pragma unroll
+                    for (int i = 0; i < kDepth / 64; i++)
+                        if (i < steps)
+                            mma_mx4(out, a + 2 * i, b + 2 * i, mx4_desc(kFeatures, NT, i % 2), tmem + S::at_w + i / 2 * 4,
+                                    tmem + S::at_x + i / 2 * 4 * S::atoms, kb > kb0 || i > 0);
+                    mma_commit(empty + 8 * ring.slot);
+                    ring.step();
+                }
+                if (!ok) break;
+                mma_commit(acc_full + 8 * acc.slot);
+                acc.step();
+            }
+        }
+        __syncwarp();
+    } else {
+        // ---- the accumulators' way out.  A warp may touch the 32 lanes of its number modulo 4.
+        const int quarter = warp % 4, f = quarter * 32 + lane;
+        Ring<S::accs> acc;
+        for (int tile = first_tile; tile < tiles; tile += tile_step) {
+            const bool ok = mbar_wait(acc_full + 8 * acc.slot, acc.parity, &gave_up);
+            if (!__all_sync(~0u, ok)) break;
+            tc_fence_after();
+            if (split > 1) break;                     // goes on below, with the other blocks of the cluster
+            const uint32_t src = tmem + ((uint32_t)(quarter * 32) << 16) + acc.slot * NT;
+            const int f0 = tile % d.f_tiles * kFeatures, t0 = tile / d.f_tiles * NT;
+            const float bias = d.bias && f0 + f < d.n ? to_f32(((const T *)d.bias)[f0 + f]) : 0.0f;
+            T *y = (T *)d.y + (int64_t)t0 * d.ys + f0 + f;
+            const int live = f0 + f < d.n ? min(NT, d.tokens - t0) : 0;
+#pragma unroll 1
+            for (int c = 0; c < NT; c += 16) {
+                uint32_t v[16];
+                tmem_load16(src + c, v);
+                tmem_wait_load16(v);
+#pragma unroll
+                for (int i = 0; i < 16; i++)
+                    if (c + i < live) y[(int64_t)(c + i) * d.ys] = from_f32<T>(__uint_as_float(v[i]) + bias);
+            }
+            tc_fence_before();
+            mbar_arrive(acc_empty + 8 * acc.slot);
+            acc.step();
+        }
+    }
+
+    if (S::accs == 1 && split > 1) {
+        // The blocks' sums are joined: each puts its own where its stages were, block r of the cluster adds up all of
+        // them for its share of the tokens, always in the same order.
+        const int f0 = first_tile % d.f_tiles * kFeatures, t0 = first_tile / d.f_tiles * NT, share = NT / split;
+        if (warp >= 2) {
+            const int quarter = warp % 4, f = quarter * 32 + lane;
+#pragma unroll 2
+            for (int c = 0; c < NT; c += 16) {
+                uint32_t v[16];
+                tmem_load16(tmem + ((uint32_t)(quarter * 32) << 16) + c, v);
+                tmem_wait_load16(v);
+#pragma unroll
+                for (int i = 0; i < 16; i++) ((uint32_t *)smem)[(c + i) * kFeatures + f] = v[i];
+            }
+            tc_fence_before();
+        }
+        __syncwarp();
+        cluster_arrive();
+        cluster_wait();
+        const int features = min(kFeatures, d.n - f0), c0 = part * share, c1 = min(c0 + share, d.tokens - t0);
+        const bool whole = features % 4 == 0 && d.ys % 4 == 0 && ((uintptr_t)d.y & 7) == 0;
+#pragma unroll 2
+        for (int i = c0 * (kFeatures / 4) + tid; i < c1 * (kFeatures / 4); i += kProductThreads) {
+            const int f = i % (kFeatures / 4) * 4, c = i / (kFeatures / 4);
+            if (f >= features) continue;
+            float4 p[kMaxSplit];
+#pragma unroll
+            for (int b = 0; b < kMaxSplit; b++)
+                p[b] = b < split ? cluster.map_shared_rank((const float4 *)smem, b)[i] : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            float v[4] = {};
+#pragma unroll
+            for (int b = 0; b < kMaxSplit; b++) {
+                v[0] += p[b].x;
+                v[1] += p[b].y;
+                v[2] += p[b].z;
+                v[3] += p[b].w;
+            }
+            T *y = (T *)d.y + (int64_t)(t0 + c) * d.ys + f0 + f;
+            __align__(8) T r[4];
+#pragma unroll
+            for (int k = 0; k < 4; k++)
+                r[k] = from_f32<T>(v[k] + (d.bias && f + k < features ? to_f32(((const T *)d.bias)[f0 + f + k]) : 0.0f));
+            if (whole) {
+                *(uint2 *)y = *(const uint2 *)r;
+            } else {
+#pragma unroll
+                for (int k = 0; k < 4; k++)
+                    if (f + k < features) y[k] = r[k];
+            }
+        }
+        cluster_arrive();                             // a block's memory stays until the others have read it
+        cluster_wait();
+    }
+    __syncthreads();
+    tc_fence_after();
+    // (nobody sets gave_up from here on)
+    if (warp == 1) {
+        if (gave_up) {                                // what was issued ends before tensor memory is given up
+            if (lane == 0) {
+                mma_commit(drained);
+                mbar_drain(drained, 0);
+            }
+            __syncwarp();
+        }
+        tmem_free(tmem, S::columns);
+    }
+    if (tid == 0 && gave_up) {                        // and loads, before the block's memory is
+        drain_loads<S::stages>(full, issued);
+        atomicExch(d.status, 1);
+    }
+}
+
+// ------------------------------------------------------------------------------------------- host
+int check_pack(const bcast_serve_pack4_args *a)
+{
+    if (!a) return BCAST_ERR_INVAL;
+    if (a->dtype != BCAST_SERVE_BF16 && a->dtype != BCAST_SERVE_FP16 && a->dtype != BCAST_SERVE_FP32) return BCAST_ERR_INVAL;
+    if (a->rows < 0 || a->rows > kMaxDim - 65536 || a->k < kBlock || a->k > 1 << 24 || a->k % kBlock) return BCAST_ERR_INVAL;
+    if (a->rows == 0) return BCAST_OK;
+    if (!stride_ok(a->values_stride, a->k, 8) || !stride_ok(a->codes_stride, a->k / 2, 16)) return BCAST_ERR_INVAL;
+    int device = 0, rc;
+    SERVE_TRY(cudaGetDevice(&device));
+    if ((rc = check_array(a->values, 16, device)) || (rc = check_array(a->codes, 16, device)) || (rc = check_array(a->scales, 16, device))) return rc;
+    return BCAST_OK;
+}
+
+PackDev pack_dev(const bcast_serve_pack4_args &a)
+{
+    PackDev d = {};
+    d.values = a.values;
+    d.codes = a.codes;
+    d.scales = a.scales;
+    d.vs = a.values_stride;
+    d.cs = a.codes_stride;
+    d.rows = a.rows;
+    d.k = (int32_t)a.k;
+    d.tiles_k = ceil_div(a.k, 4 * kBlock);
+    d.tile = 128;
+    d.atoms = 1;
+    d.padded = round_up(a.rows, 128);
+    d.segments = (int32_t)ceil_div(a.k, 8 * kPackThreads);
+    return d;
+}
+
+// `rows`: how many the blocks go over.
+template <typename F>
+int over_rows(F kernel, const PackDev &d, int64_t rows, cudaStream_t st)
+{
+    const int64_t blocks = ceil_div(rows, kPackRows) * d.segments;
+    if (blocks > kMaxDim) return BCAST_ERR_INVAL;
+    return launch(kernel, dim3((unsigned)blocks), dim3(kPackThreads), 0, st, false, 1, d);
+}
+
+// How a call is cut: tokens of a tile and parts of k.
+struct Cut {
+    int tile, split;
+};
+
+// Parts of k: the most, in powers of two, that make no more than `room` blocks, each of at least two stages.
+int parts_of(int64_t blocks, int64_t room, int64_t k_blocks, int most)
+{
+    int s = 1;
+    while (s < most && blocks * s * 2 <= room && k_blocks >= 4 * s) s *= 2;
+    return s;
+}
+
+Cut cut_of(const bcast_serve_linear4_args &a)
+{
+    Cut c = {};
+    const int64_t k_blocks = ceil_div(a.k, kDepth), f_tiles = ceil_div(a.n, kFeatures);
+    c.tile = a.tokens <= 32 ? 32 : a.tokens <= 64 ? 64 : a.tokens <= 128 || ceil_div(a.tokens, 224) * f_tiles < 2 * kSms ? 128 : 224;
+    c.split = c.tile > 128 ? 1 : parts_of(ceil_div(a.tokens, c.tile) * f_tiles, kSms, k_blocks, kMaxSplit);
+    return c;
+}
+
+int check_shape(const bcast_serve_linear4_args &a)
+{
+    if (a.dtype != BCAST_SERVE_BF16 && a.dtype != BCAST_SERVE_FP16) return BCAST_ERR_INVAL;
+    if (a.tokens < 0 || a.tokens > (1 << 21) || a.k < kBlock || a.k > (1 << 24) || a.k % kBlock || a.n < 1 || a.n > (1 << 24)) return BCAST_ERR_INVAL;
+    return BCAST_OK;
+}
+
+int64_t x_codes_bytes(const bcast_serve_linear4_args &a) { return round_up(a.tokens * (a.k / 2), 256); }
+int64_t x_scales_bytes(const bcast_serve_linear4_args &a, const Cut &c)
+{
+    return ceil_div(a.tokens, c.tile) * ceil_div(a.k, 4 * kBlock) * ceil_div(c.tile, 128) * kAtom;
+}
+
+template <typename T, int NT>
+int run_product(const bcast_serve_linear4_args &a, ProductDev d, const PackDev &p, const Cut &c, cudaStream_t st)
+{
+    using S = Tile<NT>;
+    d.f_tiles = (int32_t)ceil_div(a.n, kFeatures);
+    d.t_tiles = (int32_t)ceil_div(a.tokens, NT);
+    const int64_t tiles = (int64_t)d.f_tiles * d.t_tiles;
+    // rows of codes as rows of 16-bit numbers, four codes each
+    CUtensorMap mx, mw;
+    int rc;
+    if ((rc = tensor_map(&mx, CU_TENSOR_MAP_DATA_TYPE_UINT16, p.codes, {a.k / 4, a.tokens}, {p.cs / 2}, {64, NT}))) return rc;
+    if ((rc = tensor_map(&mw, CU_TENSOR_MAP_DATA_TYPE_UINT16, a.codes, {a.k / 4, a.n}, {a.codes_stride / 2}, {64, kFeatures}))) return rc;
+    if ((rc = allow_smem<serve_linear4_kernel<T, NT>>(S::smem))) return rc;
+    const int64_t blocks = S::accs > 1 && tiles > kSms ? kSms : tiles * c.split;
+    if (blocks > kMaxDim) return BCAST_ERR_INVAL;
+    return launch(serve_linear4_kernel<T, NT>, dim3((unsigned)blocks), dim3(kProductThreads), S::smem, st, true, c.split, mx, mw, d);
+}
+
+template <typename T>
+int run(const bcast_serve_linear4_args &a, const ProductDev &d, const PackDev &p, const Cut &c, cudaStream_t st)
+{
+    int rc = over_rows(serve_pack4_kernel<T>, p, a.tokens, st);
+    if (rc) return rc;
+    switch (c.tile) {
+    case 32: return run_product<T, 32>(a, d, p, c, st);
+    case 64: return run_product<T, 64>(a, d, p, c, st);
+    case 128: return run_product<T, 128>(a, d, p, c, st);
+    default: return run_product<T, 224>(a, d, p, c, st);
+    }
+}
+
+}  // namespace
+}  // namespace bcast_serve
+
+using namespace bcast_serve;
+
+extern "C" {
+
+int bcast_serve_pack4(const bcast_serve_pack4_args *a, void *cuda_stream)
+{
+    int rc = check_pack(a);
+    if (rc || a->rows == 0) return rc;
+    const PackDev d = pack_dev(*a);
+    const cudaStream_t st = (cudaStream_t)cuda_stream;
+    switch (a->dtype) {
+    case BCAST_SERVE_BF16: return over_rows(serve_pack4_kernel<__nv_bfloat16>, d, d.padded, st);
+    case BCAST_SERVE_FP16: return over_rows(serve_pack4_kernel<__half>, d, d.padded, st);
+    default: return over_rows(serve_pack4_kernel<float>, d, d.padded, st);
+    }
+}
+
+int bcast_serve_unpack4(const bcast_serve_pack4_args *a, void *cuda_stream)
+{
+    int rc = check_pack(a);
+    if (rc || a->rows == 0) return rc;
+    const PackDev d = pack_dev(*a);
+    const cudaStream_t st = (cudaStream_t)cuda_stream;
+    switch (a->dtype) {
+    case BCAST_SERVE_BF16: return over_rows(serve_unpack4_kernel<__nv_bfloat16>, d, d.rows, st);
+    case BCAST_SERVE_FP16: return over_rows(serve_unpack4_kernel<__half>, d, d.rows, st);
+    default: return over_rows(serve_unpack4_kernel<float>, d, d.rows, st);
+    }
+}
+
+int64_t bcast_serve_linear4_workspace(const bcast_serve_linear4_args *a)
+{
+    if (!a || check_shape(*a)) return BCAST_ERR_INVAL;
+    return BCAST_SERVE_STATUS_BYTES + x_codes_bytes(*a) + x_scales_bytes(*a, cut_of(*a));
+}
+
+int bcast_serve_linear4(const bcast_serve_linear4_args *a, void *cuda_stream)
+{
+    if (!a) return BCAST_ERR_INVAL;
+    int rc = check_shape(*a);
+    if (rc) return rc;
+    if (a->tokens == 0) return BCAST_OK;
+    if (!stride_ok(a->x_stride, a->k, 8) || !stride_ok(a->codes_stride, a->k / 2, 16) || !stride_ok(a->y_stride, a->n, 1)) return BCAST_ERR_INVAL;
+    int device = 0;
+    SERVE_TRY(cudaGetDevice(&device));
+    if ((rc = check_array(a->x, 16, device)) || (rc = check_array(a->codes, 16, device)) || (rc = check_array(a->scales, 16, device)) ||
+        (rc = check_array(a->y, 2, device)))
+        return rc;
+    if (a->bias && (rc = check_array(a->bias, 2, device))) return rc;
+    if ((rc = check_workspace(a->workspace, a->workspace_bytes, bcast_serve_linear4_workspace(a), device))) return rc;
+
+    const Cut c = cut_of(*a);
+    PackDev p = {};
+    p.values = const_cast<void *>(a->x);
+    p.codes = (uint8_t *)a->workspace + BCAST_SERVE_STATUS_BYTES;
+    p.scales = p.codes + x_codes_bytes(*a);
+    p.vs = a->x_stride;
+    p.cs = a->k / 2;
+    p.rows = p.padded = a->tokens;        // what has no token is read, as scales of features' columns that nobody keeps
+    p.k = (int32_t)a->k;
+    p.tiles_k = ceil_div(a->k, 4 * kBlock);
+    p.tile = c.tile;
+    p.atoms = (int32_t)ceil_div(c.tile, 128);
+    p.segments = (int32_t)ceil_div(a->k, 8 * kPackThreads);
+    ProductDev d = {};
+    d.bias = a->bias;
+    d.scales_w = a->scales;
+    d.scales_x = p.scales;
+    d.y = a->y;
+    d.status = (int *)a->workspace;
+    d.give_up = give_up_at_once();
+    d.ys = a->y_stride;
+    d.tiles_k = p.tiles_k;
+    d.tokens = (int32_t)a->tokens;
+    d.k = (int32_t)a->k;
+    d.n = (int32_t)a->n;
+    const cudaStream_t st = (cudaStream_t)cuda_stream;
+    return a->dtype == BCAST_SERVE_BF16 ? run<__nv_bfloat16>(*a, d, p, c, st) : run<__half>(*a, d, p, c, st);
+}
+
+}  // extern "C"

@@ -33,7 +33,8 @@ BCAST_SERVE_STATUS_BYTES = 256
 
 #: every symbol ``include/bcast_serve.h`` declares
 SYMBOLS = ("bcast_serve_linear", "bcast_serve_linear_workspace", "bcast_serve_attn", "bcast_serve_attn_workspace",
-           "bcast_serve_verify", "bcast_serve_verify_workspace", "bcast_serve_status")
+           "bcast_serve_verify", "bcast_serve_verify_workspace", "bcast_serve_append", "bcast_serve_logprobs", "bcast_serve_pack4",
+           "bcast_serve_unpack4", "bcast_serve_linear4", "bcast_serve_linear4_workspace", "bcast_serve_status")
 
 _vp, _i32, _i64, _u64, _f32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_uint64, ctypes.c_float
 _s2, _s3 = _i64 * 2, _i64 * 3
@@ -62,11 +63,38 @@ class VerifyArgs(ctypes.Structure):
                 ("workspace_bytes", _u64)]
 
 
-for _name, _args in (("linear", LinearArgs), ("attn", AttnArgs), ("verify", VerifyArgs)):
+class AppendArgs(ctypes.Structure):
+    _fields_ = [("dtype", _i32), ("batch", _i32), ("new_tokens", _i32), ("q_heads", _i32), ("kv_heads", _i32), ("dim", _i32),
+                ("page_size", _i32), ("rot", _i32), ("interleaved", _i32), ("axes", _i32), ("eps", _f32), ("own_cap", _i64),
+                ("num_pages", _i64), ("first", _i64), ("q", _vp), ("k", _vp), ("v", _vp), ("q_norm", _vp), ("k_norm", _vp),
+                ("inv_freq", _vp), ("positions", _vp), ("axis", _vp), ("own_len", _vp), ("new_len", _vp), ("page_table", _vp),
+                ("out", _vp), ("own_k", _vp), ("own_v", _vp), ("q_stride", _s3), ("k_stride", _s3), ("v_stride", _s3),
+                ("out_stride", _s3), ("own_k_stride", _s3), ("own_v_stride", _s3), ("positions_stride", _s2), ("page_table_stride", _i64)]
+
+
+class LogprobsArgs(ctypes.Structure):
+    _fields_ = [("dtype", _i32), ("top", _i32), ("rows", _i64), ("vocab", _i64), ("logits", _vp), ("tokens", _vp), ("logprobs", _vp),
+                ("entropy", _vp), ("top_logprobs", _vp), ("top_tokens", _vp), ("logits_stride", _i64)]
+
+
+class Pack4Args(ctypes.Structure):
+    _fields_ = [("dtype", _i32), ("rows", _i64), ("k", _i64), ("values", _vp), ("codes", _vp), ("scales", _vp), ("values_stride", _i64),
+                ("codes_stride", _i64)]
+
+
+class Linear4Args(ctypes.Structure):
+    _fields_ = [("dtype", _i32), ("tokens", _i64), ("k", _i64), ("n", _i64), ("x", _vp), ("bias", _vp), ("codes", _vp), ("scales", _vp),
+                ("y", _vp), ("x_stride", _i64), ("codes_stride", _i64), ("y_stride", _i64), ("workspace", _vp), ("workspace_bytes", _u64)]
+
+
+for _name, _args, _scratch in (("linear", LinearArgs, True), ("attn", AttnArgs, True), ("verify", VerifyArgs, True), ("append", AppendArgs, False),
+                               ("logprobs", LogprobsArgs, False), ("pack4", Pack4Args, False), ("unpack4", Pack4Args, False),
+                               ("linear4", Linear4Args, True)):
     _f = getattr(_lib, f"bcast_serve_{_name}")
     _f.restype, _f.argtypes = ctypes.c_int, [ctypes.POINTER(_args), _vp]
-    _f = getattr(_lib, f"bcast_serve_{_name}_workspace")
-    _f.restype, _f.argtypes = _i64, [ctypes.POINTER(_args)]
+    if _scratch:
+        _f = getattr(_lib, f"bcast_serve_{_name}_workspace")
+        _f.restype, _f.argtypes = _i64, [ctypes.POINTER(_args)]
 _lib.bcast_serve_status.restype, _lib.bcast_serve_status.argtypes = ctypes.c_int, [_vp, _vp]
 
 
@@ -134,9 +162,19 @@ def _strides(t: torch.Tensor, n: int):
     return _native.strides(t, n)
 
 
+def _raw(stream) -> int:
+    return -1 if stream is None else int(getattr(stream, "cuda_stream", stream))
+
+
+def _result(where: str, code: int, result):
+    if code == BCAST_OK:
+        return result
+    raise BcastError(code, f"{where} ({result})" if code == BCAST_ERR_INVAL and result else where)
+
+
 def _call(where: str, native, device, workspace, stream, *tensors):
     """The native call, once more with a larger workspace where it asks for one."""
-    raw = -1 if stream is None else int(getattr(stream, "cuda_stream", stream))
+    raw = _raw(stream)
     if workspace is None:
         workspace = _Fresh(device)
     code, result, captured = native(*tensors, workspace._t, workspace._of, raw)
@@ -145,9 +183,7 @@ def _call(where: str, native, device, workspace, stream, *tensors):
         code, result, captured = native(*tensors, workspace._t, workspace._of, raw)
     if captured:
         workspace._captured = True
-    if code == BCAST_OK:
-        return result
-    raise BcastError(code, f"{where} ({result})" if code == BCAST_ERR_INVAL and result else where)
+    return _result(where, code, result)
 
 
 def bcast_serve_linear(x, weight, *, bias=None, lora_a=None, lora_b=None, adapter=None, scale=None, out=None, workspace=None,
@@ -175,6 +211,45 @@ def bcast_serve_verify(logits, draft_probs, draft_tokens, uniforms, noise, tempe
     (accepted [B], tokens [B, n + 1]), both int32: the accepted drafts, the token after them, then -1."""
     return _call("bcast_serve_verify", _native.verify, logits.device, workspace, stream, logits, draft_probs, draft_tokens, uniforms, noise,
                  temperature, accepted, tokens)
+
+
+def bcast_serve_append(q, k, v, own_k, own_v, own_len, *, page_table=None, new_len=None, first=0, positions=None, inv_freq=None, axis=None,
+                       interleaved=False, q_norm=None, k_norm=None, eps=1e-6, out=None, stream=None):
+    """``q`` [B, n, HQ, D] (or None), ``k``/``v`` [B, n, H, D] of the n newest tokens of every request; the caches, ``own_len``
+    and ``page_table`` as :func:`bcast_serve_attn` takes them afterwards, the new tokens counted in ``own_len`` already.
+    Queries and keys are normed with ``q_norm``/``k_norm`` [D] and rotated by ``inv_freq`` [rot / 2] float32, where
+    given, at ``first`` + place in the cache or at ``positions`` [B, n] or [B, n, axes] int32 (``axis`` [rot / 2] int32: the axis
+    of each pair); keys and values go into the caches.  ``new_len`` [B] int32: how many of the n are there, at the end.
+    Returns the queries (``out``, which may be ``q``), None without ``q``."""
+    code, result, _ = _native.append(q, k, v, own_k, own_v, own_len, page_table, new_len, first, positions, inv_freq, axis, interleaved, q_norm,
+                                     k_norm, eps, out, _raw(stream))
+    return _result("bcast_serve_append", code, result)
+
+
+def bcast_serve_logprobs(logits, tokens, *, top=0, logprobs=None, entropy=None, top_tokens=None, top_logprobs=None, stream=None):
+    """``logits`` [T, V], ``tokens`` [T] int32.  Returns (logprobs [T], entropy [T], top_tokens [T, top] int32, top_logprobs
+    [T, top]), float32 where nothing else is said: the given tokens' log probabilities, and the ``top`` most probable tokens."""
+    code, result, _ = _native.logprobs(logits, tokens, top, logprobs, entropy, top_tokens, top_logprobs, _raw(stream))
+    return _result("bcast_serve_logprobs", code, result)
+
+
+def bcast_serve_pack4(x, *, codes=None, scales=None, stream=None):
+    """``x`` [rows, k] bf16, fp16 or fp32, k a multiple of 32.  Returns (codes [rows, k / 2], scales [ceil(rows / 128),
+    ceil(k / 128), 32, 4, 4]), both uint8: microscaled 4-bit numbers."""
+    code, result, _ = _native.pack4(x, codes, scales, _raw(stream))
+    return _result("bcast_serve_pack4", code, result)
+
+
+def bcast_serve_unpack4(codes, scales, dtype=torch.bfloat16, *, out=None, stream=None):
+    """The numbers [rows, k] that ``codes`` and ``scales`` stand for, in ``dtype``."""
+    code, result, _ = _native.unpack4(codes, scales, dtype, out, _raw(stream))
+    return _result("bcast_serve_unpack4", code, result)
+
+
+def bcast_serve_linear4(x, codes, scales, *, bias=None, out=None, workspace=None, stream=None):
+    """``x`` [T, k]; ``codes``, ``scales`` of a weight [n, k] as :func:`bcast_serve_pack4` makes them; ``bias`` [n].  Returns
+    y [T, n]: x, packed in the same way, times the weight."""
+    return _call("bcast_serve_linear4", _native.linear4, x.device, workspace, stream, x, codes, scales, bias, out)
 
 
 def bcast_serve_status(workspace: Workspace, stream=None) -> None:
