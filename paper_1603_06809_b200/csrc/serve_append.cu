@@ -1,20 +1,20 @@
 // bcast_serve_append: queries and keys of new tokens normed for each head and rotated by their positions, keys
 // and values put into the requests' caches -- one pass over what a projection left.
 //
-// A head of up to 128 numbers is `L` lanes' (a power of two, 16 numbers to a lane), which hold the two 16-byte chunks
-// whose numbers are each other's partners in the rotation, so that the rotation needs no exchange; the norm is one sum
-// over the L lanes.  A warp takes one token: the cosines and sines of its rot / 2 pairs are made once, two pairs to a
-// lane, dealt out by shuffles, and then it goes through heads, 32 / L at a time.
-// Angles: inv_freq / 2 pi as a 64-bit fraction of a turn; multiplied by the position modulo 2^64 this leaves the
-// fraction of a turn with nothing lost to the size of the position.
-// Bound by memory: what is read is written once.
+// A head of up to 128 numbers is 1, 2, 4 or 8 lanes', 16 numbers to a lane, which hold the two 16-byte chunks whose
+// numbers are each other's partners in the rotation, so that the rotation needs no exchange; the norm is one sum over
+// those lanes.  A warp takes as many heads at a time as it has lanes for ("a round": queries first, then keys, then values),
+// and all or some of a token's rounds, whose cosines and sines it makes once.
+// Angles: inv_freq / 2 pi as a 64-bit fraction of a turn; multiplied by the position modulo 2^64 this leaves the fraction
+// of a turn, off by the position's 2^-64.
 #include "serve_device.cuh"
 #include "serve_internal.h"
 
 namespace bcast_serve {
 namespace {
 
-constexpr int kAppendThreads = 128, kAtOnce = 4;      // heads of a lane whose loads are under way together
+constexpr int kAppendThreads = 64, kAppendBlocks = 10;  // of a block; blocks to an SM
+constexpr int kFlight = 2;                    // rounds of loads that a warp has under way
 
 struct AppendDev {
     const void *q, *k, *v, *q_norm, *k_norm;
@@ -22,165 +22,275 @@ struct AppendDev {
     const int32_t *positions, *axis, *own_len, *new_len, *page_table;
     void *out, *ok, *ov;
     int64_t qs[3], ks[3], vs[3], os[3], oks[3], ovs[3], ps[2];
-    int64_t own_cap, num_pages, pts, first, items;
-    int32_t fresh, q_heads, kv_heads, dim, page, rot, interleaved, axes, groups, rounds;
-    float eps;
+    int64_t own_cap, num_pages, pts, first;
+    int32_t fresh, q_heads, kv_heads, dim, page, page_shift, rot, axes, groups, rounds, lanes_shift, items;
+    float eps, per_dim;
 };
+
+enum { kStraight = 0, kHalves = 1, kNeighbours = 2 }; // what is turned: nothing, (p, p + rot / 2), (2 p, 2 p + 1)
 
 // One lane's two chunks of a head.
 struct Unit {
     uint4 a, b;
 };
 
+// Eight 16-bit numbers as four pairs of floats, and back.
 template <typename T>
-__device__ __forceinline__ void widen8(const uint4 &raw, float *x)
+__device__ __forceinline__ void widen8(const uint4 &raw, uint64_t *x)
 {
-    const T *v = (const T *)&raw;
+    const uint32_t v[4] = {raw.x, raw.y, raw.z, raw.w};
 #pragma unroll
-    for (int i = 0; i < 8; i++) x[i] = to_f32(v[i]);
+    for (int i = 0; i < 4; i++) {
+        if constexpr (std::is_same_v<T, __nv_bfloat16>) {
+            x[i] = pair(__uint_as_float(v[i] << 16), __uint_as_float(v[i] & 0xffff0000u));
+        } else {
+            const float2 f = __half22float2(*(const __half2 *)&v[i]);
+            x[i] = pair(f.x, f.y);
+        }
+    }
 }
 template <typename T>
-__device__ __forceinline__ uint4 narrow8(const float *x)
+__device__ __forceinline__ uint4 narrow8(const uint64_t *x)
 {
-    uint4 raw;
-    T *v = (T *)&raw;
+    uint32_t v[4];
 #pragma unroll
-    for (int i = 0; i < 8; i++) v[i] = from_f32<T>(x[i]);
-    return raw;
+    for (int i = 0; i < 4; i++) {
+        float a, b;
+        unpair(x[i], a, b);
+        if constexpr (std::is_same_v<T, __nv_bfloat16>) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(v[i]) : "f"(b), "f"(a));
+        else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(v[i]) : "f"(b), "f"(a));
+    }
+    return make_uint4(v[0], v[1], v[2], v[3]);
 }
 
-// Cosine and sine of pair p's angle.
-__device__ __forceinline__ float2 turn_of(const AppendDev &d, int p, int64_t row_position, const int32_t *positions)
+// Cosine and sine of `position` times `inv_freq`: inv_freq / 2 pi to 64 bits behind the point, from the float's 24-bit
+// whole number m and exponent e (inv_freq = m 2^e) and 2^66 / 2 pi; whole turns are cut off on both sides.
+__device__ __forceinline__ float2 turn_of(float inv_freq, int64_t position)
 {
-    if (p >= d.rot / 2) return make_float2(1.0f, 0.0f);
-    int64_t position = row_position;
-    if (positions) {
-        const int a = d.axis ? d.axis[p] : 0;
-        position = positions[(uint32_t)a < (uint32_t)d.axes ? a : 0];
-    }
-    const double turns = (double)d.inv_freq[p] * 0.15915494309189533577;      // 1 / (2 pi)
-    const uint64_t step = __double2ull_rz((turns - floor(turns)) * 18446744073709551616.0);
+    constexpr uint64_t per_turn = 0xa2f9836e4e44152aull;              // 2^66 / (2 pi), to nearest
+    const uint32_t bits = __float_as_uint(inv_freq), field = bits >> 23 & 255u;
+    const uint64_t m = (bits & 0x7fffffu) | (field ? 0x800000u : 0u);
+    const uint64_t low = m * per_turn, high = __umul64hi(m, per_turn);
+    const int right = 152 - (int)(field ? field : 1);                 // 2 - e
+    uint64_t step = right >= 128 ? 0 : right >= 64 ? high >> (right - 64) : right > 0 ? low >> right | high << (64 - right) : low << -right;
+    if (bits >> 31) step = 0 - step;
     const float half_turns = (float)(int32_t)((step * (uint64_t)position) >> 32) * 4.656612873077392578125e-10f;  // 2^-31
     float2 r;
     sincospif(half_turns, &r.y, &r.x);
     return r;
 }
 
-template <typename T, int L>
-__global__ void __launch_bounds__(kAppendThreads)
+// What a lane's 16 numbers are multiplied by, norm weights and rotation in one, two numbers to an entry.  Halves:
+//   y_a = x_a aa + x_b ab,  y_b = x_a ba + x_b bb       (aa = w_a cos, ab = -w_b sin, ba = w_a sin, bb = w_b cos)
+// neighbours, within each chunk:
+//   y = x aa + swapped(x) ab, and the same with bb and ba for the second
+struct Factors {
+    uint64_t aa[4], ab[4], ba[4], bb[4];
+};
+
+template <int TURN, bool NORM>
+__device__ __forceinline__ void turn_and_weigh(uint64_t *a, uint64_t *b, const Factors &f, bool turned)
+{
+#pragma unroll
+    for (int j = 0; j < 4; j++) {
+        const uint64_t p = a[j], q = b[j];
+        if (TURN == kHalves && turned) {
+            a[j] = fma2(p, f.aa[j], mul2(q, f.ab[j]));
+            b[j] = fma2(p, f.ba[j], mul2(q, f.bb[j]));
+        } else if (TURN == kNeighbours && turned) {
+            float x, y;
+            unpair(p, x, y);
+            a[j] = fma2(p, f.aa[j], mul2(pair(y, x), f.ab[j]));
+            unpair(q, x, y);
+            b[j] = fma2(q, f.bb[j], mul2(pair(y, x), f.ba[j]));
+        } else if (NORM) {
+            a[j] = mul2(p, f.aa[j]);
+            b[j] = mul2(q, f.bb[j]);
+        }
+    }
+}
+
+template <typename T, bool NORM, int TURN>
+__global__ void __launch_bounds__(kAppendThreads, kAppendBlocks)
 serve_append_kernel(const __grid_constant__ AppendDev d)
 {
-    constexpr int kHeads = 32 / L;                    // heads of a warp at a time
-    const int lane = threadIdx.x % 32, u = lane % L;
-    const int64_t item = (int64_t)blockIdx.x * (kAppendThreads / 32) + threadIdx.x / 32;
+    __shared__ __align__(16) float turns[kAppendThreads / 32][2][64];         // each warp's token's cosines and sines
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+    const int lanes = 1 << d.lanes_shift, u = lane & (lanes - 1), sub = lane >> d.lanes_shift, at_once = 32 >> d.lanes_shift;
+    const int item = blockIdx.x * (kAppendThreads / 32) + warp;
     if (item >= d.items) return;
-    const int token = (int)(item / d.groups), group = (int)(item - (int64_t)token * d.groups);
+    const int token = d.groups == 1 ? item : item / d.groups, group = item - token * d.groups;
     const int b = token / d.fresh, i = token - b * d.fresh;
     const int32_t length = d.own_len[b], fresh = d.new_len ? d.new_len[b] : d.fresh;
+    // this lane's chunks
+    const int units = d.rot / 16, chunks = d.dim / 8;
+    const bool turned = TURN != kStraight && u < units;
+    const int ca = TURN == kHalves && turned ? u : 2 * u, cb = TURN == kHalves && turned ? u + units : 2 * u + 1;
+    const bool has_a = ca < chunks, has_b = cb < chunks;
+    const int64_t gap = (cb - ca) * 8;
+
+    // which rounds: of queries 0..q_rounds - 1, of keys and of values from there on
+    const int q_rounds = (d.q_heads + at_once - 1) / at_once, kv_rounds = (d.kv_heads + at_once - 1) / at_once;
+    const int r0 = group * d.rounds, r1 = min(r0 + d.rounds, q_rounds + 2 * kv_rounds);
+    // (what is not there stays as it is)
+    const auto load = [&](Unit &x, const T *src, bool in) {
+        if (in) x.a = *(const uint4 *)src;
+        if (in && has_b) x.b = *(const uint4 *)(src + gap);
+    };
+    const auto store = [&](T *dst, const Unit &x, bool in) {
+        if (in) *(uint4 *)dst = x.a;
+        if (in && has_b) *(uint4 *)(dst + gap) = x.b;
+    };
+    const Unit nothing = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
+    // heads of this lane in rounds `from` on, of `heads` in all: positive where there is one
+    const auto heads_left = [&](int heads, int from) { return has_a ? heads - from * at_once - sub : 0; };
+
+    // the first queries' loads need not wait for the lengths
+    const T *src = (const T *)d.q + b * d.qs[0] + i * d.qs[1] + (r0 * at_once + sub) * d.qs[2] + ca * 8;
+    T *dst = (T *)d.out + b * d.os[0] + i * d.os[1] + (r0 * at_once + sub) * d.os[2] + ca * 8;
+    int64_t src_step = d.qs[2] * at_once, dst_step = d.os[2] * at_once;
+    int left = heads_left(d.q_heads, r0);
+    Unit next[kFlight];
+#pragma unroll
+    for (int k = 0; k < kFlight; k++) {
+        next[k] = nothing;
+        load(next[k], src + k * src_step, r0 + k < r1 && left > k * at_once);
+    }
     const int64_t slot = (int64_t)length - d.fresh + i;
-    const bool there = slot >= 0 && i >= (int64_t)d.fresh - fresh;
-    const int heads = d.q_heads + 2 * d.kv_heads, h0 = group * d.rounds * kHeads + lane / L;
+    if (slot < 0 || i < (int64_t)d.fresh - fresh) {           // padding
+        for (int r = r0; r < min(r1, q_rounds); r++, dst += dst_step, left -= at_once) store(dst, nothing, left > 0);
+        return;
+    }
+    if constexpr (TURN != kStraight) {
+        const int32_t *positions = d.axes ? d.positions + b * d.ps[0] + i * d.ps[1] : nullptr;
+#pragma unroll
+        for (int k = 0; k < 2; k++) {
+            const int p = lane + k * 32;
+            if (p >= d.rot / 2) break;
+            const float f = __ldg(d.inv_freq + p);
+            const int axis = d.axis ? __ldg(d.axis + p) : 0;
+            const float2 turn = turn_of(f, positions ? (int64_t)__ldg(positions + ((uint32_t)axis < (uint32_t)d.axes ? axis : 0)) : d.first + slot);
+            turns[warp][0][p] = turn.x;
+            turns[warp][1][p] = turn.y;
+        }
+        __syncwarp();
+    }
     // where the token goes
     int64_t page = b, place = slot;
-    bool stored = there && slot < d.own_cap;
+    bool stored = slot < d.own_cap;
     if (stored && d.page_table) {
-        const int32_t n = (int32_t)slot / d.page;
+        const int32_t n = d.page_shift >= 0 ? (int32_t)slot >> d.page_shift : (int32_t)slot / d.page;
         page = d.page_table[(int64_t)b * d.pts + n];
         place = slot - (int64_t)n * d.page;
         stored = page >= 0 && page < d.num_pages;
     }
-    // this lane's chunks
-    const int units = d.rot / 16, chunks = d.dim / 8;
-    const bool turned = u < units;
-    const int ca = turned && !d.interleaved ? u : 2 * u, cb = turned && !d.interleaved ? u + units : 2 * u + 1;
-    const bool has_a = ca < chunks, has_b = cb < chunks;
 
-    // cosines and sines of pairs 8 u to 8 u + 7
-    float cosine[8], sine[8];
-    if (d.rot) {
-        const int32_t *positions = d.axes ? d.positions + b * d.ps[0] + i * d.ps[1] : nullptr;
-        const float2 even = turn_of(d, 2 * lane, d.first + slot, positions), odd = turn_of(d, 2 * lane + 1, d.first + slot, positions);
+    // queries, then keys
+#pragma unroll 1
+    for (int kind = 0; kind < 2; kind++) {
+        const int base = kind ? q_rounds : 0, end = min(r1, kind ? q_rounds + kv_rounds : q_rounds);
+        int r = max(r0, base);
+        if (r >= end) continue;
+        if (kind) {
+            if (!stored) break;
+            const int h = (r - base) * at_once + sub;
+            src = (const T *)d.k + b * d.ks[0] + i * d.ks[1] + h * d.ks[2] + ca * 8;
+            dst = (T *)d.ok + page * d.oks[0] + place * d.oks[1] + h * d.oks[2] + ca * 8;
+            src_step = d.ks[2] * at_once;
+            dst_step = d.oks[2] * at_once;
+            left = heads_left(d.kv_heads, r - base);
 #pragma unroll
-        for (int j = 0; j < 8; j++) {
-            const int from = 4 * u + j / 2;
-            cosine[j] = __shfl_sync(~0u, j % 2 ? odd.x : even.x, from);
-            sine[j] = __shfl_sync(~0u, j % 2 ? odd.y : even.y, from);
+            for (int k = 0; k < kFlight; k++) load(next[k], src + k * src_step, r + k < end && left > k * at_once);
+        }
+        const T *weights = NORM ? (const T *)(kind ? d.k_norm : d.q_norm) : nullptr;
+        const bool norm = NORM && weights;
+        Factors f;
+        {
+            const uint64_t one = pair(1.0f, 1.0f);
+            uint64_t wa[4] = {one, one, one, one}, wb[4] = {one, one, one, one};
+            if (norm && has_a) widen8<T>(__ldg((const uint4 *)(weights + ca * 8)), wa);
+            if (norm && has_b) widen8<T>(__ldg((const uint4 *)(weights + cb * 8)), wb);
+#pragma unroll
+            for (int j = 0; j < 4; j++) {
+                if (TURN == kHalves && turned) {
+                    const uint64_t c = *(const uint64_t *)(turns[warp][0] + 8 * u + 2 * j), s = *(const uint64_t *)(turns[warp][1] + 8 * u + 2 * j);
+                    f.aa[j] = mul2(wa[j], c);
+                    f.ab[j] = mul2(mul2(wb[j], s), pair(-1.0f, -1.0f));
+                    f.ba[j] = mul2(wa[j], s);
+                    f.bb[j] = mul2(wb[j], c);
+                } else if (TURN == kNeighbours && turned) {
+                    const float ca_ = turns[warp][0][8 * u + j], sa = turns[warp][1][8 * u + j], cb_ = turns[warp][0][8 * u + 4 + j],
+                                sb = turns[warp][1][8 * u + 4 + j];
+                    float x, y;
+                    unpair(wa[j], x, y);
+                    f.aa[j] = pair(x * ca_, y * ca_);
+                    f.ab[j] = pair(-y * sa, x * sa);
+                    unpair(wb[j], x, y);
+                    f.bb[j] = pair(x * cb_, y * cb_);
+                    f.ba[j] = pair(-y * sb, x * sb);
+                } else {
+                    f.aa[j] = wa[j];
+                    f.bb[j] = wb[j];
+                }
+            }
+        }
+#pragma unroll 1
+        for (; r < end; r += kFlight) {
+#pragma unroll
+            for (int k = 0; k < kFlight; k++) {
+                if (r + k >= end) break;
+                Unit y = next[k];
+                load(next[k], src + kFlight * src_step, r + k + kFlight < end && left > kFlight * at_once);
+                src += src_step;
+                if (norm || TURN != kStraight) {
+                    uint64_t xa[4], xb[4];
+                    widen8<T>(y.a, xa);
+                    widen8<T>(y.b, xb);
+                    uint64_t by = 0;
+                    if (norm) {
+                        uint64_t squares = mul2(xa[0], xa[0]);
+#pragma unroll
+                        for (int j = 1; j < 4; j++) squares = fma2(xa[j], xa[j], squares);
+#pragma unroll
+                        for (int j = 0; j < 4; j++) squares = fma2(xb[j], xb[j], squares);
+                        float sum, more;
+                        unpair(squares, sum, more);
+                        sum += more;
+                        for (int o = lanes / 2; o; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
+                        const float inv = rsqrtf(sum * d.per_dim + d.eps);
+                        by = pair(inv, inv);
+                    }
+                    turn_and_weigh<TURN, NORM>(xa, xb, f, turned);
+                    if (norm) {
+#pragma unroll
+                        for (int j = 0; j < 4; j++) {
+                            xa[j] = mul2(xa[j], by);
+                            xb[j] = mul2(xb[j], by);
+                        }
+                    }
+                    if (norm || turned) y = Unit{narrow8<T>(xa), narrow8<T>(xb)};
+                }
+                store(dst, y, left > 0);
+                dst += dst_step;
+                left -= at_once;
+            }
         }
     }
-    for (int r0 = 0; r0 < d.rounds; r0 += kAtOnce) {
-        Unit x[kAtOnce];
-#pragma unroll
-        for (int r = 0; r < kAtOnce; r++) {
-            const int h = h0 + (r0 + r) * kHeads;
-            const T *src = h < d.q_heads ? (const T *)d.q + b * d.qs[0] + i * d.qs[1] + h * d.qs[2]
-                         : h < d.q_heads + d.kv_heads ? (const T *)d.k + b * d.ks[0] + i * d.ks[1] + (h - d.q_heads) * d.ks[2]
-                                                      : (const T *)d.v + b * d.vs[0] + i * d.vs[1] + (h - d.q_heads - d.kv_heads) * d.vs[2];
-            const bool read = r0 + r < d.rounds && h < heads && (h < d.q_heads ? there : stored);
-            x[r].a = read && has_a ? *(const uint4 *)(src + ca * 8) : make_uint4(0, 0, 0, 0);
-            x[r].b = read && has_b ? *(const uint4 *)(src + cb * 8) : make_uint4(0, 0, 0, 0);
-        }
-#pragma unroll
-        for (int r = 0; r < kAtOnce; r++) {
-            if (r0 + r >= d.rounds) break;
-            const int h = h0 + (r0 + r) * kHeads;
-            const bool query = h < d.q_heads, key = !query && h < d.q_heads + d.kv_heads;
-            const T *weights = query ? (const T *)d.q_norm : key ? (const T *)d.k_norm : nullptr;
-            const bool turn = turned && (query || key);
-            Unit y = x[r];
-            float xa[8], xb[8];
-            widen8<T>(y.a, xa);
-            widen8<T>(y.b, xb);
-            if (d.q_norm || d.k_norm) {               // by every lane: the sum is over lanes
-                float sum = 0.0f;
-#pragma unroll
-                for (int j = 0; j < 8; j++) sum += xa[j] * xa[j] + xb[j] * xb[j];
-#pragma unroll
-                for (int o = L / 2; o; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
-                if (weights) {
-                    const float inv = rsqrtf(sum / (float)d.dim + d.eps);
-                    float wa[8] = {}, wb[8] = {};
-                    if (has_a) widen8<T>(__ldg((const uint4 *)(weights + ca * 8)), wa);
-                    if (has_b) widen8<T>(__ldg((const uint4 *)(weights + cb * 8)), wb);
-#pragma unroll
-                    for (int j = 0; j < 8; j++) {
-                        xa[j] = xa[j] * inv * wa[j];
-                        xb[j] = xb[j] * inv * wb[j];
-                    }
-                }
-            }
-            if (turn && !d.interleaved) {
-#pragma unroll
-                for (int j = 0; j < 8; j++) {
-                    const float p = xa[j], q = xb[j];
-                    xa[j] = p * cosine[j] - q * sine[j];
-                    xb[j] = p * sine[j] + q * cosine[j];
-                }
-            } else if (turn) {
-#pragma unroll
-                for (int j = 0; j < 4; j++) {
-                    const float p = xa[2 * j], q = xa[2 * j + 1], s = xb[2 * j], t = xb[2 * j + 1];
-                    xa[2 * j] = p * cosine[j] - q * sine[j];
-                    xa[2 * j + 1] = p * sine[j] + q * cosine[j];
-                    xb[2 * j] = s * cosine[4 + j] - t * sine[4 + j];
-                    xb[2 * j + 1] = s * sine[4 + j] + t * cosine[4 + j];
-                }
-            }
-            if (turn || weights) {
-                y.a = narrow8<T>(xa);
-                y.b = narrow8<T>(xb);
-            }
-            T *dst;
-            if (query) {
-                dst = (T *)d.out + b * d.os[0] + i * d.os[1] + h * d.os[2];
-                if (!there) y = Unit{make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
-            } else {
-                if (h >= heads || !stored) continue;
-                dst = key ? (T *)d.ok + page * d.oks[0] + place * d.oks[1] + (h - d.q_heads) * d.oks[2]
-                          : (T *)d.ov + page * d.ovs[0] + place * d.ovs[1] + (h - d.q_heads - d.kv_heads) * d.ovs[2];
-            }
-            if (has_a) *(uint4 *)(dst + ca * 8) = y.a;
-            if (has_b) *(uint4 *)(dst + cb * 8) = y.b;
-        }
+    // values
+    const int base = q_rounds + kv_rounds;
+    if (r1 <= base || !stored) return;
+    int r = max(r0, base);
+    const int h = (r - base) * at_once + sub;
+    src = (const T *)d.v + b * d.vs[0] + i * d.vs[1] + h * d.vs[2] + ca * 8;
+    dst = (T *)d.ov + page * d.ovs[0] + place * d.ovs[1] + h * d.ovs[2] + ca * 8;
+    left = heads_left(d.kv_heads, r - base);
+#pragma unroll 2
+    for (; r < r1; r++, left -= at_once) {
+        Unit x = nothing;
+        load(x, src, left > 0);
+        store(dst, x, left > 0);
+        src += d.vs[2] * at_once;
+        dst += d.ovs[2] * at_once;
     }
 }
 
@@ -198,14 +308,13 @@ int check_shape(const bcast_serve_append_args &a)
 }
 
 template <typename T>
-int run(const AppendDev &d, int lanes, unsigned blocks, cudaStream_t st)
+int run(const AppendDev &d, bool norm, int turn, unsigned blocks, cudaStream_t st)
 {
-    const dim3 threads(kAppendThreads);
-    switch (lanes) {
-    case 1: return launch(serve_append_kernel<T, 1>, dim3(blocks), threads, 0, st, false, 1, d);
-    case 2: return launch(serve_append_kernel<T, 2>, dim3(blocks), threads, 0, st, false, 1, d);
-    case 4: return launch(serve_append_kernel<T, 4>, dim3(blocks), threads, 0, st, false, 1, d);
-    default: return launch(serve_append_kernel<T, 8>, dim3(blocks), threads, 0, st, false, 1, d);
+    const auto go = [&](auto kernel) { return launch(kernel, dim3(blocks), dim3(kAppendThreads), 0, st, false, 1, d); };
+    switch (turn) {
+    case kStraight: return norm ? go(serve_append_kernel<T, true, kStraight>) : go(serve_append_kernel<T, false, kStraight>);
+    case kHalves: return norm ? go(serve_append_kernel<T, true, kHalves>) : go(serve_append_kernel<T, false, kHalves>);
+    default: return norm ? go(serve_append_kernel<T, true, kNeighbours>) : go(serve_append_kernel<T, false, kNeighbours>);
     }
 }
 
@@ -280,18 +389,25 @@ extern "C" int bcast_serve_append(const bcast_serve_append_args *args, void *cud
     d.kv_heads = a.kv_heads;
     d.dim = a.dim;
     d.page = paged ? a.page_size : 1;
+    d.page_shift = -1;
+    for (int i = 0; i < 31; i++)
+        if (d.page == 1 << i) d.page_shift = i;
     d.rot = a.rot;
-    d.interleaved = a.interleaved != 0;
     d.axes = a.axes;
     d.eps = a.eps;
-    const int lanes = a.dim <= 16 ? 1 : a.dim <= 32 ? 2 : a.dim <= 64 ? 4 : 8;
-    const int64_t tokens = (int64_t)a.batch * a.new_tokens, rounds = ceil_div(a.q_heads + 2 * a.kv_heads, 32 / lanes);
-    // Few tokens: a warp to every 32 / L heads; many: several rounds to a warp, which makes the cosines once for them.
+    d.per_dim = 1.0f / (float)a.dim;
+    d.lanes_shift = a.dim <= 16 ? 0 : a.dim <= 32 ? 1 : a.dim <= 64 ? 2 : 3;
+    const int64_t tokens = (int64_t)a.batch * a.new_tokens, at_once = 32 >> d.lanes_shift;
+    const int64_t rounds = ceil_div(a.q_heads, at_once) + 2 * ceil_div(a.kv_heads, at_once);
+    // Few tokens: a warp to every round; many: a warp to a token, which makes the cosines once for all its heads.
     const bool few = tokens * rounds <= 16 * kSms;
-    d.rounds = few ? 1 : (int32_t)(rounds < 2 * kAtOnce ? rounds : 2 * kAtOnce);
+    d.rounds = few ? 1 : (int32_t)(rounds < 16 ? rounds : 16);
     d.groups = (int32_t)ceil_div(rounds, d.rounds);
-    d.items = tokens * d.groups;
-    const unsigned blocks = (unsigned)ceil_div(d.items, kAppendThreads / 32);
+    if (tokens * d.groups > kMaxDim) return BCAST_ERR_INVAL;
+    d.items = (int32_t)(tokens * d.groups);
+    const int64_t blocks = ceil_div(d.items, kAppendThreads / 32);
+    const bool norm = a.q_norm || a.k_norm;
+    const int turn = a.rot == 0 ? kStraight : a.interleaved ? kNeighbours : kHalves;
     const cudaStream_t st = (cudaStream_t)cuda_stream;
-    return a.dtype == BCAST_SERVE_BF16 ? run<__nv_bfloat16>(d, lanes, blocks, st) : run<__half>(d, lanes, blocks, st);
+    return a.dtype == BCAST_SERVE_BF16 ? run<__nv_bfloat16>(d, norm, turn, (unsigned)blocks, st) : run<__half>(d, norm, turn, (unsigned)blocks, st);
 }
