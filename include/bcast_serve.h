@@ -279,7 +279,7 @@ int bcast_serve_logprobs(const bcast_serve_logprobs_args *args /* HOST */, void 
  * and to 6 above that.  A block with NaN or an infinity in it becomes NaN.
  * bcast_serve_unpack4 -- codes and scales to values, rounded once to the data type.
  *   dtype   of values: BCAST_SERVE_BF16, BCAST_SERVE_FP16 or BCAST_SERVE_FP32
- *   0 <= rows < 2^31 - 65536;  k a multiple of 32, 32..2^24
+ *   0 <= rows < 2^31 - 65536;  k a multiple of 32, 32..2^24;  at most 2^36 numbers, both rounded up to 128
  *   values  [rows][k], rows at values_stride: at least k, a multiple of 8; starts on a 16-byte boundary
  *   codes_stride at least k / 2, a multiple of 16; codes and scales start on 16-byte boundaries
  */
@@ -299,7 +299,7 @@ int bcast_serve_unpack4(const bcast_serve_pack4_args *args /* HOST */, void *cud
  * them, x4[t] what pack4 makes of x[t].  Sums are held in 32 bits, y is rounded once.  A block of x[t] with NaN or an
  * infinity in it makes y[t] NaN, a block of W that is NaN its feature.
  *   dtype        BCAST_SERVE_BF16 or BCAST_SERVE_FP16: x, bias and y
- *   tokens       0 <= T <= 2^21;  k a multiple of 32, 32..2^24;  1 <= n <= 2^24
+ *   tokens       0 <= T <= 2^21;  k a multiple of 32, 32..2^24, T * k at most 2^36, k rounded up to 128;  1 <= n <= 2^24
  *   x [T][k], y [T][n]: rows at x_stride (a multiple of 8), y_stride;  bias [n] or NULL
  *   codes, codes_stride, scales: of W [n][k], as above
  */

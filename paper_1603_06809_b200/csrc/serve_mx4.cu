@@ -32,17 +32,29 @@ constexpr int kPackThreads = 256, kPackRows = 4;      // rows of a thread, whose
 struct PackDev {
     void *values;
     uint8_t *codes, *scales;
-    int64_t vs, cs, rows, tiles_k;        // tiles_k: of four blocks, to a row
-    int32_t k, tile, atoms, segments;     // segments: blocks of threads to a row
-    int64_t padded;                       // rows that have a place among the scales, up to which zeros are written
+    int64_t vs, cs;
+    int32_t rows, padded;                 // padded: rows that have a place among the scales, up to which zeros are written
+    int32_t k, tiles_k, eights;           // tiles_k: of four blocks, to a row; eights: threads to a row, a multiple of 16
+    int32_t tile, atoms;
+    uint32_t threads;
 };
 
-__device__ __forceinline__ int64_t scale_at(const PackDev &d, int64_t row, int32_t block)
-{
-    const int64_t tile = row / d.tile;
-    const int r = (int)(row - tile * d.tile);
-    return ((tile * d.tiles_k + block / 4) * d.atoms + r / 128) * kAtom + r % 32 * 16 + r % 128 / 32 * 4 + block % 4;
-}
+// Where a thread works: eight numbers from 8 * eight on, of rows row0 to row0 + 3.  The rows' scales are in one tile and
+// in one of its groups of 32, so 16 bytes apart from `scale` on.
+struct Eights {
+    int32_t row0, eight;
+    int64_t scale;
+    bool there;
+    __device__ __forceinline__ explicit Eights(const PackDev &d)
+    {
+        const uint32_t at = blockIdx.x * kPackThreads + threadIdx.x, group = at / (uint32_t)d.eights;
+        row0 = (int32_t)group * kPackRows;
+        eight = (int32_t)(at - group * (uint32_t)d.eights);
+        there = at < d.threads && eight * 8 < d.k;
+        const uint32_t tile = (uint32_t)row0 / (uint32_t)d.tile, r = (uint32_t)row0 - tile * (uint32_t)d.tile, block = (uint32_t)eight / 4;
+        scale = (((int64_t)tile * d.tiles_k + block / 4) * d.atoms + r / 128) * kAtom + r % 32 * 16 + r % 128 / 32 * 4 + block % 4;
+    }
+};
 
 // The scale's byte from the largest magnitude's bits: its exponent field less 2; 255 for what is not finite.
 __device__ __forceinline__ uint32_t scale_of(uint32_t most) { return most >= 0x7f800000u ? 255u : (uint32_t)max((int)(most >> 23) - 2, 0); }
@@ -64,7 +76,7 @@ __device__ __forceinline__ uint32_t codes_of(const float *x)
         : "=r"(r) : "f"(x[0]), "f"(x[1]), "f"(x[2]), "f"(x[3]), "f"(x[4]), "f"(x[5]), "f"(x[6]), "f"(x[7]));
     return r;
 }
-__device__ __forceinline__ void numbers_of(uint32_t codes, float *x)
+__device__ __forceinline__ void numbers_of(uint32_t codes, uint64_t *x)
 {
     uint32_t h[4];
     asm("{\n\t.reg .b8 a, b, c, d;\n\tmov.b32 {a, b, c, d}, %4;\n\t"
@@ -73,58 +85,101 @@ __device__ __forceinline__ void numbers_of(uint32_t codes, float *x)
 #pragma unroll
     for (int i = 0; i < 4; i++) {
         const float2 v = __half22float2(*(const __half2 *)&h[i]);
-        x[2 * i] = v.x;
-        x[2 * i + 1] = v.y;
+        x[i] = pair(v.x, v.y);
     }
 }
 
 template <typename T> struct Eight {
     uint4 v[sizeof(T) / 2];
 };
+// Eight numbers as four pairs of floats, and back.
 template <typename T>
-__device__ __forceinline__ void widen8(const Eight<T> &raw, float *x)
+__device__ __forceinline__ void widen8(const Eight<T> &raw, uint64_t *x)
 {
-    const T *v = (const T *)&raw;
+    const uint32_t *v = (const uint32_t *)&raw;
 #pragma unroll
-    for (int i = 0; i < 8; i++) x[i] = to_f32(v[i]);
+    for (int i = 0; i < 4; i++) {
+        if constexpr (std::is_same_v<T, float>) {
+            x[i] = pair(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]));
+        } else if constexpr (std::is_same_v<T, __nv_bfloat16>) {
+            x[i] = pair(__uint_as_float(v[i] << 16), __uint_as_float(v[i] & 0xffff0000u));
+        } else {
+            const float2 f = __half22float2(*(const __half2 *)&v[i]);
+            x[i] = pair(f.x, f.y);
+        }
+    }
+}
+template <typename T>
+__device__ __forceinline__ void narrow8(Eight<T> &raw, const uint64_t *x)
+{
+    uint32_t *v = (uint32_t *)&raw;
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        float a, b;
+        unpair(x[i], a, b);
+        if constexpr (std::is_same_v<T, float>) {
+            v[2 * i] = __float_as_uint(a);
+            v[2 * i + 1] = __float_as_uint(b);
+        } else if constexpr (std::is_same_v<T, __nv_bfloat16>) {
+            asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(v[i]) : "f"(b), "f"(a));
+        } else {
+            asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(v[i]) : "f"(b), "f"(a));
+        }
+    }
+}
+// The largest magnitude's bits as a float's, over the four lanes of a block; NaN is the largest.  16-bit numbers are
+// compared two at a time.
+template <typename T>
+__device__ __forceinline__ uint32_t largest(const Eight<T> &raw)
+{
+    const uint32_t *v = (const uint32_t *)&raw;
+    if constexpr (std::is_same_v<T, float>) {
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < 8; i++) m = max(m, v[i] & 0x7fffffffu);
+        m = max(m, __shfl_xor_sync(~0u, m, 1));
+        return max(m, __shfl_xor_sync(~0u, m, 2));
+    } else {
+        uint32_t m = __vmaxu2(__vmaxu2(v[0] & 0x7fff7fffu, v[1] & 0x7fff7fffu), __vmaxu2(v[2] & 0x7fff7fffu, v[3] & 0x7fff7fffu));
+        m = __vmaxu2(m, __shfl_xor_sync(~0u, m, 1));
+        m = __vmaxu2(m, __shfl_xor_sync(~0u, m, 2));
+        m = max(m & 0xffffu, m >> 16);
+        if constexpr (std::is_same_v<T, __nv_bfloat16>) return m << 16;
+        else return __float_as_uint(__half2float(__ushort_as_half((unsigned short)m)));
+    }
 }
 
-// A block of the row's eights, to codes; four neighbouring lanes hold a block of 32, sixteen a scale tile's four.
+// Four neighbouring lanes hold a block of 32, sixteen the four blocks whose scales are neighbours.
 template <typename T>
 __global__ void __launch_bounds__(kPackThreads)
 serve_pack4_kernel(const __grid_constant__ PackDev d)
 {
-    const int segment = blockIdx.x % d.segments, eight = segment * kPackThreads + threadIdx.x;
-    const int64_t row0 = (int64_t)(blockIdx.x / d.segments) * kPackRows;
-    const int lane = threadIdx.x % 32;
-    const bool in = eight * 8 < d.k;
     launch_next();
+    const Eights e(d);
     Eight<T> raw[kPackRows];
+    const T *src = (const T *)d.values + e.row0 * d.vs + e.eight * 8;
 #pragma unroll
     for (int r = 0; r < kPackRows; r++) {
-        const uint4 *src = (const uint4 *)((const T *)d.values + (row0 + r) * d.vs + (int64_t)eight * 8);
 #pragma unroll
-        for (int i = 0; i < (int)(sizeof(T) / 2); i++) raw[r].v[i] = in && row0 + r < d.rows ? __ldg(src + i) : make_uint4(0, 0, 0, 0);
+        for (int i = 0; i < (int)(sizeof(T) / 2); i++)
+            raw[r].v[i] = e.there && e.row0 + r < d.rows ? __ldg((const uint4 *)(src + r * d.vs) + i) : make_uint4(0, 0, 0, 0);
     }
+    uint8_t *codes = d.codes + e.row0 * d.cs + e.eight * 4;
 #pragma unroll
     for (int r = 0; r < kPackRows; r++) {
-        const int64_t row = row0 + r;
-        float x[8];
+        const uint32_t s = scale_of(largest<T>(raw[r]));
+        uint64_t x[4];
         widen8<T>(raw[r], x);
-        uint32_t most = 0;                    // of the magnitudes' bits: NaN is the largest
+        const float by = inverse_of(s);
+        const uint64_t two = pair(by, by);
+        float y[8];
 #pragma unroll
-        for (int i = 0; i < 8; i++) most = max(most, __float_as_uint(x[i]) & 0x7fffffffu);
-        most = max(most, __shfl_xor_sync(~0u, most, 1));
-        most = max(most, __shfl_xor_sync(~0u, most, 2));
-        const uint32_t e = scale_of(most);
-        const float by = inverse_of(e);
-#pragma unroll
-        for (int i = 0; i < 8; i++) x[i] *= by;
-        if (in && row < d.rows) *(uint32_t *)(d.codes + row * d.cs + (int64_t)eight * 4) = e == 255 ? 0u : codes_of(x);
-        uint32_t four = e | __shfl_down_sync(~0u, e, 4) << 8;
+        for (int i = 0; i < 4; i++) unpair(mul2(x[i], two), y[2 * i], y[2 * i + 1]);
+        if (e.there && e.row0 + r < d.rows) *(uint32_t *)(codes + r * d.cs) = s == 255 ? 0u : codes_of(y);
+        uint32_t four = s | __shfl_down_sync(~0u, s, 4) << 8;
         four |= __shfl_down_sync(~0u, four, 8) << 16;
         // (what is past k read as zeros, whose scale is 0)
-        if (lane % 16 == 0 && in && row < d.padded) *(uint32_t *)(d.scales + scale_at(d, row, eight / 4)) = four;
+        if (threadIdx.x % 16 == 0 && e.there && e.row0 + r < d.padded) *(uint32_t *)(d.scales + e.scale + r * 16) = four;
     }
 }
 
@@ -132,28 +187,29 @@ template <typename T>
 __global__ void __launch_bounds__(kPackThreads)
 serve_unpack4_kernel(const __grid_constant__ PackDev d)
 {
-    const int segment = blockIdx.x % d.segments, eight = segment * kPackThreads + threadIdx.x;
-    const int64_t row0 = (int64_t)(blockIdx.x / d.segments) * kPackRows;
-    if (eight * 8 >= d.k) return;
-    uint32_t codes[kPackRows], e[kPackRows];
+    const Eights e(d);
+    if (!e.there) return;
+    uint32_t codes[kPackRows], s[kPackRows];
 #pragma unroll
     for (int r = 0; r < kPackRows; r++) {
-        const bool in = row0 + r < d.rows;
-        codes[r] = in ? __ldg((const uint32_t *)(d.codes + (row0 + r) * d.cs + (int64_t)eight * 4)) : 0u;
-        e[r] = in ? __ldg(d.scales + scale_at(d, row0 + r, eight / 4)) : 0u;
+        const bool in = e.row0 + r < d.rows;
+        codes[r] = in ? __ldg((const uint32_t *)(d.codes + (e.row0 + r) * d.cs + e.eight * 4)) : 0u;
+        s[r] = in ? __ldg(d.scales + e.scale + r * 16) : 0u;
     }
+    T *dst = (T *)d.values + e.row0 * d.vs + e.eight * 8;
 #pragma unroll
     for (int r = 0; r < kPackRows; r++) {
-        if (row0 + r >= d.rows) break;
-        float x[8];
+        if (e.row0 + r >= d.rows) break;
+        uint64_t x[4];
         numbers_of(codes[r], x);
-        const float by = power_of(e[r]);
+        const float by = power_of(s[r]);
+        const uint64_t two = pair(by, by);
+#pragma unroll
+        for (int i = 0; i < 4; i++) x[i] = mul2(x[i], two);
         Eight<T> raw;
+        narrow8<T>(raw, x);
 #pragma unroll
-        for (int i = 0; i < 8; i++) ((T *)&raw)[i] = from_f32<T>(x[i] * by);
-        uint4 *dst = (uint4 *)((T *)d.values + (row0 + r) * d.vs + (int64_t)eight * 8);
-#pragma unroll
-        for (int i = 0; i < (int)(sizeof(T) / 2); i++) dst[i] = raw.v[i];
+        for (int i = 0; i < (int)(sizeof(T) / 2); i++) ((uint4 *)(dst + r * d.vs))[i] = raw.v[i];
     }
 }
 
@@ -449,6 +505,7 @@ int check_pack(const bcast_serve_pack4_args *a)
     if (!a) return BCAST_ERR_INVAL;
     if (a->dtype != BCAST_SERVE_BF16 && a->dtype != BCAST_SERVE_FP16 && a->dtype != BCAST_SERVE_FP32) return BCAST_ERR_INVAL;
     if (a->rows < 0 || a->rows > kMaxDim - 65536 || a->k < kBlock || a->k > 1 << 24 || a->k % kBlock) return BCAST_ERR_INVAL;
+    if (round_up(a->rows, 128) * round_up(a->k, 128) > 1ll << 36) return BCAST_ERR_INVAL;
     if (a->rows == 0) return BCAST_OK;
     if (!stride_ok(a->values_stride, a->k, 8) || !stride_ok(a->codes_stride, a->k / 2, 16)) return BCAST_ERR_INVAL;
     int device = 0, rc;
@@ -457,31 +514,31 @@ int check_pack(const bcast_serve_pack4_args *a)
     return BCAST_OK;
 }
 
-PackDev pack_dev(const bcast_serve_pack4_args &a)
+// Rows of `k` numbers, scales in tiles of `tile` rows.
+PackDev pack_dev(void *values, int64_t vs, uint8_t *codes, int64_t cs, uint8_t *scales, int64_t rows, int64_t k, int tile)
 {
     PackDev d = {};
-    d.values = a.values;
-    d.codes = a.codes;
-    d.scales = a.scales;
-    d.vs = a.values_stride;
-    d.cs = a.codes_stride;
-    d.rows = a.rows;
-    d.k = (int32_t)a.k;
-    d.tiles_k = ceil_div(a.k, 4 * kBlock);
-    d.tile = 128;
-    d.atoms = 1;
-    d.padded = round_up(a.rows, 128);
-    d.segments = (int32_t)ceil_div(a.k, 8 * kPackThreads);
+    d.values = values;
+    d.codes = codes;
+    d.scales = scales;
+    d.vs = vs;
+    d.cs = cs;
+    d.rows = d.padded = (int32_t)rows;
+    d.k = (int32_t)k;
+    d.tiles_k = (int32_t)ceil_div(k, 4 * kBlock);
+    d.eights = (int32_t)round_up(k / 8, 16);
+    d.tile = tile;
+    d.atoms = (int32_t)ceil_div(tile, 128);
     return d;
 }
+PackDev pack_dev(const bcast_serve_pack4_args &a) { return pack_dev(a.values, a.values_stride, a.codes, a.codes_stride, a.scales, a.rows, a.k, 128); }
 
-// `rows`: how many the blocks go over.
 template <typename F>
-int over_rows(F kernel, const PackDev &d, int64_t rows, cudaStream_t st)
+int over_rows(F kernel, PackDev d, cudaStream_t st)
 {
-    const int64_t blocks = ceil_div(rows, kPackRows) * d.segments;
-    if (blocks > kMaxDim) return BCAST_ERR_INVAL;
-    return launch(kernel, dim3((unsigned)blocks), dim3(kPackThreads), 0, st, false, 1, d);
+    const int64_t threads = ceil_div(d.padded, kPackRows) * d.eights;
+    d.threads = (uint32_t)threads;        // at most 2^31: the shapes' checks see to it
+    return launch(kernel, dim3((unsigned)ceil_div(threads, kPackThreads)), dim3(kPackThreads), 0, st, false, 1, d);
 }
 
 // How a call is cut: tokens of a tile and parts of k.
@@ -510,6 +567,7 @@ int check_shape(const bcast_serve_linear4_args &a)
 {
     if (a.dtype != BCAST_SERVE_BF16 && a.dtype != BCAST_SERVE_FP16) return BCAST_ERR_INVAL;
     if (a.tokens < 0 || a.tokens > (1 << 21) || a.k < kBlock || a.k > (1 << 24) || a.k % kBlock || a.n < 1 || a.n > (1 << 24)) return BCAST_ERR_INVAL;
+    if (a.tokens * round_up(a.k, 128) > 1ll << 36) return BCAST_ERR_INVAL;
     return BCAST_OK;
 }
 
@@ -540,7 +598,7 @@ int run_product(const bcast_serve_linear4_args &a, ProductDev d, const PackDev &
 template <typename T>
 int run(const bcast_serve_linear4_args &a, const ProductDev &d, const PackDev &p, const Cut &c, cudaStream_t st)
 {
-    int rc = over_rows(serve_pack4_kernel<T>, p, a.tokens, st);
+    int rc = over_rows(serve_pack4_kernel<T>, p, st);
     if (rc) return rc;
     switch (c.tile) {
     case 32: return run_product<T, 32>(a, d, p, c, st);
@@ -561,12 +619,13 @@ int bcast_serve_pack4(const bcast_serve_pack4_args *a, void *cuda_stream)
 {
     int rc = check_pack(a);
     if (rc || a->rows == 0) return rc;
-    const PackDev d = pack_dev(*a);
+    PackDev d = pack_dev(*a);
+    d.padded = (int32_t)round_up(a->rows, 128);
     const cudaStream_t st = (cudaStream_t)cuda_stream;
     switch (a->dtype) {
-    case BCAST_SERVE_BF16: return over_rows(serve_pack4_kernel<__nv_bfloat16>, d, d.padded, st);
-    case BCAST_SERVE_FP16: return over_rows(serve_pack4_kernel<__half>, d, d.padded, st);
-    default: return over_rows(serve_pack4_kernel<float>, d, d.padded, st);
+    case BCAST_SERVE_BF16: return over_rows(serve_pack4_kernel<__nv_bfloat16>, d, st);
+    case BCAST_SERVE_FP16: return over_rows(serve_pack4_kernel<__half>, d, st);
+    default: return over_rows(serve_pack4_kernel<float>, d, st);
     }
 }
 
@@ -577,9 +636,9 @@ int bcast_serve_unpack4(const bcast_serve_pack4_args *a, void *cuda_stream)
     const PackDev d = pack_dev(*a);
     const cudaStream_t st = (cudaStream_t)cuda_stream;
     switch (a->dtype) {
-    case BCAST_SERVE_BF16: return over_rows(serve_unpack4_kernel<__nv_bfloat16>, d, d.rows, st);
-    case BCAST_SERVE_FP16: return over_rows(serve_unpack4_kernel<__half>, d, d.rows, st);
-    default: return over_rows(serve_unpack4_kernel<float>, d, d.rows, st);
+    case BCAST_SERVE_BF16: return over_rows(serve_unpack4_kernel<__nv_bfloat16>, d, st);
+    case BCAST_SERVE_FP16: return over_rows(serve_unpack4_kernel<__half>, d, st);
+    default: return over_rows(serve_unpack4_kernel<float>, d, st);
     }
 }
 
@@ -605,18 +664,9 @@ int bcast_serve_linear4(const bcast_serve_linear4_args *a, void *cuda_stream)
     if ((rc = check_workspace(a->workspace, a->workspace_bytes, bcast_serve_linear4_workspace(a), device))) return rc;
 
     const Cut c = cut_of(*a);
-    PackDev p = {};
-    p.values = const_cast<void *>(a->x);
-    p.codes = (uint8_t *)a->workspace + BCAST_SERVE_STATUS_BYTES;
-    p.scales = p.codes + x_codes_bytes(*a);
-    p.vs = a->x_stride;
-    p.cs = a->k / 2;
-    p.rows = p.padded = a->tokens;        // what has no token is read, as scales of features' columns that nobody keeps
-    p.k = (int32_t)a->k;
-    p.tiles_k = ceil_div(a->k, 4 * kBlock);
-    p.tile = c.tile;
-    p.atoms = (int32_t)ceil_div(c.tile, 128);
-    p.segments = (int32_t)ceil_div(a->k, 8 * kPackThreads);
+    // (what has no token is read too, as scales of columns that nobody keeps)
+    uint8_t *codes = (uint8_t *)a->workspace + BCAST_SERVE_STATUS_BYTES;
+    const PackDev p = pack_dev(const_cast<void *>(a->x), a->x_stride, codes, a->k / 2, codes + x_codes_bytes(*a), a->tokens, a->k, c.tile);
     ProductDev d = {};
     d.bias = a->bias;
     d.scales_w = a->scales;
