@@ -5,7 +5,8 @@
 // A thread's m may lag behind its largest logit (the exponentials' range allows it), so few steps scale the sums.
 // The most probable tokens cost the pass nothing but what the softmax needs anyway, the largest logit of each thread:
 // the K-th largest of the threads' maxima bounds the row's K-th largest logit from below, and only the threads whose
-// maximum reaches it can hold one of the K.  A warp looks through such a thread's logits once more (from L2), what
+// maximum reaches it can hold one of the K.  The bound comes from the warps' largest, 32 in all, one to a lane,
+// sorted by every warp for itself.  A warp looks through such a thread's logits once more (from L2), what
 // reaches the bound goes to a list in shared memory, and an entry's place is the number of entries before it in
 // the order (logit, then lower token).  Lists that overflow -- many equal logits, as behind a mask of the type's lowest
 // value -- take bounds that are exact, and equals in the order of their numbers.
@@ -21,10 +22,11 @@ namespace cg = cooperative_groups;
 namespace bcast_serve {
 namespace {
 
-constexpr int kProbThreads = 256, kWarps = kProbThreads / 32, kMaxTop = 32, kListSize = 1024, kMaxParts = 8;
+constexpr int kMaxTop = 32, kListSize = 1024, kMaxParts = 8;
 constexpr int kInFlight = 4;                  // vectors that a thread has under way
 constexpr float kLag = 8.0f;                  // how far a thread's maximum may lag: weights up to e^8
 constexpr float kFloor = -150.0f;             // in powers of two: what is smaller counts as nothing
+constexpr float kFar = 1048576.0f;            // a maximum beyond it is subtracted first, not in one step with log2(e)
 
 struct ProbDev {
     const void *logits;
@@ -54,16 +56,6 @@ __device__ __forceinline__ void move_to(Sums &a, float at)
     a.s *= f;
     a.at = at;
 }
-__device__ __forceinline__ void join(Sums &a, Sums b)
-{
-    const float at = fmaxf(a.at, b.at);
-    if (at == -INFINITY) return;
-    move_to(a, at);
-    move_to(b, at);
-    a.s += b.s;
-    a.w += b.w;
-}
-
 // Whole numbers in the order of the logits.  (-infinity and NaN, which counts as it, are the lowest.)
 __device__ __forceinline__ uint32_t key_of(float l)
 {
@@ -73,14 +65,22 @@ __device__ __forceinline__ uint32_t key_of(float l)
 __device__ __forceinline__ float logit_of(uint32_t key) { return __uint_as_float(key >> 31 ? key & 0x7fffffffu : ~key); }
 constexpr uint32_t kLowest = 0x007fffffu;     // of -infinity
 
+// The statistics of all lanes, the same in each.
+__device__ __forceinline__ Sums warp_join(Sums a)
+{
+    const float at = logit_of(__reduce_max_sync(~0u, key_of(a.at)));
+    if (at == -INFINITY) return a;
+    move_to(a, at);
+#pragma unroll
+    for (int o = 16; o; o >>= 1) {
+        a.s += __shfl_xor_sync(~0u, a.s, o);
+        a.w += __shfl_xor_sync(~0u, a.w, o);
+    }
+    return a;
+}
+
 // Sixteen bytes of logits.
 template <typename T> constexpr int kPer = 16 / (int)sizeof(T);
-template <typename T>
-__device__ __forceinline__ uint4 no_logits()
-{
-    const uint32_t v = std::is_same_v<T, float> ? 0xff800000u : std::is_same_v<T, __half> ? 0xfc00fc00u : 0xff80ff80u;
-    return make_uint4(v, v, v, v);
-}
 template <typename T>
 __device__ __forceinline__ void widen(const uint4 &raw, float *l)
 {
@@ -122,11 +122,13 @@ struct Span {
     }
 };
 
+// `P`: threads of a block.
+template <int P>
 struct Shared {
-    Part part;
-    Sums warp_sums[kWarps];
-    float warp_top[kWarps], warp_low[kWarps];
-    int warp_count[kWarps];
+    Part parts[kMaxParts];                    // of the first block of a cluster: what all of them found
+    Sums warp_sums[P / 32];
+    uint32_t tops[32];                        // each warp's largest keys, 1024 / P of them
+    int warp_count[P / 32];
     int listed;
     uint64_t list[kListSize];
 };
@@ -134,7 +136,8 @@ struct Shared {
 __device__ __forceinline__ uint64_t entry_of(uint32_t key, int token) { return (uint64_t)key << 32 | (uint32_t)~token; }
 __device__ __forceinline__ int token_of(uint64_t entry) { return (int)~(uint32_t)entry; }
 
-__device__ __forceinline__ void put(Shared &sh, float l, int token, uint32_t least)
+template <int P>
+__device__ __forceinline__ void put(Shared<P> &sh, float l, int token, uint32_t least)
 {
     const uint32_t key = key_of(l);
     if (key < least) return;
@@ -142,22 +145,46 @@ __device__ __forceinline__ void put(Shared &sh, float l, int token, uint32_t lea
     if (at < kListSize) sh.list[at] = entry_of(key, token);
 }
 
-// Everything of this block's part whose key is at least `least` goes to the list (as far as that goes); `mine`: this
-// thread's largest key, its edge token's among them.
-template <typename T>
-__device__ __forceinline__ void collect(Shared &sh, const Span<T> &span, int part, uint32_t mine, uint32_t least)
+// What reaches `least` of one vector, `at` the number of its first token, goes to the list.
+template <typename T, int P>
+__device__ __forceinline__ void put_vector(Shared<P> &sh, const uint4 &raw, int at, uint32_t least)
 {
-    __syncthreads();
-    if (threadIdx.x == 0) sh.listed = 0;
-    __syncthreads();
-    const int lane = threadIdx.x % 32;
-    for (uint32_t todo = __ballot_sync(~0u, mine >= least); todo; todo &= todo - 1) {
-        const int who = threadIdx.x - lane + __ffs(todo) - 1;
-        for (int v = span.v0 + who + lane * kProbThreads; v < span.v1; v += 32 * kProbThreads) {
-            float l[kPer<T>];
-            widen<T>(__ldg(span.vec + v), l);
+    float l[kPer<T>];
+    widen<T>(raw, l);
+    float most = l[0];
 #pragma unroll
-            for (int k = 0; k < kPer<T>; k++) put(sh, l[k], span.head + v * kPer<T> + k, least);
+    for (int k = 1; k < kPer<T>; k++) most = fmaxf(most, l[k]);
+    if (key_of(most) < least) return;
+#pragma unroll
+    for (int k = 0; k < kPer<T>; k++) put(sh, l[k], at + k, least);
+}
+
+// Everything of this block's part whose key is at least `least` goes to the list (as far as that goes); `mine`: this
+// thread's largest key, its edge token's among them; `held`: its vectors, where no thread has more than kInFlight.
+template <typename T, int P>
+__device__ __forceinline__ void collect(Shared<P> &sh, const Span<T> &span, int part, uint32_t mine, uint32_t least, const uint4 *held, bool again)
+{
+    if (again) {
+        __syncthreads();
+        if (threadIdx.x == 0) sh.listed = 0;
+        __syncthreads();
+    }
+    if (span.v1 - span.v0 <= kInFlight * P) {
+        if (mine >= least) {
+#pragma unroll
+            for (int u = 0; u < kInFlight; u++) {
+                const int v = span.v0 + threadIdx.x + u * P;
+                if (v < span.v1) put_vector<T, P>(sh, held[u], span.head + v * kPer<T>, least);
+            }
+        }
+    } else {
+        // a warp to a thread's logits
+        const int lane = threadIdx.x % 32;
+        for (uint32_t todo = __ballot_sync(~0u, mine >= least); todo; todo &= todo - 1) {
+            const int who = threadIdx.x - lane + __ffs(todo) - 1;
+#pragma unroll 2
+            for (int v = span.v0 + who + lane * P; v < span.v1; v += 32 * P)
+                put_vector<T, P>(sh, __ldg(span.vec + v), span.head + v * kPer<T>, least);
         }
     }
     const int token = span.edge(threadIdx.x, part);
@@ -166,11 +193,11 @@ __device__ __forceinline__ void collect(Shared &sh, const Span<T> &span, int par
 }
 
 // How many logits of the part have a key of at least `least`.
-template <typename T>
-__device__ __forceinline__ int count_of(Shared &sh, const Span<T> &span, int part, uint32_t least)
+template <typename T, int P>
+__device__ __forceinline__ int count_of(Shared<P> &sh, const Span<T> &span, int part, uint32_t least)
 {
     int n = 0;
-    for (int v = span.v0 + threadIdx.x; v < span.v1; v += kProbThreads) {
+    for (int v = span.v0 + threadIdx.x; v < span.v1; v += P) {
         float l[kPer<T>];
         widen<T>(__ldg(span.vec + v), l);
 #pragma unroll
@@ -184,19 +211,19 @@ __device__ __forceinline__ int count_of(Shared &sh, const Span<T> &span, int par
     __syncthreads();
     n = 0;
 #pragma unroll
-    for (int w = 0; w < kWarps; w++) n += sh.warp_count[w];
+    for (int w = 0; w < P / 32; w++) n += sh.warp_count[w];
     return n;
 }
 
 // The first tokens of the part whose key is `key`, in the order of their numbers, behind what is listed, until the list
 // has `want` entries.
-template <typename T>
-__device__ __forceinline__ void add_equals(Shared &sh, const Span<T> &span, int part, uint32_t key, int want)
+template <typename T, int P>
+__device__ __forceinline__ void add_equals(Shared<P> &sh, const Span<T> &span, int part, uint32_t key, int want)
 {
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
     const int begin = part == 0 ? 0 : span.head + span.v0 * kPer<T>, end = span.head + span.v1 * kPer<T> + span.tail_count;
     int have = sh.listed;
-    for (int t0 = begin; t0 < end && have < want; t0 += kProbThreads) {
+    for (int t0 = begin; t0 < end && have < want; t0 += P) {
         const int token = t0 + threadIdx.x;
         const bool equal = token < end && key_of(to_f32(span.row[token])) == key;
         const uint32_t bits = __ballot_sync(~0u, equal);
@@ -205,7 +232,7 @@ __device__ __forceinline__ void add_equals(Shared &sh, const Span<T> &span, int 
         __syncthreads();
         int at = have;
 #pragma unroll
-        for (int w = 0; w < kWarps; w++) {
+        for (int w = 0; w < P / 32; w++) {
             if (w < warp) at += sh.warp_count[w];
             have += sh.warp_count[w];
         }
@@ -217,65 +244,62 @@ __device__ __forceinline__ void add_equals(Shared &sh, const Span<T> &span, int 
     __syncthreads();
 }
 
-// The part's `want` largest logits above -infinity, or as many as there are, in order, to part.best.
-template <typename T>
-__device__ __forceinline__ void pick(Shared &sh, const Span<T> &span, int part, float mine, float low, int want)
+// The next of the warp's largest keys, and no longer this lane's where it is the first that has it.
+__device__ __forceinline__ uint32_t next_top(uint32_t &left)
 {
-    const uint32_t key = key_of(mine);
-    // The bound: a key that `want` threads' maxima reach, and few more.  `over`: one that fewer reach.
-    uint32_t least = kLowest + 1, over = key_of(sh.part.top) + 1;
-    bool exact = false;                       // `least` is the want-th largest of the threads' maxima
-    if (__syncthreads_count(key > kLowest) >= want) {
-        uint32_t next = max(key_of(low), least);
-        for (;;) {
-            const int reach = __syncthreads_count(key >= next);
-            if (reach >= want) least = next;
-            else over = next;
-            exact = over - least <= 1;
-            if (exact || (reach >= want && reach <= want + want / 2)) break;
-            next = least + (over - least) / 2;
+    const uint32_t top = __reduce_max_sync(~0u, left);
+    if ((int)(threadIdx.x % 32) == __ffs(__ballot_sync(~0u, left == top)) - 1) left = 0;
+    return top;
+}
+// The `want`-th largest of the 32 lanes' keys.
+__device__ __forceinline__ uint32_t nth_of_lanes(uint32_t key, int want)
+{
+    const int lane = threadIdx.x % 32;
+#pragma unroll
+    for (int size = 2; size <= 32; size *= 2) {
+#pragma unroll
+        for (int d = size / 2; d; d /= 2) {
+            const uint32_t other = __shfl_xor_sync(~0u, key, d);
+            const bool up = (lane & size) != 0 && size < 32, low = (lane & d) == 0;   // (descending as a whole)
+            key = low != up ? max(key, other) : min(key, other);
         }
     }
-    collect(sh, span, part, key, least);
-    if (sh.listed > kListSize) {
-        // the exact bound, and only what is above it: where many are equal to it, that is little
-        while (!exact) {
-            const uint32_t next = least + (over - least) / 2;
-            if (__syncthreads_count(key >= next) >= want) least = next;
-            else over = next;
-            exact = over - least <= 1;
-        }
-        collect(sh, span, part, key, least + 1);
-        if (sh.listed > kListSize) {
-            // the want-th largest logit itself: fewer than `want` are above it
-            over = key_of(sh.part.top) + 1;
-            while (over - least > 1) {
-                const uint32_t next = least + (over - least) / 2;
-                if (count_of(sh, span, part, next) >= want) least = next;
-                else over = next;
-            }
-            collect(sh, span, part, key, least + 1);
-        }
-        if (sh.listed < want) add_equals(sh, span, part, least, want);
-    }
-    const int listed = sh.listed;
-    for (int i = threadIdx.x; i < listed; i += kProbThreads) {
-        const uint64_t e = sh.list[i];
-        int place = 0;
-        for (int j = 0; j < listed; j++) place += sh.list[j] > e;
-        if (place < want) sh.part.best[place] = e;
-    }
-    if (threadIdx.x == 0) sh.part.count = min(listed, want);
+    return __shfl_sync(~0u, key, want - 1);
 }
 
-// One batch of logits into a thread's sums and largest logit.
-template <typename T>
-__device__ __forceinline__ void take(Sums &a, float &top, const uint4 *raw)
+// The part's `want` largest logits above -infinity, or as many as there are, to the list; `mine`: the key of this thread's
+// largest logit.  Behind a barrier after `tops` and `listed` were written.
+template <typename T, int P>
+__device__ __forceinline__ void pick(Shared<P> &sh, const Span<T> &span, int part, uint32_t mine, int want, const uint4 *held)
+{
+    // a key that `want` threads' maxima reach, and few more; where fewer threads have a logit, the lowest there is
+    uint32_t least = max(nth_of_lanes(sh.tops[threadIdx.x % 32], want), kLowest + 1);
+    collect<T, P>(sh, span, part, mine, least, held, false);
+    if (sh.listed <= kListSize) return;
+    // only what is above the bound: where many are equal to it, that is little
+    collect<T, P>(sh, span, part, mine, least + 1, held, true);
+    if (sh.listed > kListSize) {
+        // the want-th largest logit itself: fewer than `want` are above it
+        uint32_t over = key_of(INFINITY) + 1;
+        while (over - least > 1) {
+            const uint32_t next = least + (over - least) / 2;
+            if (count_of<T, P>(sh, span, part, next) >= want) least = next;
+            else over = next;
+        }
+        collect<T, P>(sh, span, part, mine, least + 1, held, true);
+    }
+    if (sh.listed < want) add_equals<T, P>(sh, span, part, least, want);
+}
+
+// N vectors of logits into a thread's sums and largest logit; `again`: the sums are to be taken another way, because of NaN,
+// of -infinity (nothing, times an infinite exponent) or of numbers far out.
+template <typename T, int N>
+__device__ __forceinline__ void take(Sums &a, float &top, bool &again, const uint4 *raw)
 {
     float most = -INFINITY;
     if constexpr (std::is_same_v<T, float>) {
 #pragma unroll
-        for (int u = 0; u < kInFlight; u++) {
+        for (int u = 0; u < N; u++) {
             float l[4];
             widen<T>(raw[u], l);
             most = fmaxf(most, fmaxf(fmaxf(l[0], l[1]), fmaxf(l[2], l[3])));
@@ -287,7 +311,7 @@ __device__ __forceinline__ void take(Sums &a, float &top, const uint4 *raw)
         for (int k = 0; k < 4; k++) {
             m[k] = ((const T2 *)raw)[k];
 #pragma unroll
-            for (int u = 1; u < kInFlight; u++) m[k] = __hmax2(m[k], ((const T2 *)(raw + u))[k]);     // passes over NaN
+            for (int u = 1; u < N; u++) m[k] = __hmax2(m[k], ((const T2 *)(raw + u))[k]);     // passes over NaN
         }
         const T2 r = __hmax2(__hmax2(m[0], m[1]), __hmax2(m[2], m[3]));
         most = fmaxf(fmaxf(most, to_f32(r.x)), to_f32(r.y));
@@ -295,157 +319,203 @@ __device__ __forceinline__ void take(Sums &a, float &top, const uint4 *raw)
     top = fmaxf(top, most);
     if (most > a.at + kLag) move_to(a, most);
     if (a.at == -INFINITY) return;
-    const uint64_t from = pair(-a.at, -a.at), unit = pair(kLog2e, kLog2e);
+    // l log2(e) - base in one step; the base is rounded, which is made good below
+    const float base = a.at * kLog2e, off = fmaf(a.at, kLog2e, -base);
+    const uint64_t from = pair(-base, -base), unit = pair(kLog2e, kLog2e);
     uint64_t s = 0, w = 0;                    // pairs of 0.0f
 #pragma unroll
-    for (int u = 0; u < kInFlight; u++) {
+    for (int u = 0; u < N; u++) {
         float l[kPer<T>];
         widen<T>(raw[u], l);
 #pragma unroll
         for (int k = 0; k < kPer<T>; k += 2) {
+            const uint64_t z = fma2(pair(l[k], l[k + 1]), unit, from);
             float x, y;
-            unpair(mul2(add2(pair(l[k], l[k + 1]), from), unit), x, y);
-            x = fmaxf(x, kFloor);             // (NaN too)
-            y = fmaxf(y, kFloor);
+            unpair(z, x, y);
             const uint64_t e = pair(exp2_approx(x), exp2_approx(y));
             s = add2(s, e);
-            w = fma2(e, pair(x, y), w);
+            w = fma2(e, z, w);
         }
     }
     float x, y;
     unpair(s, x, y);
-    a.s += x + y;
+    const float sum = x + y;
     unpair(w, x, y);
-    a.w += x + y;
+    const float more = x + y, by = exp2_approx(-off);
+    a.s += sum * by;
+    a.w += (more - off * sum) * by;
+    again = again || more != more || fabsf(a.at) > kFar;
 }
 
-template <typename T>
-__device__ __forceinline__ void fetch(uint4 *to, const Span<T> &span, int v)
+// A thread's sums once more, one logit after the other, against its largest one.
+template <typename T, int P>
+__device__ __noinline__ Sums sums_again(const uint4 *vec, int v, int end, float top)
 {
+    Sums a{top, 0.0f, 0.0f};
+    if (top == -INFINITY) return a;
+#pragma unroll 1
+    for (; v < end; v += P) {
+        float l[kPer<T>];
+        widen<T>(__ldg(vec + v), l);
 #pragma unroll
-    for (int u = 0; u < kInFlight; u++) to[u] = v + u * kProbThreads < span.v1 ? __ldg(span.vec + v + u * kProbThreads) : no_logits<T>();
+        for (int k = 0; k < kPer<T>; k++) {
+            const float z = fmaxf((l[k] - top) * kLog2e, kFloor), e = l[k] > -INFINITY ? exp2_approx(z) : 0.0f;
+            a.s += e;
+            a.w += e * z;
+        }
+    }
+    return a;
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kProbThreads, 4)
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
+
+template <typename T, int P>
+__global__ void __launch_bounds__(P, 1024 / P)
 serve_logprobs_kernel(const __grid_constant__ ProbDev d)
 {
-    __shared__ Shared sh;
+    __shared__ Shared<P> sh;
     const cg::cluster_group cluster = cg::this_cluster();
     const int part = d.parts > 1 ? (int)cluster.block_rank() : 0, lane = threadIdx.x % 32, warp = threadIdx.x / 32;
     const int64_t r = blockIdx.x / d.parts;
     const Span<T> span(d, r, part);
+    if (d.parts > 1) cluster_arrive();
+    // the given token and its logit, under way early
+    const int32_t given = part == 0 && threadIdx.x == 0 ? d.tokens[r] : -1;
     Sums a = no_sums();
     float top = -INFINITY;
+    bool again = false;
+    uint4 next[kInFlight];
     {
-        uint4 next[kInFlight];
+        // whole batches, the next one on its way while one is worked on, then what is left, vector by vector
+        constexpr int step = kInFlight * P;
         int v = span.v0 + threadIdx.x;
-        fetch(next, span, v);
-        for (; v < span.v1; v += kInFlight * kProbThreads) {
+#pragma unroll
+        for (int u = 0; u < kInFlight; u++)
+            if (v + u * P < span.v1) next[u] = __ldg(span.vec + v + u * P);
+        for (; v + step - P < span.v1 && span.v1 - span.v0 > step; v += step) {
             uint4 raw[kInFlight];
 #pragma unroll
             for (int u = 0; u < kInFlight; u++) raw[u] = next[u];
-            fetch(next, span, v + kInFlight * kProbThreads);
-            take<T>(a, top, raw);
+#pragma unroll
+            for (int u = 0; u < kInFlight; u++)
+                if (v + step + u * P < span.v1) next[u] = __ldg(span.vec + v + step + u * P);
+            take<T, kInFlight>(a, top, again, raw);
         }
+#pragma unroll
+        for (int u = 0; u < kInFlight; u++)
+            if (v + u * P < span.v1) take<T, 1>(a, top, again, next + u);
     }
+    if (again) a = sums_again<T, P>(span.vec, span.v0 + threadIdx.x, span.v1, top);
+    const float logit = given >= 0 && given < d.vocab ? to_f32(span.row[given]) : -INFINITY;
     const int edge = span.edge(threadIdx.x, part);
     if (edge >= 0) {
         const float l = to_f32(span.row[edge]);
         if (l > -INFINITY) {
-            join(a, Sums{l, 1.0f, 0.0f});
+            if (l > a.at) move_to(a, l);
+            const float z = fmaxf((l - a.at) * kLog2e, kFloor), e = exp2_approx(z);
+            a.s += e;
+            a.w += e * z;
             top = fmaxf(top, l);
         }
     }
-    const float mine = top;
-    float low = mine == -INFINITY ? INFINITY : mine;  // the lowest of the threads' largest logits
+    const uint32_t mine = key_of(top);
+    a = warp_join(a);
+    if (lane == 0) sh.warp_sums[warp] = a;
+    uint32_t left = mine;
 #pragma unroll
-    for (int o = 16; o; o >>= 1) {
-        join(a, Sums{__shfl_xor_sync(~0u, a.at, o), __shfl_xor_sync(~0u, a.s, o), __shfl_xor_sync(~0u, a.w, o)});
-        top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
-        low = fminf(low, __shfl_xor_sync(~0u, low, o));
+    for (int k = 0; k < 1024 / P; k++) {
+        const uint32_t key = next_top(left);
+        if (lane == 0) sh.tops[warp * (1024 / P) + k] = key;
+        if (d.top <= k + 1) left = 0;                 // (one to a warp at least: the row's largest logit is among them)
     }
-    if (lane == 0) {
-        sh.warp_sums[warp] = a;
-        sh.warp_top[warp] = top;
-        sh.warp_low[warp] = low;
-    }
+    if (threadIdx.x == 0) sh.listed = 0;
     __syncthreads();
-    a = sh.warp_sums[0];
-    for (int w = 0; w < kWarps; w++) {
-        if (w) join(a, sh.warp_sums[w]);
-        top = fmaxf(top, sh.warp_top[w]);
-        low = fminf(low, sh.warp_low[w]);
+    top = logit_of(__reduce_max_sync(~0u, sh.tops[lane]));
+    const int infinite = top == INFINITY ? count_of<T, P>(sh, span, part, key_of(INFINITY)) : 0;
+    if (d.top) pick<T, P>(sh, span, part, mine, d.top, next);
+    const int listed = d.top ? sh.listed : 0, count = min(listed, d.top);
+    // an entry's place in the order; where the row has several blocks, the first one is sent the entries and the sums
+    Shared<P> *const first = d.parts > 1 ? cluster.map_shared_rank(&sh, 0) : &sh;
+    if (d.parts > 1) cluster_wait();                  // it has begun
+    uint64_t entry[kListSize / P];
+    int place[kListSize / P];
+#pragma unroll
+    for (int k = 0; k < kListSize / P; k++) {
+        const int i = threadIdx.x + k * P;
+        place[k] = kListSize;
+        if (i >= listed) continue;
+        entry[k] = sh.list[i];
+        place[k] = 0;
+#pragma unroll 8
+        for (int j = 0; j < listed; j++) place[k] += sh.list[j] > entry[k];
+        if (d.parts > 1 && place[k] < count) first->parts[part].best[place[k]] = entry[k];
     }
-    if (threadIdx.x == 0) {
-        sh.part.sums = a;
-        sh.part.top = top;
-        sh.part.count = 0;
-    }
-    __syncthreads();
-    const int infinite = top == INFINITY ? count_of(sh, span, part, key_of(INFINITY)) : 0;
-    if (threadIdx.x == 0) sh.part.infinite = infinite;
-    if (d.top && top > -INFINITY) pick(sh, span, part, mine, low, d.top);
-    if (d.parts > 1) cluster.sync();
-    else __syncthreads();
-    if (part == 0) {
-        // the row's statistics, by every thread alike
-        Sums all = sh.part.sums;
-        int infinities = sh.part.infinite;
-        float most = sh.part.top;
-        for (int p = 1; p < d.parts; p++) {
-            const Part *o = cluster.map_shared_rank(&sh.part, p);
-            join(all, o->sums);
-            infinities += o->infinite;
-            most = fmaxf(most, o->top);
+    Sums all = warp_join(lane < P / 32 ? sh.warp_sums[lane] : no_sums());
+    int infinities = infinite, total = count;
+    if (d.parts > 1) {
+        if (threadIdx.x == 0) {
+            Part &mine_there = first->parts[part];
+            mine_there.sums = all;
+            mine_there.top = top;
+            mine_there.infinite = infinite;
+            mine_there.count = count;
         }
-        const bool share = most == INFINITY;          // among the infinite ones
-        const float log_sum = share ? logf((float)infinities) : logf(all.s);
+        cluster_arrive();
+        cluster_wait();
+        if (part) return;
+        // the statistics, by every thread alike, and the entries, one to a thread
+        total = 0;
+        bool has = false;
+        for (int p = 0; p < d.parts; p++) {
+            const Part &o = sh.parts[p];
+            if (p) {
+                infinities += o.infinite;
+                top = fmaxf(top, o.top);
+            }
+            const int at = (int)threadIdx.x - total, n = o.count;
+            if (at >= 0 && at < n) {
+                entry[0] = o.best[at];
+                has = true;
+            }
+            total += n;
+        }
+        all = warp_join(lane < d.parts ? sh.parts[lane].sums : no_sums());
+        if (has) sh.list[threadIdx.x] = entry[0];
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < kListSize / P; k++) place[k] = kListSize;
+        if (has) {
+            place[0] = 0;
+#pragma unroll 8
+            for (int j = 0; j < total; j++) place[0] += sh.list[j] > entry[0];
+        }
+    }
+    {
+        const bool share = top == INFINITY;           // among the infinite ones
+        const float log_sum = logf(share ? (float)infinities : all.s);
         auto logprob = [&](float l) {
             if (!(l > -INFINITY)) return -INFINITY;
             if (share) return l == INFINITY ? -log_sum : -INFINITY;
             return l - all.at - log_sum;
         };
         if (threadIdx.x == 0) {
-            const int32_t x = d.tokens[r];
-            d.logprobs[r] = x >= 0 && x < d.vocab ? logprob(to_f32(span.row[x])) : -INFINITY;
-            if (d.entropy) d.entropy[r] = most == -INFINITY ? 0.0f : share ? log_sum : fmaxf(log_sum - all.w / all.s * kLn2, 0.0f);
+            d.logprobs[r] = logprob(logit);
+            if (d.entropy) d.entropy[r] = top == -INFINITY ? 0.0f : share ? log_sum : fmaxf(log_sum - all.w / all.s * kLn2, 0.0f);
         }
-        if (d.top) {
-            const Part *mine_of = nullptr;            // the parts' lists, a thread to an entry
-            int total = 0;
-            uint64_t e = 0;
-            for (int p = 0; p < d.parts; p++) {
-                const Part *o = d.parts > 1 ? cluster.map_shared_rank(&sh.part, p) : &sh.part;
-                const int at = (int)threadIdx.x - total, n = o->count;
-                if (at >= 0 && at < n) {
-                    mine_of = o;
-                    e = o->best[at];
-                }
-                total += n;
-            }
-            if (d.parts > 1) {                        // at most 8 x 32 entries, one to a thread
-                if (mine_of) sh.list[threadIdx.x] = e;
-                __syncthreads();
-            }
-            int place = threadIdx.x;
-            if (d.parts > 1 && mine_of) {
-                place = 0;
-                for (int j = 0; j < total; j++) place += sh.list[j] > e;
-            }
-            float l = mine_of ? logprob(logit_of((uint32_t)(e >> 32))) : -INFINITY;
-            if (mine_of && place < d.top) {
-                const bool likely = !share || l > -INFINITY;
-                d.top_tokens[r * d.top + place] = likely ? token_of(e) : -1;
-                d.top_logprobs[r * d.top + place] = l;
-            }
-            if ((int)threadIdx.x >= total && (int)threadIdx.x < d.top) {
-                d.top_tokens[r * d.top + threadIdx.x] = -1;
-                d.top_logprobs[r * d.top + threadIdx.x] = -INFINITY;
-            }
+#pragma unroll
+        for (int k = 0; k < kListSize / P; k++) {
+            if (place[k] >= d.top) continue;
+            const float l = logit_of((uint32_t)(entry[k] >> 32));
+            const bool likely = !share || l == INFINITY;
+            d.top_tokens[r * d.top + place[k]] = likely ? token_of(entry[k]) : -1;
+            d.top_logprobs[r * d.top + place[k]] = logprob(l);
+        }
+        if ((int)threadIdx.x >= total && (int)threadIdx.x < d.top) {
+            d.top_tokens[r * d.top + threadIdx.x] = -1;
+            d.top_logprobs[r * d.top + threadIdx.x] = -INFINITY;
         }
     }
-    if (d.parts > 1) cluster.sync();                  // a block's memory stays until the first one has read it
 }
 
 int check_shape(const bcast_serve_logprobs_args &a)
@@ -486,14 +556,18 @@ extern "C" int bcast_serve_logprobs(const bcast_serve_logprobs_args *args, void 
     d.stride = a.logits_stride;
     d.vocab = (int32_t)a.vocab;
     d.top = a.top;
-    // few rows: several blocks to one, of at least two batches of vectors to a thread
+    // few rows: several blocks to one, of at least 2048 logits
     d.parts = 1;
-    while (d.parts < kMaxParts && a.rows * d.parts * 2 <= 4 * kSms && a.vocab >= (int64_t)d.parts * 2 * 16384) d.parts *= 2;
-    const dim3 grid((unsigned)(a.rows * d.parts)), threads(kProbThreads);
+    while (d.parts < kMaxParts && a.rows * d.parts * 2 <= 4 * kSms && a.vocab >= (int64_t)d.parts * 2 * 2048) d.parts *= 2;
     const cudaStream_t st = (cudaStream_t)cuda_stream;
+    // short rows: blocks of 128 threads, since most of a block's time is its reductions
+    const bool small = d.parts == 1 && a.vocab <= 16384;
+    const auto go = [&](auto wide, auto narrow) {
+        return launch(small ? narrow : wide, dim3((unsigned)(a.rows * d.parts)), dim3(small ? 128 : 256), 0, st, false, (unsigned)d.parts, d);
+    };
     switch (a.dtype) {
-    case BCAST_SERVE_BF16: return launch(serve_logprobs_kernel<__nv_bfloat16>, grid, threads, 0, st, false, (unsigned)d.parts, d);
-    case BCAST_SERVE_FP16: return launch(serve_logprobs_kernel<__half>, grid, threads, 0, st, false, (unsigned)d.parts, d);
-    default: return launch(serve_logprobs_kernel<float>, grid, threads, 0, st, false, (unsigned)d.parts, d);
+    case BCAST_SERVE_BF16: return go(serve_logprobs_kernel<__nv_bfloat16, 256>, serve_logprobs_kernel<__nv_bfloat16, 128>);
+    case BCAST_SERVE_FP16: return go(serve_logprobs_kernel<__half, 256>, serve_logprobs_kernel<__half, 128>);
+    default: return go(serve_logprobs_kernel<float, 256>, serve_logprobs_kernel<float, 128>);
     }
 }
