@@ -220,17 +220,14 @@ constexpr int kProductThreads = 192;
 constexpr int kMaxSplit = 8;              // blocks of a cluster that share one tile's k
 
 template <int NT> struct Tile {
-    static constexpr int atoms = (NT + 127) / 128;                 // of the tokens' scales
-    static constexpr int codes_w = kFeatures * 128, codes_x = NT * 128, scales_w = 2 * kAtom, scales_x = 2 * atoms * kAtom;
+    static constexpr int codes_w = kFeatures * 128, codes_x = NT * 128, scales_w = 2 * kAtom, scales_x = 2 * kAtom;
     static constexpr int stage = codes_w + codes_x + scales_w + scales_x;
-    static constexpr int stages = NT > 128 ? 4 : NT == 128 ? 3 : 4;
-    static constexpr int accs = NT > 128 ? 2 : 1;                  // accumulators: a second one where blocks are persistent
-    static constexpr int at_w = accs * NT, at_x = at_w + 8;        // tensor memory's columns of scales
-    static constexpr int used = at_x + 8 * atoms;
-    static constexpr int columns = used <= 64 ? 64 : used <= 128 ? 128 : used <= 256 ? 256 : 512;
+    static constexpr int stages = NT == 128 ? 3 : 4;
+    static constexpr int at_w = NT, at_x = at_w + 8, used = at_x + 8;      // tensor memory's columns of scales
+    static constexpr int columns = used <= 64 ? 64 : used <= 128 ? 128 : 256;
     static constexpr size_t smem = (size_t)stage * stages + 1024;  // + alignment
-    static_assert(stage % 1024 == 0 && used <= columns, "");
-    static_assert(accs > 1 || NT * kFeatures * 4 <= stage * stages, "partial sums take the stages' place");
+    static_assert(NT <= 128 && stage % 1024 == 0 && used <= columns, "");
+    static_assert(NT * kFeatures * 4 <= stage * stages, "partial sums take the stages' place");
 };
 
 struct ProductDev {
@@ -239,8 +236,8 @@ struct ProductDev {
     void *y;
     int *status;
     int give_up;                          // 1: begin as if a wait had run out
-    int64_t ys, tiles_k;
-    int32_t tokens, k, n, f_tiles, t_tiles;
+    int64_t ys;
+    int32_t tokens, k, n, f_tiles, t_tiles, tiles_k;
 };
 
 // Sixteen bytes and more, both ends on 16-byte boundaries.
@@ -249,11 +246,16 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
                  ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
-// 32 rows of 16 bytes, one after the other, to 32 lanes of four columns, the same for each of the four warps' lanes.
-__device__ __forceinline__ void scales_to_tmem(uint32_t dst, uint32_t src)
+// Descriptor of 32 rows of 16 bytes, one after the other, as tcgen05.cp takes them.
+__device__ __forceinline__ uint64_t scales_desc(uint32_t src) { return (uint64_t)((src >> 4) & 0x3fffu) | (uint64_t)(128 >> 4) << 32 | 1ull << 46; }
+// The instructions that follow are issued by the thread with `lead` set of a warp in uniform control flow, so that their
+// operands stay in uniform registers, where they are wanted.  (One thread in a loop of its own took about 110 cycles to issue
+// each: 8192 tokens, 4096 -> 4096 took 105 us, however much or little was loaded.)
+// 32 rows to 32 lanes of four columns, the same for each of the four warps' lanes.
+__device__ __forceinline__ void scales_to_tmem(uint32_t lead, uint32_t dst, uint64_t src)
 {
-    const uint64_t desc = (uint64_t)((src >> 4) & 0x3fffu) | (uint64_t)(128 >> 4) << 32 | 1ull << 46;
-    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(dst), "l"(desc) : "memory");
+    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.u32 q, %2, 0;\n\t@q tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;\n\t}"
+                 ::"r"(dst), "l"(src), "r"(lead) : "memory");
 }
 // Instruction descriptor, kind::mxf4: e2m1 operands, scales that are powers of two; `which` of a column's two pairs of
 // scales the instruction takes.
@@ -261,26 +263,58 @@ __device__ __forceinline__ constexpr uint32_t mx4_desc(int m, int n, int which)
 {
     return 1u << 7 | 1u << 10 | (uint32_t)(n >> 3) << 17 | 1u << 23 | (uint32_t)(m >> 4) << 24 | (uint32_t)(2 * which) << 4 | (uint32_t)(2 * which) << 29;
 }
-__device__ __forceinline__ void mma_mx4(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t scales_a, uint32_t scales_b, bool add)
+__device__ __forceinline__ void mma_mx4(uint32_t lead, uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t scales_a, uint32_t scales_b, bool add)
 {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %6, 0;\n\t"
-                 "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.block32 [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
-                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(scales_a), "r"(scales_b), "r"((uint32_t)add) : "memory");
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %6, 0;\n\tsetp.ne.u32 q, %7, 0;\n\t"
+                 "@q tcgen05.mma.cta_group::1.kind::mxf4.block_scale.block32 [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(scales_a), "r"(scales_b), "r"((uint32_t)add), "r"(lead) : "memory");
 }
 
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
 
-// Grid: one tile per cluster where a tile's k is split over a cluster, otherwise blocks that take tiles in turn, features
-// first.  A block has one warp that loads, one that issues the matrix instructions and four that bring accumulators from
-// tensor memory to y.
+// Does `v` hold for all 128 threads of barrier `id`?
+__device__ __forceinline__ bool all_of(int id, bool v)
+{
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.and.pred q, %2, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                 : "=r"(r) : "r"((uint32_t)v), "r"(id) : "memory");
+    return r;
+}
+__device__ __forceinline__ void meet(int id) { asm volatile("bar.sync %0, 128;" ::"r"(id) : "memory"); }
+
+// Sixteen tokens of lane f's feature to rows of 128 results: `out` is the first token's row.
+template <typename T>
+__device__ __forceinline__ void put16(T *out, int f, const uint32_t *v, float bias)
+{
+#pragma unroll
+    for (int i = 0; i < 16; i++) out[i * kFeatures + f] = from_f32<T>(__uint_as_float(v[i]) + bias);
+}
+// A warp brings a row of results to y, eight bytes to a lane where that may be (`whole`).  (Straight from tensor memory, a
+// lane's two bytes at a time, a tile's way out took three times as long as its products.)
+template <typename T>
+__device__ __forceinline__ void row_to(T *y, const T *row, int features, bool whole)
+{
+    const int lane = threadIdx.x % 32;
+    if (whole) {
+        if (lane * 4 < features) *(uint2 *)(y + lane * 4) = *(const uint2 *)(row + lane * 4);
+    } else {
+#pragma unroll
+        for (int k = 0; k < 4; k++)
+            if (lane + k * 32 < features) y[lane + k * 32] = row[lane + k * 32];
+    }
+}
+__device__ __forceinline__ bool whole_rows(const ProductDev &d, int features) { return features % 4 == 0 && d.ys % 4 == 0 && ((uintptr_t)d.y & 7) == 0; }
+
+// Grid: one tile of features and tokens, features first, to a block, or to a cluster that shares its k.  A block has one warp
+// that loads, one that issues the matrix instructions and four that bring the accumulator from tensor memory to y.
 template <typename T, int NT>
-__global__ void __launch_bounds__(kProductThreads, NT > 128 ? 1 : 2)
+__global__ void __launch_bounds__(kProductThreads, 2)
 serve_linear4_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w, const __grid_constant__ ProductDev d)
 {
     using S = Tile<NT>;
     extern __shared__ uint8_t raw_smem[];
-    __shared__ __align__(8) uint64_t bars[2 * S::stages + 2 * S::accs + 1];
+    __shared__ __align__(8) uint64_t bars[2 * S::stages + 2];
     __shared__ uint32_t tmem_at;
     __shared__ int gave_up;
 
@@ -290,13 +324,12 @@ serve_linear4_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_con
 
     uint8_t *smem = (uint8_t *)(((uintptr_t)raw_smem + 1023) & ~(uintptr_t)1023);
     const uint32_t stage0 = smem_u32(smem);
-    const uint32_t full = smem_u32(bars), empty = full + 8 * S::stages, acc_full = empty + 8 * S::stages, acc_empty = acc_full + 8 * S::accs,
-                   drained = acc_empty + 8 * S::accs;
+    const uint32_t full = smem_u32(bars), empty = full + 8 * S::stages, acc_full = empty + 8 * S::stages, drained = acc_full + 8;
 
-    // which tiles, and of k which stages
+    // which tile, and of k which stages
     const int k_blocks = (d.k + kDepth - 1) / kDepth;
     const int kb0 = (int)((int64_t)k_blocks * part / split), kb1 = (int)((int64_t)k_blocks * (part + 1) / split);
-    const int first_tile = blockIdx.x / split, tiles = d.f_tiles * d.t_tiles, tile_step = gridDim.x / split;
+    const int tile = blockIdx.x / split, f_tile = tile % d.f_tiles, t_tile = tile / d.f_tiles, f0 = f_tile * kFeatures, t0 = t_tile * NT;
 
     if (warp == 1) {
         tmem_alloc(smem_u32(&tmem_at), S::columns);
@@ -306,10 +339,7 @@ serve_linear4_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_con
             mbar_init(full + 8 * i, 1);
             mbar_init(empty + 8 * i, 1);
         }
-        for (int i = 0; i < S::accs; i++) {
-            mbar_init(acc_full + 8 * i, 1);
-            mbar_init(acc_empty + 8 * i, 128);
-        }
+        mbar_init(acc_full, 1);
         mbar_init(drained, 1);
         mbar_init_fence();
         tma_prefetch(&map_x);
@@ -325,112 +355,90 @@ serve_linear4_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_con
         if (lane == 0) {
             // ---- loads.  W is there already: its first stages are on their way before x is packed.
             Ring<S::stages> ring;
-            bool ok = true, waited = false;
-            for (int tile = first_tile; tile < tiles && ok; tile += tile_step) {
-                const int f_tile = tile % d.f_tiles, t_tile = tile / d.f_tiles;
-                auto load = [&](int kb, int slot, bool w) {
-                    const uint32_t bar = full + 8 * slot, at = stage0 + slot * S::stage;
-                    const int64_t kt = 2 * (int64_t)kb, have = min((int64_t)2, d.tiles_k - kt);      // tiles of scales
-                    if (w) {
-                        mbar_expect(bar, S::codes_w + S::codes_x + (uint32_t)have * (1 + S::atoms) * kAtom);
-                        tma_load(at, &map_w, kb * 64, f_tile * kFeatures, bar);
-                        bulk_load(at + S::codes_w + S::codes_x, d.scales_w + (f_tile * d.tiles_k + kt) * kAtom, (uint32_t)have * kAtom, bar);
-                        issued++;
-                    } else {
-                        tma_load(at + S::codes_w, &map_x, kb * 64, t_tile * NT, bar);
-                        bulk_load(at + S::codes_w + S::codes_x + S::scales_w, d.scales_x + (t_tile * d.tiles_k + kt) * S::atoms * kAtom,
-                                  (uint32_t)have * S::atoms * kAtom, bar);
-                    }
-                };
-                int ahead = 0;
-                if (!waited) {
-                    ahead = min(S::stages, kb1 - kb0);
-                    for (int i = 0; i < ahead; i++) load(kb0 + i, i, true);
-                    wait_previous();                  // the codes and scales of x
-                    waited = true;
+            auto load = [&](int kb, int slot, bool w) {
+                const uint32_t bar = full + 8 * slot, at = stage0 + slot * S::stage, scales = at + S::codes_w + S::codes_x;
+                const int kt = 2 * kb, have = min(2, d.tiles_k - kt);              // tiles of scales
+                if (w) {
+                    mbar_expect(bar, S::codes_w + S::codes_x + have * 2 * kAtom);
+                    tma_load(at, &map_w, kb * 64, f0, bar);
+                    bulk_load(scales, d.scales_w + ((int64_t)f_tile * d.tiles_k + kt) * kAtom, have * kAtom, bar);
+                    issued++;
+                } else {
+                    tma_load(at + S::codes_w, &map_x, kb * 64, t0, bar);
+                    bulk_load(scales + S::scales_w, d.scales_x + ((int64_t)t_tile * d.tiles_k + kt) * kAtom, have * kAtom, bar);
                 }
-                for (int kb = kb0; kb < kb1; kb++) {
-                    if (kb - kb0 >= ahead) {
-                        if (!(ok = mbar_wait(empty + 8 * ring.slot, ring.parity ^ 1u, &gave_up))) break;
-                        load(kb, ring.slot, true);
-                    }
-                    load(kb, ring.slot, false);
-                    ring.step();
+            };
+            const int ahead = min(S::stages, kb1 - kb0);
+            for (int i = 0; i < ahead; i++) load(kb0 + i, i, true);
+            wait_previous();                          // the codes and scales of x
+            for (int kb = kb0; kb < kb1; kb++) {
+                if (kb - kb0 >= ahead) {
+                    if (!mbar_wait(empty + 8 * ring.slot, ring.parity ^ 1u, &gave_up)) break;
+                    load(kb, ring.slot, true);
                 }
+                load(kb, ring.slot, false);
+                ring.step();
             }
         }
         __syncwarp();
     } else if (warp == 1) {
-        if (lane == 0) {
-            // ---- matrix instructions
-            Ring<S::stages> ring;
-            Ring<S::accs> acc;
-            bool ok = true;
-            for (int tile = first_tile; tile < tiles && ok; tile += tile_step) {
-                if (!(ok = mbar_wait(acc_empty + 8 * acc.slot, acc.parity ^ 1u, &gave_up))) break;
-                tc_fence_after();
-                const uint32_t out = tmem + acc.slot * NT;
-                for (int kb = kb0; kb < kb1; kb++) {
-                    if (!(ok = mbar_wait(full + 8 * ring.slot, ring.parity, &gave_up))) break;
-                    tc_fence_after();
-                    const uint32_t at = stage0 + ring.slot * S::stage, scales = at + S::codes_w + S::codes_x;
-                    const uint64_t a = smem_desc(at), b = smem_desc(at + S::codes_w);
-                    const int steps = min(kDepth / 64, (d.k - kb * kDepth + 63) / 64);
+        // ---- matrix instructions.  A wait that gives up does not leave the loop: the ones after it give up at once, and what
+        // is still issued only touches this block's own memory.
+        const uint32_t lead = elect_one();
+        const uint64_t a0 = smem_desc(stage0), b0 = smem_desc(stage0 + S::codes_w), s0 = scales_desc(stage0 + S::codes_w + S::codes_x);
+        Ring<S::stages> ring;
+        for (int kb = kb0; kb < kb1; kb++) {
+            mbar_wait(full + 8 * ring.slot, ring.parity, &gave_up);
+            __syncwarp();
+            tc_fence_after();
+            const uint64_t step = (uint64_t)(ring.slot * (S::stage >> 4)), a = a0 + step, b = b0 + step, s = s0 + step;
+            const int steps = min(kDepth / 64, (d.k - kb * kDepth + 63) / 64);
 #pragma unroll
-                    for (int h = 0; h < 2; h++) {
-                        if (2 * h >= steps) break;
-                        scales_to_tmem(tmem + S::at_w + 4 * h, scales + h * kAtom);
-#pragma unroll
-                        for (int i = 0; i < S::atoms; i++)
-                            scales_to_tmem(tmem + S::at_x + 4 * (h * S::atoms + i), scales + S::scales_w + (h * S::atoms + i) * kAtom);
-                    }
-#pragma unroll
-                    for (int i = 0; i < kDepth / 64; i++)
-                        if (i < steps)
-                            mma_mx4(out, a + 2 * i, b + 2 * i, mx4_desc(kFeatures, NT, i % 2), tmem + S::at_w + i / 2 * 4,
-                                    tmem + S::at_x + i / 2 * 4 * S::atoms, kb > kb0 || i > 0);
-                    mma_commit(empty + 8 * ring.slot);
-                    ring.step();
-                }
-                if (!ok) break;
-                mma_commit(acc_full + 8 * acc.slot);
-                acc.step();
+            for (int h = 0; h < 2; h++) {
+                if (2 * h >= steps) break;
+                scales_to_tmem(lead, tmem + S::at_w + 4 * h, s + h * (kAtom >> 4));
+                scales_to_tmem(lead, tmem + S::at_x + 4 * h, s + ((S::scales_w + h * kAtom) >> 4));
             }
+#pragma unroll
+            for (int i = 0; i < kDepth / 64; i++) {
+                if (i >= steps) break;
+                mma_mx4(lead, tmem, a + 2 * i, b + 2 * i, mx4_desc(kFeatures, NT, i % 2), tmem + S::at_w + i / 2 * 4, tmem + S::at_x + i / 2 * 4, kb > kb0 || i > 0);
+            }
+            mma_commit_warp(lead, empty + 8 * ring.slot);
+            ring.step();
         }
+        mma_commit_warp(lead, acc_full);
         __syncwarp();
     } else {
-        // ---- the accumulators' way out.  A warp may touch the 32 lanes of its number modulo 4.
+        // ---- the accumulator's way out.  A warp may touch the 32 lanes of its number modulo 4.
         const int quarter = warp % 4, f = quarter * 32 + lane;
-        Ring<S::accs> acc;
-        for (int tile = first_tile; tile < tiles; tile += tile_step) {
-            const bool ok = mbar_wait(acc_full + 8 * acc.slot, acc.parity, &gave_up);
-            if (!__all_sync(~0u, ok)) break;
-            tc_fence_after();
-            if (split > 1) break;                     // goes on below, with the other blocks of the cluster
-            const uint32_t src = tmem + ((uint32_t)(quarter * 32) << 16) + acc.slot * NT;
-            const int f0 = tile % d.f_tiles * kFeatures, t0 = tile / d.f_tiles * NT;
+        const bool ok = all_of(1, mbar_wait(acc_full, 0, &gave_up));
+        tc_fence_after();
+        if (ok && split == 1) {
+            // through the stages' memory, which nobody needs any more
+            T *out = (T *)smem;
             const float bias = d.bias && f0 + f < d.n ? to_f32(((const T *)d.bias)[f0 + f]) : 0.0f;
-            T *y = (T *)d.y + (int64_t)t0 * d.ys + f0 + f;
-            const int live = f0 + f < d.n ? min(NT, d.tokens - t0) : 0;
-#pragma unroll 1
+            const uint32_t src = tmem + ((uint32_t)(quarter * 32) << 16);
+#pragma unroll 2
             for (int c = 0; c < NT; c += 16) {
                 uint32_t v[16];
                 tmem_load16(src + c, v);
                 tmem_wait_load16(v);
-#pragma unroll
-                for (int i = 0; i < 16; i++)
-                    if (c + i < live) y[(int64_t)(c + i) * d.ys] = from_f32<T>(__uint_as_float(v[i]) + bias);
+                put16(out + c * kFeatures, f, v, bias);
             }
-            tc_fence_before();
-            mbar_arrive(acc_empty + 8 * acc.slot);
-            acc.step();
+            meet(1);
+            const int features = min(kFeatures, d.n - f0), live = min(NT, d.tokens - t0);
+            const bool whole = whole_rows(d, features);
+#pragma unroll 4
+            for (int c = warp - 2; c < live; c += 4) row_to((T *)d.y + (int64_t)(t0 + c) * d.ys + f0, out + c * kFeatures, features, whole);
         }
+        tc_fence_before();
     }
 
-    if (S::accs == 1 && split > 1) {
+    if (split > 1) {
         // The blocks' sums are joined: each puts its own where its stages were, block r of the cluster adds up all of
         // them for its share of the tokens, always in the same order.
-        const int f0 = first_tile % d.f_tiles * kFeatures, t0 = first_tile / d.f_tiles * NT, share = NT / split;
+        const int share = NT / split;
         if (warp >= 2) {
             const int quarter = warp % 4, f = quarter * 32 + lane;
 #pragma unroll 2
@@ -447,7 +455,7 @@ serve_linear4_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_con
         cluster_arrive();
         cluster_wait();
         const int features = min(kFeatures, d.n - f0), c0 = part * share, c1 = min(c0 + share, d.tokens - t0);
-        const bool whole = features % 4 == 0 && d.ys % 4 == 0 && ((uintptr_t)d.y & 7) == 0;
+        const bool whole = whole_rows(d, features);
 #pragma unroll 2
         for (int i = c0 * (kFeatures / 4) + tid; i < c1 * (kFeatures / 4); i += kProductThreads) {
             const int f = i % (kFeatures / 4) * 4, c = i / (kFeatures / 4);
@@ -497,6 +505,260 @@ serve_linear4_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_con
         drain_loads<S::stages>(full, issued);
         atomicExch(d.status, 1);
     }
+}
+
+// ------------------------------------------------------------------------------------------- product, two SMs to a tile
+// Many tokens: the two blocks of a cluster take 256 features x 224 tokens together.  Each holds its own 128 features' rows
+// of W and half of the tokens' rows, which the pair's instruction (cta_group::2, issued by the first block) reads from
+// both, so that each block fetches 240 rows for what takes 352 alone.  Accumulators and scales (its own features', all
+// tokens') are in each block's tensor memory.  Both blocks' loads arrive on barriers of the first, a ring of them for
+// each; the matrix instructions' completion on both blocks'.
+constexpr int kPairTokens = 224, kPairThreads = 320;
+
+struct PairTile {
+    static constexpr int half = kPairTokens / 2;
+    static constexpr int codes_w = kFeatures * 128, codes_x = half * 128, scales_w = 2 * kAtom, scales_x = 4 * kAtom;
+    static constexpr int stage = codes_w + codes_x + scales_w + scales_x, stages = 6;
+    static constexpr int at_scales = 2 * kPairTokens, scales = 24;     // columns: two accumulators, then two stages' scales
+    static constexpr int out = 16 * kFeatures * 2;                     // bytes of 16 rows of results; four such
+    static constexpr size_t smem = (size_t)stage * stages + 4 * out + 1024;
+    static_assert(stage % 1024 == 0 && codes_x % 1024 == 0 && at_scales + 2 * scales <= 512, "");
+};
+
+// The first block's copy of a barrier.
+__device__ __forceinline__ uint32_t of_first(uint32_t bar)
+{
+    uint32_t r;
+    asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(bar));
+    return r;
+}
+__device__ __forceinline__ void arrive_at(uint32_t bar)
+{
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void expect_at(uint32_t bar, uint32_t bytes)
+{
+    asm volatile("mbarrier.arrive.expect_tx.shared::cluster.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+// Into this block's memory, arriving on a barrier of the pair's first block.
+__device__ __forceinline__ void pair_load(uint32_t dst, const CUtensorMap *m, int x, int y, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+                 ::"r"(dst), "l"((uint64_t)m), "r"(x), "r"(y), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void pair_scales(uint32_t lead, uint32_t dst, uint64_t src)
+{
+    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.u32 q, %2, 0;\n\t@q tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;\n\t}"
+                 ::"r"(dst), "l"(src), "r"(lead) : "memory");
+}
+__device__ __forceinline__ void pair_mma(uint32_t lead, uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t scales_a, uint32_t scales_b, bool add)
+{
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %6, 0;\n\tsetp.ne.u32 q, %7, 0;\n\t"
+                 "@q tcgen05.mma.cta_group::2.kind::mxf4.block_scale.block32 [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(scales_a), "r"(scales_b), "r"((uint32_t)add), "r"(lead) : "memory");
+}
+// Both blocks' barriers of that place are arrived on.
+__device__ __forceinline__ void pair_commit(uint32_t lead, uint32_t bar)
+{
+    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.u32 q, %2, 0;\n\t"
+                 "@q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;\n\t}"
+                 ::"r"(bar), "h"((uint16_t)3), "r"(lead) : "memory");
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1)
+serve_linear4_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w,
+                          const __grid_constant__ CUtensorMap map_sx, const __grid_constant__ CUtensorMap map_sw, const __grid_constant__ ProductDev d)
+{
+    using S = PairTile;
+    extern __shared__ uint8_t raw_smem[];
+    __shared__ __align__(8) uint64_t bars[3 * S::stages + 2 * 2 + 1];
+    __shared__ uint32_t tmem_at;
+    __shared__ int gave_up, other[2];                 // of the first block: how many loads the other one issued, and whether it gave up
+
+    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
+    const int rank = (int)cg::this_cluster().block_rank();
+
+    uint8_t *smem = (uint8_t *)(((uintptr_t)raw_smem + 1023) & ~(uintptr_t)1023);
+    const uint32_t stage0 = smem_u32(smem);
+    const uint32_t full = smem_u32(bars), empty = full + 16 * S::stages, acc_full = empty + 8 * S::stages, acc_empty = acc_full + 16, drained = acc_empty + 16;
+    const int k_blocks = (d.k + kDepth - 1) / kDepth;
+    const int first_tile = blockIdx.x / 2, f_pairs = (d.f_tiles + 1) / 2, tiles = f_pairs * d.t_tiles, tile_step = gridDim.x / 2;
+
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&tmem_at)) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    } else if (tid == 0) {
+        gave_up = d.give_up;
+        for (int i = 0; i < S::stages; i++) {
+            mbar_init(full + 8 * i, 1);               // of the first block's loads
+            mbar_init(full + 8 * (S::stages + i), 1); // of the second's
+            mbar_init(empty + 8 * i, 1);
+        }
+        for (int i = 0; i < 2; i++) {
+            mbar_init(acc_full + 8 * i, 1);
+            mbar_init(acc_empty + 8 * i, 16);         // a lane of each warp that empties it, in both blocks
+        }
+        mbar_init(drained, 1);
+        mbar_init_fence();
+        tma_prefetch(&map_x);
+        tma_prefetch(&map_w);
+        tma_prefetch(&map_sx);
+        tma_prefetch(&map_sw);
+    }
+    tc_fence_before();
+    __syncthreads();
+    cluster_arrive();                                 // the other block's barriers are there too
+    cluster_wait();
+    tc_fence_after();
+    const uint32_t tmem = tmem_at;
+
+    int issued = 0;                                   // loads, of the thread that issues them
+    if (warp == 0) {
+        if (lane == 0) {
+            // ---- loads.  W is there already: its first stages are on their way before x is packed.
+            Ring<S::stages> ring;
+            bool ok = true, waited = false;
+            for (int tile = first_tile; tile < tiles && ok; tile += tile_step) {
+                const int f_tile = tile % f_pairs * 2 + rank, t_tile = tile / f_pairs;
+                auto load = [&](int kb, int slot, bool w) {
+                    const uint32_t bar = of_first(full + 8 * (rank * S::stages + slot)), at = stage0 + slot * S::stage, scales = at + S::codes_w + S::codes_x;
+                    if (w) {
+                        expect_at(bar, S::stage);
+                        pair_load(at, &map_w, kb * 64, f_tile * kFeatures, bar);
+                        pair_load(scales, &map_sw, kb * 256, f_tile, bar);
+                        issued++;
+                    } else {
+                        pair_load(at + S::codes_w, &map_x, kb * 64, t_tile * kPairTokens + rank * S::half, bar);
+                        pair_load(scales + S::scales_w, &map_sx, kb * 512, t_tile, bar);
+                        pair_load(scales + S::scales_w + 2 * kAtom, &map_sx, kb * 512 + 256, t_tile, bar);
+                    }
+                };
+                int ahead = 0;
+                if (!waited) {
+                    ahead = min(S::stages, k_blocks);
+                    for (int i = 0; i < ahead; i++) load(i, i, true);
+                    wait_previous();                  // the codes and scales of x
+                    waited = true;
+                }
+                for (int kb = 0; kb < k_blocks; kb++) {
+                    if (kb >= ahead) {
+                        if (!(ok = mbar_wait(empty + 8 * ring.slot, ring.parity ^ 1u, &gave_up))) break;
+                        load(kb, ring.slot, true);
+                    }
+                    load(kb, ring.slot, false);
+                    ring.step();
+                }
+            }
+        }
+        __syncwarp();
+    } else if (warp == 1) {
+        if (rank == 0) {
+            // ---- matrix instructions, for both blocks; waits that give up as above
+            const uint32_t lead = elect_one();
+            const uint64_t a0 = smem_desc(stage0), b0 = smem_desc(stage0 + S::codes_w), s0 = scales_desc(stage0 + S::codes_w + S::codes_x);
+            auto wait = [&](uint32_t bar, uint32_t parity) {
+                mbar_wait(bar, parity, &gave_up);
+                __syncwarp();
+            };
+            Ring<S::stages> ring;
+            Ring<2> acc;
+            uint32_t odd = 0;                         // which of two places the stage's scales go to
+            for (int tile = first_tile; tile < tiles; tile += tile_step) {
+                wait(acc_empty + 8 * acc.slot, acc.parity ^ 1u);
+                const uint32_t out = tmem + acc.slot * kPairTokens;
+                for (int kb = 0; kb < k_blocks; kb++) {
+                    wait(full + 8 * ring.slot, ring.parity);
+                    wait(full + 8 * (S::stages + ring.slot), ring.parity);
+                    tc_fence_after();
+                    const uint64_t step = (uint64_t)(ring.slot * (S::stage >> 4)), a = a0 + step, b = b0 + step, s = s0 + step;
+                    const uint32_t to_w = tmem + S::at_scales + odd * S::scales, to_x = to_w + 8;
+                    const int steps = min(kDepth / 64, (d.k - kb * kDepth + 63) / 64);
+#pragma unroll
+                    for (int h = 0; h < 2; h++) {
+                        pair_scales(lead, to_w + 4 * h, s + h * (kAtom >> 4));
+                        pair_scales(lead, to_x + 8 * h, s + ((S::scales_w + 2 * h * kAtom) >> 4));
+                        pair_scales(lead, to_x + 8 * h + 4, s + ((S::scales_w + (2 * h + 1) * kAtom) >> 4));
+                    }
+#pragma unroll
+                    for (int i = 0; i < kDepth / 64; i++) {
+                        if (i >= steps) break;
+                        pair_mma(lead, out, a + 2 * i, b + 2 * i, mx4_desc(2 * kFeatures, kPairTokens, i % 2), to_w + i / 2 * 4, to_x + i / 2 * 8, kb > 0 || i > 0);
+                    }
+                    pair_commit(lead, empty + 8 * ring.slot);
+                    ring.step();
+                    odd ^= 1u;
+                }
+                pair_commit(lead, acc_full + 8 * acc.slot);
+                acc.step();
+            }
+        }
+        __syncwarp();
+    } else {
+        // ---- the accumulators' way out: lane f of this block is one of its own 128 features.  Four warps take the tile's
+        // first tokens, four the others, 16 at a time through shared memory.
+        const int quarter = warp % 4, f = quarter * 32 + lane, side = (warp - 2) / 4, id = 1 + side;
+        T *const out = (T *)(smem + S::stages * S::stage + side * 2 * S::out);
+        Ring<2> acc;
+        for (int tile = first_tile; tile < tiles; tile += tile_step) {
+            // (the four warps go on together, or none does)
+            if (!all_of(id, mbar_wait(acc_full + 8 * acc.slot, acc.parity, &gave_up))) break;
+            tc_fence_after();
+            const uint32_t src = tmem + ((uint32_t)(quarter * 32) << 16) + acc.slot * kPairTokens + side * S::half;
+            const int f0 = (tile % f_pairs * 2 + rank) * kFeatures, t0 = tile / f_pairs * kPairTokens + side * S::half;
+            const float bias = d.bias && f0 + f < d.n ? to_f32(((const T *)d.bias)[f0 + f]) : 0.0f;
+            const int features = min(kFeatures, d.n - f0), live = min(S::half, d.tokens - t0);
+            const bool whole = whole_rows(d, features);
+            uint32_t v[2][16];
+            tmem_load16(src, v[0]);
+#pragma unroll
+            for (int c = 0; c < S::half / 16; c++) {
+                tmem_wait_load16(v[c & 1]);
+                if (c + 1 < S::half / 16) {
+                    tmem_load16(src + (c + 1) * 16, v[(c + 1) & 1]);
+                } else {
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) arrive_at(of_first(acc_empty + 8 * acc.slot));
+                }
+                T *const rows = out + (c & 1) * 16 * kFeatures;
+                put16(rows, f, v[c & 1], bias);
+                meet(id);                             // (what a warp still reads of the other 16 rows is not written before the next one)
+#pragma unroll
+                for (int k = 0; k < 4; k++) {
+                    const int at = quarter * 4 + k;
+                    if (c * 16 + at < live) row_to((T *)d.y + (int64_t)(t0 + c * 16 + at) * d.ys + f0, rows + at * kFeatures, features, whole);
+                }
+            }
+            acc.step();
+        }
+        tc_fence_before();
+    }
+    __syncthreads();
+    tc_fence_after();
+    // (nobody sets gave_up from here on)
+    if (tid == 0 && rank) {
+        int *there = cg::this_cluster().map_shared_rank(other, 0);
+        there[0] = issued;
+        there[1] = gave_up;
+    }
+    cluster_arrive();
+    cluster_wait();
+    if (rank == 0 && (gave_up || other[1])) {         // what was issued ends before tensor memory and the blocks' memory are given up
+        if (tid == 32) {
+            pair_commit(1, drained);
+            mbar_drain(drained, 0);
+        }
+        if (tid == 0) {
+            drain_loads<S::stages>(full, issued);
+            drain_loads<S::stages>(full + 8 * S::stages, other[0]);
+            atomicExch(d.status, 1);
+        }
+    }
+    __syncthreads();
+    cluster_arrive();                                 // the first block has no more use for the other's memory
+    cluster_wait();
+    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
 }
 
 // ------------------------------------------------------------------------------------------- host
@@ -590,9 +852,28 @@ int run_product(const bcast_serve_linear4_args &a, ProductDev d, const PackDev &
     if ((rc = tensor_map(&mx, CU_TENSOR_MAP_DATA_TYPE_UINT16, p.codes, {a.k / 4, a.tokens}, {p.cs / 2}, {64, NT}))) return rc;
     if ((rc = tensor_map(&mw, CU_TENSOR_MAP_DATA_TYPE_UINT16, a.codes, {a.k / 4, a.n}, {a.codes_stride / 2}, {64, kFeatures}))) return rc;
     if ((rc = allow_smem<serve_linear4_kernel<T, NT>>(S::smem))) return rc;
-    const int64_t blocks = S::accs > 1 && tiles > kSms ? kSms : tiles * c.split;
+    const int64_t blocks = tiles * c.split;
     if (blocks > kMaxDim) return BCAST_ERR_INVAL;
     return launch(serve_linear4_kernel<T, NT>, dim3((unsigned)blocks), dim3(kProductThreads), S::smem, st, true, c.split, mx, mw, d);
+}
+
+template <typename T>
+int run_pairs(const bcast_serve_linear4_args &a, ProductDev d, const PackDev &p, cudaStream_t st)
+{
+    using S = PairTile;
+    d.f_tiles = (int32_t)ceil_div(a.n, kFeatures);
+    d.t_tiles = (int32_t)ceil_div(a.tokens, kPairTokens);
+    CUtensorMap mx, mw, msx, msw;
+    int rc;
+    if ((rc = tensor_map(&mx, CU_TENSOR_MAP_DATA_TYPE_UINT16, p.codes, {a.k / 4, a.tokens}, {p.cs / 2}, {64, S::half}))) return rc;
+    if ((rc = tensor_map(&mw, CU_TENSOR_MAP_DATA_TYPE_UINT16, a.codes, {a.k / 4, a.n}, {a.codes_stride / 2}, {64, kFeatures}))) return rc;
+    if ((rc = flat_map(&msx, p.scales, p.tiles_k * 256, d.t_tiles, p.tiles_k * 256, 256))) return rc;
+    if ((rc = flat_map(&msw, a.scales, p.tiles_k * 128, d.f_tiles, p.tiles_k * 128, 256))) return rc;
+    if ((rc = allow_smem<serve_linear4_pair_kernel<T>>(S::smem))) return rc;
+    const int64_t pairs = (int64_t)ceil_div(d.f_tiles, 2) * d.t_tiles;
+    if (pairs > kMaxDim) return BCAST_ERR_INVAL;
+    return launch(serve_linear4_pair_kernel<T>, dim3((unsigned)(2 * (pairs < kSms / 2 ? pairs : kSms / 2))), dim3(kPairThreads), S::smem, st, true, 1, mx,
+                  mw, msx, msw, d);
 }
 
 template <typename T>
@@ -604,7 +885,7 @@ int run(const bcast_serve_linear4_args &a, const ProductDev &d, const PackDev &p
     case 32: return run_product<T, 32>(a, d, p, c, st);
     case 64: return run_product<T, 64>(a, d, p, c, st);
     case 128: return run_product<T, 128>(a, d, p, c, st);
-    default: return run_product<T, 224>(a, d, p, c, st);
+    default: return run_pairs<T>(a, d, p, st);
     }
 }
 
