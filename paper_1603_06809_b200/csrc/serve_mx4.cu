@@ -240,17 +240,29 @@ struct ProductDev {
     int32_t tokens, k, n, f_tiles, t_tiles, tiles_k;
 };
 
-// Sixteen bytes and more, both ends on 16-byte boundaries.
-__device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar)
-{
-    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-                 ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
-}
 // Descriptor of 32 rows of 16 bytes, one after the other, as tcgen05.cp takes them.
 __device__ __forceinline__ uint64_t scales_desc(uint32_t src) { return (uint64_t)((src >> 4) & 0x3fffu) | (uint64_t)(128 >> 4) << 32 | 1ull << 46; }
 // The instructions that follow are issued by the thread with `lead` set of a warp in uniform control flow, so that their
 // operands stay in uniform registers, where they are wanted.  (One thread in a loop of its own took about 110 cycles to issue
 // each: 8192 tokens, 4096 -> 4096 took 105 us, however much or little was loaded.)
+// A tile; sixteen bytes and more, both ends on 16-byte boundaries; the bytes that a barrier is to wait for.
+__device__ __forceinline__ void load_tile(uint32_t lead, uint32_t dst, const CUtensorMap *m, int x, int y, uint32_t bar)
+{
+    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.u32 q, %5, 0;\n\t"
+                 "@q cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];\n\t}"
+                 ::"r"(dst), "l"((uint64_t)m), "r"(x), "r"(y), "r"(bar), "r"(lead) : "memory");
+}
+__device__ __forceinline__ void load_bytes(uint32_t lead, uint32_t dst, const void *src, uint32_t bytes, uint32_t bar)
+{
+    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.u32 q, %4, 0;\n\t"
+                 "@q cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];\n\t}"
+                 ::"r"(dst), "l"(src), "r"(bytes), "r"(bar), "r"(lead) : "memory");
+}
+__device__ __forceinline__ void expect(uint32_t lead, uint32_t bar, uint32_t bytes)
+{
+    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.u32 q, %2, 0;\n\t@q mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n\t}"
+                 ::"r"(bar), "r"(bytes), "r"(lead) : "memory");
+}
 // 32 rows to 32 lanes of four columns, the same for each of the four warps' lanes.
 __device__ __forceinline__ void scales_to_tmem(uint32_t lead, uint32_t dst, uint64_t src)
 {
@@ -352,33 +364,32 @@ serve_linear4_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_con
 
     int issued = 0;                                   // loads, of the thread that issues them
     if (warp == 0) {
-        if (lane == 0) {
-            // ---- loads.  W is there already: its first stages are on their way before x is packed.
-            Ring<S::stages> ring;
-            auto load = [&](int kb, int slot, bool w) {
-                const uint32_t bar = full + 8 * slot, at = stage0 + slot * S::stage, scales = at + S::codes_w + S::codes_x;
-                const int kt = 2 * kb, have = min(2, d.tiles_k - kt);              // tiles of scales
-                if (w) {
-                    mbar_expect(bar, S::codes_w + S::codes_x + have * 2 * kAtom);
-                    tma_load(at, &map_w, kb * 64, f0, bar);
-                    bulk_load(scales, d.scales_w + ((int64_t)f_tile * d.tiles_k + kt) * kAtom, have * kAtom, bar);
-                    issued++;
-                } else {
-                    tma_load(at + S::codes_w, &map_x, kb * 64, t0, bar);
-                    bulk_load(scales + S::scales_w, d.scales_x + ((int64_t)t_tile * d.tiles_k + kt) * kAtom, have * kAtom, bar);
-                }
-            };
-            const int ahead = min(S::stages, kb1 - kb0);
-            for (int i = 0; i < ahead; i++) load(kb0 + i, i, true);
-            wait_previous();                          // the codes and scales of x
-            for (int kb = kb0; kb < kb1; kb++) {
-                if (kb - kb0 >= ahead) {
-                    if (!mbar_wait(empty + 8 * ring.slot, ring.parity ^ 1u, &gave_up)) break;
-                    load(kb, ring.slot, true);
-                }
-                load(kb, ring.slot, false);
-                ring.step();
+        // ---- loads.  W is there already: its first stages are on their way before x is packed.
+        const uint32_t lead = elect_one();
+        Ring<S::stages> ring;
+        auto load = [&](int kb, int slot, bool w) {
+            const uint32_t bar = full + 8 * slot, at = stage0 + slot * S::stage, scales = at + S::codes_w + S::codes_x;
+            const int kt = 2 * kb, have = min(2, d.tiles_k - kt);                  // tiles of scales
+            if (w) {
+                expect(lead, bar, S::codes_w + S::codes_x + have * 2 * kAtom);
+                load_tile(lead, at, &map_w, kb * 64, f0, bar);
+                load_bytes(lead, scales, d.scales_w + ((int64_t)f_tile * d.tiles_k + kt) * kAtom, have * kAtom, bar);
+                issued++;
+            } else {
+                load_tile(lead, at + S::codes_w, &map_x, kb * 64, t0, bar);
+                load_bytes(lead, scales + S::scales_w, d.scales_x + ((int64_t)t_tile * d.tiles_k + kt) * kAtom, have * kAtom, bar);
             }
+        };
+        const int ahead = min(S::stages, kb1 - kb0);
+        for (int i = 0; i < ahead; i++) load(kb0 + i, i, true);
+        wait_previous();                              // the codes and scales of x
+        for (int kb = kb0; kb < kb1; kb++) {
+            if (kb - kb0 >= ahead) {
+                if (!__all_sync(~0u, mbar_wait(empty + 8 * ring.slot, ring.parity ^ 1u, &gave_up))) break;
+                load(kb, ring.slot, true);
+            }
+            load(kb, ring.slot, false);
+            ring.step();
         }
         __syncwarp();
     } else if (warp == 1) {
@@ -511,9 +522,10 @@ serve_linear4_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_con
 // Many tokens: the two blocks of a cluster take 256 features x 224 tokens together.  Each holds its own 128 features' rows
 // of W and half of the tokens' rows, which the pair's instruction (cta_group::2, issued by the first block) reads from
 // both, so that each block fetches 240 rows for what takes 352 alone.  Accumulators and scales (its own features', all
-// tokens') are in each block's tensor memory.  Both blocks' loads arrive on barriers of the first, a ring of them for
-// each; the matrix instructions' completion on both blocks'.
-constexpr int kPairTokens = 224, kPairThreads = 320;
+// tokens') are in each block's tensor memory.  A warp of each block brings W, another one x; all four arrive on one barrier
+// of the first block (four barriers to a stage cost the warp that issues the products more time than the products take), and
+// the matrix instructions' completion arrives on both blocks'.
+constexpr int kPairTokens = 224, kPairThreads = 352;
 
 struct PairTile {
     static constexpr int half = kPairTokens / 2;
@@ -536,15 +548,17 @@ __device__ __forceinline__ void arrive_at(uint32_t bar)
 {
     asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
-__device__ __forceinline__ void expect_at(uint32_t bar, uint32_t bytes)
+__device__ __forceinline__ void expect_at(uint32_t lead, uint32_t bar, uint32_t bytes)
 {
-    asm volatile("mbarrier.arrive.expect_tx.shared::cluster.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.u32 q, %2, 0;\n\t@q mbarrier.arrive.expect_tx.shared::cluster.b64 _, [%0], %1;\n\t}"
+                 ::"r"(bar), "r"(bytes), "r"(lead) : "memory");
 }
 // Into this block's memory, arriving on a barrier of the pair's first block.
-__device__ __forceinline__ void pair_load(uint32_t dst, const CUtensorMap *m, int x, int y, uint32_t bar)
+__device__ __forceinline__ void pair_load(uint32_t lead, uint32_t dst, const CUtensorMap *m, int x, int y, uint32_t bar)
 {
-    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
-                 ::"r"(dst), "l"((uint64_t)m), "r"(x), "r"(y), "r"(bar) : "memory");
+    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.u32 q, %5, 0;\n\t"
+                 "@q cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];\n\t}"
+                 ::"r"(dst), "l"((uint64_t)m), "r"(x), "r"(y), "r"(bar), "r"(lead) : "memory");
 }
 __device__ __forceinline__ void pair_scales(uint32_t lead, uint32_t dst, uint64_t src)
 {
@@ -572,16 +586,16 @@ serve_linear4_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __gri
 {
     using S = PairTile;
     extern __shared__ uint8_t raw_smem[];
-    __shared__ __align__(8) uint64_t bars[3 * S::stages + 2 * 2 + 1];
+    __shared__ __align__(8) uint64_t bars[2 * S::stages + 2 * 2 + 1];
     __shared__ uint32_t tmem_at;
-    __shared__ int gave_up, other[2];                 // of the first block: how many loads the other one issued, and whether it gave up
+    __shared__ int gave_up, issued[5];                // of the first block: stages that the four brought, and whether the other block gave up
 
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
     const int rank = (int)cg::this_cluster().block_rank();
 
     uint8_t *smem = (uint8_t *)(((uintptr_t)raw_smem + 1023) & ~(uintptr_t)1023);
     const uint32_t stage0 = smem_u32(smem);
-    const uint32_t full = smem_u32(bars), empty = full + 16 * S::stages, acc_full = empty + 8 * S::stages, acc_empty = acc_full + 16, drained = acc_empty + 16;
+    const uint32_t full = smem_u32(bars), empty = full + 8 * S::stages, acc_full = empty + 8 * S::stages, acc_empty = acc_full + 16, drained = acc_empty + 16;
     const int k_blocks = (d.k + kDepth - 1) / kDepth;
     const int first_tile = blockIdx.x / 2, f_pairs = (d.f_tiles + 1) / 2, tiles = f_pairs * d.t_tiles, tile_step = gridDim.x / 2;
 
@@ -591,8 +605,7 @@ serve_linear4_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __gri
     } else if (tid == 0) {
         gave_up = d.give_up;
         for (int i = 0; i < S::stages; i++) {
-            mbar_init(full + 8 * i, 1);               // of the first block's loads
-            mbar_init(full + 8 * (S::stages + i), 1); // of the second's
+            mbar_init(full + 8 * i, 4);
             mbar_init(empty + 8 * i, 1);
         }
         for (int i = 0; i < 2; i++) {
@@ -613,44 +626,35 @@ serve_linear4_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __gri
     tc_fence_after();
     const uint32_t tmem = tmem_at;
 
-    int issued = 0;                                   // loads, of the thread that issues them
-    if (warp == 0) {
-        if (lane == 0) {
-            // ---- loads.  W is there already: its first stages are on their way before x is packed.
-            Ring<S::stages> ring;
-            bool ok = true, waited = false;
-            for (int tile = first_tile; tile < tiles && ok; tile += tile_step) {
-                const int f_tile = tile % f_pairs * 2 + rank, t_tile = tile / f_pairs;
-                auto load = [&](int kb, int slot, bool w) {
-                    const uint32_t bar = of_first(full + 8 * (rank * S::stages + slot)), at = stage0 + slot * S::stage, scales = at + S::codes_w + S::codes_x;
-                    if (w) {
-                        expect_at(bar, S::stage);
-                        pair_load(at, &map_w, kb * 64, f_tile * kFeatures, bar);
-                        pair_load(scales, &map_sw, kb * 256, f_tile, bar);
-                        issued++;
-                    } else {
-                        pair_load(at + S::codes_w, &map_x, kb * 64, t_tile * kPairTokens + rank * S::half, bar);
-                        pair_load(scales + S::scales_w, &map_sx, kb * 512, t_tile, bar);
-                        pair_load(scales + S::scales_w + 2 * kAtom, &map_sx, kb * 512 + 256, t_tile, bar);
-                    }
-                };
-                int ahead = 0;
-                if (!waited) {
-                    ahead = min(S::stages, k_blocks);
-                    for (int i = 0; i < ahead; i++) load(i, i, true);
-                    wait_previous();                  // the codes and scales of x
-                    waited = true;
+    if (warp == 0 || warp == 2) {
+        // ---- loads: W, or x.  W is there already, x once it is packed.
+        const uint32_t lead = elect_one();
+        const int which = warp / 2;
+        int count = 0;
+        Ring<S::stages> ring;
+        bool ok = true;
+        if (which) wait_previous();
+        for (int tile = first_tile; tile < tiles && ok; tile += tile_step) {
+            const int f_tile = tile % f_pairs * 2 + rank, t_tile = tile / f_pairs;
+            for (int kb = 0; kb < k_blocks; kb++) {
+                ok = __all_sync(~0u, mbar_wait(empty + 8 * ring.slot, ring.parity ^ 1u, &gave_up));
+                if (!ok) break;
+                const uint32_t bar = of_first(full + 8 * ring.slot), at = stage0 + ring.slot * S::stage, scales = at + S::codes_w + S::codes_x;
+                if (which == 0) {
+                    expect_at(lead, bar, S::codes_w + S::scales_w);
+                    pair_load(lead, at, &map_w, kb * 64, f_tile * kFeatures, bar);
+                    pair_load(lead, scales, &map_sw, kb * 256, f_tile, bar);
+                } else {
+                    // (where the tiles of scales are odd in number, the last of them comes with one that nobody uses)
+                    expect_at(lead, bar, S::codes_x + S::scales_x);
+                    pair_load(lead, at + S::codes_w, &map_x, kb * 64, t_tile * kPairTokens + rank * S::half, bar);
+                    pair_load(lead, scales + S::scales_w, &map_sx, 0, t_tile * d.tiles_k + 2 * kb, bar);
                 }
-                for (int kb = 0; kb < k_blocks; kb++) {
-                    if (kb >= ahead) {
-                        if (!(ok = mbar_wait(empty + 8 * ring.slot, ring.parity ^ 1u, &gave_up))) break;
-                        load(kb, ring.slot, true);
-                    }
-                    load(kb, ring.slot, false);
-                    ring.step();
-                }
+                count++;
+                ring.step();
             }
         }
+        if (lane == 0) cg::this_cluster().map_shared_rank(issued, 0)[2 * rank + which] = count;
         __syncwarp();
     } else if (warp == 1) {
         if (rank == 0) {
@@ -669,7 +673,6 @@ serve_linear4_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __gri
                 const uint32_t out = tmem + acc.slot * kPairTokens;
                 for (int kb = 0; kb < k_blocks; kb++) {
                     wait(full + 8 * ring.slot, ring.parity);
-                    wait(full + 8 * (S::stages + ring.slot), ring.parity);
                     tc_fence_after();
                     const uint64_t step = (uint64_t)(ring.slot * (S::stage >> 4)), a = a0 + step, b = b0 + step, s = s0 + step;
                     const uint32_t to_w = tmem + S::at_scales + odd * S::scales, to_x = to_w + 8;
@@ -697,7 +700,7 @@ serve_linear4_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __gri
     } else {
         // ---- the accumulators' way out: lane f of this block is one of its own 128 features.  Four warps take the tile's
         // first tokens, four the others, 16 at a time through shared memory.
-        const int quarter = warp % 4, f = quarter * 32 + lane, side = (warp - 2) / 4, id = 1 + side;
+        const int quarter = warp % 4, f = quarter * 32 + lane, side = (warp - 3) / 4, id = 1 + side;
         T *const out = (T *)(smem + S::stages * S::stage + side * 2 * S::out);
         Ring<2> acc;
         for (int tile = first_tile; tile < tiles; tile += tile_step) {
@@ -737,21 +740,21 @@ serve_linear4_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __gri
     __syncthreads();
     tc_fence_after();
     // (nobody sets gave_up from here on)
-    if (tid == 0 && rank) {
-        int *there = cg::this_cluster().map_shared_rank(other, 0);
-        there[0] = issued;
-        there[1] = gave_up;
-    }
+    if (tid == 0 && rank) cg::this_cluster().map_shared_rank(issued, 0)[4] = gave_up;
     cluster_arrive();
     cluster_wait();
-    if (rank == 0 && (gave_up || other[1])) {         // what was issued ends before tensor memory and the blocks' memory are given up
+    if (rank == 0 && (gave_up || issued[4])) {        // what was issued ends before tensor memory and the blocks' memory are given up
         if (tid == 32) {
             pair_commit(1, drained);
             mbar_drain(drained, 0);
         }
         if (tid == 0) {
-            drain_loads<S::stages>(full, issued);
-            drain_loads<S::stages>(full + 8 * S::stages, other[0]);
+            // (a stage that only some of the four came to is arrived on for the others)
+            int most = 0;
+            for (int k = 0; k < 4; k++) most = max(most, issued[k]);
+            for (int k = 0; k < 4; k++)
+                for (int i = issued[k]; i < most; i++) mbar_arrive(full + 8 * (i % S::stages));
+            drain_loads<S::stages>(full, most);
             atomicExch(d.status, 1);
         }
     }
@@ -867,8 +870,8 @@ int run_pairs(const bcast_serve_linear4_args &a, ProductDev d, const PackDev &p,
     int rc;
     if ((rc = tensor_map(&mx, CU_TENSOR_MAP_DATA_TYPE_UINT16, p.codes, {a.k / 4, a.tokens}, {p.cs / 2}, {64, S::half}))) return rc;
     if ((rc = tensor_map(&mw, CU_TENSOR_MAP_DATA_TYPE_UINT16, a.codes, {a.k / 4, a.n}, {a.codes_stride / 2}, {64, kFeatures}))) return rc;
-    if ((rc = flat_map(&msx, p.scales, p.tiles_k * 256, d.t_tiles, p.tiles_k * 256, 256))) return rc;
-    if ((rc = flat_map(&msw, a.scales, p.tiles_k * 128, d.f_tiles, p.tiles_k * 128, 256))) return rc;
+    if ((rc = flat_map(&msx, p.scales, 256, (int64_t)d.t_tiles * p.tiles_k, 256, 256, 2))) return rc;
+    if ((rc = flat_map(&msw, a.scales, p.tiles_k * 128, d.f_tiles, p.tiles_k * 128, 256, 1))) return rc;
     if ((rc = allow_smem<serve_linear4_pair_kernel<T>>(S::smem))) return rc;
     const int64_t pairs = (int64_t)ceil_div(d.f_tiles, 2) * d.t_tiles;
     if (pairs > kMaxDim) return BCAST_ERR_INVAL;

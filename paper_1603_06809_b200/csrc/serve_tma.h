@@ -46,13 +46,13 @@ inline int tensor_map(CUtensorMap *map, CUtensorMapDataType type, const void *ba
     return r == CUDA_SUCCESS ? BCAST_OK : bcast_internal_cuda_failed((int)cudaErrorInvalidValue);
 }
 
-// Rows of 32-bit words, `stride` words from one to the next, read a row's `box` words at a time, as they lie.
-inline int flat_map(CUtensorMap *map, const void *base, int64_t words, int64_t rows, int64_t stride, int box)
+// Rows of 32-bit words, `stride` words from one to the next, read `box` words of `box_rows` rows at a time, as they lie.
+inline int flat_map(CUtensorMap *map, const void *base, int64_t words, int64_t rows, int64_t stride, int box, int box_rows)
 {
     const auto encode = encode_tiled();
     if (!encode) return bcast_internal_cuda_failed((int)cudaErrorSymbolNotFound);
     const cuuint64_t s[2] = {(cuuint64_t)words, (cuuint64_t)rows}, st[1] = {(cuuint64_t)stride * 4};
-    const cuuint32_t b[2] = {(cuuint32_t)box, 1}, one[2] = {1, 1};
+    const cuuint32_t b[2] = {(cuuint32_t)box, (cuuint32_t)box_rows}, one[2] = {1, 1};
     const CUresult r = encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT32, 2, const_cast<void *>(base), s, st, b, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
                               CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS ? BCAST_OK : bcast_internal_cuda_failed((int)cudaErrorInvalidValue);
