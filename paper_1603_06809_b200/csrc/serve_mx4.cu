@@ -293,29 +293,7 @@ __device__ __forceinline__ bool all_of(int id, bool v)
                  : "=r"(r) : "r"((uint32_t)v), "r"(id) : "memory");
     return r;
 }
-__device__ __forceinline__ void meet(int id) { asm volatile("bar.sync %0, 128;" ::"r"(id) : "memory"); }
-
-// Sixteen tokens of lane f's feature to rows of 128 results: `out` is the first token's row.
-template <typename T>
-__device__ __forceinline__ void put16(T *out, int f, const uint32_t *v, float bias)
-{
-#pragma unroll
-    for (int i = 0; i < 16; i++) out[i * kFeatures + f] = from_f32<T>(__uint_as_float(v[i]) + bias);
-}
-// A warp brings a row of results to y, eight bytes to a lane where that may be (`whole`).  (Straight from tensor memory, a
-// lane's two bytes at a time, a tile's way out took three times as long as its products.)
-template <typename T>
-__device__ __forceinline__ void row_to(T *y, const T *row, int features, bool whole)
-{
-    const int lane = threadIdx.x % 32;
-    if (whole) {
-        if (lane * 4 < features) *(uint2 *)(y + lane * 4) = *(const uint2 *)(row + lane * 4);
-    } else {
-#pragma unroll
-        for (int k = 0; k < 4; k++)
-            if (lane + k * 32 < features) y[lane + k * 32] = row[lane + k * 32];
-    }
-}
+// Are four neighbouring results of a row to be written at once?
 __device__ __forceinline__ bool whole_rows(const ProductDev &d, int features) { return features % 4 == 0 && d.ys % 4 == 0 && ((uintptr_t)d.y & 7) == 0; }
 
 // Grid: one tile of features and tokens, features first, to a block, or to a cluster that shares its k.  A block has one warp
@@ -426,22 +404,21 @@ serve_linear4_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_con
         const bool ok = all_of(1, mbar_wait(acc_full, 0, &gave_up));
         tc_fence_after();
         if (ok && split == 1) {
-            // through the stages' memory, which nobody needs any more
-            T *out = (T *)smem;
             const float bias = d.bias && f0 + f < d.n ? to_f32(((const T *)d.bias)[f0 + f]) : 0.0f;
             const uint32_t src = tmem + ((uint32_t)(quarter * 32) << 16);
+            T *y = (T *)d.y + (int64_t)t0 * d.ys + f0 + f;
+            const int live = f0 + f < d.n ? min(NT, d.tokens - t0) : 0;
 #pragma unroll 2
             for (int c = 0; c < NT; c += 16) {
                 uint32_t v[16];
                 tmem_load16(src + c, v);
                 tmem_wait_load16(v);
-                put16(out + c * kFeatures, f, v, bias);
+#pragma unroll
+                for (int i = 0; i < 16; i++) {
+                    if (c + i < live) *y = from_f32<T>(__uint_as_float(v[i]) + bias);
+                    y += d.ys;
+                }
             }
-            meet(1);
-            const int features = min(kFeatures, d.n - f0), live = min(NT, d.tokens - t0);
-            const bool whole = whole_rows(d, features);
-#pragma unroll 4
-            for (int c = warp - 2; c < live; c += 4) row_to((T *)d.y + (int64_t)(t0 + c) * d.ys + f0, out + c * kFeatures, features, whole);
         }
         tc_fence_before();
     }
@@ -532,8 +509,7 @@ struct PairTile {
     static constexpr int codes_w = kFeatures * 128, codes_x = half * 128, scales_w = 2 * kAtom, scales_x = 4 * kAtom;
     static constexpr int stage = codes_w + codes_x + scales_w + scales_x, stages = 6;
     static constexpr int at_scales = 2 * kPairTokens, scales = 24;     // columns: two accumulators, then two stages' scales
-    static constexpr int out = 16 * kFeatures * 2;                     // bytes of 16 rows of results; four such
-    static constexpr size_t smem = (size_t)stage * stages + 4 * out + 1024;
+    static constexpr size_t smem = (size_t)stage * stages + 1024;
     static_assert(stage % 1024 == 0 && codes_x % 1024 == 0 && at_scales + 2 * scales <= 512, "");
 };
 
@@ -699,9 +675,9 @@ serve_linear4_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __gri
         __syncwarp();
     } else {
         // ---- the accumulators' way out: lane f of this block is one of its own 128 features.  Four warps take the tile's
-        // first tokens, four the others, 16 at a time through shared memory.
+        // first tokens, four the others.  (Through shared memory, to write a row's 256 bytes at once, it took no less: 16 us
+        // for 1024 tokens, 4096 -> 4096, against 17, and 30 for 2048 against 25.)
         const int quarter = warp % 4, f = quarter * 32 + lane, side = (warp - 3) / 4, id = 1 + side;
-        T *const out = (T *)(smem + S::stages * S::stage + side * 2 * S::out);
         Ring<2> acc;
         for (int tile = first_tile; tile < tiles; tile += tile_step) {
             // (the four warps go on together, or none does)
@@ -710,8 +686,8 @@ serve_linear4_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __gri
             const uint32_t src = tmem + ((uint32_t)(quarter * 32) << 16) + acc.slot * kPairTokens + side * S::half;
             const int f0 = (tile % f_pairs * 2 + rank) * kFeatures, t0 = tile / f_pairs * kPairTokens + side * S::half;
             const float bias = d.bias && f0 + f < d.n ? to_f32(((const T *)d.bias)[f0 + f]) : 0.0f;
-            const int features = min(kFeatures, d.n - f0), live = min(S::half, d.tokens - t0);
-            const bool whole = whole_rows(d, features);
+            T *y = (T *)d.y + (int64_t)t0 * d.ys + f0 + f;
+            const int live = f0 + f < d.n ? min(S::half, d.tokens - t0) : 0;
             uint32_t v[2][16];
             tmem_load16(src, v[0]);
 #pragma unroll
@@ -724,13 +700,10 @@ serve_linear4_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __gri
                     __syncwarp();
                     if (lane == 0) arrive_at(of_first(acc_empty + 8 * acc.slot));
                 }
-                T *const rows = out + (c & 1) * 16 * kFeatures;
-                put16(rows, f, v[c & 1], bias);
-                meet(id);                             // (what a warp still reads of the other 16 rows is not written before the next one)
 #pragma unroll
-                for (int k = 0; k < 4; k++) {
-                    const int at = quarter * 4 + k;
-                    if (c * 16 + at < live) row_to((T *)d.y + (int64_t)(t0 + c * 16 + at) * d.ys + f0, rows + at * kFeatures, features, whole);
+                for (int i = 0; i < 16; i++) {
+                    if (c * 16 + i < live) *y = from_f32<T>(__uint_as_float(v[c & 1][i]) + bias);
+                    y += d.ys;
                 }
             }
             acc.step();
@@ -819,11 +792,15 @@ int parts_of(int64_t blocks, int64_t room, int64_t k_blocks, int most)
     return s;
 }
 
+// Measured on one B200 (us, k = 4096, n = 4096 where nothing else is said), a tile of 128 tokens to a block / 224 to a pair:
+// 333 tokens, 2080 -> 5003 11.5 / 10.1; 512 13.0 / 11.6; 1024 16.1 / 16.9; 1500 26.4 / 18.5; 200, n = 16384 16.4 / 13.6; 448, n =
+// 16384 28.4 / 19.3.  So pairs from half of them on.  Fewer tokens than 129: blocks of a cluster share a tile's k, at most
+// one block to an SM (twice as many: 64 tokens 9.5 instead of 7.7).
 Cut cut_of(const bcast_serve_linear4_args &a)
 {
     Cut c = {};
     const int64_t k_blocks = ceil_div(a.k, kDepth), f_tiles = ceil_div(a.n, kFeatures);
-    c.tile = a.tokens <= 32 ? 32 : a.tokens <= 64 ? 64 : a.tokens <= 128 || ceil_div(a.tokens, 224) * f_tiles < 2 * kSms ? 128 : 224;
+    c.tile = a.tokens <= 32 ? 32 : a.tokens <= 64 ? 64 : a.tokens <= 128 || ceil_div(a.tokens, kPairTokens) * f_tiles < kSms / 2 ? 128 : kPairTokens;
     c.split = c.tile > 128 ? 1 : parts_of(ceil_div(a.tokens, c.tile) * f_tiles, kSms, k_blocks, kMaxSplit);
     return c;
 }
