@@ -115,6 +115,8 @@ __global__ void __launch_bounds__(kAppendThreads, kAppendBlocks)
 serve_append_kernel(const __grid_constant__ AppendDev d)
 {
     __shared__ __align__(16) float turns[kAppendThreads / 32][2][64];         // each warp's token's cosines and sines
+    wait_previous();
+    launch_next();
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
     const int lanes = 1 << d.lanes_shift, u = lane & (lanes - 1), sub = lane >> d.lanes_shift, at_once = 32 >> d.lanes_shift;
     const int item = blockIdx.x * (kAppendThreads / 32) + warp;
@@ -310,7 +312,7 @@ int check_shape(const bcast_serve_append_args &a)
 template <typename T>
 int run(const AppendDev &d, bool norm, int turn, unsigned blocks, cudaStream_t st)
 {
-    const auto go = [&](auto kernel) { return launch(kernel, dim3(blocks), dim3(kAppendThreads), 0, st, false, 1, d); };
+    const auto go = [&](auto kernel) { return launch(kernel, dim3(blocks), dim3(kAppendThreads), 0, st, true, 1, d); };
     switch (turn) {
     case kStraight: return norm ? go(serve_append_kernel<T, true, kStraight>) : go(serve_append_kernel<T, false, kStraight>);
     case kHalves: return norm ? go(serve_append_kernel<T, true, kHalves>) : go(serve_append_kernel<T, false, kHalves>);

@@ -375,6 +375,8 @@ __global__ void __launch_bounds__(P, 1024 / P)
 serve_logprobs_kernel(const __grid_constant__ ProbDev d)
 {
     __shared__ Shared<P> sh;
+    wait_previous();
+    launch_next();
     const cg::cluster_group cluster = cg::this_cluster();
     const int part = d.parts > 1 ? (int)cluster.block_rank() : 0, lane = threadIdx.x % 32, warp = threadIdx.x / 32;
     const int64_t r = blockIdx.x / d.parts;
@@ -563,7 +565,7 @@ extern "C" int bcast_serve_logprobs(const bcast_serve_logprobs_args *args, void 
     // short rows: blocks of 128 threads, since most of a block's time is its reductions
     const bool small = d.parts == 1 && a.vocab <= 16384;
     const auto go = [&](auto wide, auto narrow) {
-        return launch(small ? narrow : wide, dim3((unsigned)(a.rows * d.parts)), dim3(small ? 128 : 256), 0, st, false, (unsigned)d.parts, d);
+        return launch(small ? narrow : wide, dim3((unsigned)(a.rows * d.parts)), dim3(small ? 128 : 256), 0, st, true, (unsigned)d.parts, d);
     };
     switch (a.dtype) {
     case BCAST_SERVE_BF16: return go(serve_logprobs_kernel<__nv_bfloat16, 256>, serve_logprobs_kernel<__nv_bfloat16, 128>);

@@ -154,6 +154,8 @@ template <typename T>
 __global__ void __launch_bounds__(kPackThreads)
 serve_pack4_kernel(const __grid_constant__ PackDev d)
 {
+    // (in this order: the kernel of a product reads W before it waits for this one, and W may be what came before this one)
+    wait_previous();
     launch_next();
     const Eights e(d);
     Eight<T> raw[kPackRows];
@@ -187,6 +189,8 @@ template <typename T>
 __global__ void __launch_bounds__(kPackThreads)
 serve_unpack4_kernel(const __grid_constant__ PackDev d)
 {
+    wait_previous();
+    launch_next();
     const Eights e(d);
     if (!e.there) return;
     uint32_t codes[kPackRows], s[kPackRows];
@@ -776,7 +780,7 @@ int over_rows(F kernel, PackDev d, cudaStream_t st)
 {
     const int64_t threads = ceil_div(d.padded, kPackRows) * d.eights;
     d.threads = (uint32_t)threads;        // at most 2^31: the shapes' checks see to it
-    return launch(kernel, dim3((unsigned)ceil_div(threads, kPackThreads)), dim3(kPackThreads), 0, st, false, 1, d);
+    return launch(kernel, dim3((unsigned)ceil_div(threads, kPackThreads)), dim3(kPackThreads), 0, st, true, 1, d);
 }
 
 // How a call is cut: tokens of a tile and parts of k.
