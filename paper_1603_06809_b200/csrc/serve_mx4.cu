@@ -5,7 +5,8 @@
 //   y[t][f] = sum over blocks  2^(eW + ex) * (sum of 32 products of codes)  + bias
 // The tensor cores take both operands as they lie (kind::mxf4: 64 values of k to an instruction, a scale to every 32 of
 // a row), so W is read once, in 17/32 of a byte a number, and nothing is unpacked on the way.
-//   pack kernel     x to codes and scales, four lanes to a block: the call's own x first, in the workspace
+//   pack kernel     x to codes and scales, four lanes to a block: the call's own x first, in the workspace (up to 8 tokens
+//                   the product's blocks do it themselves)
 //   product kernel  tiles of 128 features x NT tokens as in bcast_serve_linear: features on the 128 lanes of tensor memory,
 //                   tokens the instruction's N.  A stage is 256 values of k: codes by TMA, rows of 128 bytes, and scales,
 //                   which are laid out so that a stage's are one run of memory, by bulk copies; tcgen05.cp brings
@@ -220,13 +221,14 @@ serve_unpack4_kernel(const __grid_constant__ PackDev d)
 // ------------------------------------------------------------------------------------------- product
 constexpr int kFeatures = 128;            // features per tile: the lanes of tensor memory
 constexpr int kDepth = 256;               // values of k per stage: 128 bytes of codes, one swizzled row
-constexpr int kProductThreads = 192;
+constexpr int kProductThreads = 192, kFusedThreads = 320;
+constexpr int kFusedTokens = 8;          // up to which the product's blocks pack x themselves
 constexpr int kMaxSplit = 8;              // blocks of a cluster that share one tile's k
 
-template <int NT> struct Tile {
+template <int NT, bool FUSED> struct Tile {
     static constexpr int codes_w = kFeatures * 128, codes_x = NT * 128, scales_w = 2 * kAtom, scales_x = 2 * kAtom;
     static constexpr int stage = codes_w + codes_x + scales_w + scales_x;
-    static constexpr int stages = NT == 128 ? 3 : 4;
+    static constexpr int stages = FUSED ? 8 : NT == 128 ? 3 : 4;   // FUSED: one to each warp that packs x
     static constexpr int at_w = NT, at_x = at_w + 8, used = at_x + 8;      // tensor memory's columns of scales
     static constexpr int columns = used <= 64 ? 64 : used <= 128 ? 128 : 256;
     static constexpr size_t smem = (size_t)stage * stages + 1024;  // + alignment
@@ -235,7 +237,8 @@ template <int NT> struct Tile {
 };
 
 struct ProductDev {
-    const void *bias;
+    const void *bias, *x;
+    int64_t xs;
     const uint8_t *scales_w, *scales_x;
     void *y;
     int *status;
@@ -300,15 +303,39 @@ __device__ __forceinline__ bool all_of(int id, bool v)
 // Are four neighbouring results of a row to be written at once?
 __device__ __forceinline__ bool whole_rows(const ProductDev &d, int features) { return features % 4 == 0 && d.ys % 4 == 0 && ((uintptr_t)d.y & 7) == 0; }
 
+// One row's 256 values of k from `k0` on to codes and scales in shared memory, a warp to the row, as TMA and the scales'
+// layout would have brought them.
+template <typename T>
+__device__ __forceinline__ void pack_row(uint8_t *codes, uint8_t *scales, int row, const Eight<T> &raw)
+{
+    const int lane = threadIdx.x % 32;
+    const uint32_t s = scale_of(largest<T>(raw));
+    uint64_t x[4];
+    widen8<T>(raw, x);
+    const float by = inverse_of(s);
+    const uint64_t two = pair(by, by);
+    float y[8];
+#pragma unroll
+    for (int i = 0; i < 4; i++) unpair(mul2(x[i], two), y[2 * i], y[2 * i + 1]);
+    *(uint32_t *)(codes + swizzled(row, lane / 4, 128) + lane % 4 * 4) = s == 255 ? 0u : codes_of(y);
+    uint32_t four = s | __shfl_down_sync(~0u, s, 4) << 8;
+    four |= __shfl_down_sync(~0u, four, 8) << 16;
+    if (lane % 16 == 0) *(uint32_t *)(scales + lane / 16 * kAtom + row % 32 * 16 + row / 32 * 4) = four;
+}
+
 // Grid: one tile of features and tokens, features first, to a block, or to a cluster that shares its k.  A block has one warp
 // that loads, one that issues the matrix instructions and four that bring the accumulator from tensor memory to y.
-template <typename T, int NT>
-__global__ void __launch_bounds__(kProductThreads, 2)
+// FUSED: few tokens, whose x eight warps pack for their own block, a stage to a warp: each block does it again for itself, but
+// a call is one launch.  Device time in us with a kernel for x / without, k = 4096, n = 4096: 1 token, 2048 -> 2048 5.2 / 3.7 (a
+// public call among others 9.5 / 5.8); 4 6.3 / 5.7; 16 6.7 / 8.8; 1, n = 16384 10.4 / 8.8.
+template <typename T, int NT, bool FUSED>
+__global__ void __launch_bounds__(FUSED ? kFusedThreads : kProductThreads, FUSED ? 1 : 2)
 serve_linear4_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w, const __grid_constant__ ProductDev d)
 {
-    using S = Tile<NT>;
+    using S = Tile<NT, FUSED>;
+    constexpr int threads = FUSED ? kFusedThreads : kProductThreads;
     extern __shared__ uint8_t raw_smem[];
-    __shared__ __align__(8) uint64_t bars[2 * S::stages + 2];
+    __shared__ __align__(8) uint64_t bars[3 * S::stages + 2];
     __shared__ uint32_t tmem_at;
     __shared__ int gave_up;
 
@@ -318,7 +345,8 @@ serve_linear4_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_con
 
     uint8_t *smem = (uint8_t *)(((uintptr_t)raw_smem + 1023) & ~(uintptr_t)1023);
     const uint32_t stage0 = smem_u32(smem);
-    const uint32_t full = smem_u32(bars), empty = full + 8 * S::stages, acc_full = empty + 8 * S::stages, drained = acc_full + 8;
+    const uint32_t full = smem_u32(bars), empty = full + 8 * S::stages, filled = empty + 8 * S::stages, acc_full = filled + 8 * S::stages,
+                   drained = acc_full + 8;
 
     // which tile, and of k which stages
     const int k_blocks = (d.k + kDepth - 1) / kDepth;
@@ -332,17 +360,22 @@ serve_linear4_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_con
         for (int i = 0; i < S::stages; i++) {
             mbar_init(full + 8 * i, 1);
             mbar_init(empty + 8 * i, 1);
+            if (FUSED) mbar_init(filled + 8 * i, 1);
         }
         mbar_init(acc_full, 1);
         mbar_init(drained, 1);
         mbar_init_fence();
-        tma_prefetch(&map_x);
+        if (!FUSED) tma_prefetch(&map_x);
         tma_prefetch(&map_w);
     }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = tmem_at;
+    if (FUSED) {
+        wait_previous();
+        launch_next();
+    }
 
     int issued = 0;                                   // loads, of the thread that issues them
     if (warp == 0) {
@@ -353,7 +386,7 @@ serve_linear4_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_con
             const uint32_t bar = full + 8 * slot, at = stage0 + slot * S::stage, scales = at + S::codes_w + S::codes_x;
             const int kt = 2 * kb, have = min(2, d.tiles_k - kt);                  // tiles of scales
             if (w) {
-                expect(lead, bar, S::codes_w + S::codes_x + have * 2 * kAtom);
+                expect(lead, bar, S::codes_w + have * kAtom + (FUSED ? 0 : S::codes_x + have * kAtom));
                 load_tile(lead, at, &map_w, kb * 64, f0, bar);
                 load_bytes(lead, scales, d.scales_w + ((int64_t)f_tile * d.tiles_k + kt) * kAtom, have * kAtom, bar);
                 issued++;
@@ -364,13 +397,13 @@ serve_linear4_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_con
         };
         const int ahead = min(S::stages, kb1 - kb0);
         for (int i = 0; i < ahead; i++) load(kb0 + i, i, true);
-        wait_previous();                              // the codes and scales of x
+        if (!FUSED) wait_previous();                  // the codes and scales of x
         for (int kb = kb0; kb < kb1; kb++) {
             if (kb - kb0 >= ahead) {
                 if (!__all_sync(~0u, mbar_wait(empty + 8 * ring.slot, ring.parity ^ 1u, &gave_up))) break;
                 load(kb, ring.slot, true);
             }
-            load(kb, ring.slot, false);
+            if (!FUSED) load(kb, ring.slot, false);
             ring.step();
         }
         __syncwarp();
@@ -382,6 +415,7 @@ serve_linear4_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_con
         Ring<S::stages> ring;
         for (int kb = kb0; kb < kb1; kb++) {
             mbar_wait(full + 8 * ring.slot, ring.parity, &gave_up);
+            if (FUSED) mbar_wait(filled + 8 * ring.slot, ring.parity, &gave_up);
             __syncwarp();
             tc_fence_after();
             const uint64_t step = (uint64_t)(ring.slot * (S::stage >> 4)), a = a0 + step, b = b0 + step, s = s0 + step;
@@ -403,9 +437,47 @@ serve_linear4_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_con
         mma_commit_warp(lead, acc_full);
         __syncwarp();
     } else {
+        if (FUSED) {
+            // ---- x: a warp to a stage, every eighth, which so is always in the same place; four rows to a batch, of which
+            // the next is under way while one is packed
+            constexpr int at_once = 4;
+            const T *x = (const T *)d.x + (int64_t)t0 * d.xs + lane * 8;
+            const int live = min(NT, d.tokens - t0), slot = warp - 2;
+            uint8_t *codes = smem + slot * S::stage + S::codes_w, *scales = codes + S::codes_x + S::scales_w;
+            auto fetch = [&](Eight<T> *raw, int kb, int r0) {
+#pragma unroll
+                for (int r = 0; r < at_once; r++)
+                    if (kb < kb1 && r0 + r < live)
+                        raw[r].v[0] = kb * kDepth + lane * 8 < d.k ? __ldg((const uint4 *)(x + (r0 + r) * d.xs + (int64_t)kb * kDepth)) : make_uint4(0, 0, 0, 0);
+            };
+            Eight<T> next[at_once];
+            int kb = kb0 + slot, r0 = 0;
+            uint32_t parity = 1;
+            fetch(next, kb, 0);
+            while (kb < kb1) {
+                Eight<T> raw[at_once];
+#pragma unroll
+                for (int r = 0; r < at_once; r++) raw[r] = next[r];
+                const bool last = r0 + at_once >= live;
+                fetch(next, last ? kb + S::stages : kb, last ? 0 : r0 + at_once);
+                if (r0 == 0 && !__all_sync(~0u, mbar_wait(empty + 8 * slot, parity, &gave_up))) break;
+#pragma unroll
+                for (int r = 0; r < at_once; r++)
+                    if (r0 + r < live) pack_row<T>(codes, scales, r0 + r, raw[r]);
+                r0 += at_once;
+                if (!last) continue;
+                fence_async_proxy();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(filled + 8 * slot);
+                r0 = 0;
+                kb += S::stages;
+                parity ^= 1u;
+            }
+            __syncwarp();
+        }
         // ---- the accumulator's way out.  A warp may touch the 32 lanes of its number modulo 4.
         const int quarter = warp % 4, f = quarter * 32 + lane;
-        const bool ok = all_of(1, mbar_wait(acc_full, 0, &gave_up));
+        const bool ok = warp < 6 && all_of(1, mbar_wait(acc_full, 0, &gave_up));
         tc_fence_after();
         if (ok && split == 1) {
             const float bias = d.bias && f0 + f < d.n ? to_f32(((const T *)d.bias)[f0 + f]) : 0.0f;
@@ -431,7 +503,7 @@ serve_linear4_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_con
         // The blocks' sums are joined: each puts its own where its stages were, block r of the cluster adds up all of
         // them for its share of the tokens, always in the same order.
         const int share = NT / split;
-        if (warp >= 2) {
+        if (warp >= 2 && warp < 6) {
             const int quarter = warp % 4, f = quarter * 32 + lane;
 #pragma unroll 2
             for (int c = 0; c < NT; c += 16) {
@@ -449,7 +521,7 @@ serve_linear4_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_con
         const int features = min(kFeatures, d.n - f0), c0 = part * share, c1 = min(c0 + share, d.tokens - t0);
         const bool whole = whole_rows(d, features);
 #pragma unroll 2
-        for (int i = c0 * (kFeatures / 4) + tid; i < c1 * (kFeatures / 4); i += kProductThreads) {
+        for (int i = c0 * (kFeatures / 4) + tid; i < c1 * (kFeatures / 4); i += threads) {
             const int f = i % (kFeatures / 4) * 4, c = i / (kFeatures / 4);
             if (f >= features) continue;
             float4 p[kMaxSplit];
@@ -817,28 +889,31 @@ int check_shape(const bcast_serve_linear4_args &a)
     return BCAST_OK;
 }
 
-int64_t x_codes_bytes(const bcast_serve_linear4_args &a) { return round_up(a.tokens * (a.k / 2), 256); }
+// x in the workspace, where it is packed by a kernel of its own.
+int64_t x_codes_bytes(const bcast_serve_linear4_args &a) { return a.tokens <= kFusedTokens ? 0 : round_up(a.tokens * (a.k / 2), 256); }
 int64_t x_scales_bytes(const bcast_serve_linear4_args &a, const Cut &c)
 {
-    return ceil_div(a.tokens, c.tile) * ceil_div(a.k, 4 * kBlock) * ceil_div(c.tile, 128) * kAtom;
+    return a.tokens <= kFusedTokens ? 0 : ceil_div(a.tokens, c.tile) * ceil_div(a.k, 4 * kBlock) * ceil_div(c.tile, 128) * kAtom;
 }
 
-template <typename T, int NT>
+template <typename T, int NT, bool FUSED>
 int run_product(const bcast_serve_linear4_args &a, ProductDev d, const PackDev &p, const Cut &c, cudaStream_t st)
 {
-    using S = Tile<NT>;
+    using S = Tile<NT, FUSED>;
     d.f_tiles = (int32_t)ceil_div(a.n, kFeatures);
     d.t_tiles = (int32_t)ceil_div(a.tokens, NT);
     const int64_t tiles = (int64_t)d.f_tiles * d.t_tiles;
     // rows of codes as rows of 16-bit numbers, four codes each
     CUtensorMap mx, mw;
     int rc;
-    if ((rc = tensor_map(&mx, CU_TENSOR_MAP_DATA_TYPE_UINT16, p.codes, {a.k / 4, a.tokens}, {p.cs / 2}, {64, NT}))) return rc;
     if ((rc = tensor_map(&mw, CU_TENSOR_MAP_DATA_TYPE_UINT16, a.codes, {a.k / 4, a.n}, {a.codes_stride / 2}, {64, kFeatures}))) return rc;
-    if ((rc = allow_smem<serve_linear4_kernel<T, NT>>(S::smem))) return rc;
+    mx = mw;
+    if (!FUSED && (rc = tensor_map(&mx, CU_TENSOR_MAP_DATA_TYPE_UINT16, p.codes, {a.k / 4, a.tokens}, {p.cs / 2}, {64, NT}))) return rc;
+    if ((rc = allow_smem<serve_linear4_kernel<T, NT, FUSED>>(S::smem))) return rc;
     const int64_t blocks = tiles * c.split;
     if (blocks > kMaxDim) return BCAST_ERR_INVAL;
-    return launch(serve_linear4_kernel<T, NT>, dim3((unsigned)blocks), dim3(kProductThreads), S::smem, st, true, c.split, mx, mw, d);
+    return launch(serve_linear4_kernel<T, NT, FUSED>, dim3((unsigned)blocks), dim3(FUSED ? kFusedThreads : kProductThreads), S::smem, st, true, c.split,
+                  mx, mw, d);
 }
 
 template <typename T>
@@ -863,12 +938,13 @@ int run_pairs(const bcast_serve_linear4_args &a, ProductDev d, const PackDev &p,
 template <typename T>
 int run(const bcast_serve_linear4_args &a, const ProductDev &d, const PackDev &p, const Cut &c, cudaStream_t st)
 {
-    int rc = over_rows(serve_pack4_kernel<T>, p, st);
+    if (a.tokens <= kFusedTokens) return run_product<T, 32, true>(a, d, p, c, st);
+    const int rc = over_rows(serve_pack4_kernel<T>, p, st);
     if (rc) return rc;
     switch (c.tile) {
-    case 32: return run_product<T, 32>(a, d, p, c, st);
-    case 64: return run_product<T, 64>(a, d, p, c, st);
-    case 128: return run_product<T, 128>(a, d, p, c, st);
+    case 32: return run_product<T, 32, false>(a, d, p, c, st);
+    case 64: return run_product<T, 64, false>(a, d, p, c, st);
+    case 128: return run_product<T, 128, false>(a, d, p, c, st);
     default: return run_pairs<T>(a, d, p, st);
     }
 }
@@ -934,6 +1010,8 @@ int bcast_serve_linear4(const bcast_serve_linear4_args *a, void *cuda_stream)
     const PackDev p = pack_dev(const_cast<void *>(a->x), a->x_stride, codes, a->k / 2, codes + x_codes_bytes(*a), a->tokens, a->k, c.tile);
     ProductDev d = {};
     d.bias = a->bias;
+    d.x = a->x;
+    d.xs = a->x_stride;
     d.scales_w = a->scales;
     d.scales_x = p.scales;
     d.y = a->y;
