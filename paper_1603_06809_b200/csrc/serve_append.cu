@@ -13,8 +13,8 @@
 namespace bcast_serve {
 namespace {
 
-constexpr int kAppendThreads = 64, kAppendBlocks = 10;  // of a block; blocks to an SM
-constexpr int kFlight = 2;                    // rounds of loads that a warp has under way
+constexpr int kAppendThreads = 64, kAppendBlocks = 8;  // of a block; blocks to an SM
+constexpr int kFlight = 4;                    // rounds of loads that a warp has under way
 
 struct AppendDev {
     const void *q, *k, *v, *q_norm, *k_norm;
@@ -89,25 +89,36 @@ struct Factors {
 };
 
 template <int TURN, bool NORM>
-__device__ __forceinline__ void turn_and_weigh(uint64_t *a, uint64_t *b, const Factors &f, bool turned)
+__device__ __forceinline__ void turn_and_weigh(uint64_t *a, uint64_t *b, const Factors &f, bool turned_a, bool turned_b)
 {
 #pragma unroll
     for (int j = 0; j < 4; j++) {
         const uint64_t p = a[j], q = b[j];
-        if (TURN == kHalves && turned) {
+        float x, y;
+        if (TURN == kHalves && turned_a) {            // (one with the other)
             a[j] = fma2(p, f.aa[j], mul2(q, f.ab[j]));
             b[j] = fma2(p, f.ba[j], mul2(q, f.bb[j]));
-        } else if (TURN == kNeighbours && turned) {
-            float x, y;
+            continue;
+        }
+        if (TURN == kNeighbours && turned_a) {
             unpair(p, x, y);
             a[j] = fma2(p, f.aa[j], mul2(pair(y, x), f.ab[j]));
+        } else if (NORM) {
+            a[j] = mul2(p, f.aa[j]);
+        }
+        if (TURN == kNeighbours && turned_b) {
             unpair(q, x, y);
             b[j] = fma2(q, f.bb[j], mul2(pair(y, x), f.ba[j]));
         } else if (NORM) {
-            a[j] = mul2(p, f.aa[j]);
             b[j] = mul2(q, f.bb[j]);
         }
     }
+}
+
+// Sixteen bytes on their way to shared memory; nothing where `in` does not hold.
+__device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool in)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %2, 0;\n\t@p cp.async.cg.shared.global [%0], [%1], 16;\n\t}" ::"r"(dst), "l"(src), "r"((uint32_t)in) : "memory");
 }
 
 template <typename T, bool NORM, int TURN>
@@ -115,6 +126,7 @@ __global__ void __launch_bounds__(kAppendThreads, kAppendBlocks)
 serve_append_kernel(const __grid_constant__ AppendDev d)
 {
     __shared__ __align__(16) float turns[kAppendThreads / 32][2][64];         // each warp's token's cosines and sines
+    __shared__ __align__(16) uint4 ring[kFlight][2][kAppendThreads];          // each lane's chunks of the next rounds
     wait_previous();
     launch_next();
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
@@ -124,45 +136,66 @@ serve_append_kernel(const __grid_constant__ AppendDev d)
     const int token = d.groups == 1 ? item : item / d.groups, group = item - token * d.groups;
     const int b = token / d.fresh, i = token - b * d.fresh;
     const int32_t length = d.own_len[b], fresh = d.new_len ? d.new_len[b] : d.fresh;
+    const int64_t slot = (int64_t)length - d.fresh + i;
     // this lane's chunks
     const int units = d.rot / 16, chunks = d.dim / 8;
-    const bool turned = TURN != kStraight && u < units;
-    const int ca = TURN == kHalves && turned ? u : 2 * u, cb = TURN == kHalves && turned ? u + units : 2 * u + 1;
+    // (neighbouring lanes have neighbouring chunks, so that whole sectors come and go: partners in the halves' rotation, or
+    // as many chunks apart as there are lanes)
+    const bool paired = TURN == kHalves && u < units;
+    const int ca = TURN != kHalves || paired ? u : 2 * u, cb = TURN != kHalves ? u + lanes : paired ? u + units : 2 * u + 1;
     const bool has_a = ca < chunks, has_b = cb < chunks;
+    const bool turned_a = TURN == kHalves ? paired : TURN == kNeighbours && ca * 8 < d.rot, turned_b = TURN == kHalves ? paired : TURN == kNeighbours && cb * 8 < d.rot;
     const int64_t gap = (cb - ca) * 8;
 
     // which rounds: of queries 0..q_rounds - 1, of keys and of values from there on
     const int q_rounds = (d.q_heads + at_once - 1) / at_once, kv_rounds = (d.kv_heads + at_once - 1) / at_once;
     const int r0 = group * d.rounds, r1 = min(r0 + d.rounds, q_rounds + 2 * kv_rounds);
-    // (what is not there stays as it is)
-    const auto load = [&](Unit &x, const T *src, bool in) {
-        if (in) x.a = *(const uint4 *)src;
-        if (in && has_b) x.b = *(const uint4 *)(src + gap);
-    };
+    const auto kind_of = [&](int r) { return r < q_rounds ? 0 : r < q_rounds + kv_rounds ? 1 : 2; };
+    const auto base_of = [&](int kind) { return kind == 0 ? 0 : kind == 1 ? q_rounds : q_rounds + kv_rounds; };
     const auto store = [&](T *dst, const Unit &x, bool in) {
         if (in) *(uint4 *)dst = x.a;
         if (in && has_b) *(uint4 *)(dst + gap) = x.b;
     };
-    const Unit nothing = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
-    // heads of this lane in rounds `from` on, of `heads` in all: positive where there is one
-    const auto heads_left = [&](int heads, int from) { return has_a ? heads - from * at_once - sub : 0; };
-
-    // the first queries' loads need not wait for the lengths
-    const T *src = (const T *)d.q + b * d.qs[0] + i * d.qs[1] + (r0 * at_once + sub) * d.qs[2] + ca * 8;
-    T *dst = (T *)d.out + b * d.os[0] + i * d.os[1] + (r0 * at_once + sub) * d.os[2] + ca * 8;
-    int64_t src_step = d.qs[2] * at_once, dst_step = d.os[2] * at_once;
-    int left = heads_left(d.q_heads, r0);
-    Unit next[kFlight];
-#pragma unroll
-    for (int k = 0; k < kFlight; k++) {
-        next[k] = nothing;
-        load(next[k], src + k * src_step, r0 + k < r1 && left > k * at_once);
-    }
-    const int64_t slot = (int64_t)length - d.fresh + i;
-    if (slot < 0 || i < (int64_t)d.fresh - fresh) {           // padding
-        for (int r = r0; r < min(r1, q_rounds); r++, dst += dst_step, left -= at_once) store(dst, nothing, left > 0);
+    if (d.new_len && (slot < 0 || i < (int64_t)d.fresh - fresh)) {    // padding, of which there may be much: not read
+        T *dst = (T *)d.out + b * d.os[0] + i * d.os[1] + ca * 8;
+        for (int r = r0; r < min(r1, q_rounds); r++) {
+            const int h = r * at_once + sub;
+            store(dst + h * d.os[2], Unit{make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)}, has_a && h < d.q_heads);
+        }
         return;
     }
+
+    // The loads, kFlight rounds ahead.  (Without new_len they need not wait for the lengths.)  What is not there is zero.
+    const T *src = nullptr;
+    int64_t src_step = 0;
+    int ahead = r0, src_end = r0, src_left = 0;
+    const uint32_t mine = smem_u32(&ring[0][0][threadIdx.x]);
+    constexpr uint32_t chunk_b = sizeof(ring[0][0]), round_bytes = sizeof(ring[0]);
+#pragma unroll
+    for (int k = 0; k < kFlight; k++) ring[k][0][threadIdx.x] = ring[k][1][threadIdx.x] = make_uint4(0, 0, 0, 0);
+    const auto load = [&](int place) {
+        if (ahead < r1) {
+            if (ahead == src_end) {                   // the next kind begins
+                const int kind = kind_of(ahead), h = (ahead - base_of(kind)) * at_once + sub;
+                src = kind == 0 ? (const T *)d.q + b * d.qs[0] + i * d.qs[1] + h * d.qs[2]
+                    : kind == 1 ? (const T *)d.k + b * d.ks[0] + i * d.ks[1] + h * d.ks[2] : (const T *)d.v + b * d.vs[0] + i * d.vs[1] + h * d.vs[2];
+                src += ca * 8;
+                src_step = (kind == 0 ? d.qs[2] : kind == 1 ? d.ks[2] : d.vs[2]) * at_once;
+                src_left = has_a ? (kind ? d.kv_heads : d.q_heads) - h : 0;
+                src_end = kind == 2 ? r1 : base_of(kind + 1);
+            }
+            copy16(mine + place * round_bytes, src, src_left > 0);
+            copy16(mine + place * round_bytes + chunk_b, src + gap, src_left > 0 && has_b);
+            src += src_step;
+            src_left -= at_once;
+            ahead++;
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+#pragma unroll
+    for (int k = 0; k < kFlight; k++) load(k);
+
+    const bool there = slot >= 0;
     if constexpr (TURN != kStraight) {
         const int32_t *positions = d.axes ? d.positions + b * d.ps[0] + i * d.ps[1] : nullptr;
 #pragma unroll
@@ -178,122 +211,104 @@ serve_append_kernel(const __grid_constant__ AppendDev d)
         __syncwarp();
     }
     // where the token goes
-    int64_t page = b, place = slot;
-    bool stored = slot < d.own_cap;
+    int64_t page = b, to = slot;
+    bool stored = there && slot < d.own_cap;
     if (stored && d.page_table) {
         const int32_t n = d.page_shift >= 0 ? (int32_t)slot >> d.page_shift : (int32_t)slot / d.page;
         page = d.page_table[(int64_t)b * d.pts + n];
-        place = slot - (int64_t)n * d.page;
+        to = slot - (int64_t)n * d.page;
         stored = page >= 0 && page < d.num_pages;
     }
 
-    // queries, then keys
+    int r = r0, place = 0;
 #pragma unroll 1
-    for (int kind = 0; kind < 2; kind++) {
-        const int base = kind ? q_rounds : 0, end = min(r1, kind ? q_rounds + kv_rounds : q_rounds);
-        int r = max(r0, base);
+    for (int kind = 0; kind < 3; kind++) {
+        const int base = base_of(kind), end = min(r1, kind == 2 ? r1 : base_of(kind + 1));
         if (r >= end) continue;
-        if (kind) {
-            if (!stored) break;
-            const int h = (r - base) * at_once + sub;
-            src = (const T *)d.k + b * d.ks[0] + i * d.ks[1] + h * d.ks[2] + ca * 8;
-            dst = (T *)d.ok + page * d.oks[0] + place * d.oks[1] + h * d.oks[2] + ca * 8;
-            src_step = d.ks[2] * at_once;
-            dst_step = d.oks[2] * at_once;
-            left = heads_left(d.kv_heads, r - base);
-#pragma unroll
-            for (int k = 0; k < kFlight; k++) load(next[k], src + k * src_step, r + k < end && left > k * at_once);
-        }
-        const T *weights = NORM ? (const T *)(kind ? d.k_norm : d.q_norm) : nullptr;
-        const bool norm = NORM && weights;
+        const int h = (r - base) * at_once + sub;
+        T *dst = kind == 0 ? (T *)d.out + b * d.os[0] + i * d.os[1] + h * d.os[2]
+               : kind == 1 ? (T *)d.ok + page * d.oks[0] + to * d.oks[1] + h * d.oks[2] : (T *)d.ov + page * d.ovs[0] + to * d.ovs[1] + h * d.ovs[2];
+        dst += ca * 8;
+        const int64_t dst_step = (kind == 0 ? d.os[2] : kind == 1 ? d.oks[2] : d.ovs[2]) * at_once;
+        int left = has_a && (kind == 0 || stored) ? (kind ? d.kv_heads : d.q_heads) - h : 0;
+        const T *weights = NORM && kind < 2 ? (const T *)(kind ? d.k_norm : d.q_norm) : nullptr;
+        const bool norm = NORM && weights, turn = TURN != kStraight && kind < 2;
         Factors f;
-        {
+        if (norm || turn) {
             const uint64_t one = pair(1.0f, 1.0f);
             uint64_t wa[4] = {one, one, one, one}, wb[4] = {one, one, one, one};
             if (norm && has_a) widen8<T>(__ldg((const uint4 *)(weights + ca * 8)), wa);
             if (norm && has_b) widen8<T>(__ldg((const uint4 *)(weights + cb * 8)), wb);
 #pragma unroll
             for (int j = 0; j < 4; j++) {
-                if (TURN == kHalves && turned) {
+                f.aa[j] = wa[j];
+                f.bb[j] = wb[j];
+                if (TURN == kHalves && paired) {
                     const uint64_t c = *(const uint64_t *)(turns[warp][0] + 8 * u + 2 * j), s = *(const uint64_t *)(turns[warp][1] + 8 * u + 2 * j);
                     f.aa[j] = mul2(wa[j], c);
                     f.ab[j] = mul2(mul2(wb[j], s), pair(-1.0f, -1.0f));
                     f.ba[j] = mul2(wa[j], s);
                     f.bb[j] = mul2(wb[j], c);
-                } else if (TURN == kNeighbours && turned) {
-                    const float ca_ = turns[warp][0][8 * u + j], sa = turns[warp][1][8 * u + j], cb_ = turns[warp][0][8 * u + 4 + j],
-                                sb = turns[warp][1][8 * u + 4 + j];
-                    float x, y;
+                }
+                float x, y;
+                if (TURN == kNeighbours && turned_a) {
+                    const float c = turns[warp][0][4 * ca + j], s = turns[warp][1][4 * ca + j];
                     unpair(wa[j], x, y);
-                    f.aa[j] = pair(x * ca_, y * ca_);
-                    f.ab[j] = pair(-y * sa, x * sa);
+                    f.aa[j] = pair(x * c, y * c);
+                    f.ab[j] = pair(-y * s, x * s);
+                }
+                if (TURN == kNeighbours && turned_b) {
+                    const float c = turns[warp][0][4 * cb + j], s = turns[warp][1][4 * cb + j];
                     unpair(wb[j], x, y);
-                    f.bb[j] = pair(x * cb_, y * cb_);
-                    f.ba[j] = pair(-y * sb, x * sb);
-                } else {
-                    f.aa[j] = wa[j];
-                    f.bb[j] = wb[j];
+                    f.bb[j] = pair(x * c, y * c);
+                    f.ba[j] = pair(-y * s, x * s);
                 }
             }
         }
 #pragma unroll 1
-        for (; r < end; r += kFlight) {
+        for (; r < end; r++) {
+            asm volatile("cp.async.wait_group %0;" ::"n"(kFlight - 1) : "memory");
+            Unit y;
+            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(y.a.x), "=r"(y.a.y), "=r"(y.a.z), "=r"(y.a.w) : "r"(mine + place * round_bytes) : "memory");
+            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(y.b.x), "=r"(y.b.y), "=r"(y.b.z), "=r"(y.b.w) : "r"(mine + place * round_bytes + chunk_b) : "memory");
+            if (norm || turn) {
+                uint64_t xa[4], xb[4];
+                widen8<T>(y.a, xa);
+                widen8<T>(y.b, xb);
+                uint64_t by = 0;
+                if (norm) {
+                    uint64_t squares = mul2(xa[0], xa[0]);
 #pragma unroll
-            for (int k = 0; k < kFlight; k++) {
-                if (r + k >= end) break;
-                Unit y = next[k];
-                load(next[k], src + kFlight * src_step, r + k + kFlight < end && left > kFlight * at_once);
-                src += src_step;
-                if (norm || TURN != kStraight) {
-                    uint64_t xa[4], xb[4];
-                    widen8<T>(y.a, xa);
-                    widen8<T>(y.b, xb);
-                    uint64_t by = 0;
-                    if (norm) {
-                        uint64_t squares = mul2(xa[0], xa[0]);
+                    for (int j = 1; j < 4; j++) squares = fma2(xa[j], xa[j], squares);
 #pragma unroll
-                        for (int j = 1; j < 4; j++) squares = fma2(xa[j], xa[j], squares);
-#pragma unroll
-                        for (int j = 0; j < 4; j++) squares = fma2(xb[j], xb[j], squares);
-                        float sum, more;
-                        unpair(squares, sum, more);
-                        sum += more;
-                        for (int o = lanes / 2; o; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
-                        const float inv = rsqrtf(sum * d.per_dim + d.eps);
-                        by = pair(inv, inv);
-                    }
-                    turn_and_weigh<TURN, NORM>(xa, xb, f, turned);
-                    if (norm) {
-#pragma unroll
-                        for (int j = 0; j < 4; j++) {
-                            xa[j] = mul2(xa[j], by);
-                            xb[j] = mul2(xb[j], by);
-                        }
-                    }
-                    if (norm || turned) y = Unit{narrow8<T>(xa), narrow8<T>(xb)};
+                    for (int j = 0; j < 4; j++) squares = fma2(xb[j], xb[j], squares);
+                    float sum, more;
+                    unpair(squares, sum, more);
+                    sum += more;
+                    for (int o = lanes / 2; o; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
+                    const float inv = rsqrtf(sum * d.per_dim + d.eps);
+                    by = pair(inv, inv);
                 }
-                store(dst, y, left > 0);
-                dst += dst_step;
-                left -= at_once;
+                if (kind < 2) turn_and_weigh<TURN, NORM>(xa, xb, f, turned_a, turned_b);
+                if (norm) {
+#pragma unroll
+                    for (int j = 0; j < 4; j++) {
+                        xa[j] = mul2(xa[j], by);
+                        xb[j] = mul2(xb[j], by);
+                    }
+                }
+                if (norm || turned_a) y.a = narrow8<T>(xa);
+                if (norm || turned_b) y.b = narrow8<T>(xb);
             }
+            if (kind == 0 && !there) y = Unit{make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
+            load(place);                              // into the place that was just read
+            store(dst, y, left > 0);
+            place = place + 1 == kFlight ? 0 : place + 1;
+            dst += dst_step;
+            left -= at_once;
         }
     }
-    // values
-    const int base = q_rounds + kv_rounds;
-    if (r1 <= base || !stored) return;
-    int r = max(r0, base);
-    const int h = (r - base) * at_once + sub;
-    src = (const T *)d.v + b * d.vs[0] + i * d.vs[1] + h * d.vs[2] + ca * 8;
-    dst = (T *)d.ov + page * d.ovs[0] + place * d.ovs[1] + h * d.ovs[2] + ca * 8;
-    left = heads_left(d.kv_heads, r - base);
-#pragma unroll 2
-    for (; r < r1; r++, left -= at_once) {
-        Unit x = nothing;
-        load(x, src, left > 0);
-        store(dst, x, left > 0);
-        src += d.vs[2] * at_once;
-        dst += d.ovs[2] * at_once;
-    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
 }
 
 int check_shape(const bcast_serve_append_args &a)
