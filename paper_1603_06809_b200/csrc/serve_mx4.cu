@@ -28,6 +28,19 @@ constexpr int kAtom = 512;                // bytes of the scales of 128 rows x 4
 // ------------------------------------------------------------------------------------------- to 4 bits and back
 constexpr int kPackThreads = 256, kPackRows = 4;      // rows of a thread, whose loads are under way together
 
+// Division by a number that the host knows: the quotient of n < 2^31 is (n + the upper half of n * mul) >> shift.
+struct Divisor {
+    uint32_t of, mul, shift;
+    __device__ __forceinline__ uint32_t quotient(uint32_t n) const { return (__umulhi(n, mul) + n) >> shift; }
+};
+Divisor divisor(uint32_t of)
+{
+    Divisor d{of, 0, 0};
+    while ((1ull << d.shift) < of) d.shift++;
+    d.mul = (uint32_t)((((1ull << d.shift) - of) << 32) / of + 1);
+    return d;
+}
+
 // Rows of codes, and scales in tiles of `tile` rows of `atoms` x 128 places each, of which each four blocks along k lie
 // together: tile r / tile, then block / 4, then the atom.  (Of weights: tile = 128, one atom.)
 struct PackDev {
@@ -35,8 +48,8 @@ struct PackDev {
     uint8_t *codes, *scales;
     int64_t vs, cs;
     int32_t rows, padded;                 // padded: rows that have a place among the scales, up to which zeros are written
-    int32_t k, tiles_k, eights;           // tiles_k: of four blocks, to a row; eights: threads to a row, a multiple of 16
-    int32_t tile, atoms;
+    int32_t k, tiles_k, atoms;            // tiles_k: of four blocks, to a row
+    Divisor eights, tile;                 // eights: threads to a row, a multiple of 16
     uint32_t threads;
 };
 
@@ -48,11 +61,11 @@ struct Eights {
     bool there;
     __device__ __forceinline__ explicit Eights(const PackDev &d)
     {
-        const uint32_t at = blockIdx.x * kPackThreads + threadIdx.x, group = at / (uint32_t)d.eights;
+        const uint32_t at = blockIdx.x * kPackThreads + threadIdx.x, group = d.eights.quotient(at);
         row0 = (int32_t)group * kPackRows;
-        eight = (int32_t)(at - group * (uint32_t)d.eights);
+        eight = (int32_t)(at - group * d.eights.of);
         there = at < d.threads && eight * 8 < d.k;
-        const uint32_t tile = (uint32_t)row0 / (uint32_t)d.tile, r = (uint32_t)row0 - tile * (uint32_t)d.tile, block = (uint32_t)eight / 4;
+        const uint32_t tile = d.tile.quotient(row0), r = (uint32_t)row0 - tile * d.tile.of, block = (uint32_t)eight / 4;
         scale = (((int64_t)tile * d.tiles_k + block / 4) * d.atoms + r / 128) * kAtom + r % 32 * 16 + r % 128 / 32 * 4 + block % 4;
     }
 };
@@ -141,9 +154,15 @@ __device__ __forceinline__ uint32_t largest(const Eight<T> &raw)
         m = max(m, __shfl_xor_sync(~0u, m, 1));
         return max(m, __shfl_xor_sync(~0u, m, 2));
     } else {
-        uint32_t m = __vmaxu2(__vmaxu2(v[0] & 0x7fff7fffu, v[1] & 0x7fff7fffu), __vmaxu2(v[2] & 0x7fff7fffu, v[3] & 0x7fff7fffu));
-        m = __vmaxu2(m, __shfl_xor_sync(~0u, m, 1));
-        m = __vmaxu2(m, __shfl_xor_sync(~0u, m, 2));
+        const auto larger = [](uint32_t a, uint32_t b) {              // NaN, whose bits are above infinity's, stays
+            uint32_t r;
+            if constexpr (std::is_same_v<T, __nv_bfloat16>) asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+            else asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+            return r;
+        };
+        uint32_t m = larger(larger(v[0] & 0x7fff7fffu, v[1] & 0x7fff7fffu), larger(v[2] & 0x7fff7fffu, v[3] & 0x7fff7fffu));
+        m = larger(m, __shfl_xor_sync(~0u, m, 1));
+        m = larger(m, __shfl_xor_sync(~0u, m, 2));
         m = max(m & 0xffffu, m >> 16);
         if constexpr (std::is_same_v<T, __nv_bfloat16>) return m << 16;
         else return __float_as_uint(__half2float(__ushort_as_half((unsigned short)m)));
@@ -165,7 +184,8 @@ serve_pack4_kernel(const __grid_constant__ PackDev d)
     for (int r = 0; r < kPackRows; r++) {
 #pragma unroll
         for (int i = 0; i < (int)(sizeof(T) / 2); i++)
-            raw[r].v[i] = e.there && e.row0 + r < d.rows ? __ldg((const uint4 *)(src + r * d.vs) + i) : make_uint4(0, 0, 0, 0);
+            raw[r].v[i] = e.there && e.row0 + r < d.rows ? __ldg((const uint4 *)src + i) : make_uint4(0, 0, 0, 0);
+        src += d.vs;
     }
     uint8_t *codes = d.codes + e.row0 * d.cs + e.eight * 4;
 #pragma unroll
@@ -178,7 +198,8 @@ serve_pack4_kernel(const __grid_constant__ PackDev d)
         float y[8];
 #pragma unroll
         for (int i = 0; i < 4; i++) unpair(mul2(x[i], two), y[2 * i], y[2 * i + 1]);
-        if (e.there && e.row0 + r < d.rows) *(uint32_t *)(codes + r * d.cs) = s == 255 ? 0u : codes_of(y);
+        if (e.there && e.row0 + r < d.rows) *(uint32_t *)codes = s == 255 ? 0u : codes_of(y);
+        codes += d.cs;
         uint32_t four = s | __shfl_down_sync(~0u, s, 4) << 8;
         four |= __shfl_down_sync(~0u, four, 8) << 16;
         // (what is past k read as zeros, whose scale is 0)
@@ -840,8 +861,8 @@ PackDev pack_dev(void *values, int64_t vs, uint8_t *codes, int64_t cs, uint8_t *
     d.rows = d.padded = (int32_t)rows;
     d.k = (int32_t)k;
     d.tiles_k = (int32_t)ceil_div(k, 4 * kBlock);
-    d.eights = (int32_t)round_up(k / 8, 16);
-    d.tile = tile;
+    d.eights = divisor((uint32_t)round_up(k / 8, 16));
+    d.tile = divisor((uint32_t)tile);
     d.atoms = (int32_t)ceil_div(tile, 128);
     return d;
 }
@@ -850,7 +871,7 @@ PackDev pack_dev(const bcast_serve_pack4_args &a) { return pack_dev(a.values, a.
 template <typename F>
 int over_rows(F kernel, PackDev d, cudaStream_t st)
 {
-    const int64_t threads = ceil_div(d.padded, kPackRows) * d.eights;
+    const int64_t threads = ceil_div(d.padded, kPackRows) * d.eights.of;
     d.threads = (uint32_t)threads;        // at most 2^31: the shapes' checks see to it
     return launch(kernel, dim3((unsigned)ceil_div(threads, kPackThreads)), dim3(kPackThreads), 0, st, true, 1, d);
 }
