@@ -206,7 +206,8 @@ int64_t bcast_serve_verify_workspace(const bcast_serve_verify_args *args);
  *     stored; their queries are still written.  Nothing else of the caches is touched.
  *   - Where two tokens of a call have the same place (a page that stands in the table twice), either may
  *     stay.
- *   - An axis outside 0..axes-1 is taken as 0.  inv_freq is finite.
+ *   - An axis outside 0..axes-1 is taken as 0.  inv_freq is finite.  A normed head's sum of squares is in the range of
+ *     32-bit floats.
  *   dtype        BCAST_SERVE_BF16 or BCAST_SERVE_FP16: q, k, v, q_norm, k_norm, out and the caches
  *   0 <= batch, new_tokens <= 65535, at most 2^24 tokens and 2^31 - 1 heads of them in all;  0 <= q_heads <= 65535, 1 <= kv_heads
  *   <= 1024;  dim a multiple of 8, 8..128;  rot a multiple of 16, 0..dim (0: no rotation; inv_freq, axis and positions are then not

@@ -4,9 +4,15 @@
 // A head of up to 128 numbers is 1, 2, 4 or 8 lanes', 16 numbers to a lane, which hold the two 16-byte chunks whose
 // numbers are each other's partners in the rotation, so that the rotation needs no exchange; the norm is one sum over
 // those lanes.  A warp takes as many heads at a time as it has lanes for ("a round": queries first, then keys, then values),
-// and all or some of a token's rounds, whose cosines and sines it makes once.
+// and all or some of a token's rounds, whose cosines and sines it makes once and, with the norm's weights, turns into one set
+// of factors for all heads of a kind.  Rounds come through shared memory, four ahead.
 // Angles: inv_freq / 2 pi as a 64-bit fraction of a turn; multiplied by the position modulo 2^64 this leaves the fraction
 // of a turn, off by the position's 2^-64.
+// What bounds it, and what it takes on one B200 (bf16, 32 query and 8 key/value heads of 128; in brackets the bytes at the
+// measured copy rate): 16384 tokens 64 us without norms (62), 74 with: issuing instructions, 2.7 to a cycle and SM, half of the
+// time on conversions.  1024 tokens 9 us (4), 128 4.2: a token's chain of length, angle, head after head.  One token with
+// 12 heads of 64 2.4, a launch.  Measured against it: cosines by each block of a token's warps (92 us for 16384 normed
+// tokens), blocks that stay and take token after token (81 to 136), loads into registers instead of shared memory (80).
 #include "serve_device.cuh"
 #include "serve_internal.h"
 
