@@ -217,6 +217,31 @@ def test_append_cache_beyond_32_bits():
     assert torch.equal(got, want) and torch.equal(far, own) and bool(own[2, :4].any()) and not bool(own[:2].any())
 
 
+def test_append_many_tokens_at_once_and_one_by_one():
+    c = append_case(18, 700, 100, 3, 1, 32, "bf16", page=8, cap=120, norm=True, axes=2)
+    d = {k: on_gpu(v) if torch.is_tensor(v) else v for k, v in c.items()}
+    args = [d.pop(x) for x in ("q", "k", "v", "own_k", "own_v", "own_len")]
+    own = args[3].clone(), args[4].clone()
+    whole = S.bcast_serve_append(*args, **d)
+    for i in range(0, 100, 25):                               # the last 25 tokens are the last 25 of a call for fewer
+        part = {k: v[:, i:i + 25] if k == "positions" else v for k, v in d.items()}
+        got = S.bcast_serve_append(args[0][:, i:i + 25], args[1][:, i:i + 25], args[2][:, i:i + 25], *own, args[5] - (75 - i), **part)
+        assert torch.equal(got, whole[:, i:i + 25])
+    assert torch.equal(own[0], args[3]) and torch.equal(own[1], args[4])
+
+
+def test_append_page_that_stands_in_the_table_twice():
+    c = append_case(19, 2, 1, 2, 1, 64, "bf16", page=4, cap=8, lengths=[3, 3])
+    c["page_table"][:] = 0
+    d = {k: on_gpu(v) if torch.is_tensor(v) else v for k, v in c.items()}
+    before = d["own_v"].clone()
+    S.bcast_serve_append(d["q"], d["k"], d["v"], d["own_k"], d["own_v"], d["own_len"], page_table=d["page_table"])
+    got = d["own_v"][0, 2]
+    assert torch.equal(got, d["v"][0, 0]) or torch.equal(got, d["v"][1, 0])
+    before[0, 2] = got
+    assert torch.equal(before, d["own_v"])
+
+
 # ------------------------------------------------------------------------------------------ logprobs
 def logprobs_case(seed, T, V, dtype, std=2.0):
     g = gen(seed)
@@ -340,6 +365,39 @@ def test_logprobs_given_outputs():
         assert e.value.code == BCAST_ERR_INVAL and name in str(e.value)
 
 
+def test_logprobs_many_rows():
+    l, x = logprobs_case(7, 70001, 40, "fp32")
+    d, e = on_gpu(l), on_gpu(x)
+    lp, h, ids, best = S.bcast_serve_logprobs(d, e, top=3)
+    for a in (0, 65530, 69000):
+        rows = slice(a, a + 12)
+        want = R.logprobs(l[rows], x[rows], 3)
+        close(lp[rows], *want[0], "logprobs")
+        close(h[rows], *want[1], "entropy")
+        assert torch.equal(ids[rows].cpu(), want[2])
+    order = torch.sort(d, dim=-1, descending=True, stable=True).indices[:, :3]
+    assert torch.equal(ids, order.int())
+
+
+@pytest.mark.parametrize("T,V,dtype", [(2, 3000001, "fp16"), (600, 300007, "bf16"), (600, 150001, "fp32")])
+def test_logprobs_long_rows(T, V, dtype):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(V)
+    l = (torch.randn(T, V, generator=g, device=DEV) * 2).to(TYPES[dtype])
+    x = torch.arange(T, device=DEV, dtype=torch.int32) * 7
+    lp, h, ids, best = S.bcast_serve_logprobs(l, x, top=32)
+    rows = sorted({0, 1, T // 2, T - 1})
+    want = R.logprobs(l[rows].cpu(), x[rows].cpu(), 32)
+    close(lp[rows], *want[0], "logprobs")
+    close(h[rows], *want[1], "entropy")
+    assert torch.equal(ids[rows].cpu(), want[2])
+    close(best[rows], *want[3], "top_logprobs")
+    # all rows, found another way
+    bits = l.float().view(torch.int32)
+    key = (torch.where(bits < 0, bits ^ 0x7fffffff, bits).long() << 32) + torch.arange(V - 1, -1, -1, device=DEV)
+    assert torch.equal(ids.long(), V - 1 - (key.topk(32, dim=-1).values & 0xffffffff))
+
+
 def test_logprobs_beyond_32_bits():
     T, V = 17000, 131072                                      # 2.2e9 logits
     l = torch.zeros(T, V, dtype=torch.bfloat16, device=DEV)
@@ -458,6 +516,19 @@ def test_linear4_sums_of_its_own_numbers_are_exact():
         assert torch.equal(R.values(codes, scales), w.double()) and torch.equal(R.values(*R.pack(x)), x.double())
         y = call_linear4(dict(x=x.bfloat16(), w_codes=codes, w_scales=scales, bias=None))
         assert torch.equal(y.cpu(), (x.double() @ w.double().T).bfloat16())
+
+
+@pytest.mark.parametrize("T,K,N", [(70001, 32, 130), (3, 32, 70000), (5000, 96, 4099), (9, 16384, 40), (8, 16384, 300)])
+def test_linear4_long_sides(T, K, N):
+    # whole numbers again: exact, whatever the order of the sums
+    g = gen(T + N)
+    x = torch.tensor([0.0, 1, 2, 3, 4, -1, -2, -3, -4])[torch.randint(0, 9, (T, K), generator=g)]
+    w = torch.tensor([0.0, 0.5, 1, 1.5, 2, 3, 4, -0.5, -6])[torch.randint(0, 9, (N, K), generator=g)]
+    x[:, ::32], w[:, ::32] = 4.0, 4.0
+    codes, s = S.bcast_serve_pack4(on_gpu(w))
+    y = S.bcast_serve_linear4(on_gpu(x.bfloat16()), codes, s)
+    for a in range(0, T, 10000):
+        assert torch.equal(y[a:a + 10000].cpu(), (x[a:a + 10000] @ w.T).bfloat16())
 
 
 def test_linear4_scales_of_all_sizes():
@@ -623,6 +694,50 @@ def test_two_streams_at_once():
     assert all(torch.equal(o[k], want[i][k]) for i in (0, 1) for o in got[i] for k in o)
 
 
+def test_two_graphs_with_one_workspace():
+    # replayed one after the other on one stream, in any order, each as it was captured
+    cases = [all_inputs(27), all_inputs(28)]
+    want = [run_all(c, S.Workspace(DEV)) for c in cases]
+    ws = S.Workspace(DEV)
+    outs = [{k: torch.zeros_like(v) for k, v in w.items()} for w in want]
+    for c, o in zip(cases, outs):
+        run_all(c, ws, o)
+    torch.cuda.synchronize()
+    graphs = []
+    for c, o in zip(cases, outs):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            run_all(c, ws, o)
+    for order in ((0, 1), (1, 0), (0, 0, 1, 1, 0)):
+        for o in outs:
+            for t in o.values():
+                t.zero_()
+        for i in order:
+            graphs[i].replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(outs[i][k], want[i][k]) for i in (0, 1) for k in want[i])
+    S.bcast_serve_status(ws)
+
+
+def test_weights_made_right_before_the_product():
+    # the product's blocks begin early: not before the kernels ahead of them on the stream have written W and x
+    g = gen(29)
+    for T in (1, 8, 40, 500):
+        w, x = on_gpu(rand(g, 3000, 512)), on_gpu(rand(g, T, 512, dtype=torch.bfloat16))
+        codes, scales = S.bcast_serve_pack4(w)
+        want = S.bcast_serve_linear4(x, codes, scales)
+        torch.cuda.synchronize()
+        ws, xx, cc, ss = S.Workspace(DEV, 1 << 22), torch.zeros_like(x), torch.zeros_like(codes), torch.zeros_like(scales)
+        for _ in range(20):
+            cc.zero_()
+            xx.zero_()
+            S.bcast_serve_pack4(w, codes=cc, scales=ss)
+            y0 = S.bcast_serve_linear4(xx, cc, ss, workspace=ws)
+            xx.copy_(x)
+            y = S.bcast_serve_linear4(xx, cc, ss, workspace=ws)
+            assert not bool(y0.any()) and torch.equal(y, want)
+
+
 def test_workspace_that_is_too_small_in_a_capture():
     c = linear4_case(26, 100, 512, 200, "bf16")
     d = (on_gpu(c["x"]), on_gpu(R.bytes_of(c["w_codes"])), on_gpu(R.tiled(c["w_scales"])))
@@ -644,7 +759,8 @@ import test_serve_more_gpu as T
 from paper_1603_06809_b200 import serve as S
 from paper_1603_06809_b200.bcast import BcastError
 ws = S.Workspace("cuda:0")
-for i, (n, k, f) in enumerate([(1, 64, 100), (20, 4096, 256), (60, 2048, 500), (300, 544, 300), (2000, 544, 6000), (449, 64, 19200)]):
+for i, (n, k, f) in enumerate([(1, 64, 100), (20, 4096, 256), (60, 2048, 500), (300, 544, 300), (2000, 544, 6000), (449, 64, 19200), (5, 8192, 300),
+                               (8, 4096, 19000)]):
     c = T.linear4_case(i, n, k, f, "bf16")
     y = T.call_linear4(c, workspace=ws)
     try:
@@ -665,4 +781,4 @@ def test_waits_that_run_out_end_the_kernels(given_up):
     out = subprocess.run([sys.executable, "-c", WAITS_CHILD, ROOT], env=env, capture_output=True, text=True, timeout=300)
     assert out.returncode == 0, out.stderr[-2000:]
     want = BCAST_ERR_TIMEOUT if given_up else 0
-    assert out.stdout.split("\n") == [f"CALL {i} {want}" for i in range(6)] + ["END", ""], out.stdout
+    assert out.stdout.split("\n") == [f"CALL {i} {want}" for i in range(8)] + ["END", ""], out.stdout
