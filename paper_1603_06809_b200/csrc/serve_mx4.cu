@@ -248,7 +248,7 @@ serve_unpack4_kernel(const __grid_constant__ PackDev d)
 constexpr int kFeatures = 128;            // features per tile: the lanes of tensor memory
 constexpr int kDepth = 256;               // values of k per stage: 128 bytes of codes, one swizzled row
 constexpr int kProductThreads = 192, kFusedThreads = 320;
-constexpr int kFusedTokens = 8;          // up to which the product's blocks pack x themselves
+constexpr int kFusedTokens = 8;           // up to which the product's blocks pack x themselves
 constexpr int kMaxSplit = 8;              // blocks of a cluster that share one tile's k
 
 template <int NT, bool FUSED> struct Tile {
@@ -275,9 +275,11 @@ struct ProductDev {
 
 // Descriptor of 32 rows of 16 bytes, one after the other, as tcgen05.cp takes them.
 __device__ __forceinline__ uint64_t scales_desc(uint32_t src) { return (uint64_t)((src >> 4) & 0x3fffu) | (uint64_t)(128 >> 4) << 32 | 1ull << 46; }
+
 // The instructions that follow are issued by the thread with `lead` set of a warp in uniform control flow, so that their
 // operands stay in uniform registers, where they are wanted.  (One thread in a loop of its own took about 110 cycles to issue
 // each: 8192 tokens, 4096 -> 4096 took 105 us, however much or little was loaded.)
+
 // A tile; sixteen bytes and more, both ends on 16-byte boundaries; the bytes that a barrier is to wait for.
 __device__ __forceinline__ void load_tile(uint32_t lead, uint32_t dst, const CUtensorMap *m, int x, int y, uint32_t bar)
 {
@@ -426,7 +428,8 @@ serve_linear4_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_con
         if (!FUSED) wait_previous();                  // the codes and scales of x
         for (int kb = kb0; kb < kb1; kb++) {
             if (kb - kb0 >= ahead) {
-                if (!__all_sync(~0u, mbar_wait(empty + 8 * ring.slot, ring.parity ^ 1u, &gave_up))) break;
+                // (the warp that issues the products goes on after it gave up: a slot may be free then whose load is under way)
+                if (!__all_sync(~0u, mbar_wait(empty + 8 * ring.slot, ring.parity ^ 1u, &gave_up) && !*(volatile int *)&gave_up)) break;
                 load(kb, ring.slot, true);
             }
             if (!FUSED) load(kb, ring.slot, false);
@@ -486,7 +489,7 @@ serve_linear4_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_con
                 for (int r = 0; r < at_once; r++) raw[r] = next[r];
                 const bool last = r0 + at_once >= live;
                 fetch(next, last ? kb + S::stages : kb, last ? 0 : r0 + at_once);
-                if (r0 == 0 && !__all_sync(~0u, mbar_wait(empty + 8 * slot, parity, &gave_up))) break;
+                if (r0 == 0 && !__all_sync(~0u, mbar_wait(empty + 8 * slot, parity, &gave_up) && !*(volatile int *)&gave_up)) break;
 #pragma unroll
                 for (int r = 0; r < at_once; r++)
                     if (r0 + r < live) pack_row<T>(codes, scales, r0 + r, raw[r]);
@@ -703,6 +706,12 @@ serve_linear4_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __gri
     cluster_wait();
     tc_fence_after();
     const uint32_t tmem = tmem_at;
+    // A wait for all lanes alike.  One that runs out ends the other block's waits too.
+    const auto wait = [&](uint32_t bar, uint32_t parity) {
+        const bool ok = __all_sync(~0u, mbar_wait(bar, parity, &gave_up));
+        if (!ok && lane == 0) *(volatile int *)cg::this_cluster().map_shared_rank(&gave_up, rank ^ 1) = 1;
+        return ok;
+    };
 
     if (warp == 0 || warp == 2) {
         // ---- loads: W, or x.  W is there already, x once it is packed.
@@ -715,7 +724,7 @@ serve_linear4_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __gri
         for (int tile = first_tile; tile < tiles && ok; tile += tile_step) {
             const int f_tile = tile % f_pairs * 2 + rank, t_tile = tile / f_pairs;
             for (int kb = 0; kb < k_blocks; kb++) {
-                ok = __all_sync(~0u, mbar_wait(empty + 8 * ring.slot, ring.parity ^ 1u, &gave_up));
+                ok = wait(empty + 8 * ring.slot, ring.parity ^ 1u);
                 if (!ok) break;
                 const uint32_t bar = of_first(full + 8 * ring.slot), at = stage0 + ring.slot * S::stage, scales = at + S::codes_w + S::codes_x;
                 if (which == 0) {
@@ -736,21 +745,18 @@ serve_linear4_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __gri
         __syncwarp();
     } else if (warp == 1) {
         if (rank == 0) {
-            // ---- matrix instructions, for both blocks; waits that give up as above
+            // ---- matrix instructions, for both blocks.  (Nothing is told to be empty after a wait gave up.)
             const uint32_t lead = elect_one();
             const uint64_t a0 = smem_desc(stage0), b0 = smem_desc(stage0 + S::codes_w), s0 = scales_desc(stage0 + S::codes_w + S::codes_x);
-            auto wait = [&](uint32_t bar, uint32_t parity) {
-                mbar_wait(bar, parity, &gave_up);
-                __syncwarp();
-            };
             Ring<S::stages> ring;
             Ring<2> acc;
             uint32_t odd = 0;                         // which of two places the stage's scales go to
-            for (int tile = first_tile; tile < tiles; tile += tile_step) {
-                wait(acc_empty + 8 * acc.slot, acc.parity ^ 1u);
+            bool ok = true;
+            for (int tile = first_tile; tile < tiles && ok; tile += tile_step) {
+                if (!(ok = wait(acc_empty + 8 * acc.slot, acc.parity ^ 1u))) break;
                 const uint32_t out = tmem + acc.slot * kPairTokens;
                 for (int kb = 0; kb < k_blocks; kb++) {
-                    wait(full + 8 * ring.slot, ring.parity);
+                    if (!(ok = wait(full + 8 * ring.slot, ring.parity))) break;
                     tc_fence_after();
                     const uint64_t step = (uint64_t)(ring.slot * (S::stage >> 4)), a = a0 + step, b = b0 + step, s = s0 + step;
                     const uint32_t to_w = tmem + S::at_scales + odd * S::scales, to_x = to_w + 8;
@@ -770,6 +776,7 @@ serve_linear4_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __gri
                     ring.step();
                     odd ^= 1u;
                 }
+                if (!ok) break;
                 pair_commit(lead, acc_full + 8 * acc.slot);
                 acc.step();
             }
@@ -783,7 +790,7 @@ serve_linear4_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __gri
         Ring<2> acc;
         for (int tile = first_tile; tile < tiles; tile += tile_step) {
             // (the four warps go on together, or none does)
-            if (!all_of(id, mbar_wait(acc_full + 8 * acc.slot, acc.parity, &gave_up))) break;
+            if (!all_of(id, wait(acc_full + 8 * acc.slot, acc.parity))) break;
             tc_fence_after();
             const uint32_t src = tmem + ((uint32_t)(quarter * 32) << 16) + acc.slot * kPairTokens + side * S::half;
             const int f0 = (tile % f_pairs * 2 + rank) * kFeatures, t0 = tile / f_pairs * kPairTokens + side * S::half;
