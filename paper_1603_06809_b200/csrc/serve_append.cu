@@ -3,15 +3,15 @@
 //
 // A head of up to 128 numbers is 1, 2, 4 or 8 lanes', 16 numbers to a lane, which hold the two 16-byte chunks whose
 // numbers are each other's partners in the rotation, so that the rotation needs no exchange; the norm is one sum over
-// those lanes.  A warp takes as many heads at a time as it has lanes for ("a round": queries first, then keys, then values),
-// and all or some of a token's rounds, whose cosines and sines it makes once and, with the norm's weights, turns into one set
-// of factors for all heads of a kind.  Rounds come through shared memory, four ahead.
+// those lanes.  A token is a warp's, which takes as many heads at a time as it has lanes for ("a round": queries first, then
+// keys, then values), or a half's or a quarter's of one where it has few heads.  Its cosines and sines are made once and, with
+// the norm's weights, turned into one set of factors for all heads of a kind.  Rounds come through shared memory, four ahead.
 // Angles: inv_freq / 2 pi as a 64-bit fraction of a turn; multiplied by the position modulo 2^64 this leaves the fraction
 // of a turn, off by the position's 2^-64.
 // What bounds it, and what it takes on one B200 (bf16, 32 query and 8 key/value heads of 128; in brackets the bytes at the
 // measured copy rate): 16384 tokens 64 us without norms (62), 74 with: issuing instructions, 2.7 to a cycle and SM, half of the
-// time on conversions.  1024 tokens 9 us (4), 128 4.2: a token's chain of length, angle, head after head.  One token with
-// 12 heads of 64 2.4, a launch.  Measured against it: cosines by each block of a token's warps (92 us for 16384 normed
+// time on conversions.  1024 tokens 10 us (4), 128 4.8: a token's chain of length, angle, head after head.  One token with
+// 12 heads of 64 2.6, a launch.  Measured against it: cosines by each block of a token's warps (92 us for 16384 normed
 // tokens), blocks that stay and take token after token (81 to 136), loads into registers instead of shared memory (80).
 #include "serve_device.cuh"
 #include "serve_internal.h"
@@ -19,7 +19,8 @@
 namespace bcast_serve {
 namespace {
 
-constexpr int kAppendThreads = 64, kAppendBlocks = 8;  // of a block; blocks to an SM
+constexpr int kAppendThreads = 64, kAppendBlocks = 9;  // of a block; blocks to an SM
+constexpr int kFill = 16 * kSms;              // warps that are enough
 constexpr int kFlight = 4;                    // rounds of loads that a warp has under way
 
 struct AppendDev {
@@ -29,7 +30,7 @@ struct AppendDev {
     void *out, *ok, *ov;
     int64_t qs[3], ks[3], vs[3], os[3], oks[3], ovs[3], ps[2];
     int64_t own_cap, num_pages, pts, first;
-    int32_t fresh, q_heads, kv_heads, dim, page, page_shift, rot, axes, groups, rounds, lanes_shift, items;
+    int32_t fresh, q_heads, kv_heads, dim, page, page_shift, rot, axes, groups, rounds, lanes_shift, width_shift, items, tokens;
     float eps, per_dim;
 };
 
@@ -131,27 +132,30 @@ template <typename T, bool NORM, int TURN>
 __global__ void __launch_bounds__(kAppendThreads, kAppendBlocks)
 serve_append_kernel(const __grid_constant__ AppendDev d)
 {
-    __shared__ __align__(16) float turns[kAppendThreads / 32][2][64];         // each warp's token's cosines and sines
     __shared__ __align__(16) uint4 ring[kFlight][2][kAppendThreads];          // each lane's chunks of the next rounds
+    __shared__ __align__(16) float turns_of[kAppendThreads / 8][2][64];       // each token's cosines and sines
     wait_previous();
     launch_next();
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
-    const int lanes = 1 << d.lanes_shift, u = lane & (lanes - 1), sub = lane >> d.lanes_shift, at_once = 32 >> d.lanes_shift;
+    // a token has `width` lanes, a head `lanes` of them
+    const int lanes = 1 << d.lanes_shift, width = 1 << d.width_shift;
+    const int u = lane & (lanes - 1), sub = (lane & (width - 1)) >> d.lanes_shift, at_once = width >> d.lanes_shift;
     const int item = blockIdx.x * (kAppendThreads / 32) + warp;
     if (item >= d.items) return;
-    const int token = d.groups == 1 ? item : item / d.groups, group = item - token * d.groups;
-    const int b = token / d.fresh, i = token - b * d.fresh;
+    const int share = d.groups == 1 ? item : item / d.groups, group = item - share * d.groups;
+    const int token = (share << (5 - d.width_shift)) + (lane >> d.width_shift);
+    const bool exists = token < d.tokens;
+    const int b = exists ? token / d.fresh : 0, i = exists ? token - b * d.fresh : 0;
     const int32_t length = d.own_len[b], fresh = d.new_len ? d.new_len[b] : d.fresh;
     const int64_t slot = (int64_t)length - d.fresh + i;
-    // this lane's chunks
+    // this lane's chunks (neighbouring lanes have neighbouring chunks, so that whole sectors come and go: partners in the
+    // halves' rotation, or as many chunks apart as there are lanes)
     const int units = d.rot / 16, chunks = d.dim / 8;
-    // (neighbouring lanes have neighbouring chunks, so that whole sectors come and go: partners in the halves' rotation, or
-    // as many chunks apart as there are lanes)
     const bool paired = TURN == kHalves && u < units;
     const int ca = TURN != kHalves || paired ? u : 2 * u, cb = TURN != kHalves ? u + lanes : paired ? u + units : 2 * u + 1;
-    const bool has_a = ca < chunks, has_b = cb < chunks;
+    const bool has_a = exists && ca < chunks, has_b = exists && cb < chunks;
     const bool turned_a = TURN == kHalves ? paired : TURN == kNeighbours && ca * 8 < d.rot, turned_b = TURN == kHalves ? paired : TURN == kNeighbours && cb * 8 < d.rot;
-    const int64_t gap = (cb - ca) * 8;
+    const int gap = (cb - ca) * 8;
 
     // which rounds: of queries 0..q_rounds - 1, of keys and of values from there on
     const int q_rounds = (d.q_heads + at_once - 1) / at_once, kv_rounds = (d.kv_heads + at_once - 1) / at_once;
@@ -162,13 +166,18 @@ serve_append_kernel(const __grid_constant__ AppendDev d)
         if (in) *(uint4 *)dst = x.a;
         if (in && has_b) *(uint4 *)(dst + gap) = x.b;
     };
-    if (d.new_len && (slot < 0 || i < (int64_t)d.fresh - fresh)) {    // padding, of which there may be much: not read
-        T *dst = (T *)d.out + b * d.os[0] + i * d.os[1] + ca * 8;
-        for (int r = r0; r < min(r1, q_rounds); r++) {
-            const int h = r * at_once + sub;
-            store(dst + h * d.os[2], Unit{make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)}, has_a && h < d.q_heads);
+    const Unit nothing = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
+    bool there = true;                                // (of a token that is not padding)
+    if (d.new_len) {                                  // there may be much padding, which is not read
+        there = slot >= 0 && i >= (int64_t)d.fresh - fresh;
+        if (!__any_sync(~0u, exists && there)) {
+            T *dst = (T *)d.out + b * d.os[0] + i * d.os[1] + ca * 8;
+            for (int r = r0; r < min(r1, q_rounds); r++) {
+                const int h = r * at_once + sub;
+                store(dst + h * d.os[2], nothing, has_a && h < d.q_heads);
+            }
+            return;
         }
-        return;
     }
 
     // The loads, kFlight rounds ahead.  (Without new_len they need not wait for the lengths.)  What is not there is zero.
@@ -179,6 +188,7 @@ serve_append_kernel(const __grid_constant__ AppendDev d)
     constexpr uint32_t chunk_b = sizeof(ring[0][0]), round_bytes = sizeof(ring[0]);
 #pragma unroll
     for (int k = 0; k < kFlight; k++) ring[k][0][threadIdx.x] = ring[k][1][threadIdx.x] = make_uint4(0, 0, 0, 0);
+    const bool read = has_a && there;
     const auto load = [&](int place) {
         if (ahead < r1) {
             if (ahead == src_end) {                   // the next kind begins
@@ -187,7 +197,7 @@ serve_append_kernel(const __grid_constant__ AppendDev d)
                     : kind == 1 ? (const T *)d.k + b * d.ks[0] + i * d.ks[1] + h * d.ks[2] : (const T *)d.v + b * d.vs[0] + i * d.vs[1] + h * d.vs[2];
                 src += ca * 8;
                 src_step = (kind == 0 ? d.qs[2] : kind == 1 ? d.ks[2] : d.vs[2]) * at_once;
-                src_left = has_a ? (kind ? d.kv_heads : d.q_heads) - h : 0;
+                src_left = read ? (kind ? d.kv_heads : d.q_heads) - h : 0;
                 src_end = kind == 2 ? r1 : base_of(kind + 1);
             }
             copy16(mine + place * round_bytes, src, src_left > 0);
@@ -201,18 +211,17 @@ serve_append_kernel(const __grid_constant__ AppendDev d)
 #pragma unroll
     for (int k = 0; k < kFlight; k++) load(k);
 
-    const bool there = slot >= 0;
+    there = there && slot >= 0;
+    float (*const turns)[64] = turns_of[warp * 4 + (lane >> d.width_shift)];
     if constexpr (TURN != kStraight) {
         const int32_t *positions = d.axes ? d.positions + b * d.ps[0] + i * d.ps[1] : nullptr;
-#pragma unroll
-        for (int k = 0; k < 2; k++) {
-            const int p = lane + k * 32;
-            if (p >= d.rot / 2) break;
+#pragma unroll 2
+        for (int p = lane & (width - 1); p < d.rot / 2; p += width) {
             const float f = __ldg(d.inv_freq + p);
             const int axis = d.axis ? __ldg(d.axis + p) : 0;
             const float2 turn = turn_of(f, positions ? (int64_t)__ldg(positions + ((uint32_t)axis < (uint32_t)d.axes ? axis : 0)) : d.first + slot);
-            turns[warp][0][p] = turn.x;
-            turns[warp][1][p] = turn.y;
+            turns[0][p] = turn.x;
+            turns[1][p] = turn.y;
         }
         __syncwarp();
     }
@@ -250,7 +259,7 @@ serve_append_kernel(const __grid_constant__ AppendDev d)
                 f.aa[j] = wa[j];
                 f.bb[j] = wb[j];
                 if (TURN == kHalves && paired) {
-                    const uint64_t c = *(const uint64_t *)(turns[warp][0] + 8 * u + 2 * j), s = *(const uint64_t *)(turns[warp][1] + 8 * u + 2 * j);
+                    const uint64_t c = *(const uint64_t *)(turns[0] + 8 * u + 2 * j), s = *(const uint64_t *)(turns[1] + 8 * u + 2 * j);
                     f.aa[j] = mul2(wa[j], c);
                     f.ab[j] = mul2(mul2(wb[j], s), pair(-1.0f, -1.0f));
                     f.ba[j] = mul2(wa[j], s);
@@ -258,13 +267,13 @@ serve_append_kernel(const __grid_constant__ AppendDev d)
                 }
                 float x, y;
                 if (TURN == kNeighbours && turned_a) {
-                    const float c = turns[warp][0][4 * ca + j], s = turns[warp][1][4 * ca + j];
+                    const float c = turns[0][4 * ca + j], s = turns[1][4 * ca + j];
                     unpair(wa[j], x, y);
                     f.aa[j] = pair(x * c, y * c);
                     f.ab[j] = pair(-y * s, x * s);
                 }
                 if (TURN == kNeighbours && turned_b) {
-                    const float c = turns[warp][0][4 * cb + j], s = turns[warp][1][4 * cb + j];
+                    const float c = turns[0][4 * cb + j], s = turns[1][4 * cb + j];
                     unpair(wb[j], x, y);
                     f.bb[j] = pair(x * c, y * c);
                     f.ba[j] = pair(-y * s, x * s);
@@ -306,7 +315,7 @@ serve_append_kernel(const __grid_constant__ AppendDev d)
                 if (norm || turned_a) y.a = narrow8<T>(xa);
                 if (norm || turned_b) y.b = narrow8<T>(xb);
             }
-            if (kind == 0 && !there) y = Unit{make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
+            if (!there) y = nothing;
             load(place);                              // into the place that was just read
             store(dst, y, left > 0);
             place = place + 1 == kFlight ? 0 : place + 1;
@@ -420,14 +429,25 @@ extern "C" int bcast_serve_append(const bcast_serve_append_args *args, void *cud
     d.eps = a.eps;
     d.per_dim = 1.0f / (float)a.dim;
     d.lanes_shift = a.dim <= 16 ? 0 : a.dim <= 32 ? 1 : a.dim <= 64 ? 2 : 3;
-    const int64_t tokens = (int64_t)a.batch * a.new_tokens, at_once = 32 >> d.lanes_shift;
-    const int64_t rounds = ceil_div(a.q_heads, at_once) + 2 * ceil_div(a.kv_heads, at_once);
-    // Few tokens: a warp to every round; many: a warp to a token, which makes the cosines once for all its heads.
+    const int64_t tokens = (int64_t)a.batch * a.new_tokens;
+    // How many lanes a token has.  A warp, as a rule; half or a quarter of one, a warp's tokens then sharing its instructions,
+    // where its heads leave much of the warp idle and the tokens still fill the SMs.  Measured (us, 32 / 8 lanes): 40362 tokens of
+    // 2 + 2 + 2 heads of 64 50 / 24, 14514 of 16 + 2 + 2 normed 37 / 26; 16384 of 32 + 8 + 8 of 128 64 / 70, of 64 37 / 39.
+    // So from 1.5 times on, by the rounds and two more for what comes before them.
+    d.tokens = (int32_t)tokens;
+    const auto rounds_of = [&](int shift) {
+        const int64_t heads = (1 << shift) >> d.lanes_shift;
+        return ceil_div(a.q_heads, heads) + 2 * ceil_div(a.kv_heads, heads);
+    };
+    d.width_shift = 5;
+    for (int shift = 4; shift >= 3; shift--)
+        if (shift >= d.lanes_shift && tokens << shift >= 32 * kFill && 3 * (rounds_of(shift) + 2) << shift <= 2 * (rounds_of(5) + 2) << 5) d.width_shift = shift;
+    const int64_t rounds = rounds_of(d.width_shift);
+    // Few tokens: a warp to every round; otherwise to all of a token's.
     const bool few = tokens * rounds <= 16 * kSms;
-    d.rounds = few ? 1 : (int32_t)(rounds < 16 ? rounds : 16);
+    d.rounds = (int32_t)(few ? 1 : rounds);
     d.groups = (int32_t)ceil_div(rounds, d.rounds);
-    if (tokens * d.groups > kMaxDim) return BCAST_ERR_INVAL;
-    d.items = (int32_t)(tokens * d.groups);
+    d.items = (int32_t)(ceil_div(tokens << d.width_shift, 32) * d.groups);
     const int64_t blocks = ceil_div(d.items, kAppendThreads / 32);
     const bool norm = a.q_norm || a.k_norm;
     const int turn = a.rot == 0 ? kStraight : a.interleaved ? kNeighbours : kHalves;

@@ -230,6 +230,26 @@ def test_append_many_tokens_at_once_and_one_by_one():
     assert torch.equal(own[0], args[3]) and torch.equal(own[1], args[4])
 
 
+# so many tokens of so few heads that two or four of them share a warp, against calls for one request at a time
+@pytest.mark.parametrize("B,n", [(16, 300), (41, 301)])
+@pytest.mark.parametrize("HQ,H,D,more", [(1, 1, 128, dict(norm=True)), (0, 1, 96, dict(interleaved=True, norm=True)), (3, 1, 64, dict(axes=3)), (2, 2, 40, dict(rot=32)),
+                                         (5, 1, 16, dict(norm=True, rot=0)), (8, 1, 8, dict())])
+@pytest.mark.parametrize("ragged", [False, True])
+def test_append_several_tokens_to_a_warp(B, n, HQ, H, D, more, ragged):
+    g = gen(B + D)
+    c = append_case(B + D, B, n, HQ, H, D, "bf16", page=16, cap=n + 40, new=torch.randint(0, n + 1, (B,), generator=g).tolist() if ragged else None,
+                    lengths=torch.randint(0, n + 60, (B,), generator=g).tolist(), **more)
+    d = {k: on_gpu(v) if torch.is_tensor(v) else v for k, v in c.items()}
+    args = [d.pop(x) for x in ("q", "k", "v", "own_k", "own_v", "own_len")]
+    own = args[3].clone(), args[4].clone()
+    whole = S.bcast_serve_append(*args, **d)
+    for b in range(B):
+        part = {k: v[b:b + 1] if k in ("positions", "page_table", "new_len") else v for k, v in d.items()}
+        got = S.bcast_serve_append(None if args[0] is None else args[0][b:b + 1], args[1][b:b + 1], args[2][b:b + 1], *own, args[5][b:b + 1], **part)
+        assert got is None if whole is None else torch.equal(got, whole[b:b + 1])
+    assert torch.equal(own[0], args[3]) and torch.equal(own[1], args[4])
+
+
 def test_append_page_that_stands_in_the_table_twice():
     c = append_case(19, 2, 1, 2, 1, 64, "bf16", page=4, cap=8, lengths=[3, 3])
     c["page_table"][:] = 0
