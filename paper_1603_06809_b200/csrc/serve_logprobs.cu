@@ -10,7 +10,7 @@
 // reaches the bound goes to a list in shared memory, and an entry's place is the number of entries before it in
 // the order (logit, then lower token).  Lists that overflow -- many equal logits, as behind a mask of the type's lowest
 // value -- take bounds that are exact, and equals in the order of their numbers.
-// A row is a block's, or a cluster's where the rows are few: its first block joins the parts, which the others send it
+// A row is a block's (of one warp, where rows are short and many), or a cluster's where the rows are few: its first block joins the parts, which the others send it
 // through distributed shared memory (fetched by it, one after the other, a cluster's join took 5 us).
 // What bounds it, and what it takes on one B200 (in brackets the bytes at the measured copy rate): 4096 rows of 131072 bf16
 // logits 175 us without alternatives, 197 with eight (164): loads and exponentials (64 % of their unit) while a block streams,
@@ -27,7 +27,8 @@ namespace cg = cooperative_groups;
 namespace bcast_serve {
 namespace {
 
-constexpr int kMaxTop = 32, kListSize = 1024, kMaxParts = 8;
+constexpr int kMaxTop = 32, kMaxParts = 8;
+template <int P> constexpr int kListSize = P == 32 ? 256 : 1024;          // (blocks of one warp are many to an SM)
 constexpr int kInFlight = 4;                  // vectors that a thread has under way
 constexpr float kLag = 8.0f;                  // how far a thread's maximum may lag: weights up to e^8
 constexpr float kFloor = -150.0f;             // in powers of two: what is smaller counts as nothing
@@ -135,7 +136,7 @@ struct Shared {
     uint32_t tops[32];                        // each warp's largest keys, 1024 / P of them
     int warp_count[P / 32];
     int listed;
-    uint64_t list[kListSize];
+    uint64_t list[kListSize<P>];
 };
 
 __device__ __forceinline__ uint64_t entry_of(uint32_t key, int token) { return (uint64_t)key << 32 | (uint32_t)~token; }
@@ -147,7 +148,7 @@ __device__ __forceinline__ void put(Shared<P> &sh, float l, int token, uint32_t 
     const uint32_t key = key_of(l);
     if (key < least) return;
     const int at = atomicAdd(&sh.listed, 1);
-    if (at < kListSize) sh.list[at] = entry_of(key, token);
+    if (at < kListSize<P>) sh.list[at] = entry_of(key, token);
 }
 
 // What reaches `least` of one vector, `at` the number of its first token, goes to the list.
@@ -183,13 +184,27 @@ __device__ __forceinline__ void collect(Shared<P> &sh, const Span<T> &span, int 
             }
         }
     } else {
-        // a warp to a thread's logits
-        const int lane = threadIdx.x % 32;
-        for (uint32_t todo = __ballot_sync(~0u, mine >= least); todo; todo &= todo - 1) {
-            const int who = threadIdx.x - lane + __ffs(todo) - 1;
+        const int lane = threadIdx.x % 32, each = (span.v1 - span.v0 + P - 1) / P;
+        const uint32_t which = __ballot_sync(~0u, mine >= least);
+        if (__popc(which) * ((each + 31) / 32) < each) {
+            // a warp to a thread's logits
+            for (uint32_t todo = which; todo; todo &= todo - 1) {
+                const int who = threadIdx.x - lane + __ffs(todo) - 1;
 #pragma unroll 2
-            for (int v = span.v0 + who + lane * P; v < span.v1; v += 32 * P)
-                put_vector<T, P>(sh, __ldg(span.vec + v), span.head + v * kPer<T>, least);
+                for (int v = span.v0 + who + lane * P; v < span.v1; v += 32 * P)
+                    put_vector<T, P>(sh, __ldg(span.vec + v), span.head + v * kPer<T>, least);
+            }
+        } else {
+            // many threads of a short row: each its own (4096 rows of 3292, twenty alternatives: 30 us, so 37)
+            for (int v = span.v0 + threadIdx.x; v < span.v1; v += kInFlight * P) {
+                uint4 raw[kInFlight];
+#pragma unroll
+                for (int u = 0; u < kInFlight; u++)
+                    if (v + u * P < span.v1) raw[u] = __ldg(span.vec + v + u * P);
+#pragma unroll
+                for (int u = 0; u < kInFlight; u++)
+                    if (v + u * P < span.v1) put_vector<T, P>(sh, raw[u], span.head + (v + u * P) * kPer<T>, least);
+            }
         }
     }
     const int token = span.edge(threadIdx.x, part);
@@ -280,10 +295,10 @@ __device__ __forceinline__ void pick(Shared<P> &sh, const Span<T> &span, int par
     // a key that `want` threads' maxima reach, and few more; where fewer threads have a logit, the lowest there is
     uint32_t least = max(nth_of_lanes(sh.tops[threadIdx.x % 32], want), kLowest + 1);
     collect<T, P>(sh, span, part, mine, least, held, false);
-    if (sh.listed <= kListSize) return;
+    if (sh.listed <= kListSize<P>) return;
     // only what is above the bound: where many are equal to it, that is little
     collect<T, P>(sh, span, part, mine, least + 1, held, true);
-    if (sh.listed > kListSize) {
+    if (sh.listed > kListSize<P>) {
         // the want-th largest logit itself: fewer than `want` are above it
         uint32_t over = key_of(INFINITY) + 1;
         while (over - least > 1) {
@@ -429,12 +444,14 @@ serve_logprobs_kernel(const __grid_constant__ ProbDev d)
     const uint32_t mine = key_of(top);
     a = warp_join(a);
     if (lane == 0) sh.warp_sums[warp] = a;
-    uint32_t left = mine;
-#pragma unroll
-    for (int k = 0; k < 1024 / P; k++) {
-        const uint32_t key = next_top(left);
-        if (lane == 0) sh.tops[warp * (1024 / P) + k] = key;
-        if (d.top <= k + 1) left = 0;                 // (one to a warp at least: the row's largest logit is among them)
+    if constexpr (P == 32) {
+        sh.tops[lane] = mine;
+    } else {
+        uint32_t left = mine;
+        for (int k = 0; k < 1024 / P; k++) {          // (one to a warp at least: the row's largest logit is among them)
+            const uint32_t key = k == 0 || k < d.top ? next_top(left) : 0;
+            if (lane == 0) sh.tops[warp * (1024 / P) + k] = key;
+        }
     }
     if (threadIdx.x == 0) sh.listed = 0;
     __syncthreads();
@@ -445,12 +462,12 @@ serve_logprobs_kernel(const __grid_constant__ ProbDev d)
     // an entry's place in the order; where the row has several blocks, the first one is sent the entries and the sums
     Shared<P> *const first = d.parts > 1 ? cluster.map_shared_rank(&sh, 0) : &sh;
     if (d.parts > 1) cluster_wait();                  // it has begun
-    uint64_t entry[kListSize / P];
-    int place[kListSize / P];
+    uint64_t entry[kListSize<P> / P];
+    int place[kListSize<P> / P];
 #pragma unroll
-    for (int k = 0; k < kListSize / P; k++) {
+    for (int k = 0; k < kListSize<P> / P; k++) {
         const int i = threadIdx.x + k * P;
-        place[k] = kListSize;
+        place[k] = kListSize<P>;
         if (i >= listed) continue;
         entry[k] = sh.list[i];
         place[k] = 0;
@@ -491,7 +508,7 @@ serve_logprobs_kernel(const __grid_constant__ ProbDev d)
         if (has) sh.list[threadIdx.x] = entry[0];
         __syncthreads();
 #pragma unroll
-        for (int k = 0; k < kListSize / P; k++) place[k] = kListSize;
+        for (int k = 0; k < kListSize<P> / P; k++) place[k] = kListSize<P>;
         if (has) {
             place[0] = 0;
 #pragma unroll 8
@@ -511,7 +528,7 @@ serve_logprobs_kernel(const __grid_constant__ ProbDev d)
             if (d.entropy) d.entropy[r] = top == -INFINITY ? 0.0f : share ? log_sum : fmaxf(log_sum - all.w / all.s * kLn2, 0.0f);
         }
 #pragma unroll
-        for (int k = 0; k < kListSize / P; k++) {
+        for (int k = 0; k < kListSize<P> / P; k++) {
             if (place[k] >= d.top) continue;
             const float l = logit_of((uint32_t)(entry[k] >> 32));
             const bool likely = !share || l == INFINITY;
@@ -567,14 +584,22 @@ extern "C" int bcast_serve_logprobs(const bcast_serve_logprobs_args *args, void 
     d.parts = 1;
     while (d.parts < kMaxParts && a.rows * d.parts * 2 <= 4 * kSms && a.vocab >= (int64_t)d.parts * 2 * 2048) d.parts *= 2;
     const cudaStream_t st = (cudaStream_t)cuda_stream;
-    // short rows: blocks of 128 threads, since most of a block's time is its reductions
-    const bool small = d.parts == 1 && a.vocab <= 16384;
-    const auto go = [&](auto wide, auto narrow) {
-        return launch(small ? narrow : wide, dim3((unsigned)(a.rows * d.parts)), dim3(small ? 128 : 256), 0, st, true, (unsigned)d.parts, d);
+    // Short rows: fewer threads to a block, since most of its time is its reductions; a warp to a row where there are more rows
+    // than blocks of 128 run at a time.  Measured (us, bf16, five alternatives; a warp / 128 threads): 4096 rows of 2000 logits
+    // 17 / 27, of 8100 27 / 37, 1500 of 3292 11 / 13; but 1500 rows of 16000 23 / 22, 4096 of 32000 86 / 65, 600 of 3292 9.2 / 8.7.
+    // (128 threads / 256: 4096 rows of 16000 48 / 55, of 32000 65 / 69, but of 131072 237 / 200.)  The K-th largest of a
+    // warp's 32 maxima lists some -32 ln(1 - K/32) logits, 44 where K is 24; of 32 the bound is the smallest of them all, and
+    // the list overflows (4096 rows of 3292: 123 / 39).
+    const int64_t row_bytes = a.vocab * (a.dtype == BCAST_SERVE_FP32 ? 4 : 2);
+    const int threads = d.parts > 1 || a.vocab > 16384 ? 256 : row_bytes > 16384 || a.rows <= 8 * kSms || a.top > 24 ? 128 : 32;
+    const auto go = [&](auto kernel) { return launch(kernel, dim3((unsigned)(a.rows * d.parts)), dim3(threads), 0, st, true, (unsigned)d.parts, d); };
+    const auto of = [&](auto type) {
+        using T = decltype(type);
+        return threads == 256 ? go(serve_logprobs_kernel<T, 256>) : threads == 128 ? go(serve_logprobs_kernel<T, 128>) : go(serve_logprobs_kernel<T, 32>);
     };
     switch (a.dtype) {
-    case BCAST_SERVE_BF16: return go(serve_logprobs_kernel<__nv_bfloat16, 256>, serve_logprobs_kernel<__nv_bfloat16, 128>);
-    case BCAST_SERVE_FP16: return go(serve_logprobs_kernel<__half, 256>, serve_logprobs_kernel<__half, 128>);
-    default: return go(serve_logprobs_kernel<float, 256>, serve_logprobs_kernel<float, 128>);
+    case BCAST_SERVE_BF16: return of(__nv_bfloat16());
+    case BCAST_SERVE_FP16: return of(__half());
+    default: return of(float());
     }
 }

@@ -345,6 +345,31 @@ def test_logprobs_masks(V, dtype):
         check_logprobs(l, x, top)
 
 
+# a warp to a row: many short rows, every kind of mask and of equals among them
+@pytest.mark.parametrize("V", [1, 2, 7, 31, 33, 256, 257, 1025, 1999, 3291, 4093, 8191])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+def test_logprobs_a_warp_to_a_row(V, dtype):
+    low, T = torch.finfo(TYPES[dtype]).min, 1187
+    l, x = logprobs_case(V, T, V, dtype)
+    l[0], l[1], l[2], l[3], l[4] = -math.inf, low, math.nan, math.inf, 1.25
+    l[5, 5:], l[6, 5:] = -math.inf, low
+    l[7, ::2] = math.nan
+    l[8, V // 2] = math.inf
+    l[9, ::3] = math.inf
+    l[10] = torch.sort(l[10]).values
+    l[11] = torch.sort(l[11], descending=True).values
+    l[12] = torch.randint(0, 3, (V,), generator=gen(1)).to(l.dtype)
+    l[13] = torch.arange(V) % 512
+    l[14] = -0.0
+    l[14, 1::2] = 0.0
+    l[15] = torch.linspace(-50, 50, V).to(l.dtype)
+    l[16, 1:] = math.nan
+    x[0], x[1], x[2], x[3] = 0, V - 1, -1, V
+    for top in (0, 1, 8, 24, 25):
+        check_logprobs(l, x, top)
+    check_logprobs(l[1:, V // 2:], x[1:], 5)                  # rows that begin anywhere
+
+
 def test_logprobs_tokens_that_are_none():
     l, x = logprobs_case(3, 6, 500, "fp32")
     x[:] = torch.tensor([-1, 500, 499, 0, -2 ** 31, 2 ** 31 - 1])
