@@ -10,8 +10,9 @@
 // reaches the bound goes to a list in shared memory, and an entry's place is the number of entries before it in
 // the order (logit, then lower token).  Lists that overflow -- many equal logits, as behind a mask of the type's lowest
 // value -- take bounds that are exact, and equals in the order of their numbers.
-// A row is a block's (of one warp, where rows are short and many), or a cluster's where the rows are few: its first block joins the parts, which the others send it
-// through distributed shared memory (fetched by it, one after the other, a cluster's join took 5 us).
+// A row is a block's (of one warp, where rows are short and many), or a cluster's where the rows are few: its first block
+// joins the parts, which the others send it through distributed shared memory (fetched by it, one after the other, a
+// cluster's join took 5 us).
 // What bounds it, and what it takes on one B200 (in brackets the bytes at the measured copy rate): 4096 rows of 131072 bf16
 // logits 175 us without alternatives, 197 with eight (164): loads and exponentials (64 % of their unit) while a block streams,
 // nothing while it reduces and picks.  37 rows of 50001 with twenty 11 us, one row of 32000 5: latency, of which a launch,
