@@ -15,7 +15,7 @@
 // cluster's join took 5 us).
 // What bounds it, and what it takes on one B200 (in brackets the bytes at the measured copy rate): 4096 rows of 131072 bf16
 // logits 175 us without alternatives, 197 with eight (164): loads and exponentials (64 % of their unit) while a block streams,
-// nothing while it reduces and picks.  37 rows of 50001 with twenty 11 us, one row of 32000 5: latency, of which a launch,
+// nothing while it reduces and picks.  37 rows of 50001 with twenty 10 us, one row of 32000 5: latency, of which a launch,
 // the loads, the reductions and the pick have about a third each.  Bringing the next row's beginning to L2 during the pick
 // cost 2 to 50 %.
 #include "serve_device.cuh"
@@ -581,9 +581,19 @@ extern "C" int bcast_serve_logprobs(const bcast_serve_logprobs_args *args, void 
     d.stride = a.logits_stride;
     d.vocab = (int32_t)a.vocab;
     d.top = a.top;
-    // few rows: several blocks to one, of at least 2048 logits
+    // Few rows: several blocks to one, of at least 2048 logits each, in powers of two.  As long as all of them find a place at
+    // once, clusters together: up to 7/4 of the SMs (37 rows of 50001 fp16, twenty alternatives: 8 blocks to a row 11.0 us, 4 9.9);
+    // up to four to an SM where each has 64 KB (148 rows of 50257 fp32: 1 block 16.2, 2 12.8; but 74 of 32000 bf16: 4 blocks 11.0,
+    // 1 6.8).  Two save little of a row that one block takes in four rounds of loads, and their join costs 2 us (128 rows of 32000
+    // bf16: 2 blocks 8.8, 1 7.0).
+    const int64_t row_bytes = a.vocab * (a.dtype == BCAST_SERVE_FP32 ? 4 : 2);
     d.parts = 1;
-    while (d.parts < kMaxParts && a.rows * d.parts * 2 <= 4 * kSms && a.vocab >= (int64_t)d.parts * 2 * 2048) d.parts *= 2;
+    while (d.parts < kMaxParts && a.vocab >= d.parts * 2 * 2048ll) {
+        const int64_t blocks = a.rows * d.parts * 2;
+        if (blocks > 4 * kSms || (blocks * 4 > 7 * kSms && row_bytes < d.parts * 2 * 65536ll)) break;
+        d.parts *= 2;
+    }
+    if (d.parts == 2 && a.vocab > 16384 && row_bytes < 131072) d.parts = 1;
     const cudaStream_t st = (cudaStream_t)cuda_stream;
     // Short rows: fewer threads to a block, since most of its time is its reductions; a warp to a row where there are more rows
     // than blocks of 128 run at a time.  Measured (us, bf16, five alternatives; a warp / 128 threads): 4096 rows of 2000 logits
@@ -591,7 +601,6 @@ extern "C" int bcast_serve_logprobs(const bcast_serve_logprobs_args *args, void 
     // (128 threads / 256: 4096 rows of 16000 48 / 55, of 32000 65 / 69, but of 131072 237 / 200.)  The K-th largest of a
     // warp's 32 maxima lists some -32 ln(1 - K/32) logits, 44 where K is 24; of 32 the bound is the smallest of them all, and
     // the list overflows (4096 rows of 3292: 123 / 39).
-    const int64_t row_bytes = a.vocab * (a.dtype == BCAST_SERVE_FP32 ? 4 : 2);
     const int threads = d.parts > 1 || a.vocab > 16384 ? 256 : row_bytes > 16384 || a.rows <= 8 * kSms || a.top > 24 ? 128 : 32;
     const auto go = [&](auto kernel) { return launch(kernel, dim3((unsigned)(a.rows * d.parts)), dim3(threads), 0, st, true, (unsigned)d.parts, d); };
     const auto of = [&](auto type) {

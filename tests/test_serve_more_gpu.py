@@ -292,6 +292,14 @@ def test_logprobs_rows(T, dtype):
     check_logprobs(*logprobs_case(T, T, 17003, dtype), 5)
 
 
+# on both sides of what makes a row another number of blocks'
+@pytest.mark.parametrize("T,V", [(32, 33001), (33, 33001), (64, 17003), (65, 17003), (129, 65537), (130, 65537), (129, 16384), (130, 16385), (37, 262147), (74, 131075), (148, 65535),
+                                 (148, 65536), (149, 65539), (296, 65536), (4, 4095), (4, 4096), (4, 8192), (64, 16385)])
+@pytest.mark.parametrize("dtype,top", [("bf16", 5), ("fp32", 20)])
+def test_logprobs_blocks_to_a_row(T, V, dtype, top):
+    check_logprobs(*logprobs_case(V + T, T, V, dtype), top)
+
+
 @pytest.mark.parametrize("top", [0, 1, 2, 8, 31, 32])
 @pytest.mark.parametrize("V", [20, 40, 9001, 70000])
 def test_logprobs_tops(top, V):
