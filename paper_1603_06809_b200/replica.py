@@ -2,13 +2,15 @@
 
 The message of the broadcast is a model's weights, its low-rank adapters and the cache of a prompt that every
 request starts with, one array after the other (:class:`Layout`).  After ``bcast_exec`` every rank's buffer
-holds all of it, and a :class:`Replica` is a set of views into one of those buffers: nothing is copied out.
+holds all of it, and a :class:`Replica` is a set of views into one of those buffers: a step answers from what the
+buffer holds when it runs, also after another broadcast into it.
 One :meth:`Replica.step` checks drafted tokens for a batch of requests with the serving operators: the
 shared projection with the requests' adapters, the new tokens' norms, rotation and places in the cache, attention
 behind the shared prompt, the shared output projection, the acceptance of the drafts, and, if asked for, the log
 probabilities of what is answered.  The model is one attention layer between the projections, with as many heads
 and as wide as asked for; its weights are random.  With ``Shape.bits`` 4 the projections travel in microscaled 4-bit
-numbers: the output projection is used as it came, the first one, which takes adapters, is unpacked by each replica.
+numbers: the output projection is used as it came, the first one, which takes adapters, is unpacked by every step into
+memory that the replica keeps for it.
 
     python -m paper_1603_06809_b200.replica [--ranks 4] [--requests 16] [--drafts 3] [--prompt 2048] [--steps 20] [--bits 4] [--top 5]
 
@@ -104,13 +106,15 @@ def random_model(s: Shape, layout: Layout, seed: int, device) -> torch.Tensor:
 
 
 class Replica:
-    """One rank: views into its buffer, the requests' own cache, and a workspace."""
+    """One rank: views into its buffer, the requests' own cache, and a workspace; with 4-bit weights also room for the first
+    projection's in 16 bits."""
 
     def __init__(self, s: Shape, layout: Layout, buf: torch.Tensor, requests: int, own_cap: int):
         self.s = s
         self.shared = layout.views(buf)
         if s.bits == 4:                                   # its adapters are in 16 bits, and so is its product
-            self.shared["w_qkv"] = S.bcast_serve_unpack4(self.shared["w_qkv_codes"], self.shared["w_qkv_scales"], s.dtype)
+            self.shared["w_qkv"] = torch.empty((s.qkv, s.hidden), dtype=s.dtype, device=buf.device)
+            self._unpack()
         self.inv_freq = None
         if s.rotation:
             pairs = torch.arange(s.dim // 16 * 8, device=buf.device, dtype=torch.float64)
@@ -123,6 +127,11 @@ class Replica:
         self.length = torch.zeros(requests, dtype=torch.int32, device=buf.device)
         self.cap, self.at_most = each * s.page, 0         # tokens of a request's cache; no length is above at_most
         self.workspace = S.Workspace(buf.device)
+
+    def _unpack(self) -> None:
+        # the first projection in 16 bits, as the buffer has it now: a broadcast may have filled it again
+        w = self.shared
+        S.bcast_serve_unpack4(w["w_qkv_codes"], w["w_qkv_scales"], self.s.dtype, out=w["w_qkv"])
 
     def _make_room(self, n: int) -> None:
         # The lengths are on the GPU, which is waited for only when all drafts so far would have filled the cache.
@@ -141,6 +150,8 @@ class Replica:
         s, w = self.s, self.shared
         R, n, _ = x.shape
         self._make_room(n)
+        if s.bits == 4:
+            self._unpack()
         # the projection of all tokens at once, each with its request's adapter
         qkv = S.bcast_serve_linear(x.reshape(R * n, s.hidden), w["w_qkv"], lora_a=w["lora_a"], lora_b=w["lora_b"],
                                    adapter=adapter.repeat_interleave(n), scale=w["lora_scale"], workspace=self.workspace)
