@@ -402,15 +402,6 @@ py::tuple append(const Maybe &q, const Tensor &k, const Tensor &v, const Tensor 
     });
 }
 
-// A result among several in one piece of memory, from 32-bit number `at` on.
-Tensor part_of(const Tensor &whole, int64_t at, at::IntArrayRef shape, at::ScalarType type)
-{
-    Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(whole.storage()), whole.key_set(), c10::scalarTypeToTypeMeta(type));
-    t.unsafeGetTensorImpl()->set_sizes_contiguous(shape);
-    t.unsafeGetTensorImpl()->set_storage_offset(at);
-    return t;
-}
-
 py::tuple logprobs(const Tensor &logits, const Tensor &tokens, int64_t top, const Maybe &logprobs, const Maybe &entropy, const Maybe &top_tokens,
                    const Maybe &top_logprobs, int64_t raw)
 {
@@ -425,20 +416,9 @@ py::tuple logprobs(const Tensor &logits, const Tensor &tokens, int64_t top, cons
         expect(tokens, "tokens", at::kInt, {T}, dev);
         const Place place(logits, raw);
         place.use({&logits, &tokens, given(logprobs), given(entropy), given(top_tokens), given(top_logprobs)});
-        Tensor lp, h, x, l;
-        if (!logprobs && !entropy && !top_tokens && !top_logprobs && T > 0) {
-            // (four results of their own took 2 us longer than one piece of memory for them)
-            const Tensor all = output(std::nullopt, "", {T * (2 + 2 * top)}, at::kFloat, dev);
-            lp = part_of(all, 0, {T}, at::kFloat);
-            h = part_of(all, T, {T}, at::kFloat);
-            l = part_of(all, 2 * T, {T, top}, at::kFloat);
-            x = part_of(all, (2 + top) * T, {T, top}, at::kInt);
-        } else {
-            lp = output(logprobs, "logprobs", {T}, at::kFloat, dev);
-            h = output(entropy, "entropy", {T}, at::kFloat, dev);
-            x = output(top_tokens, "top_tokens", {T, top}, at::kInt, dev);
-            l = output(top_logprobs, "top_logprobs", {T, top}, at::kFloat, dev);
-        }
+        // (each in memory of its own: what is kept or saved of them is no more than was asked for)
+        const Tensor lp = output(logprobs, "logprobs", {T}, at::kFloat, dev), h = output(entropy, "entropy", {T}, at::kFloat, dev);
+        const Tensor x = output(top_tokens, "top_tokens", {T, top}, at::kInt, dev), l = output(top_logprobs, "top_logprobs", {T, top}, at::kFloat, dev);
         need(tokens.is_contiguous() && lp.is_contiguous() && h.is_contiguous() && x.is_contiguous() && l.is_contiguous(), "tokens and results are contiguous");
         a.rows = T;
         a.vocab = V;

@@ -1,11 +1,33 @@
-"""Replicas whose buffers a second broadcast fills, on the GPU."""
+"""Edges of log probabilities and of replicas on the GPU: results that stand by themselves, buffers that a second broadcast fills."""
+import io
+
 import pytest
 import torch
 
 from paper_1603_06809_b200 import replica as P
-from test_serve_gpu import DEV
+from paper_1603_06809_b200 import serve as S
+from test_serve_gpu import DEV, gen, rand
 
 pytestmark = pytest.mark.gpu
+
+
+# ------------------------------------------------------------------------------------------ results that stand by themselves
+@pytest.mark.parametrize("T", [1, 7])
+@pytest.mark.parametrize("top", [0, 1, 20])
+def test_logprobs_results_are_kept_and_saved_each_by_itself(T, top):
+    g = gen(T + top)
+    out = S.bcast_serve_logprobs(rand(g, T, 500).to(DEV), torch.arange(T, dtype=torch.int32, device=DEV), top=top)
+    # a result holds no more memory than its own, and writing to one changes no other
+    assert [t.untyped_storage().nbytes() for t in out] == [4 * t.numel() for t in out]
+    want = [t.clone() for t in out]
+    for i, t in enumerate(out):
+        t.zero_()
+        assert all(torch.equal(a, b) for a, b in zip(out[i + 1:], want[i + 1:]))
+        t.copy_(want[i])
+    file = io.BytesIO()
+    torch.save(out, file)
+    file.seek(0)
+    assert all(torch.equal(a, b) and a.dtype == b.dtype for a, b in zip(torch.load(file), want))
 
 
 # ------------------------------------------------------------------------------------------ buffers that are filled again
