@@ -56,7 +56,7 @@ def _build_bind(nvcc: str) -> None:
                os.path.join(cuda, "include"), sysconfig.get_paths()["include"]]
     _run([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-DTORCH_API_INCLUDE_EXTENSION_H",
           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", *[a for d in include for a in ("-isystem", d)], *BIND_SOURCES,
-          LIB_PATH, f"-L{troot}/lib", "-lc10", "-lc10_cuda", "-ltorch", "-ltorch_cpu", "-ltorch_cuda", "-ltorch_python",
+          LIB_PATH, f"-L{troot}/lib", "-lc10", "-lc10_cuda", "-ltorch", "-ltorch_cpu", "-ltorch_python",
           "-Wl,-rpath,$ORIGIN", f"-Wl,-rpath,{troot}/lib"], BIND_PATH)
 
 

@@ -3,14 +3,13 @@
 // A call's tensors are checked against each other here (types, shapes, device, contiguous innermost dimension)
 // and described to the C entry point, which checks the rest; nothing is computed.  Native because a decode step's
 // kernels take about as long as marshalling a dozen tensors in Python does (33 us of 44 us measured).
-// Every function returns (code, outputs or what was wrong, whether the stream is being captured into a graph).
+// Every function returns (code, outputs or what was wrong, whether the workspace is a graph's now).
 #include <ATen/core/Tensor.h>
-#include <ATen/cuda/EmptyTensor.h>
-#include <ATen/ops/empty.h>
 #include <c10/cuda/CUDACachingAllocator.h>
 #include <c10/cuda/CUDAGraphsC10Utils.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
+#include <c10/util/safe_numerics.h>
 #include <torch/csrc/utils/pybind.h>
 
 #include <initializer_list>
@@ -114,21 +113,31 @@ struct Place {
     }
 };
 
-// (on a GPU straight from its allocator: through the dispatcher a result took 1.4 us, a launch takes 4)
+// A result: the one that was given, or new memory, straight from the allocator of the GPU that is current by now.  (What torch
+// looks at before is known here: 0.2 us less for each, through the dispatcher one took 1.4; a launch takes 4.)
 Tensor output(const Maybe &out, const char *name, at::IntArrayRef shape, at::ScalarType type, const at::Device &dev)
 {
-    if (!out && dev.is_cuda()) return Tensor(at::detail::empty_cuda(shape, type, dev, std::nullopt));
-    if (!out) return at::empty(shape, at::TensorOptions().dtype(type).device(dev));
-    expect(*out, name, type, shape, dev);
-    return *out;
+    if (out) {
+        expect(*out, name, type, shape, dev);
+        return *out;
+    }
+    int64_t bytes = (int64_t)c10::elementSize(type);
+    for (int64_t n : shape)
+        if (c10::mul_overflows(bytes, n, &bytes)) throw Refused{std::string(name) + ": " + list(shape) + " is too large"};
+    c10::Allocator *const from = c10::cuda::CUDACachingAllocator::get();
+    Tensor t = at::detail::make_tensor<c10::TensorImpl>(
+        c10::Storage(c10::Storage::use_byte_size_t(), (size_t)bytes, from->allocate((size_t)bytes), from, true),
+        c10::DispatchKeySet(c10::DispatchKey::CUDA), c10::scalarTypeToTypeMeta(type));
+    t.unsafeGetTensorImpl()->set_sizes_contiguous(shape);
+    return t;
 }
 
-// How a call that was made ended.
-py::tuple ended(int code, py::object outputs)
+// How a call that was made ended, and whether a graph has it now: a workspace has to know, a call without one does not ask.
+py::tuple ended(int code, py::object outputs, bool workspace = false)
 {
     if (code) return py::make_tuple(code, "", false);
     // (asked of the stream of `place`, which is the current one here)
-    return py::make_tuple(code, std::move(outputs), c10::cuda::currentStreamCaptureStatusMayInitCtx() != c10::cuda::CaptureStatus::None);
+    return py::make_tuple(code, std::move(outputs), workspace && c10::cuda::currentStreamCaptureStatusMayInitCtx() != c10::cuda::CaptureStatus::None);
 }
 
 // The call itself; BCAST_ERR_CAPACITY comes back with the bytes that are needed.
@@ -138,7 +147,7 @@ py::tuple finish(int (*call)(const Args *, void *), int64_t (*size)(const Args *
     int64_t bytes = size(&a);
     int code = bytes < 0 ? (int)bytes : (uint64_t)bytes > a.workspace_bytes ? BCAST_ERR_CAPACITY : call(&a, place.stream.stream());
     if (code == BCAST_ERR_CAPACITY) return py::make_tuple(code, bytes, false);
-    return ended(code, std::move(outputs));
+    return ended(code, std::move(outputs), true);
 }
 
 template <typename F>
