@@ -243,7 +243,7 @@ int bcast_serve_append(const bcast_serve_append_args *args /* HOST */, void *cud
  *     entropy[r]      = -sum p log p
  *     top_tokens[r]   = the `top` tokens with the largest logits, the lower number first among equals
  *     top_logprobs[r] = their log p
- * Statistics are held in 32 bits, the logits read once (a few of them twice).
+ * Statistics are held in 32 bits, the logits read once (a few of them twice).  No log p is above 0, no entropy below.
  *   - A logit that is NaN counts as -infinity; where some are +infinity, these share the probability evenly.
  *     Tokens that so have no probability, and those outside 0..vocab-1, have -infinity as their log p.  They are no
  *     alternatives: where there are fewer than `top` others, the row goes on with token -1 and -infinity.  A row

@@ -522,7 +522,7 @@ serve_logprobs_kernel(const __grid_constant__ ProbDev d)
         auto logprob = [&](float l) {
             if (!(l > -INFINITY)) return -INFINITY;
             if (share) return l == INFINITY ? -log_sum : -INFINITY;
-            return l - all.at - log_sum;
+            return fminf(l - all.at - log_sum, 0.0f);     // (a sum of one term and little more may be rounded below it)
         };
         if (threadIdx.x == 0) {
             d.logprobs[r] = logprob(logit);

@@ -1,4 +1,5 @@
-"""Edges of log probabilities and of replicas on the GPU: results that stand by themselves, buffers that a second broadcast fills."""
+"""Edges of log probabilities and of replicas on the GPU: results that stand by themselves, log probabilities at their upper end, buffers
+that a second broadcast fills."""
 import io
 
 import pytest
@@ -6,7 +7,7 @@ import torch
 
 from paper_1603_06809_b200 import replica as P
 from paper_1603_06809_b200 import serve as S
-from test_serve_gpu import DEV, gen, rand
+from test_serve_gpu import DEV, TYPES, gen, rand
 
 pytestmark = pytest.mark.gpu
 
@@ -28,6 +29,23 @@ def test_logprobs_results_are_kept_and_saved_each_by_itself(T, top):
     torch.save(out, file)
     file.seek(0)
     assert all(torch.equal(a, b) and a.dtype == b.dtype for a, b in zip(torch.load(file), want))
+
+
+# ------------------------------------------------------------------------------------------ log probabilities at their upper end
+@pytest.mark.parametrize("T,V", [(600, 300), (3000, 2000), (500, 20000), (3, 70001)])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+def test_logprobs_are_never_above_zero(T, V, dtype):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(T + V)
+    # one token that has all of the probability, wherever it is and whatever its logit
+    l = torch.randn(T, V, generator=g, device=DEV)
+    best = torch.randint(0, V, (T, 1), generator=g, device=DEV)
+    l.scatter_(1, best, torch.rand(T, 1, generator=g, device=DEV) * 400 + 25)
+    l[::3].clamp_(min=0.0).mul_(50.0)
+    x = best[:, 0].to(torch.int32)
+    lp, h, ids, top = S.bcast_serve_logprobs(l.to(TYPES[dtype]), x, top=3)
+    assert bool((lp <= 0).all()) and bool((top <= 0).all()) and bool((h >= 0).all())
+    assert bool((lp > -1e-3).any()) and torch.equal(torch.exp(lp) <= 1, torch.ones_like(lp, dtype=torch.bool))
 
 
 # ------------------------------------------------------------------------------------------ buffers that are filled again
