@@ -198,8 +198,9 @@ int64_t bcast_serve_verify_workspace(const bcast_serve_verify_args *args);
  * R turns the pairs of the first `rot` numbers of a head, pair p = 0..rot/2-1 being (p, p + rot/2), or
  * (2p, 2p + 1) where `interleaved`: (x, y) -> (x cos t - y sin t, x sin t + y cos t),
  *     t = position * inv_freq[p],  position = first + slot, or positions[b][i][axis[p]] where given.
- * The angle is reduced exactly, however far the position.  Arithmetic is in 32 bits, results are rounded
- * once; what is neither normed nor rotated is copied bit for bit.
+ * The angle is reduced in whole numbers, to 2^-63 of a turn, for every finite inv_freq and every position; one below 2^-6 keeps
+ * all of its digits.  Arithmetic is in 32 bits, results are rounded once; what is neither normed nor rotated is copied bit
+ * for bit.
  *   - A token is padding if i < new_tokens - new_len[b] (where new_len is given: a request with fewer new tokens
  *     has them at the end), or if its slot is negative.  Padding goes nowhere, and its rows of out are zero.
  *   - Keys and values whose slot is not below own_cap, or whose page is outside 0..num_pages-1, are not

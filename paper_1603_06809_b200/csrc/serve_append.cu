@@ -6,8 +6,8 @@
 // those lanes.  A token is a warp's, which takes as many heads at a time as it has lanes for ("a round": queries first, then
 // keys, then values), or a half's or a quarter's of one where it has few heads.  Its cosines and sines are made once and, with
 // the norm's weights, turned into one set of factors for all heads of a kind.  Rounds come through shared memory, four ahead.
-// Angles: inv_freq / 2 pi as a 64-bit fraction of a turn; multiplied by the position modulo 2^64 this leaves the fraction
-// of a turn, off by the position's 2^-64.
+// Angles: inv_freq / 2 pi as a 96-bit fraction of a turn, times the position, whole turns cut off: to 2^-63 of a turn, for every
+// finite inv_freq and every position; small angles in floats.
 // What bounds it, and what it takes on one B200 (bf16, 32 query and 8 key/value heads of 128; in brackets the bytes at the
 // measured copy rate): 16384 tokens 64 us without norms (62), 74 with: issuing instructions, 2.7 to a cycle and SM, half of the
 // time on conversions.  1024 tokens 10 us (4), 128 4.8: a token's chain of length, angle, head after head.  One token with
@@ -70,20 +70,62 @@ __device__ __forceinline__ uint4 narrow8(const uint64_t *x)
     return make_uint4(v[0], v[1], v[2], v[3]);
 }
 
-// Cosine and sine of `position` times `inv_freq`: inv_freq / 2 pi to 64 bits behind the point, from the float's 24-bit
-// whole number m and exponent e (inv_freq = m 2^e) and 2^66 / 2 pi; whole turns are cut off on both sides.
+// Cosine and sine of `position` times `inv_freq` = m 2^e, m a whole number of 24 bits.  The angle is reduced in whole numbers, as
+// Payne and Hanek do it: m times the 128 bits of 1 / 2 pi that matter behind 2^e is the fraction of a turn that one position
+// makes, that times the position the fraction that all of them make, whole turns cut off, to 2^-63.  What is left of the nearest
+// quarter of a turn goes to sincospi as a float, so that small sines and cosines keep their digits.  An angle below 2^-6 needs no
+// reduction and is multiplied out in floats: a fixed number of places behind the point would leave it few.
 __device__ __forceinline__ float2 turn_of(float inv_freq, int64_t position)
 {
-    constexpr uint64_t per_turn = 0xa2f9836e4e44152aull;              // 2^66 / (2 pi), to nearest
+    uint32_t k0 = 0x28be60dbu, k1 = 0x9391054au, k2 = 0x7f09d5f4u, k3 = 0x7d4d3770u;       // 1 / 2 pi, 32 bits each
     const uint32_t bits = __float_as_uint(inv_freq), field = bits >> 23 & 255u;
-    const uint64_t m = (bits & 0x7fffffu) | (field ? 0x800000u : 0u);
-    const uint64_t low = m * per_turn, high = __umul64hi(m, per_turn);
-    const int right = 152 - (int)(field ? field : 1);                 // 2 - e
-    uint64_t step = right >= 128 ? 0 : right >= 64 ? high >> (right - 64) : right > 0 ? low >> right | high << (64 - right) : low << -right;
-    if (bits >> 31) step = 0 - step;
-    const float half_turns = (float)(int32_t)((step * (uint64_t)position) >> 32) * 4.656612873077392578125e-10f;  // 2^-31
-    float2 r;
+    const uint32_t m = (bits & 0x7fffffu) | (field ? 0x800000u : 0u);
+    const uint32_t by = (uint32_t)(position < 0 ? -position : position);                   // below 2^32: both parts of a sum are below 2^31
+    int e = (int)(field ? field : 1u) - 150;
+    if (e > 0) {
+        // (from 2^24 on: the bits from e on)
+        uint32_t k4 = 0x36d8a566u, k5 = 0x4f10e410u, k6 = 0x7f9458eau, k7 = 0xf7aef158u;
+        for (; e >= 32; e -= 32) {
+            k0 = k1, k1 = k2, k2 = k3, k3 = k4;
+            k4 = k5, k5 = k6, k6 = k7, k7 = 0;
+        }
+        k0 = __funnelshift_l(k1, k0, e);
+        k1 = __funnelshift_l(k2, k1, e);
+        k2 = __funnelshift_l(k3, k2, e);
+        k3 = __funnelshift_l(k4, k3, e);
+        e = 0;
+    }
+    uint64_t t = (uint64_t)m * k3;
+    t = (uint64_t)m * k2 + (t >> 32);
+    uint32_t s0 = (uint32_t)t;                        // s0 to s3: from 2^-96 up; the places below make less than 2^-64 of a turn
+    t = (uint64_t)m * k1 + (t >> 32);
+    uint32_t s1 = (uint32_t)t;
+    t = (uint64_t)m * k0 + (t >> 32);
+    uint32_t s2 = (uint32_t)t, s3 = (uint32_t)(t >> 32);
+    // (angles from 2^-6 on have e of -61 at least)
+    const int right = -e;
+    if (right >= 32) {
+        s0 = s1, s1 = s2, s2 = s3, s3 = 0;
+    }
+    s0 = __funnelshift_r(s0, s1, right);
+    s1 = __funnelshift_r(s1, s2, right);
+    s2 = __funnelshift_r(s2, s3, right);
+    // s0 to s2 are 2^-96, 2^-64 and 2^-32 of a turn
+    t = (uint64_t)s0 * by;
+    t = (uint64_t)s1 * by + (t >> 32);
+    const uint64_t turns = (t & 0xffffffffu) | (uint64_t)((uint32_t)(t >> 32) + s2 * by) << 32;
+    uint32_t quarters = (uint32_t)((turns + (1ull << 61)) >> 62);
+    float half_turns = (float)(int64_t)(turns - ((uint64_t)quarters << 62)) * 1.0842021724855044e-19f;      // 2^-63
+    const float angle = fabsf(inv_freq) * (float)by;
+    if (angle < 0.015625f) {
+        half_turns = angle * 0.318309886f;
+        quarters = 0;
+    }
+    float2 r, q;
     sincospif(half_turns, &r.y, &r.x);
+    q = quarters & 1u ? make_float2(-r.y, r.x) : r;
+    r = quarters & 2u ? make_float2(-q.x, -q.y) : q;
+    if ((bits >> 31 != 0) != (position < 0)) r.y = -r.y;
     return r;
 }
 

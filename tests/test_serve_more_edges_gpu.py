@@ -1,15 +1,82 @@
-"""Edges of log probabilities and of replicas on the GPU: results that stand by themselves, log probabilities at their upper end, buffers
-that a second broadcast fills."""
+"""Edges of cache appends and log probabilities, and of replicas that use them: angles of all sizes, results that stand by
+themselves, log probabilities at their upper end, buffers that a second broadcast fills."""
 import io
+import math
+from fractions import Fraction
 
 import pytest
 import torch
 
+import serve_more_reference as R
 from paper_1603_06809_b200 import replica as P
 from paper_1603_06809_b200 import serve as S
 from test_serve_gpu import DEV, TYPES, gen, rand
 
 pytestmark = pytest.mark.gpu
+
+
+# ------------------------------------------------------------------------------------------ angles
+def two_pi(bits):
+    """2 pi to that many bits behind the point, by Machin's formula in whole numbers."""
+    def arctan(n):
+        x = (1 << bits + 20) // n
+        total, k, sign = x, 3, -1
+        while x:
+            x //= n * n
+            total += sign * (x // k)
+            k, sign = k + 2, -sign
+        return total
+    return Fraction(8 * (4 * arctan(5) - arctan(239)), 1 << bits + 20)
+
+
+TWO_PI = two_pi(300)
+# zero, of all exponents, of either sign, those of bases 1e4 to 1e7, neighbours of 2^26 and of powers of 2^32
+FREQUENCIES = [0.0, 1e-45, 3e-39, 2e-38, 1e-30, 1e-20, 3e-13, 1e-9, 1e-7, 1.2409e-07, 2.5e-7, 1.1547e-4, 0.01, 0.5, 0.99999994, 1.0, 1.7, math.pi, 2 * math.pi, 37.5,
+               4096.0, 2.0 ** 20 + 1, 2.0 ** 24, 1.5 * 2.0 ** 24, 2.0 ** 25 + 6, 7.3 * 2.0 ** 26, 1.9 * 2.0 ** 40, 1e15, 1e18, 3e20, 1e25, 6.5e26, 2.0 ** 89, 1e30, 1e38, 3.4e38,
+               -1.0, -1e-7, -0.37, -37.5, -4097.0, -1e20, -2.0 ** 120, -3e-20, -0.0]
+POSITIONS = [0, 1, 2, 3, -1, -5, 11, 1000, -77777, 131071, 2 ** 20 + 3, 12345678, 2 ** 31 - 1, -2 ** 31, 1 - 2 ** 31]
+
+
+def turned(x, frequency, position):
+    """x (cos t, sin t) with t = position * frequency, the angle reduced in whole numbers."""
+    t = Fraction(frequency) * position
+    quarters = round(t / (TWO_PI / 4))
+    rest = float(t - quarters * TWO_PI / 4)
+    c, s = math.cos(rest), math.sin(rest)
+    c, s = ((c, s), (-s, c), (-c, -s), (s, -c))[quarters % 4]
+    return x * c, x * s
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("by", ["positions", "slots"])
+def test_append_angles_of_all_sizes(dtype, interleaved, by):
+    # Pairs (x, 0): each result is one product, so that a small sine shows with all its digits.
+    dt, pairs = TYPES[dtype], 48
+    x = 1.0 if dtype == "bf16" else 32768.0
+    f = torch.tensor((FREQUENCIES + [1.0] * pairs)[:pairs], dtype=torch.float32)
+    places = POSITIONS if by == "positions" else [0, 1, 7, 1000, 131071, 2 ** 20 + 3, 2 ** 31 - 1]
+    n = len(places)
+    k = torch.zeros(n, 1, 1, 96, dtype=dt)
+    k[..., (slice(0, 96, 2) if interleaved else slice(0, 48))] = x
+    d = k.to(DEV)
+    own_k, own_v = torch.zeros(n, 1, 1, 96, dtype=dt, device=DEV), torch.zeros(n, 1, 1, 96, dtype=dt, device=DEV)
+    one = torch.ones(n, dtype=torch.int32, device=DEV)
+    if by == "positions":
+        q = S.bcast_serve_append(d, d, d, own_k, own_v, one, positions=torch.tensor(places, dtype=torch.int32, device=DEV)[:, None], inv_freq=f.to(DEV), interleaved=interleaved)
+    else:
+        q = torch.cat([S.bcast_serve_append(d[i:i + 1], d[i:i + 1], d[i:i + 1], own_k[i:i + 1], own_v[i:i + 1], one[i:i + 1], first=p, inv_freq=f.to(DEV), interleaved=interleaved)
+                       for i, p in enumerate(places)])
+    assert torch.equal(q, own_k)
+    got = q.double().cpu().reshape(n, 2, 48) if not interleaved else q.double().cpu().reshape(n, 48, 2).transpose(1, 2)
+    want = torch.tensor([[turned(x, float(v), p) for v in f] for p in places], dtype=torch.float64).transpose(1, 2)
+    # The reduced angle: four roundings, of the position, the frequency's product with it, 1 / pi and the product with that,
+    # and 2^-63 of a turn; cosine and sine to two units (2^-23 each); the product with x, and a sum with zero.
+    err = want.abs() * (4 * R.E + 2 * 2.0 ** -23 + 2 * R.E) + x * 2 * math.pi * 2.0 ** -63
+    over = (got - want).abs() - R.rounded(want, err, dt)
+    worst = int(over.argmax())
+    i, _, j = worst // (2 * pairs), worst // pairs % 2, worst % pairs
+    assert bool((over <= 0).all()), f"frequency {float(f[j])}, position {places[i]}: {got[i, :, j].tolist()}, not {want[i, :, j].tolist()}"
 
 
 # ------------------------------------------------------------------------------------------ results that stand by themselves
