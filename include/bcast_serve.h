@@ -10,8 +10,8 @@
  *
  *   bcast_serve_linear   a projection that all tokens share, plus the low-rank adapter of each
  *                        token's request
- *   bcast_serve_linear4  the same without adapters, the weights in 4 bits: a message a quarter as
- *                        long.  bcast_serve_pack4 makes such weights before the broadcast,
+ *   bcast_serve_linear4  the same without adapters, the weights in 4 bits: a message 3.8 times
+ *                        shorter.  bcast_serve_pack4 makes such weights before the broadcast,
  *                        bcast_serve_unpack4 makes numbers of them again
  *   bcast_serve_append   new tokens' queries and keys normed and rotated, keys and values put into
  *                        the requests' caches
@@ -244,7 +244,9 @@ int bcast_serve_append(const bcast_serve_append_args *args /* HOST */, void *cud
  *     entropy[r]      = -sum p log p
  *     top_tokens[r]   = the `top` tokens with the largest logits, the lower number first among equals
  *     top_logprobs[r] = their log p
- * Statistics are held in 32 bits, the logits read once (a few of them twice).  No log p is above 0, no entropy below.
+ * Statistics are held in 32 bits.  The logits are read once, a few of them twice; up to all of them twice in rows with
+ * -infinity, NaN, the lowest number of bf16 or fp32, or logits beyond 2^20, and more often where hundreds of equal ones are
+ * among the largest.  No log p is above 0, no entropy below.
  *   - A logit that is NaN counts as -infinity; where some are +infinity, these share the probability evenly.
  *     Tokens that so have no probability, and those outside 0..vocab-1, have -infinity as their log p.  They are no
  *     alternatives: where there are fewer than `top` others, the row goes on with token -1 and -infinity.  A row
@@ -300,6 +302,8 @@ int bcast_serve_unpack4(const bcast_serve_pack4_args *args /* HOST */, void *cud
  * bcast_serve_linear4 -- y[t] = W x4[t] + bias: W in microscaled 4-bit numbers as bcast_serve_pack4 makes
  * them, x4[t] what pack4 makes of x[t].  Sums are held in 32 bits, y is rounded once.  A block of x[t] with NaN or an
  * infinity in it makes y[t] NaN, a block of W that is NaN its feature.
+ * 4 bits on both sides are coarse: for normally distributed x and W, y is off by 0.16 of its size (root mean square; with W
+ * alone in 4 bits it would be 0.115, with both in bf16 0.003).
  *   dtype        BCAST_SERVE_BF16 or BCAST_SERVE_FP16: x, bias and y
  *   tokens       0 <= T <= 2^21;  k a multiple of 32, 32..2^24, T * k at most 2^36, k rounded up to 128;  1 <= n <= 2^24
  *   x [T][k], y [T][n]: rows at x_stride (a multiple of 8), y_stride;  bias [n] or NULL

@@ -9,9 +9,10 @@
 // Angles: inv_freq / 2 pi as a 96-bit fraction of a turn, times the position, whole turns cut off: to 2^-63 of a turn, for every
 // finite inv_freq and every position; small angles in floats.
 // What bounds it, and what it takes on one B200 (bf16, 32 query and 8 key/value heads of 128; in brackets the bytes at the
-// measured copy rate): 16384 tokens 64 us without norms (62), 74 with: issuing instructions, 2.7 to a cycle and SM, half of the
-// time on conversions.  1024 tokens 10 us (4), 128 4.8: a token's chain of length, angle, head after head.  One token with
-// 12 heads of 64 2.6, a launch.  Measured against it: cosines by each block of a token's warps (92 us for 16384 normed
+// measured copy rate): 16384 tokens 64 us without norms (62), 74.5 with: issuing instructions, 2.7 to a cycle and SM, half of the
+// time on conversions.  (Norms and rotation together spill 14 to 15 of the 96 registers that 18 warps to an SM leave, around
+// the rounds: 1 % of the instructions.)  1024 tokens 10 us (4), 128 5.0: a token's chain of length, angle, head after head.
+// One token with 12 heads of 64 2.6, a launch.  Measured against it: cosines by each block of a token's warps (92 us for 16384 normed
 // tokens), blocks that stay and take token after token (81 to 136), loads into registers instead of shared memory (80).
 #include "serve_device.cuh"
 #include "serve_internal.h"

@@ -12,10 +12,11 @@
 //                   which are laid out so that a stage's are one run of memory, by bulk copies; tcgen05.cp brings
 //                   them to tensor memory, where the instruction wants them
 // What bounds them, and what they take on one B200 (bf16; device time, in brackets the bytes at the measured copy rate):
-// 65536 x 4096 to codes and back 214 us (208): memory.  8192 tokens, 4096 -> 4096 67 us (22), of which x 15: the product's 52
+// 65536 x 4096 to codes and back 214 us (208): memory.  8192 tokens, 4096 -> 4096 68 us (22), of which x 15: the product's 52
 // are 5.3 PFLOP/s; its pairs of blocks wait on the ring of six stages, about 2700 cycles from a stage's last product to
-// its next one's arrival, where the products of six stages take 2690.  64 tokens, 4096 -> 4096 7.5 us, one, 2048 -> 2048 3.7: launches and
-// the latency of the loads.
+// its next one's arrival, where the products of six stages take 2690.  The stages are 640 MB in all, 12.3 TB/s out of L2, about
+// what a broadcast moves through it (12.5): those cycles may be a queue, which no deeper ring would shorten.  64 tokens, 4096 ->
+// 4096 7.5 us, one, 2048 -> 2048 3.8: launches and the latency of the loads.
 #include "serve_device.cuh"
 #include "serve_internal.h"
 #include "serve_tma.h"
@@ -33,7 +34,8 @@ constexpr int kAtom = 512;                // bytes of the scales of 128 rows x 4
 // ------------------------------------------------------------------------------------------- to 4 bits and back
 constexpr int kPackThreads = 256, kPackRows = 4;      // rows of a thread, whose loads are under way together
 
-// Division by a number that the host knows: the quotient of n < 2^31 is (n + the upper half of n * mul) >> shift.
+// Division by a number that the host knows, as a multiplication (Granlund and Montgomery's): the quotient of n < 2^31 is
+// (n + the upper half of n * mul) >> shift.
 struct Divisor {
     uint32_t of, mul, shift;
     __device__ __forceinline__ uint32_t quotient(uint32_t n) const { return (__umulhi(n, mul) + n) >> shift; }
